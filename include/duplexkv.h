@@ -505,6 +505,163 @@ int32_t kv_table_get_stats(kv_table_t *table, kv_table_stats_t *out);
  * counterpart; this is how the all-or-nothing promise of kv_req_rotate and kv_eager_rotate is tested.) */
 int32_t kv_table_fail_pool_call(kv_table_t *table, int64_t after_calls, int32_t code);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators on the device cache: what a model does with the blocks the pool moves.  (The paper's engine
+ * sits beside a model runner that has these; they are operators of this library.)
+ *
+ *   kv_append   writes new tokens into the cache: rotary positions (several axes) on q and k, then k and v
+ *               into their slots
+ *   kv_attend   attention of one new token per sequence over its cache, with the slots' attention weights
+ *               added up on request
+ *   kv_evict    keeps the slots with the largest added-up weights and frees the rest of the cache
+ *
+ * Slot s of a sequence lies in row s % block_size of device block table[s / block_size], for every layer, K
+ * and V plane and KV head.  Elements are bf16 or f16; sums, softmax statistics and weights are float32.
+ *
+ * Conventions
+ *   - All array arguments are DEVICE pointers unless a comment says HOST; strides count elements.  Nothing is
+ *     copied to or from the host, nothing is allocated except the context's workspace (see kv_ops_reserve).
+ *   - Every call runs on the context's stream, asynchronously, and may be captured into a CUDA graph (reserve
+ *     the workspace first).  A call without sequences, tokens or layers is a no-op.
+ *   - The context knows nothing of the pool's transfers: order the stream after swap-ins with kv_stream_wait,
+ *     and finish the stream (kv_ops_sync) before blocks it still reads or writes are rotated out, released
+ *     (kv_req_shrink, kv_req_preempt, kv_req_finish) or handed to another stream.
+ *   - Bad arguments are refused before anything is launched.  What only the device can see is checked there:
+ *     a block id outside the pool or a length outside [0, max_len] touches no memory (the slot counts as masked,
+ *     the token or row is not written, the sequence counts as empty), sets the context's status word, and
+ *     kv_ops_sync returns KV_ERR_RANGE from then on.
+ */
+typedef struct kv_ops kv_ops_t;     /* operator context of one stream; opaque, owned by the library */
+
+#define KV_DT_BF16 0
+#define KV_DT_F16  1
+
+/* Where and how the cache lies in device memory: a pool's device side, or any memory of that layout. */
+typedef struct {
+    void   *device_base;            /* 16-byte aligned                                                  */
+    int32_t num_layers, block_size, kv_heads, head_dim;   /* head_dim: a multiple of 8, at most 256     */
+    int64_t num_gpu_blocks;
+    int32_t device_layout;          /* KV_DEV_LAYER_FIRST or KV_DEV_BLOCK_FIRST                         */
+    int32_t dtype;                  /* KV_DT_*: of the cache, q and the outputs                         */
+} kv_cache_t;
+
+/* A context for `stream` (a cudaStream_t of device_id that outlives it; NULL = the default stream).  Sets the
+ * current device.  One caller thread. */
+int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out);
+/* Waits for the stream, then frees the context and its workspace. */
+int32_t kv_ops_destroy(kv_ops_t *ops);
+/* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA / KV_ERR_TIMEOUT of earlier calls. */
+int32_t kv_ops_sync(kv_ops_t *ops);
+/* Makes the workspace at least `bytes` large.  A call that needs more than there is does this itself, with a
+ * cudaMalloc (not possible during stream capture: KV_ERR_NOMEM).  Outgrown workspaces stay allocated until
+ * kv_ops_destroy, so graphs captured with them keep working. */
+int32_t kv_ops_reserve(kv_ops_t *ops, int64_t bytes);
+/* Text of the latest error of this context (never NULL); with NULL: of the latest kv_ops_create failure. */
+const char *kv_ops_last_error(kv_ops_t *ops);
+/* The pool's device side as a kv_cache_t. */
+int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
+
+/*
+ * Attention of one new token per sequence.  For sequence i, query head g of KV head h = g / (q_heads/kv_heads),
+ * over the slots t in [max(0, lens[i] - window), lens[i]) (window 0: all):
+ *     s_t = scale * q . K_t,  p_t = exp(s_t) / sum exp(s),  out = sum p_t V_t,  lse = log sum exp(s)
+ *     weights_out[i][h][t] = weights_in[i][h][t] + sum over h's query heads of p_t      (t < lens[i])
+ * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing.
+ */
+typedef struct {
+    int32_t layer, num_seqs, q_heads, window;
+    int64_t max_len;                /* HOST bound of lens: sizes the launch and the workspace           */
+    float   scale;                  /* 0 = 1 / sqrt(head_dim)                                           */
+    int32_t table_width;            /* entries per row of block_tables; table_width*block_size >= max_len */
+    const void *q;                  /* [num_seqs][q_heads][head_dim]                                    */
+    int64_t q_seq_stride, q_head_stride;
+    void   *out;                    /* same shape; may be q                                             */
+    int64_t out_seq_stride, out_head_stride;
+    float  *lse;                    /* [num_seqs][q_heads], natural logarithm, or NULL                  */
+    const int32_t *block_tables;    /* [num_seqs][table_width]; entries of slots >= lens[i] are not read */
+    int64_t table_stride;
+    const int32_t *lens;            /* [num_seqs], with the new token                                   */
+    const float *weights_in;        /* [num_seqs][kv_heads][>= max_len], or NULL = 0; may be weights_out */
+    float  *weights_out;            /* or NULL: not wanted.  Slots >= lens[i] are not written           */
+    int64_t w_seq_stride, w_head_stride;   /* of both                                                   */
+} kv_attend_args_t;
+int32_t kv_attend(kv_ops_t *ops, const kv_cache_t *cache, const kv_attend_args_t *args);
+/* Bytes of workspace that such a call uses (its pointers are not looked at). */
+int32_t kv_attend_workspace(kv_ops_t *ops, const kv_cache_t *cache, const kv_attend_args_t *args, int64_t *bytes);
+
+/*
+ * New tokens into the cache.  Token j of sequence i's n_i new ones goes to slot lens[i] - n_i + j.  Frequency f <
+ * rotary_dim/2 turns by positions[axis_of[f]][token] * inv_freq[f] (time, height and width of a patch as three
+ * axes, equal for text; one axis: plain rotary positions), the product taken exactly and reduced in float64:
+ *     (x, y) -> (x cos - y sin, x sin + y cos),   x, y = elements f and f + rotary_dim/2, or 2f and 2f + 1
+ * for every head of q and k; elements from rotary_dim on pass unchanged.  q_out = turned q, K = turned k, V = v.
+ * weights[i][h][slot] = 0 and order[i][h][slot] = the token's number, where given.  A sequence of length 0 (an idle
+ * place of a batch of fixed size) gets its q turned and nothing written.
+ */
+typedef struct {
+    int32_t layer, num_seqs, q_heads;
+    int32_t rotary_dim;             /* even, at most head_dim; 0 = no rotation                          */
+    int32_t pair_style;             /* 0: elements f and f + rotary_dim/2, 1: elements 2f and 2f + 1    */
+    int32_t num_axes;               /* 1 .. 4                                                           */
+    int64_t num_tokens;             /* of all sequences together                                        */
+    const void *q, *k, *v;          /* [num_tokens][heads][head_dim]; q may be NULL                     */
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    void   *q_out;                  /* may be q                                                         */
+    int64_t qo_token_stride, qo_head_stride;
+    const int32_t *positions;       /* [num_axes][num_tokens], rows axis_stride apart                   */
+    int64_t axis_stride;
+    const float *inv_freq;          /* [rotary_dim/2]                                                   */
+    const int32_t *seq_starts;      /* [num_seqs + 1]: sequence i has tokens seq_starts[i] .. seq_starts[i+1]-1;
+                                       NULL: one token each (num_tokens = num_seqs)                     */
+    const int32_t *block_tables;    /* [num_seqs][table_width]                                          */
+    int64_t table_stride;
+    const int32_t *lens;            /* [num_seqs], with the new tokens                                  */
+    int32_t table_width, pad_;
+    float   *weights;               /* [num_seqs][kv_heads][slots] or NULL                              */
+    int32_t *order;                 /* [num_seqs][kv_heads][slots] or NULL; both with the strides below */
+    int64_t m_seq_stride, m_head_stride;
+    const int32_t *token_order;     /* [num_tokens]: what goes into order; NULL = positions of axis 0   */
+    uint8_t axis_of[128];           /* HOST, by value: axis of each frequency                           */
+} kv_append_args_t;
+int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t *args);
+
+/*
+ * Eviction by accumulated attention weight, in all layers first_layer .. first_layer + num_layers - 1 at once.  Each
+ * (layer, sequence, KV head) with more than `keep` slots keeps `keep` of them: first the protected ones (order[s] >=
+ * seen[i] - recent: the newest, or order[s] < sink: the first), then those with the largest weights; equals go to
+ * the lower slot, NaN counts less than any number.  Kept slots at or above `keep` move, in ascending order, into the
+ * evicted slots below it, also ascending; the others stay where they are.  (Attention does not mind the order of
+ * the slots, so nothing else needs to move.)  K and V rows move in place; weights and ages of the kept slots go to
+ * weights_out / order_out, or move in place.  Rows from `keep` on stay as they were.  New lengths: min(lens[i], keep).
+ * The blocks from ceil(keep/block_size) on are no longer used; kv_req_shrink tells the block table.
+ */
+typedef struct {
+    int32_t first_layer, num_layers, num_seqs, keep;
+    int32_t recent, sink;           /* recent + sink <= keep                                            */
+    int64_t max_len;                /* HOST bound of lens                                               */
+    const int32_t *block_tables;    /* [num_seqs][table_width]                                          */
+    int64_t table_stride;
+    const int32_t *lens;            /* [num_seqs]                                                       */
+    int32_t table_width, pad_;
+    const float *weights;           /* [num_layers][num_seqs][kv_heads][>= max_len]                     */
+    const int32_t *order;           /* same shape and strides, or NULL: a slot's own number             */
+    int64_t m_layer_stride, m_seq_stride, m_head_stride;
+    const int32_t *seen;            /* [num_seqs]: number the next token will get; NULL: lens           */
+    float   *weights_out;           /* [num_layers][num_seqs][kv_heads][>= keep], or NULL: in place     */
+    int32_t *order_out;             /* likewise; needs order                                            */
+    int64_t o_layer_stride, o_seq_stride, o_head_stride;
+    int32_t *lens_out;              /* [num_seqs] or NULL; not lens itself                              */
+} kv_evict_args_t;
+int32_t kv_evict(kv_ops_t *ops, const kv_cache_t *cache, const kv_evict_args_t *args);
+int32_t kv_evict_workspace(kv_ops_t *ops, const kv_cache_t *cache, const kv_evict_args_t *args, int64_t *bytes);
+
+/* The request's cache was made smaller on the device (kv_evict): it now has `tokens` tokens (1 .. its present
+ * number), its blocks beyond them become free, and every host copy is stale, since rows have moved.  The request must
+ * be on the GPU, and the kernels that moved the rows must have finished (kv_ops_sync): released blocks may be
+ * swapped into at once.  Eager copies issued before the rows moved are the caller's to order (kv_stream_wait
+ * before kv_evict). */
+int32_t kv_req_shrink(kv_table_t *table, int64_t req, int64_t tokens);
+
 #ifdef __cplusplus
 }
 #endif

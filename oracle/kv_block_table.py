@@ -98,6 +98,19 @@ class BlockTableModel:
         self.cursor = self.cursor % len(self.order) if self.order else 0
         return OK
 
+    def shrink(self, rid, tokens):
+        """The request keeps `tokens` tokens; rows have moved, so the content of every block left is a new version."""
+        r = self.reqs.get(rid)
+        if r is None or not r.on_gpu or tokens < 1 or tokens > r.tokens:
+            return ERR_INVALID_ARG
+        n = self.nblocks(tokens)
+        self.free_gpu += len(r.version) - n
+        self.free_host += sum(1 for v in r.host_version[n:] if v is not None)
+        r.version = [v + 1 for v in r.version[:n]]
+        r.host_version = r.host_version[:n]
+        r.tokens = tokens
+        return OK
+
     # ---- background copies of full blocks
     def eager(self, max_blocks):
         """Returns the list of (request, logical block) copied to host memory in this step."""

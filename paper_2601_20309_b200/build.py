@@ -1,7 +1,8 @@
 """Compile the CUDA library for sm_100a with nvcc, in-tree.
 
 ``build()`` produces ``paper_2601_20309_b200/libduplexkv.so`` from ``csrc/duplexkv.cu``
-(kernels in ``csrc/kv_kernels.cuh``) and ``csrc/kv_table.cu`` (block table, host code) and ``libkvtestutil.so`` from ``csrc/kv_testutil.cu``
+(kernels in ``csrc/kv_kernels.cuh``), ``csrc/kv_table.cu`` (block table, host code) and ``csrc/kv_ops.cu``
+(operators on the device cache; kernels in ``csrc/kv_{attend,append,evict}.cuh``), and ``libkvtestutil.so`` from ``csrc/kv_testutil.cu``
 (pool fill / checksum helpers used by tests and the bench to make and check inputs; not
 part of the rotation path).  nvcc cross-compiles without a GPU.
 """
@@ -36,8 +37,9 @@ def _stale(target: str, sources) -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     # (target, files to compile, further files the target depends on)
-    main_src = [os.path.join(CSRC, "duplexkv.cu"), os.path.join(CSRC, "kv_table.cu")]
-    main_dep = [os.path.join(CSRC, "kv_kernels.cuh"), os.path.join(os.path.dirname(HERE), "include", "duplexkv.h")]
+    main_src = [os.path.join(CSRC, "duplexkv.cu"), os.path.join(CSRC, "kv_table.cu"), os.path.join(CSRC, "kv_ops.cu")]
+    main_dep = [os.path.join(CSRC, f) for f in ("kv_kernels.cuh", "kv_ops.cuh", "kv_attend.cuh", "kv_append.cuh", "kv_evict.cuh")]
+    main_dep += [os.path.join(os.path.dirname(HERE), "include", "duplexkv.h")]
     jobs = [(LIB, main_src, main_dep)]
     util_src = os.path.join(CSRC, "kv_testutil.cu")
     if os.path.exists(util_src):

@@ -1941,6 +1941,15 @@ int32_t kv_pool_shape(kv_pool_t *p, kv_pool_shape_t *out)
     return KV_OK;
 }
 
+int32_t kv_pool_cache(kv_pool_t *p, int32_t dtype, kv_cache_t *out)
+{
+    if (!p || !out) return KV_ERR_INVALID_ARG;
+    if (dtype != KV_DT_BF16 && dtype != KV_DT_F16) return fail(p, KV_ERR_INVALID_ARG, "unknown element type");
+    *out = kv_cache_t{p->dev, p->cfg.num_layers, p->cfg.block_size, p->cfg.kv_heads, p->cfg.head_dim, p->cfg.num_gpu_blocks,
+                      p->cfg.device_layout, dtype};
+    return KV_OK;
+}
+
 int32_t kv_host_ptr(kv_pool_t *p, void **base, int64_t *bytes)
 {
     if (!p || !base || !bytes) return KV_ERR_INVALID_ARG;

@@ -1,0 +1,388 @@
+// Host side of the operators on the device cache: argument checks, workspace, launches.
+#include "../../include/duplexkv.h"
+
+#include <algorithm>
+#include <cstdio>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "kv_append.cuh"
+#include "kv_attend.cuh"
+#include "kv_evict.cuh"
+
+struct kv_ops {
+    int device = 0, sms = 0;
+    cudaStream_t stream = nullptr;
+    uint8_t *ws = nullptr;
+    size_t ws_bytes = 0;
+    std::vector<void *> outgrown;    // earlier workspaces: captured graphs may hold them
+    unsigned *status_host = nullptr, *status_dev = nullptr;
+    int32_t sticky = KV_OK;
+    char err[256];
+};
+
+namespace {
+
+char g_ops_err[256] = "no error";
+
+int32_t fail(kv_ops *o, int32_t code, const char *msg)
+{
+    snprintf(o ? o->err : g_ops_err, 256, "%s", msg);
+    return code;
+}
+
+int32_t fail_cuda(kv_ops *o, cudaError_t e, const char *what)
+{
+    (void)cudaGetLastError();
+    snprintf(o ? o->err : g_ops_err, 256, "%s: %s", what, cudaGetErrorString(e));
+    if (o && o->sticky == KV_OK) o->sticky = KV_ERR_CUDA;
+    return KV_ERR_CUDA;
+}
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t align256(int64_t a) { return (a + 255) / 256 * 256; }
+
+int32_t grow_workspace(kv_ops *o, int64_t bytes)
+{
+    if (bytes < 0) return fail(o, KV_ERR_INVALID_ARG, "negative size");
+    if ((size_t)bytes <= o->ws_bytes) return KV_OK;
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(o->stream, &st) != cudaSuccess) (void)cudaGetLastError();
+    if (st != cudaStreamCaptureStatusNone) return fail(o, KV_ERR_NOMEM, "the workspace cannot grow during stream capture: kv_ops_reserve it first");
+    const size_t want = std::max<size_t>((size_t)bytes, o->ws_bytes + o->ws_bytes / 2);
+    void *p = nullptr;
+    try {
+        o->outgrown.reserve(o->outgrown.size() + 1);
+    } catch (...) {
+        return fail(o, KV_ERR_NOMEM, "out of host memory");
+    }
+    if (cudaMalloc(&p, want) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return fail(o, KV_ERR_NOMEM, "no device memory for the operators' workspace");
+    }
+    if (o->ws) o->outgrown.push_back(o->ws);
+    o->ws = (uint8_t *)p;
+    o->ws_bytes = want;
+    return KV_OK;
+}
+
+// the checks that all calls share, and the address rule
+int32_t make_view(kv_ops *o, const kv_cache_t *c, KvView &v)
+{
+    if (!c || !c->device_base) return fail(o, KV_ERR_INVALID_ARG, "no cache");
+    if (c->num_layers <= 0 || c->block_size <= 0 || c->kv_heads <= 0 || c->head_dim <= 0 || c->num_gpu_blocks <= 0 || c->num_gpu_blocks > INT32_MAX)
+        return fail(o, KV_ERR_INVALID_ARG, "bad cache shape");
+    if (c->device_layout != KV_DEV_LAYER_FIRST && c->device_layout != KV_DEV_BLOCK_FIRST) return fail(o, KV_ERR_INVALID_ARG, "unknown device layout");
+    if (c->dtype != KV_DT_BF16 && c->dtype != KV_DT_F16) return fail(o, KV_ERR_INVALID_ARG, "unknown element type");
+    if (c->head_dim % 8 || c->head_dim > 256) return fail(o, KV_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most 256");
+    if ((uintptr_t)c->device_base % 16) return fail(o, KV_ERR_INVALID_ARG, "the cache must be 16-byte aligned");
+    const int64_t row = (int64_t)c->kv_heads * c->head_dim * 2, seg = row * c->block_size;
+    if (seg > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "a plane of one block exceeds 2 GiB");
+    v.base = (uint8_t *)c->device_base;
+    v.blk_stride = c->device_layout == KV_DEV_BLOCK_FIRST ? seg * 2 * c->num_layers : seg;
+    v.plane_stride = c->device_layout == KV_DEV_BLOCK_FIRST ? seg : seg * c->num_gpu_blocks;
+    v.row_stride = (int)row;
+    v.head_stride = c->head_dim * 2;
+    v.bs = c->block_size;
+    v.nb = (int)c->num_gpu_blocks;
+    v.heads = c->kv_heads;
+    v.dim = c->head_dim;
+    v.status = o->status_dev;
+    return KV_OK;
+}
+
+int32_t set_tables(kv_ops *o, KvView &v, const int32_t *tables, int64_t stride, int32_t width, const int32_t *lens, int64_t max_len)
+{
+    if (!tables || !lens) return fail(o, KV_ERR_INVALID_ARG, "block_tables and lens are needed");
+    if (width <= 0 || stride < 0) return fail(o, KV_ERR_INVALID_ARG, "bad block table shape");
+    if (max_len < 0 || max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
+    if (max_len > (int64_t)width * v.bs) return fail(o, KV_ERR_INVALID_ARG, "the block tables are too narrow for max_len");
+    v.tables = tables;
+    v.table_stride = stride;
+    v.lens = lens;
+    v.max_len = max_len;
+    return KV_OK;
+}
+
+int32_t launched(kv_ops *o, const char *what)
+{
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? KV_OK : fail_cuda(o, e, what);
+}
+
+// ---- attend
+
+struct AttendPlan {
+    int64_t scores, lse, total;
+};
+
+int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, KvAttend &k, AttendPlan &p)
+{
+    if (!a) return fail(o, KV_ERR_INVALID_ARG, "no arguments");
+    int32_t rc = make_view(o, c, k.c);
+    if (rc != KV_OK) return rc;
+    if (a->layer < 0 || a->layer >= c->num_layers) return fail(o, KV_ERR_RANGE, "no such layer");
+    if (a->num_seqs < 0 || a->num_seqs > 65535 || a->q_heads <= 0 || a->window < 0) return fail(o, KV_ERR_INVALID_ARG, "bad count");
+    if (a->q_heads % c->kv_heads) return fail(o, KV_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
+    if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
+    p.scores = 0;
+    p.lse = align256((int64_t)a->num_seqs * a->q_heads * a->max_len * 4);
+    p.total = p.lse + (int64_t)a->num_seqs * a->q_heads * 4;
+    return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char *kv_ops_last_error(kv_ops_t *o) { return o ? o->err : g_ops_err; }
+
+int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out)
+{
+    if (!out) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
+    *out = nullptr;
+    cudaError_t e = cudaSetDevice(device_id);
+    if (e != cudaSuccess) return fail_cuda(nullptr, e, "cudaSetDevice");
+    kv_ops *o = new (std::nothrow) kv_ops();
+    if (!o) return fail(nullptr, KV_ERR_NOMEM, "out of host memory");
+    o->device = device_id;
+    o->stream = (cudaStream_t)stream;
+    snprintf(o->err, 256, "no error");
+    e = cudaDeviceGetAttribute(&o->sms, cudaDevAttrMultiProcessorCount, device_id);
+    if (e == cudaSuccess) e = cudaHostAlloc((void **)&o->status_host, 64, cudaHostAllocMapped);
+    if (e == cudaSuccess) {
+        *o->status_host = 0;
+        e = cudaHostGetDevicePointer((void **)&o->status_dev, o->status_host, 0);
+    }
+    if (e != cudaSuccess) {
+        const int32_t rc = fail_cuda(nullptr, e, "kv_ops_create");
+        if (o->status_host) cudaFreeHost(o->status_host);
+        delete o;
+        return rc;
+    }
+    *out = o;
+    return KV_OK;
+}
+
+int32_t kv_ops_destroy(kv_ops_t *o)
+{
+    if (!o) return KV_ERR_INVALID_ARG;
+    (void)cudaStreamSynchronize(o->stream);
+    if (o->ws) cudaFree(o->ws);
+    for (void *p : o->outgrown) cudaFree(p);
+    if (o->status_host) cudaFreeHost(o->status_host);
+    (void)cudaGetLastError();
+    delete o;
+    return KV_OK;
+}
+
+int32_t kv_ops_reserve(kv_ops_t *o, int64_t bytes)
+{
+    if (!o) return KV_ERR_INVALID_ARG;
+    return grow_workspace(o, bytes);
+}
+
+int32_t kv_ops_sync(kv_ops_t *o)
+{
+    if (!o) return KV_ERR_INVALID_ARG;
+    const cudaError_t e = cudaStreamSynchronize(o->stream);
+    if (e != cudaSuccess) return fail_cuda(o, e, "cudaStreamSynchronize");
+    const unsigned st = *(volatile unsigned *)o->status_host;
+    if (st && o->sticky == KV_OK) {
+        o->sticky = KV_ERR_RANGE;
+        snprintf(o->err, 256, "a kernel met %s and skipped it (status 0x%x)",
+                 st & KV_OPS_BAD_BLOCK ? "a block id outside the cache" : "a length outside its bounds", st);
+    }
+    return o->sticky;
+}
+
+int32_t kv_attend_workspace(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *args, int64_t *bytes)
+{
+    if (!o || !bytes) return fail(o, KV_ERR_INVALID_ARG, "null argument");
+    KvAttend k;
+    AttendPlan p;
+    const int32_t rc = plan_attend(o, cache, args, k, p);
+    if (rc == KV_OK) *bytes = p.total;
+    return rc;
+}
+
+int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *a)
+{
+    if (!o) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
+    KvAttend k;
+    AttendPlan p;
+    int32_t rc = plan_attend(o, cache, a, k, p);
+    if (rc != KV_OK) return rc;
+    if (a->num_seqs == 0) return KV_OK;
+    if (!a->q || !a->out) return fail(o, KV_ERR_INVALID_ARG, "q and out are needed");
+    if (a->weights_in && !a->weights_out) return fail(o, KV_ERR_INVALID_ARG, "weights_in without weights_out");
+    if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens, a->max_len)) != KV_OK) return rc;
+    if ((rc = grow_workspace(o, p.total)) != KV_OK) return rc;
+    k.layer = a->layer;
+    k.q_heads = a->q_heads;
+    k.group = a->q_heads / cache->kv_heads;
+    k.window = a->window;
+    k.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cache->head_dim);
+    k.q = a->q;
+    k.q_seq = a->q_seq_stride;
+    k.q_head = a->q_head_stride;
+    k.out = a->out;
+    k.o_seq = a->out_seq_stride;
+    k.o_head = a->out_head_stride;
+    k.lse = a->lse;
+    k.w_in = a->weights_in;
+    k.w_out = a->weights_out;
+    k.w_seq = a->w_seq_stride;
+    k.w_head = a->w_head_stride;
+    k.scores = (float *)(o->ws + p.scores);
+    k.row_lse = (float *)(o->ws + p.lse);
+    const dim3 grid(a->q_heads, a->num_seqs);
+    if (cache->dtype == KV_DT_BF16) kv_attend_rows<__nv_bfloat16><<<grid, 128, 0, o->stream>>>(k);
+    else kv_attend_rows<__half><<<grid, 128, 0, o->stream>>>(k);
+    if (a->weights_out && a->max_len > 0)
+        kv_attend_weights<<<dim3((unsigned)ceil_div(a->max_len, 256), cache->kv_heads, a->num_seqs), 256, 0, o->stream>>>(k);
+    return launched(o, "kv_attend");
+}
+
+int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *a)
+{
+    if (!o) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
+    if (!a) return fail(o, KV_ERR_INVALID_ARG, "no arguments");
+    KvAppend k;
+    int32_t rc = make_view(o, cache, k.c);
+    if (rc != KV_OK) return rc;
+    if (a->layer < 0 || a->layer >= cache->num_layers) return fail(o, KV_ERR_RANGE, "no such layer");
+    if (a->num_seqs < 0 || a->num_tokens < 0 || a->num_tokens > INT32_MAX || (a->q && a->q_heads <= 0)) return fail(o, KV_ERR_INVALID_ARG, "bad count");
+    if (a->rotary_dim < 0 || a->rotary_dim > cache->head_dim || a->rotary_dim % 2) return fail(o, KV_ERR_INVALID_ARG, "rotary_dim must be even, at most head_dim");
+    if (a->pair_style != 0 && a->pair_style != 1) return fail(o, KV_ERR_INVALID_ARG, "unknown pair_style");
+    if (a->num_axes < 1 || a->num_axes > 4) return fail(o, KV_ERR_INVALID_ARG, "num_axes must be 1 to 4");
+    for (int f = 0; f < a->rotary_dim / 2; ++f)
+        if (a->axis_of[f] >= a->num_axes) return fail(o, KV_ERR_RANGE, "axis_of names an axis that positions does not have");
+    if (a->num_tokens == 0 || a->num_seqs == 0) return KV_OK;
+    if (!a->seq_starts && a->num_tokens != a->num_seqs) return fail(o, KV_ERR_INVALID_ARG, "without seq_starts every sequence has one token");
+    if (!a->k || !a->v) return fail(o, KV_ERR_INVALID_ARG, "k and v are needed");
+    if (a->q && !a->q_out) return fail(o, KV_ERR_INVALID_ARG, "q without q_out");
+    if (a->rotary_dim && (!a->positions || !a->inv_freq)) return fail(o, KV_ERR_INVALID_ARG, "rotation needs positions and inv_freq");
+    if (a->order && !a->token_order && !a->positions) return fail(o, KV_ERR_INVALID_ARG, "order needs token_order or positions");
+    if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens,
+                         std::min<int64_t>((int64_t)a->table_width * cache->block_size, INT32_MAX / 2))) != KV_OK) return rc;
+    k.layer = a->layer;
+    k.num_seqs = a->num_seqs;
+    k.q_heads = a->q_heads;
+    k.rotary = a->rotary_dim;
+    k.pairs_style = a->pair_style;
+    k.q = a->q;
+    k.k = a->k;
+    k.v = a->v;
+    k.q_tok = a->q_token_stride;
+    k.q_head = a->q_head_stride;
+    k.k_tok = a->k_token_stride;
+    k.k_head = a->k_head_stride;
+    k.v_tok = a->v_token_stride;
+    k.v_head = a->v_head_stride;
+    k.q_out = a->q_out;
+    k.qo_tok = a->qo_token_stride;
+    k.qo_head = a->qo_head_stride;
+    k.positions = a->positions;
+    k.axis_stride = a->axis_stride;
+    k.inv_freq = a->inv_freq;
+    k.starts = a->seq_starts;
+    k.weights = a->weights;
+    k.order = a->order;
+    k.m_seq = a->m_seq_stride;
+    k.m_head = a->m_head_stride;
+    k.token_order = a->token_order;
+    memcpy(k.axis_of, a->axis_of, sizeof(k.axis_of));
+    if (cache->dtype == KV_DT_BF16) kv_append_tokens<__nv_bfloat16><<<(unsigned)a->num_tokens, 128, 0, o->stream>>>(k);
+    else kv_append_tokens<__half><<<(unsigned)a->num_tokens, 128, 0, o->stream>>>(k);
+    return launched(o, "kv_append");
+}
+
+}  // extern "C"
+
+namespace {
+
+struct EvictPlan {
+    int64_t problems, cap, count, holes, srcs, total;
+};
+
+int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvEvict &k, EvictPlan &p)
+{
+    if (!a) return fail(o, KV_ERR_INVALID_ARG, "no arguments");
+    int32_t rc = make_view(o, c, k.c);
+    if (rc != KV_OK) return rc;
+    if (a->num_layers < 0 || a->num_seqs < 0 || a->num_seqs > 65535 || a->num_layers > 65535 || a->keep < 1 || a->recent < 0 || a->sink < 0)
+        return fail(o, KV_ERR_INVALID_ARG, "bad count");
+    if (a->first_layer < 0 || (int64_t)a->first_layer + a->num_layers > c->num_layers) return fail(o, KV_ERR_RANGE, "no such layers");
+    if ((int64_t)a->recent + a->sink > a->keep) return fail(o, KV_ERR_INVALID_ARG, "recent + sink exceeds keep");
+    if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
+    p.problems = (int64_t)a->num_layers * a->num_seqs * c->kv_heads;
+    p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
+    p.count = 0;
+    p.holes = align256(p.problems * 4);
+    p.srcs = p.holes + align256(p.problems * p.cap * 4);
+    p.total = p.srcs + p.problems * p.cap * 4;
+    if (p.problems > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
+    return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t kv_evict_workspace(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *args, int64_t *bytes)
+{
+    if (!o || !bytes) return fail(o, KV_ERR_INVALID_ARG, "null argument");
+    KvEvict k;
+    EvictPlan p;
+    const int32_t rc = plan_evict(o, cache, args, k, p);
+    if (rc == KV_OK) *bytes = p.total;
+    return rc;
+}
+
+int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
+{
+    if (!o) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
+    KvEvict k;
+    EvictPlan p;
+    int32_t rc = plan_evict(o, cache, a, k, p);
+    if (rc != KV_OK) return rc;
+    if (p.problems == 0) return KV_OK;
+    if (!a->weights) return fail(o, KV_ERR_INVALID_ARG, "weights are needed");
+    if (a->order_out && !a->order) return fail(o, KV_ERR_INVALID_ARG, "order_out without order");
+    if (a->order && !a->order_out != !a->weights_out) return fail(o, KV_ERR_INVALID_ARG, "weights and order go to outputs both, or are both changed in place");
+    if (a->order && a->weights_out && (a->weights_out == a->weights) != (a->order_out == a->order))
+        return fail(o, KV_ERR_INVALID_ARG, "weights and order go to outputs both, or are both changed in place");
+    if (a->lens_out == a->lens) return fail(o, KV_ERR_INVALID_ARG, "lens_out must not be lens");
+    if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens, a->max_len)) != KV_OK) return rc;
+    if ((rc = grow_workspace(o, p.total)) != KV_OK) return rc;
+    k.first_layer = a->first_layer;
+    k.layers = a->num_layers;
+    k.seqs = a->num_seqs;
+    k.keep = a->keep;
+    k.recent = a->recent;
+    k.sink = a->sink;
+    k.w = a->weights;
+    k.order = a->order;
+    k.m_layer = a->m_layer_stride;
+    k.m_seq = a->m_seq_stride;
+    k.m_head = a->m_head_stride;
+    k.seen = a->seen;
+    const bool apart = a->weights_out && a->weights_out != a->weights;
+    k.w_out = apart ? a->weights_out : (float *)a->weights;
+    k.order_out = apart ? a->order_out : (int *)a->order;
+    k.o_layer = apart ? a->o_layer_stride : a->m_layer_stride;
+    k.o_seq = apart ? a->o_seq_stride : a->m_seq_stride;
+    k.o_head = apart ? a->o_head_stride : a->m_head_stride;
+    k.lens_out = a->lens_out;
+    k.count = (int *)(o->ws + p.count);
+    k.holes = (int *)(o->ws + p.holes);
+    k.srcs = (int *)(o->ws + p.srcs);
+    k.cap = (int)p.cap;
+    kv_evict_select<<<dim3(cache->kv_heads, a->num_seqs, a->num_layers), EV_THREADS, 0, o->stream>>>(k);
+    if (p.cap > 0) kv_evict_move<<<dim3((unsigned)p.problems, (unsigned)std::min<int64_t>(ceil_div(p.cap, 32), 64)), 256, 0, o->stream>>>(k);
+    return launched(o, "kv_evict");
+}
+
+}  // extern "C"

@@ -558,6 +558,33 @@ int32_t kv_req_finish(kv_table_t *t, int64_t req)
     return KV_OK;
 }
 
+int32_t kv_req_shrink(kv_table_t *t, int64_t req, int64_t tokens)
+{
+    if (!t) return KV_ERR_INVALID_ARG;
+    TReq *r = find(t, req);
+    if (!r) return tfail(t, KV_ERR_INVALID_ARG, "unknown request");
+    if (!r->on_gpu) return tfail(t, KV_ERR_INVALID_ARG, "only a request that is on the GPU can shrink");
+    if (tokens < 1 || tokens > r->tokens) return tfail(t, KV_ERR_INVALID_ARG, "a request shrinks to between one token and its present number");
+    const TPending seq = now(t);                    // an eager copy of its blocks may still be in flight
+    const size_t want = (size_t)blocks_for(t, tokens);
+    try {
+        while (r->blocks.size() > want) {           // from the back, so that running out of memory leaves a shorter, whole request
+            TBlock &b = r->blocks.back();
+            b.host_valid = false;
+            if (b.h >= 0) t->host_free.give(b.h);
+            b.h = -1;
+            release_gpu(t, b.g, seq);
+            r->blocks.pop_back();
+            r->tokens = std::min(r->tokens, (int64_t)r->blocks.size() * t->block_size);
+        }
+    } catch (...) {
+        return tfail(t, KV_ERR_NOMEM, "out of host memory");
+    }
+    r->tokens = tokens;
+    for (auto &b : r->blocks) b.host_valid = false; // rows moved: what the host holds is no longer the block's content
+    return KV_OK;
+}
+
 int32_t kv_req_info(kv_table_t *t, int64_t req, kv_req_info_t *out)
 {
     if (!t || !out) return KV_ERR_INVALID_ARG;
