@@ -19,6 +19,7 @@ struct kv_ops {
     std::vector<void *> outgrown;    // earlier workspaces: captured graphs may hold them
     unsigned *status_host = nullptr, *status_dev = nullptr;
     int32_t sticky = KV_OK;
+    bool attend_ready[2][3][2] = {};   // [bf16][head dimension][query tiles]: shared-memory limit raised
     char err[256];
 };
 
@@ -114,8 +115,14 @@ int32_t launched(kv_ops *o, const char *what)
 // ---- attend
 
 struct AttendPlan {
-    int64_t scores, lse, total;
+    int dp, nt, warps;                       // kernel shape: padded head dimension, tiles of 8 query heads, warps per CTA
+    size_t smem;
+    int64_t lse, part_ml, part_o, total;     // workspace offsets (the scores lie at 0)
 };
+
+constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, less the kernel's static share
+constexpr int ATTEND_ALONE_STEPS = 8;                // rows of up to this many steps are never split
+constexpr int ATTEND_MIN_STEPS = 4;
 
 int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, KvAttend &k, AttendPlan &p)
 {
@@ -125,11 +132,43 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     if (a->layer < 0 || a->layer >= c->num_layers) return fail(o, KV_ERR_RANGE, "no such layer");
     if (a->num_seqs < 0 || a->num_seqs > 65535 || a->q_heads <= 0 || a->window < 0) return fail(o, KV_ERR_INVALID_ARG, "bad count");
     if (a->q_heads % c->kv_heads) return fail(o, KV_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
+    if (a->q_heads / c->kv_heads > KV_MAX_GROUP || c->kv_heads > 65535) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
     if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
-    p.scores = 0;
-    p.lse = align256((int64_t)a->num_seqs * a->q_heads * a->max_len * 4);
-    p.total = p.lse + (int64_t)a->num_seqs * a->q_heads * 4;
+    k.group = a->q_heads / c->kv_heads;
+    p.dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    p.nt = k.group <= 8 ? 1 : 2;
+    const int most = p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
+    k.hc = 1;
+    for (int d = 2; d <= most; ++d)
+        if (c->kv_heads % d == 0) k.hc = d;
+    k.tw = 1;
+    while (k.hc * k.tw * 2 <= most) k.tw *= 2;
+    p.warps = k.hc * k.tw;
+    k.head_chunks = c->kv_heads / k.hc;
+    k.group_chunks = (int)ceil_div(k.group, 8 * p.nt);
+    const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * p.nt * (p.dp / 16 + 1) * 4 * 32 * 4 : 0;
+    const int64_t stage = (int64_t)p.warps * 64 * p.dp;
+    k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
+    // rows of few steps are not worth a second kernel; several query-head chunks would all add to the same weights
+    const int64_t longest = ceil_div(a->max_len + 15, 16 * k.tw);
+    const bool split = longest > ATTEND_ALONE_STEPS || (a->weights_out && k.group_chunks > 1);
+    if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
+    p.smem = (size_t)(k.stages * stage + box);
+    k.pieces = split ? o->sms : 0;
+    k.min_steps = ATTEND_MIN_STEPS;
+    const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
+    p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
+    p.part_ml = p.lse + align256((int64_t)a->num_seqs * a->q_heads * 4);
+    p.part_o = p.part_ml + align256(parts * 8);
+    p.total = p.part_o + parts * c->head_dim * 4;
     return KV_OK;
+}
+
+template <typename T> const void *attend_kernel(int dp, int nt)
+{
+    if (dp == 64) return nt == 1 ? (const void *)kv_attend_stream<T, 64, 1> : (const void *)kv_attend_stream<T, 64, 2>;
+    if (dp == 128) return nt == 1 ? (const void *)kv_attend_stream<T, 128, 1> : (const void *)kv_attend_stream<T, 128, 2>;
+    return nt == 1 ? (const void *)kv_attend_stream<T, 256, 1> : (const void *)kv_attend_stream<T, 256, 2>;
 }
 
 }  // namespace
@@ -220,13 +259,14 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens, a->max_len)) != KV_OK) return rc;
     if ((rc = grow_workspace(o, p.total)) != KV_OK) return rc;
     k.layer = a->layer;
+    k.seqs = a->num_seqs;
     k.q_heads = a->q_heads;
-    k.group = a->q_heads / cache->kv_heads;
     k.window = a->window;
-    k.scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cache->head_dim);
+    k.scale2 = (a->scale != 0.f ? a->scale : 1.f / sqrtf((float)cache->head_dim)) * 1.44269504088896340736f;
     k.q = a->q;
     k.q_seq = a->q_seq_stride;
     k.q_head = a->q_head_stride;
+    k.q_pairs = (uintptr_t)a->q % 4 == 0 && a->q_seq_stride % 2 == 0 && a->q_head_stride % 2 == 0;
     k.out = a->out;
     k.o_seq = a->out_seq_stride;
     k.o_head = a->out_head_stride;
@@ -235,14 +275,39 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.w_out = a->weights_out;
     k.w_seq = a->w_seq_stride;
     k.w_head = a->w_head_stride;
-    k.scores = (float *)(o->ws + p.scores);
+    k.scores = a->weights_out ? (float *)o->ws : nullptr;
     k.row_lse = (float *)(o->ws + p.lse);
-    const dim3 grid(a->q_heads, a->num_seqs);
-    if (cache->dtype == KV_DT_BF16) kv_attend_rows<__nv_bfloat16><<<grid, 128, 0, o->stream>>>(k);
-    else kv_attend_rows<__half><<<grid, 128, 0, o->stream>>>(k);
-    if (a->weights_out && a->max_len > 0)
-        kv_attend_weights<<<dim3((unsigned)ceil_div(a->max_len, 256), cache->kv_heads, a->num_seqs), 256, 0, o->stream>>>(k);
-    return launched(o, "kv_attend");
+    k.part_ml = (float2 *)(o->ws + p.part_ml);
+    k.part_o = (float *)(o->ws + p.part_o);
+
+    const bool bf16 = cache->dtype == KV_DT_BF16;
+    const void *kernel = bf16 ? attend_kernel<__nv_bfloat16>(p.dp, p.nt) : attend_kernel<__half>(p.dp, p.nt);
+    bool &ready = o->attend_ready[bf16][p.dp / 128][p.nt - 1];
+    if (!ready) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(227 * 1024 - 4096));
+        if (e != cudaSuccess) return fail_cuda(o, e, "cudaFuncSetAttribute");
+        ready = true;
+    }
+    void *params[] = {&k};
+    const unsigned rows = (unsigned)(k.seqs * k.head_chunks * k.group_chunks);
+    cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3(p.warps * 32), params, p.smem, o->stream);
+    if (e != cudaSuccess) return fail_cuda(o, e, "kv_attend");
+    if (k.pieces) {
+        // programmatic dependent launch: the join's CTAs come up while the last of the stream's finish
+        cudaLaunchAttribute early;
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        const int64_t tiles = a->weights_out ? ceil_div(a->max_len, KV_JOIN_SLOTS) : 0;
+        cfg.gridDim = dim3((unsigned)std::max<int64_t>(k.group, tiles), cache->kv_heads, k.seqs);
+        cfg.blockDim = dim3(KV_JOIN_THREADS);
+        cfg.stream = o->stream;
+        cfg.attrs = &early;
+        cfg.numAttrs = 1;
+        e = bf16 ? cudaLaunchKernelEx(&cfg, kv_attend_join<__nv_bfloat16>, k, 8 * p.nt) : cudaLaunchKernelEx(&cfg, kv_attend_join<__half>, k, 8 * p.nt);
+        if (e != cudaSuccess) return fail_cuda(o, e, "kv_attend");
+    }
+    return KV_OK;
 }
 
 int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *a)
