@@ -41,6 +41,7 @@ struct KvAttend {
     int pieces;          // CTAs the line of steps is cut for; 0: every row is one CTA's (no join)
     int min_steps;       // no piece is shorter
     int q_pairs;         // q may be read in pairs of elements
+    int whole_tiles;     // the block size is a multiple of 16: a tile lies in one block
     float *scores;       // [seq][kv_head][max_len][group], base 2; nullptr: no weights wanted
     float *row_lse;      // [seq][q_head], base 2
     float2 *part_ml;     // [piece][2][hc][8*NT]: maximum and sum
@@ -118,48 +119,67 @@ struct KvSpan {
     __device__ __forceinline__ int steps(const KvAttend &a) const { return (n - base + 16 * a.tw - 1) / (16 * a.tw); }
 };
 
-// Sums the steps of one row over the sequences in front of `upto` and over all of them (every thread gets both).
-// Block-wide; `red` holds two values per warp.
-__device__ __forceinline__ void kv_attend_sums(const KvAttend &a, int upto, long long *red, long long &before, long long &all)
-{
-    long long b = 0, s = 0;
-    for (int i = threadIdx.x; i < a.seqs; i += blockDim.x) {
-        const int k = KvSpan(a, i).steps(a);
-        s += k;
-        if (i < upto) b += k;
-    }
+// The line of steps, searched by a whole CTA: every thread sums the steps of a run of sequences.
+struct KvLine {
+    int before, mine, total;         // steps in front of the thread's run, in it, and of all sequences (fewer than 2^31)
+    int lo, hi;
+    // `red` holds one value per warp
+    __device__ __forceinline__ KvLine(const KvAttend &a, int *red)
+    {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows_of_seq = a.head_chunks * a.group_chunks;
+        const int run = (a.seqs + blockDim.x - 1) / blockDim.x;
+        lo = min((int)threadIdx.x * run, a.seqs);
+        hi = min(lo + run, a.seqs);
+        mine = 0;
+        for (int i = lo; i < hi; ++i) mine += KvSpan(a, i).steps(a);
+        mine *= rows_of_seq;
+        int x = mine;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        s += __shfl_xor_sync(~0u, s, o);
-        b += __shfl_xor_sync(~0u, b, o);
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) red[warp] = x;
+        __syncthreads();
+        before = total = 0;
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {
+            if (w < warp) before += red[w];
+            total += red[w];
+        }
+        before += x - mine;
     }
-    const int warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) == 0) {
-        red[threadIdx.x >> 5] = s;
-        red[warps + (threadIdx.x >> 5)] = b;
+    // the sequence, its row and the step in it that step s < total of the line is; `at` holds two values
+    __device__ __forceinline__ void find(const KvAttend &a, int s, int *at, int &i, int &row, int &k) const
+    {
+        const int rows_of_seq = a.head_chunks * a.group_chunks;
+        if (s >= before && s < before + mine) {
+            int j = lo;
+            int left = s - before;
+            for (; j < hi - 1; ++j) {
+                const int n = KvSpan(a, j).steps(a) * rows_of_seq;
+                if (left < n) break;
+                left -= n;
+            }
+            at[0] = j;
+            at[1] = left;
+        }
+        __syncthreads();
+        i = at[0];
+        const int steps = KvSpan(a, i).steps(a);
+        row = at[1] / steps;
+        k = at[1] - row * steps;
     }
-    __syncthreads();
-    before = all = 0;
-    for (int w = 0; w < warps; ++w) {
-        all += red[w];
-        before += red[warps + w];
-    }
-    __syncthreads();
-}
+};
 
-__device__ __forceinline__ long long kv_attend_piece(const KvAttend &a, long long total)
-{
-    const long long q = (total + a.pieces - 1) / a.pieces;
-    return q > a.min_steps ? q : a.min_steps;
-}
+__device__ __forceinline__ int kv_attend_piece(const KvAttend &a, int total) { return max((total + a.pieces - 1) / a.pieces, a.min_steps); }
 
+// 128 registers where that is enough (one query tile, heads of up to 128): the join's CTAs then fit beside this kernel's
 template <typename T, int DP, int NT>
-__global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP * NT <= 128 ? 2 : 1) kv_attend_stream(const __grid_constant__ KvAttend a)
 {
     constexpr int ROW = DP * 2, TILE = 16 * ROW, KS = DP / 16, LANES = DP / 8, PASS = 32 / LANES, HEADS = 8 * NT;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long red[2 * KV_ATTEND_WARPS];
-    __shared__ long long s_at[2];
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ int red[KV_ATTEND_WARPS], s_at[2];
     __shared__ int4 info[KV_ATTEND_WARPS][KV_ATTEND_STAGES];
     __shared__ float s_lse[KV_ATTEND_WARPS][HEADS];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
@@ -178,51 +198,18 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
 
     // ---- this CTA's piece of the line of steps: the row and step it begins at, and how many steps it has
     int pi, pch, pk;                 // sequence, row of the sequence, step: where the next tile to be loaded lies
-    long long todo;
+    int todo;
     if (a.pieces == 0) {
         pi = blockIdx.x / rows_of_seq;
         pch = blockIdx.x % rows_of_seq;
         pk = 0;
         todo = KvSpan(a, pi).steps(a);
     } else {
-        // every thread sums a run of sequences; the one whose run holds the piece's first step walks it
-        const int run = (a.seqs + blockDim.x - 1) / blockDim.x, lo = min(tid * run, a.seqs), hi = min(lo + run, a.seqs);
-        long long mine = 0;
-        for (int i = lo; i < hi; ++i) mine += KvSpan(a, i).steps(a);
-        long long x = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(~0u, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) red[warp] = x;
-        __syncthreads();
-        long long before = 0, total = 0;
-        for (int w = 0; w < warps; ++w) {
-            if (w < warp) before += red[w];
-            total += red[w];
-        }
-        before = (before + x - mine) * rows_of_seq;
-        total *= rows_of_seq;
-        const long long piece = kv_attend_piece(a, total), s0 = blockIdx.x * piece;
-        todo = min(total, s0 + piece) - s0;
+        const KvLine line(a, red);
+        const int piece = kv_attend_piece(a, line.total), s0 = (int)min((long long)blockIdx.x * piece, (long long)line.total);
+        todo = min(line.total - s0, piece);
         if (todo <= 0) return;
-        if (s0 >= before && s0 < before + mine * rows_of_seq) {
-            int i = lo;
-            long long left = s0 - before;
-            for (; i < hi; ++i) {
-                const long long k = (long long)KvSpan(a, i).steps(a) * rows_of_seq;
-                if (left < k) break;
-                left -= k;
-            }
-            s_at[0] = i;
-            s_at[1] = left;
-        }
-        __syncthreads();
-        pi = (int)s_at[0];
-        const int k = KvSpan(a, pi).steps(a);
-        pch = (int)(s_at[1] / k);
-        pk = (int)(s_at[1] % k);
+        line.find(a, s0, s_at, pi, pch, pk);
     }
     if (todo <= 0) return;
 
@@ -230,67 +217,88 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
     const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
     int4 *my_info = info[warp];
 
-    // ---- producer: the next tile's position, its block ids (lane r holds row r's) and what the consumer has to know
-    long long left = todo;
-    int psteps, id = -1, off = 0, t0 = 0, flags = 0, ti = 0, tch = 0;
-    bool live = false;
+    // ---- producer.  The block ids of two tiles of a row are read at once, lane r for row r % 16 of tile r / 16, and used
+    // one tile later, so that no load waits for its address.  With blocks of whole tiles one address serves a tile.
+    int unseen = todo;               // tiles whose ids have not been read
+    int id = -1, off = 0, t0 = 0, ti = 0, tch = 0, have = 0, half = 0, tk = 0, tsteps = 0;
+    unsigned masks = 0;
+    const uint8_t *rowp = a.c.base;
+    bool live = false, exists = false, fresh = true;   // fresh: the next tile begins this CTA's run in its row
+    const int chunk = lane % LANES, chunk_on = chunk * 8 < a.c.dim;
+    const int lane_off = lane / LANES * a.c.row_stride + chunk * 16;
     KvSpan span(a, pi);
-    psteps = span.steps(a);
-    bool fresh = true;               // the tile begins a run of this CTA in its row
+    int psteps = span.steps(a);
     auto peek = [&]() {
-        if (left <= 0) return;
-        const int h = pch / a.group_chunks * a.hc + hw;
+        have = min(min(2, psteps - pk), unseen);
+        half = 0;
+        if (have == 0) return;
         t0 = span.base + (pk * a.tw + way) * 16;
-        const int t = t0 + (lane & 15);
-        live = t >= span.first && t < span.n;
-        id = -1;
-        off = h * a.c.head_stride;
-        if (live) {
-            id = a.c.tables[pi * a.c.table_stride + t / a.c.bs];
-            off += t % a.c.bs * a.c.row_stride;
+        const int tile = t0 + (lane >> 4) * a.tw * 16, t = tile + (lane & 15);
+        live = (lane >> 4) < have && t >= span.first && t < span.n;
+        exists = a.whole_tiles ? (lane >> 4) < have && tile < span.n : live;
+        if (exists) {
+            const int b = t / a.c.bs;
+            id = a.c.tables[pi * a.c.table_stride + b];
+            off = (pch / a.group_chunks * a.hc + hw) * a.c.head_stride + (t - b * a.c.bs) * a.c.row_stride;
         }
         ti = pi;
         tch = pch;
-        flags = (fresh ? 1 << 16 : 0) | (pk == 0 ? 1 << 18 : 0) | (pk == psteps - 1 ? 1 << 19 : 0);
-        fresh = false;
-        --left;
-        if (left == 0 || pk == psteps - 1) flags |= 1 << 17;
-        if (++pk == psteps) {
+        tk = pk;
+        tsteps = psteps;
+        unseen -= have;
+        pk += have;
+        if (pk == psteps && unseen > 0) {
             pk = 0;
-            fresh = true;
             if (++pch == rows_of_seq) {
                 pch = 0;
-                if (left > 0) {
-                    do span = KvSpan(a, ++pi);
-                    while (span.n == 0);
-                    psteps = span.steps(a);
-                }
+                do span = KvSpan(a, ++pi);
+                while (span.n == 0);
+                psteps = span.steps(a);
             }
         }
     };
-    long long unissued = todo;
     int put = 0;
     auto issue = [&]() {
-        if (unissued > 0) {
-            --unissued;
-            const bool ok = live && (unsigned)id < (unsigned)a.c.nb;
-            if (live && !ok) atomicOr(a.c.status, KV_OPS_BAD_BLOCK);
-            const unsigned mask = __ballot_sync(~0u, ok) & 0xffffu;
-            if (lane == 0) my_info[put] = make_int4((int)mask | flags, t0, ti, tch);
-            const unsigned stage = ring + put * 2 * TILE;
-            const int chunk = lane % LANES;
+        if (half < have) {
+            if (half == 0) {
+                const bool known = exists && (unsigned)id < (unsigned)a.c.nb;
+                if (live && !known) atomicOr(a.c.status, KV_OPS_BAD_BLOCK);
+                masks = __ballot_sync(~0u, live && known);
+                rowp = known ? kbase + id * a.c.blk_stride + off : a.c.base;
+            }
+            const unsigned mask = (masks >> (half * 16)) & 0xffffu;
+            const bool ends = tk + half == tsteps - 1;
+            if (lane == 0) {
+                const int flags = (fresh ? 1 << 16 : 0) | (ends || (unseen == 0 && half == have - 1) ? 1 << 17 : 0) | (tk + half == 0 ? 1 << 18 : 0) |
+                                  (ends ? 1 << 19 : 0);
+                my_info[put] = make_int4((int)mask | flags, t0 + half * a.tw * 16, ti, tch);
+            }
+            fresh = ends;
+            unsigned dst = ring + put * 2 * TILE + lane / LANES * ROW;
+            const unsigned on = chunk_on ? mask >> (lane / LANES) : 0u;
+            if (a.whole_tiles) {
+                const uint8_t *src = (const uint8_t *)__shfl_sync(~0u, (unsigned long long)rowp, half * 16) + (mask ? lane_off : 0);
+                const int step = mask ? PASS * a.c.row_stride : 0;
 #pragma unroll
-            for (int j = 0; j < 16 / PASS; ++j) {
-                const int r = j * PASS + lane / LANES;
-                const int rid = __shfl_sync(~0u, id, r), roff = __shfl_sync(~0u, off, r);
-                const bool on = (mask >> r & 1) && chunk * 8 < a.c.dim;
-                const uint8_t *src = on ? kbase + rid * a.c.blk_stride + roff + chunk * 16 : a.c.base;
-                const unsigned dst = stage + r * ROW + ((chunk ^ (r & 7)) << 4);
-                kv_cp16(dst, src, on);
-                kv_cp16(dst + TILE, on ? src + a.c.plane_stride : src, on);
+                for (int j = 0; j < 16 / PASS; ++j, src += step) {
+                    const unsigned to = dst + j * PASS * ROW + ((chunk ^ (j * PASS + lane / LANES) & 7) << 4);
+                    kv_cp16(to, src, on >> (j * PASS) & 1);
+                    kv_cp16(to + TILE, src + a.c.plane_stride, on >> (j * PASS) & 1);
+                }
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < 16 / PASS; ++j) {
+                    const int r = j * PASS + lane / LANES;
+                    const uint8_t *src = (const uint8_t *)__shfl_sync(~0u, (unsigned long long)rowp, half * 16 + r);
+                    const bool row_on = on >> (j * PASS) & 1;
+                    const unsigned to = dst + j * PASS * ROW + ((chunk ^ (r & 7)) << 4);
+                    if (row_on) src += chunk * 16;
+                    kv_cp16(to, src, row_on);
+                    kv_cp16(to + TILE, row_on ? src + a.c.plane_stride : src, row_on);
+                }
             }
             put = put + 1 == a.stages ? 0 : put + 1;
-            peek();
+            if (++half == have) peek();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -302,7 +310,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
     float o[NT][KS][4], m[NT][2], l[NT][2];
     int take = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
-    for (long long n = 0; n < todo; ++n) {
+    for (int n = 0; n < todo; ++n) {
         __syncwarp();                // the stage about to be filled is no longer read
         issue();
         // the tile that is computed now was committed stages - 1 groups ago
@@ -344,22 +352,24 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
             }
         }
         if (mask) {
-            float s[NT][4];
+            float s[NT][4], s2[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-            {
-                const int r = lane & 15, c0 = lane >> 4;
-                const unsigned krow = stage + r * ROW;
+                for (int e = 0; e < 4; ++e) s[nt][e] = s2[nt][e] = 0.f;
+            // chunk 2 ks + c of row r lies at chunk (2 ks + c) ^ (r & 7): with rows aligned to their size, one xor
+            const unsigned krow = stage + (lane & 15) * ROW + ((lane >> 4 ^ lane & 7) << 4);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    unsigned k[4];
-                    kv_ldmatrix(k, krow + (((2 * ks + c0) ^ (r & 7)) << 4));
+            for (int ks = 0; ks < KS; ++ks) {
+                unsigned k[4];
+                kv_ldmatrix(k, krow ^ ks << 5);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) KvMma<T>::mma(s[nt], k, qf[nt][ks][0], qf[nt][ks][1]);
-                }
+                for (int nt = 0; nt < NT; ++nt) KvMma<T>::mma(ks & 1 ? s2[nt] : s[nt], k, qf[nt][ks][0], qf[nt][ks][1]);   // two chains
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] += s2[nt][e];
             const bool lo = mask >> (lane >> 2) & 1, hi = mask >> (8 + (lane >> 2)) & 1;
             unsigned pf[NT][2];
 #pragma unroll
@@ -402,12 +412,11 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[nt][ks][e] *= alpha[e & 1];
             }
-            const int r = (lane & 7) + (lane >> 4) * 8, c0 = lane >> 3 & 1;
-            const unsigned vrow = stage + TILE + r * ROW;
+            const unsigned vrow = stage + TILE + ((lane & 7) + (lane >> 4) * 8) * ROW + ((lane >> 3 & 1 ^ lane & 7) << 4);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 unsigned v[4];
-                kv_ldmatrix_t(v, vrow + (((2 * ks + c0) ^ (r & 7)) << 4));
+                kv_ldmatrix_t(v, vrow ^ ks << 5);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) KvMma<T>::mma(o[nt][ks], v, pf[nt][0], pf[nt][1]);
             }
@@ -537,115 +546,235 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32) kv_attend_stream(const _
     }
 }
 
-// Joins the pieces of rows that more than one CTA worked on, in the order of the slots, and adds up the weights of all
-// rows.  CTA (x, KV head, sequence): query heads x, x + gridDim.x, ... of the group, slots from x * KV_JOIN_SLOTS on.
-constexpr int KV_JOIN_SLOTS = 1024, KV_JOIN_THREADS = 256, KV_MAX_GROUP = 256;
+// ---- join: what is left when rows were split.
+//
+// KV_JOIN_CTAS CTAs per piece.  The first joins output rows: it looks whether the piece begins inside a row; the pieces
+// that cut one row share its output, in units of 32 elements of a head, among them.  The others add up the weights of the
+// piece's slots with the sums of all parts of their rows.  Everything that depends on the lengths alone is done before
+// the wait for the first kernel, beside which these CTAs fit.  After it, every load that can be in flight is: what such
+// a kernel takes is the number of loads that wait for one another, each about a microsecond.
+constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_CTAS = 4, KV_MAX_GROUP = 256;
+
+// maximum and sum of two sets of slots together
+__device__ __forceinline__ void kv_meet(float &top, float &sum, float top2, float sum2)
+{
+    const float t = fmaxf(top, top2), ref = kv_ref(t);
+    sum = sum * kv_exp2(top - ref) + sum2 * kv_exp2(top2 - ref);
+    top = t;
+}
+
+// log2 of a row's sum of exponentials for one query head, from its parts c0 .. c1 or as the finished row left it: by a
+// whole warp (`lanes` 32), or by every thread for itself (`lanes` 1)
+template <int lanes>
+__device__ __forceinline__ float kv_join_lse(const KvAttend &a, int c0, int c1, int hw, int heads_of_chunk, int g, const float *row_lse)
+{
+    if (c0 == c1) return *row_lse;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int c = c0 + (lanes == 1 ? 0 : threadIdx.x & 31); c <= c1; c += lanes) {
+        const float2 ml = a.part_ml[((c * 2 + (c == c0 ? 1 : 0)) * a.hc + hw) * heads_of_chunk + g];
+        kv_meet(top, sum, ml.x, ml.y);
+    }
+#pragma unroll
+    for (int o = lanes / 2; o; o >>= 1) kv_meet(top, sum, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, sum, o));
+    return sum == 0.f ? -INFINITY : top + log2f(sum);
+}
+
+template <int n> struct KvCount { static constexpr int value = n; };
+
+__device__ __forceinline__ void kv_join_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// floats of shared memory the row CTAs need: a factor for every part of every head a CTA shares in (a row of more than
+// eight parts is shared by eight CTAs or more), and a float4 per thread
+__host__ __device__ constexpr int kv_join_floats(int hc, int heads_of_chunk, int pieces)
+{
+    const int few = hc * heads_of_chunk * 8, many = (hc * heads_of_chunk / 8 + 2) * (pieces + 1);
+    return (few > many ? few : many) + 4 * KV_JOIN_THREADS;
+}
 
 template <typename T>
-__global__ void __launch_bounds__(KV_JOIN_THREADS) kv_attend_join(const __grid_constant__ KvAttend a, int heads_of_chunk)
+__device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chunk, int b, int piece, int i, int row, int k, float *smem)
 {
-    __shared__ long long red[2 * KV_JOIN_THREADS / 32];
-    __shared__ float lse2[KV_MAX_GROUP];
-    __shared__ float box[KV_JOIN_THREADS / 32][256];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int x = blockIdx.x, h = blockIdx.y, i = blockIdx.z;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const KvSpan sp(a, i);
-    if (sp.n == 0) return;
-    if (x >= a.group && (!a.scores || x * KV_JOIN_SLOTS >= sp.n)) return;
-    long long before, total;
-    kv_attend_sums(a, i, red, before, total);
-    const int rows_of_seq = a.head_chunks * a.group_chunks, steps = sp.steps(a);
-    before *= rows_of_seq;
-    const long long piece = kv_attend_piece(a, total * rows_of_seq);
-    const int hw = h % a.hc;
-    for (int gc = 0; gc < a.group_chunks; ++gc) {
-        const long long first = before + (long long)(h / a.hc * a.group_chunks + gc) * steps;
-        const long long c0 = first / piece, c1 = (first + steps - 1) / piece;
-        const int heads = min(heads_of_chunk, a.group - gc * heads_of_chunk);
-        // the parts of this row: the first is its CTA's second, all others their CTA's first
-        auto part = [&](long long c) { return ((c * 2 + (c == c0 ? 1 : 0)) * a.hc + hw) * heads_of_chunk; };
-        for (int g = warp; g < heads; g += KV_JOIN_THREADS / 32) {
-            const int gg = gc * heads_of_chunk + g;
-            const long long row = (long long)i * a.q_heads + h * a.group + gg;
-            if (c0 == c1) {
-                if (lane == 0) lse2[gg] = a.row_lse[row];
-                continue;
-            }
-            float top = -INFINITY, sum = 0.f;
-            for (long long c = c0 + lane; c <= c1; c += 32) {
-                const float2 ml = a.part_ml[part(c) + g];
-                const float t = fmaxf(top, ml.x), ref = kv_ref(t);
-                sum = sum * kv_exp2(top - ref) + ml.y * kv_exp2(ml.x - ref);
-                top = t;
-            }
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                const float t2 = __shfl_xor_sync(~0u, top, o), s2 = __shfl_xor_sync(~0u, sum, o);
-                const float t = fmaxf(top, t2), ref = kv_ref(t);
-                sum = sum * kv_exp2(top - ref) + s2 * kv_exp2(t2 - ref);
-                top = t;
-            }
-            if (lane == 0) {
-                lse2[gg] = sum == 0.f ? -INFINITY : top + log2f(sum);
-                if (a.lse && x == 0) a.lse[row] = lse2[gg] * KV_LN2;
-            }
+    kv_join_wait();
+    if (k == 0) return;              // the piece begins with a row
+    const int first = b * piece - k, c0 = first / piece, c1 = (first + KvSpan(a, i).steps(a) - 1) / piece, parts = c1 - c0 + 1;
+    const int g0 = row % a.group_chunks * heads_of_chunk, heads = min(heads_of_chunk, a.group - g0), h0 = row / a.group_chunks * a.hc;
+    // units (KV head, query head, 32 elements) of this piece, one of the parts - 1 that cut the row
+    const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = b - c0 - 1;
+    const int u0 = all * turn / (parts - 1), u1 = all * (turn + 1) / (parts - 1), p0 = u0 / slices, pairs = u1 > u0 ? (u1 - 1) / slices - p0 + 1 : 0;
+    float *factor = smem + 4 * KV_JOIN_THREADS;
+    auto index = [&](int c, int pair) { return ((c * 2 + (c == c0 ? 1 : 0)) * a.hc + pair / heads) * heads_of_chunk + pair % heads; };
+    auto finish = [&](int pair, float z) {
+        if (a.lse && pair * slices >= u0) a.lse[(long long)i * a.q_heads + (h0 + pair / heads) * a.group + g0 + pair % heads] = z * KV_LN2;
+    };
+    if (parts <= 8) {
+        for (int n = tid; n < pairs; n += KV_JOIN_THREADS) {
+            const float z = kv_join_lse<1>(a, c0, c1, (p0 + n) / heads, heads_of_chunk, (p0 + n) % heads, nullptr);
+            finish(p0 + n, z);
+            for (int c = 0; c < parts; ++c) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(a.part_ml[index(c0 + c, p0 + n)].x - z);
         }
-        __syncthreads();
-        if (c0 != c1)
-            for (int g = x; g < a.group; g += gridDim.x) {
-                if (g / heads_of_chunk != gc) continue;
-                float acc[8];
-#pragma unroll
-                for (int d = 0; d < 8; ++d) acc[d] = 0.f;
-                const float z = lse2[g];
-                if (z != -INFINITY)
-#pragma unroll 4
-                    for (long long c = c0 + warp; c <= c1; c += KV_JOIN_THREADS / 32) {
-                        const long long p = part(c) + g - gc * heads_of_chunk;
-                        const float f = kv_exp2(a.part_ml[p].x - z);
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-                            if (b * 128 + lane * 4 < a.c.dim) {
-                                const float4 v = *(const float4 *)(a.part_o + p * a.c.dim + b * 128 + lane * 4);
-                                acc[4 * b] += f * v.x;
-                                acc[4 * b + 1] += f * v.y;
-                                acc[4 * b + 2] += f * v.z;
-                                acc[4 * b + 3] += f * v.w;
-                            }
-                    }
-#pragma unroll
-                for (int d = 0; d < 8; ++d) box[warp][(d >> 2) * 128 + lane * 4 + (d & 3)] = acc[d];
-                __syncthreads();
-                if (tid < a.c.dim) {
-                    float v = 0.f;
-#pragma unroll
-                    for (int w = 0; w < KV_JOIN_THREADS / 32; ++w) v += box[w][tid];
-                    ((T *)a.out)[i * a.o_seq + (h * a.group + g) * a.o_head + tid] = kv_round<T>(v);
-                }
-                __syncthreads();
-            }
+    } else {
+        for (int n = warp; n < pairs; n += KV_JOIN_WARPS) {
+            const float z = kv_join_lse<32>(a, c0, c1, (p0 + n) / heads, heads_of_chunk, (p0 + n) % heads, nullptr);
+            if (lane == 0) finish(p0 + n, z);
+            for (int c = lane; c < parts; c += 32) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(a.part_ml[index(c0 + c, p0 + n)].x - z);
+        }
     }
-    if (!a.scores) return;
     __syncthreads();
-    const long long at = i * a.w_seq + h * a.w_head;
-    for (int t = x * KV_JOIN_SLOTS + tid; t < min((x + 1) * KV_JOIN_SLOTS, sp.n); t += KV_JOIN_THREADS) {
-        float w = 0.f;
-        if (t >= sp.first) {
-            const float *from = a.scores + (((long long)i * a.c.heads + h) * a.c.max_len + t) * a.group;
-            if ((a.group & 3) == 0) {
-                for (int g = 0; g < a.group; g += 4) {
-                    const float4 s = *(const float4 *)(from + g);
-                    const float part[4] = {s.x, s.y, s.z, s.w};
+    const int tasks = (u1 - u0) * 8;
+    // element 4 * (task % 8) of unit task / 8: where it lies in a part, whether it exists
+    auto place = [&](int t, int &pair, int &d) {
+        const int u = u0 + t / 8;
+        pair = u / slices;
+        d = (u - pair * slices) * 32 + t % 8 * 4;
+        return t < tasks && d < a.c.dim;
+    };
+    auto put = [&](int pair, int d, const float4 &v) {
+        T *to = (T *)a.out + i * a.o_seq + ((h0 + pair / heads) * a.group + g0 + pair % heads) * a.o_head + d;
+        to[0] = kv_round<T>(v.x);
+        to[1] = kv_round<T>(v.y);
+        to[2] = kv_round<T>(v.z);
+        to[3] = kv_round<T>(v.w);
+    };
+    auto add = [&](float4 &acc, int c, int pair, int d) {
+        const float4 v = *(const float4 *)(a.part_o + (long long)index(c0 + c, pair) * a.c.dim + d);
+        const float f = factor[(pair - p0) * parts + c];
+        // a factor of 0 leaves out what a part without any weight holds
+        if (f != 0.f) acc = make_float4(acc.x + f * v.x, acc.y + f * v.y, acc.z + f * v.z, acc.w + f * v.w);
+    };
+    if (tasks > KV_JOIN_THREADS / 2) {           // few parts: four outputs per thread at once
+        for (int t0 = tid; t0 < tasks; t0 += 4 * KV_JOIN_THREADS) {
+            float4 acc[4];
+            int pair[4], d[4];
+            bool on[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (lse2[g + e] != -INFINITY) w += kv_exp2(part[e] - lse2[g + e]);
-                }
-            } else {
-                for (int g = 0; g < a.group; ++g)
-                    if (lse2[g] != -INFINITY) w += kv_exp2(from[g] - lse2[g]);
+            for (int j = 0; j < 4; ++j) {
+                acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                on[j] = place(t0 + j * KV_JOIN_THREADS, pair[j], d[j]);
             }
+#pragma unroll 2
+            for (int c = 0; c < parts; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (on[j]) add(acc[j], c, pair[j], d[j]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (on[j]) put(pair[j], d[j], acc[j]);
         }
-        a.w_out[at + t] = (a.w_in ? a.w_in[at + t] : 0.f) + w;
+    } else if (tasks > 0) {                      // many parts: several threads to an output
+        int ways = 2;
+        while (ways * 2 * tasks <= KV_JOIN_THREADS) ways *= 2;
+        const int t = tid % tasks, way = tid / tasks;
+        int pair, d;
+        const bool on = place(t, pair, d) && way < ways;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), *box = (float4 *)smem;
+        if (on)
+#pragma unroll 8
+            for (int c = way; c < parts; c += ways) add(acc, c, pair, d);
+        box[tid] = acc;
+        __syncthreads();
+        if (way == 0 && on) {
+            for (int w = 1; w < ways; ++w) {
+                const float4 v = box[w * tasks + t];
+                acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+            }
+            put(pair, d, acc);
+        }
     }
+}
+
+// steps s .. s + todo - 1 of the line, which begin at step k of the sequence's row; `share` of `shares` for the rest
+__device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int s, int todo, int piece, int i, int row, int k, int share, int shares,
+                                                float *lse2)
+{
+    const int tid = threadIdx.x, warp = tid >> 5;
+    kv_join_wait();
+    while (todo > 0) {
+        const KvSpan sp(a, i);
+        const int steps = sp.steps(a), n = min(steps - k, todo);
+        if (n > 0 && row % a.group_chunks == 0) {
+            // this row's sums, and those of the further query-head chunks of the same KV heads, which follow it in the line
+            const int pairs = a.hc * a.group;
+            auto lse_of = [&](int p, auto lanes) {
+                const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk, first = s - k + gc * steps;
+                return kv_join_lse<decltype(lanes)::value>(a, first / piece, (first + steps - 1) / piece, hw, heads_of_chunk, g - gc * heads_of_chunk,
+                                                           a.row_lse + (long long)i * a.q_heads + (row / a.group_chunks * a.hc + hw) * a.group + g);
+            };
+            // few parts: a thread for every pair of KV and query head; many: a warp
+            if (steps <= 8 * piece)
+                for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = lse_of(p, KvCount<1>());
+            else
+                for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
+                    const float z = lse_of(p, KvCount<32>());
+                    if ((tid & 31) == 0) lse2[p] = z;
+                }
+            __syncthreads();
+            const int t0 = sp.base + k * a.tw * 16, count = min(sp.base + (k + n) * a.tw * 16, sp.n) - t0, h0 = row / a.group_chunks * a.hc;
+            // one warp per KV head, or several
+            const int lanes = KV_JOIN_THREADS / a.hc / 32 * 32, hw = tid / lanes;
+            if (hw < a.hc) {
+                const float *from = a.scores + (((long long)i * a.c.heads + h0 + hw) * a.c.max_len + t0) * a.group, *z = lse2 + hw * a.group;
+                const long long w = i * a.w_seq + (h0 + hw) * a.w_head + t0;
+#pragma unroll 4
+                for (int t = tid - hw * lanes; t < count; t += lanes) {
+                    const float had = a.w_in ? a.w_in[w + t] : 0.f;
+                    float add = 0.f;
+                    if (t0 + t >= sp.first) {
+                        if ((a.group & 3) == 0) {
+                            for (int g = 0; g < a.group; g += 4) {
+                                const float4 x = *(const float4 *)(from + (long long)t * a.group + g);
+                                const float part[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                                for (int d = 0; d < 4; ++d)
+                                    if (z[g + d] != -INFINITY) add += kv_exp2(part[d] - z[g + d]);
+                            }
+                        } else {
+                            for (int g = 0; g < a.group; ++g)
+                                if (z[g] != -INFINITY) add += kv_exp2(from[(long long)t * a.group + g] - z[g]);
+                        }
+                    }
+                    a.w_out[w + t] = had + add;
+                }
+            }
+            __syncthreads();
+        }
+        s += n;
+        todo -= n;
+        k = 0;
+        if (n == 0) ++i;             // a sequence without slots
+        else if (++row == a.head_chunks * a.group_chunks) {
+            row = 0;
+            ++i;
+        }
+    }
+    // slots before the window keep their weight
+    if (a.window > 0 && a.w_out != a.w_in)
+        for (int r = 0; r < a.seqs * a.c.heads; ++r) {
+            const KvSpan sp(a, r / a.c.heads);
+            const long long w = r / a.c.heads * a.w_seq + r % a.c.heads * a.w_head;
+            for (int t = share * KV_JOIN_THREADS + tid; t < sp.base; t += shares * KV_JOIN_THREADS) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
+        }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(KV_JOIN_THREADS, 4) kv_attend_join(const __grid_constant__ KvAttend a, int heads_of_chunk)
+{
+    extern __shared__ __align__(16) float join_smem[];
+    __shared__ int red[KV_JOIN_WARPS], at[2];
+    const KvLine line(a, red);
+    const int per = a.scores ? KV_JOIN_CTAS : 1, c = blockIdx.x / per, role = blockIdx.x % per, piece = kv_attend_piece(a, line.total);
+    // the piece's steps, or this CTA's share of them
+    const long long at0 = (long long)c * piece;
+    int n = at0 < line.total ? min(line.total - (int)at0, piece) : 0, s = n ? (int)at0 : 0;
+    if (role > 0) {
+        const int lo = (int)((long long)n * (role - 1) / (per - 1)), hi = (int)((long long)n * role / (per - 1));
+        s += lo;
+        n = hi - lo;
+    }
+    int i = 0, row = 0, k = 0;
+    if (n > 0) line.find(a, s, at, i, row, k);
+    if (role > 0) kv_join_weights(a, heads_of_chunk, s, n, piece, i, row, k, c * (per - 1) + role - 1, a.pieces * (per - 1), join_smem);
+    else if (n > 0) kv_join_rows<T>(a, heads_of_chunk, c, piece, i, row, k, join_smem);
+    else kv_join_wait();
 }

@@ -154,8 +154,11 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     const bool split = longest > ATTEND_ALONE_STEPS || (a->weights_out && k.group_chunks > 1);
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
+    if (ceil_div(a->max_len + 15, 16 * k.tw) * a->num_seqs * k.head_chunks * k.group_chunks > INT32_MAX)
+        return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
+    k.whole_tiles = c->block_size % 16 == 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
     p.part_ml = p.lse + align256((int64_t)a->num_seqs * a->q_heads * 4);
@@ -298,8 +301,8 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
         early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         early.val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t cfg = {};
-        const int64_t tiles = a->weights_out ? ceil_div(a->max_len, KV_JOIN_SLOTS) : 0;
-        cfg.gridDim = dim3((unsigned)std::max<int64_t>(k.group, tiles), cache->kv_heads, k.seqs);
+        cfg.gridDim = dim3(k.pieces * (k.scores ? KV_JOIN_CTAS : 1));
+        cfg.dynamicSmemBytes = std::max((size_t)kv_join_floats(k.hc, 8 * p.nt, k.pieces), (size_t)k.hc * k.group) * 4;
         cfg.blockDim = dim3(KV_JOIN_THREADS);
         cfg.stream = o->stream;
         cfg.attrs = &early;
