@@ -43,9 +43,11 @@ struct KvAttend {
     int q_pairs;         // q may be read in pairs of elements
     int whole_tiles;     // the block size is a multiple of 16: a tile lies in one block
     float *scores;       // [seq][kv_head][max_len][group], base 2; nullptr: no weights wanted
-    float *row_lse;      // [seq][q_head], base 2
     float2 *part_ml;     // [piece][2][hc][8*NT]: maximum and sum
     float *part_o;       // [piece][2][hc][8*NT][dim]
+    int4 *part_of;       // [piece]: the sequence and row that the piece begins inside of, the row's place in the line and its steps (0: none)
+    int4 *row_of;        // [seq][row]: its place in the line, its steps, the length of a piece, whether one CTA has all of it
+    float *row_lse;      // [seq][q_head], base 2, of rows that one CTA has
 };
 
 constexpr int KV_ATTEND_WARPS = 8, KV_ATTEND_STAGES = 6;
@@ -187,6 +189,8 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
     const int rows_of_seq = a.head_chunks * a.group_chunks;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
+    if (a.pieces && tid == 0) a.part_of[blockIdx.x] = make_int4(0, 0, 0, 0);
+
     // sequences without slots
     for (int i = blockIdx.x; i < a.seqs; i += gridDim.x)
         if (a.c.len(i) == 0) {
@@ -198,7 +202,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 
     // ---- this CTA's piece of the line of steps: the row and step it begins at, and how many steps it has
     int pi, pch, pk;                 // sequence, row of the sequence, step: where the next tile to be loaded lies
-    int todo;
+    int todo, s0 = 0, piece = 0;
     if (a.pieces == 0) {
         pi = blockIdx.x / rows_of_seq;
         pch = blockIdx.x % rows_of_seq;
@@ -206,12 +210,14 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
         todo = KvSpan(a, pi).steps(a);
     } else {
         const KvLine line(a, red);
-        const int piece = kv_attend_piece(a, line.total), s0 = (int)min((long long)blockIdx.x * piece, (long long)line.total);
+        piece = kv_attend_piece(a, line.total);
+        s0 = (int)min((long long)blockIdx.x * piece, (long long)line.total);
         todo = min(line.total - s0, piece);
         if (todo <= 0) return;
         line.find(a, s0, s_at, pi, pch, pk);
     }
     if (todo <= 0) return;
+    const int k0 = pk;
 
     const unsigned ring = (unsigned)__cvta_generic_to_shared(smem) + warp * a.stages * 2 * TILE;
     const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
@@ -310,18 +316,10 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
     float o[NT][KS][4], m[NT][2], l[NT][2];
     int take = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
+    int n0 = 0;                      // its first tile
     for (int n = 0; n < todo; ++n) {
         __syncwarp();                // the stage about to be filled is no longer read
         issue();
-        // the tile that is computed now was committed stages - 1 groups ago
-        switch (a.stages) {
-        case 1: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-        case 2: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-        case 3: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-        case 4: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-        case 5: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-        default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-        }
         __syncwarp();
         const int4 tile = my_info[take];
         const unsigned mask = tile.x & 0xffff, stage = ring + take * 2 * TILE;
@@ -329,6 +327,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
         const int heads = min(HEADS, a.group - g0);
         if (tile.x & 1 << 16) {
             began = tile.x & 1 << 18;
+            n0 = n;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int g = nt * 8 + (lane >> 2);
@@ -351,6 +350,16 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                 l[nt][0] = l[nt][1] = 0.f;
             }
         }
+        // the tile that is computed now was committed stages - 1 groups ago
+        switch (a.stages) {
+        case 1: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        }
+        __syncwarp();
         if (mask) {
             float s[NT][4], s2[NT][4];
 #pragma unroll
@@ -421,6 +430,11 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                 for (int nt = 0; nt < NT; ++nt) KvMma<T>::mma(o[nt][ks], v, pf[nt][0], pf[nt][1]);
             }
         }
+        else if (a.scores)           // nothing of the tile counts
+            for (int e = lane; e < 16 * heads; e += 32)
+                if (tile.y + e / heads < a.c.max_len)
+                    a.scores[(((long long)tile.z * a.c.heads + h) * a.c.max_len + tile.y + e / heads) * a.group + g0 + e % heads] = -INFINITY;
+        __syncwarp();
         take = take + 1 == a.stages ? 0 : take + 1;
 
         if (tile.x & 1 << 17) {      // the CTA's last step in this row
@@ -475,6 +489,10 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
             }
             if (way == 0) {
                 const long long part = ((long long)blockIdx.x * 2 + (began ? 1 : 0)) * a.hc + hw;
+                if (a.pieces && tid == 0) {
+                    if (began) a.row_of[(long long)tile.z * rows_of_seq + tile.w] = make_int4(s0 + n0, KvSpan(a, tile.z).steps(a), piece, whole);
+                    else a.part_of[blockIdx.x] = make_int4(tile.z, tile.w, s0 - k0, KvSpan(a, tile.z).steps(a));
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -495,8 +513,9 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                                 }
                             if (lane < 4) {
                                 if (a.lse) a.lse[(long long)tile.z * a.q_heads + gq] = lse2 * KV_LN2;
-                                a.row_lse[(long long)tile.z * a.q_heads + gq] = lse2;
-                                if (a.pieces == 0) s_lse[hw][g] = lse2;
+                                // a row without any weight has scores of -inf: less +inf they give 0
+                                s_lse[hw][g] = lse2 == -INFINITY ? INFINITY : lse2;
+                                if (a.pieces) a.row_lse[(long long)tile.z * a.q_heads + gq] = lse2;
                             }
                         } else {
                             float *to = a.part_o + (part * HEADS + g) * a.c.dim;
@@ -511,36 +530,36 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                         }
                     }
             }
-        }
-    }
-
-    // ---- rows that are one CTA's add up their weights here: every thread reads the scores it wrote itself
-    if (a.pieces == 0 && a.scores) {
-        __syncthreads();
-        const int i = blockIdx.x / rows_of_seq, h = blockIdx.x % rows_of_seq / a.group_chunks * a.hc + hw;
-        const KvSpan sp(a, i);
-        const long long at = i * a.w_seq + h * a.w_head;
-        for (int t = way * 32 + lane; t < sp.base; t += a.tw * 32) a.w_out[at + t] = a.w_in ? a.w_in[at + t] : 0.f;
-        const int steps = sp.steps(a);
-        for (int k = 0; k < steps; ++k) {
-            const int t0 = sp.base + (k * a.tw + way) * 16;
+            // where there is no second kernel, the weights are added up here: every thread reads the scores it wrote itself
+            if (a.pieces == 0 && a.scores) {
+                if (a.tw > 1) __syncthreads();
+                else __syncwarp();
+                const KvSpan sp(a, tile.z);
+                const float *from = a.scores + ((long long)tile.z * a.c.heads + h) * a.c.max_len * a.group;
+                const long long w = tile.z * a.w_seq + h * a.w_head;
+                for (int t = way * 32 + lane; t < sp.base; t += a.tw * 32) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
+                for (int t0 = sp.base + way * 16; t0 < sp.n; t0 += a.tw * 16) {
+                    float add[2] = {0.f, 0.f};
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int t = t0 + b * 8 + (lane >> 2);
-                float w = 0.f;
-                if (t < sp.n && t >= sp.first) {
-                    const float *from = a.scores + (((long long)i * a.c.heads + h) * a.c.max_len + t) * a.group;
+                    for (int b = 0; b < 2; ++b)
+                        if (t0 + b * 8 + (lane >> 2) < sp.n)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int g = nt * 8 + (lane & 3) * 2 + e;
-                            if (g < a.group && s_lse[hw][g] != -INFINITY) w += kv_exp2(from[g] - s_lse[hw][g]);
-                        }
+                                for (int e = 0; e < 2; ++e) {
+                                    const int g = nt * 8 + (lane & 3) * 2 + e;
+                                    if (g < heads) add[b] += kv_exp2(from[(long long)(t0 + b * 8 + (lane >> 2)) * a.group + g] - s_lse[hw][g]);
+                                }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        add[b] += __shfl_xor_sync(~0u, add[b], 1);
+                        add[b] += __shfl_xor_sync(~0u, add[b], 2);
+                        const int t = t0 + b * 8 + (lane >> 2);
+                        if ((lane & 3) == 0 && t < sp.n) a.w_out[w + t] = (a.w_in ? a.w_in[w + t] : 0.f) + add[b];
+                    }
                 }
-                w += __shfl_xor_sync(~0u, w, 1);
-                w += __shfl_xor_sync(~0u, w, 2);
-                if ((lane & 3) == 0 && t < sp.n) a.w_out[at + t] = (a.w_in ? a.w_in[at + t] : 0.f) + w;
+                if (a.tw > 1) __syncthreads();           // the next row's sums take the place of these
+                else __syncwarp();
             }
         }
     }
@@ -548,12 +567,13 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 
 // ---- join: what is left when rows were split.
 //
-// KV_JOIN_CTAS CTAs per piece.  The first joins output rows: it looks whether the piece begins inside a row; the pieces
-// that cut one row share its output, in units of 32 elements of a head, among them.  The others add up the weights of the
-// piece's slots with the sums of all parts of their rows.  Everything that depends on the lengths alone is done before
-// the wait for the first kernel, beside which these CTAs fit.  After it, every load that can be in flight is: what such
-// a kernel takes is the number of loads that wait for one another, each about a microsecond.
-constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_CTAS = 4, KV_MAX_GROUP = 256;
+// KV_JOIN_ROWS CTAs per piece join output rows: where the piece begins inside a row, the pieces that cut that row share
+// its output, in units of 32 elements of a head, among them.  Behind them come CTAs that add up the weights, each for
+// KV_JOIN_SLOTS weights of one sequence and chunk of KV heads, with the sums of all parts of the row.  What such a kernel
+// takes is the number of loads that wait for one another, each close to a microsecond: the first kernel leaves
+// what lies where, so there are three in a chain (what, the row's sums, the data), and every load that can be in
+// flight together is.
+constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_ROWS = 4, KV_JOIN_SLOTS = 2048, KV_MAX_GROUP = 256;
 
 // maximum and sum of two sets of slots together
 __device__ __forceinline__ void kv_meet(float &top, float &sum, float top2, float sum2)
@@ -563,12 +583,11 @@ __device__ __forceinline__ void kv_meet(float &top, float &sum, float top2, floa
     top = t;
 }
 
-// log2 of a row's sum of exponentials for one query head, from its parts c0 .. c1 or as the finished row left it: by a
-// whole warp (`lanes` 32), or by every thread for itself (`lanes` 1)
+// log2 of a row's sum of exponentials for one query head, from its parts c0 .. c1: by a whole warp (`lanes` 32), or by every
+// thread for itself (`lanes` 1)
 template <int lanes>
-__device__ __forceinline__ float kv_join_lse(const KvAttend &a, int c0, int c1, int hw, int heads_of_chunk, int g, const float *row_lse)
+__device__ __forceinline__ float kv_join_lse(const KvAttend &a, int c0, int c1, int hw, int heads_of_chunk, int g)
 {
-    if (c0 == c1) return *row_lse;
     float top = -INFINITY, sum = 0.f;
 #pragma unroll 4
     for (int c = c0 + (lanes == 1 ? 0 : threadIdx.x & 31); c <= c1; c += lanes) {
@@ -582,8 +601,6 @@ __device__ __forceinline__ float kv_join_lse(const KvAttend &a, int c0, int c1, 
 
 template <int n> struct KvCount { static constexpr int value = n; };
 
-__device__ __forceinline__ void kv_join_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // floats of shared memory the row CTAs need: a factor for every part of every head a CTA shares in (a row of more than
 // eight parts is shared by eight CTAs or more), and a float4 per thread
 __host__ __device__ constexpr int kv_join_floats(int hc, int heads_of_chunk, int pieces)
@@ -593,188 +610,171 @@ __host__ __device__ constexpr int kv_join_floats(int hc, int heads_of_chunk, int
 }
 
 template <typename T>
-__device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chunk, int b, int piece, int i, int row, int k, float *smem)
+__device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chunk, int b, int sub, float *smem)
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    kv_join_wait();
-    if (k == 0) return;              // the piece begins with a row
-    const int first = b * piece - k, c0 = first / piece, c1 = (first + KvSpan(a, i).steps(a) - 1) / piece, parts = c1 - c0 + 1;
+    const int4 of = a.part_of[b];
+    if (of.w == 0) return;
+    const int i = of.x, row = of.y, piece = a.row_of[(long long)i * a.head_chunks * a.group_chunks + row].z;
+    const int c0 = of.z / piece, c1 = (of.z + of.w - 1) / piece, parts = c1 - c0 + 1;
     const int g0 = row % a.group_chunks * heads_of_chunk, heads = min(heads_of_chunk, a.group - g0), h0 = row / a.group_chunks * a.hc;
     // units (KV head, query head, 32 elements) of this piece, one of the parts - 1 that cut the row
-    const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = b - c0 - 1;
-    const int u0 = all * turn / (parts - 1), u1 = all * (turn + 1) / (parts - 1), p0 = u0 / slices, pairs = u1 > u0 ? (u1 - 1) / slices - p0 + 1 : 0;
+    const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = (b - c0 - 1) * KV_JOIN_ROWS + sub, turns = (parts - 1) * KV_JOIN_ROWS;
+    const int u0 = all * turn / turns, u1 = all * (turn + 1) / turns, p0 = u0 / slices, pairs = u1 > u0 ? (u1 - 1) / slices - p0 + 1 : 0;
     float *factor = smem + 4 * KV_JOIN_THREADS;
-    auto index = [&](int c, int pair) { return ((c * 2 + (c == c0 ? 1 : 0)) * a.hc + pair / heads) * heads_of_chunk + pair % heads; };
-    auto finish = [&](int pair, float z) {
-        if (a.lse && pair * slices >= u0) a.lse[(long long)i * a.q_heads + (h0 + pair / heads) * a.group + g0 + pair % heads] = z * KV_LN2;
+    const int stride = a.hc * heads_of_chunk;            // entries of a part
+    auto slot = [&](int c) { return (c * 2 + (c == c0 ? 1 : 0)) * stride; };
+    auto weigh = [&](int n, auto lanes) {
+        constexpr int step = decltype(lanes)::value;
+        const int pair = p0 + n, hw = pair / heads, g = pair - hw * heads;
+        const float2 *ml = a.part_ml + hw * heads_of_chunk + g;
+        const float z = kv_join_lse<step>(a, c0, c1, hw, heads_of_chunk, g);
+        const int own = step == 1 ? 0 : lane;
+        if (a.lse && own == 0 && pair * slices >= u0) a.lse[(long long)i * a.q_heads + (h0 + hw) * a.group + g0 + g] = z * KV_LN2;
+#pragma unroll 4
+        for (int c = own; c < parts; c += step) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(ml[slot(c0 + c)].x - z);
     };
-    if (parts <= 8) {
-        for (int n = tid; n < pairs; n += KV_JOIN_THREADS) {
-            const float z = kv_join_lse<1>(a, c0, c1, (p0 + n) / heads, heads_of_chunk, (p0 + n) % heads, nullptr);
-            finish(p0 + n, z);
-            for (int c = 0; c < parts; ++c) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(a.part_ml[index(c0 + c, p0 + n)].x - z);
-        }
-    } else {
-        for (int n = warp; n < pairs; n += KV_JOIN_WARPS) {
-            const float z = kv_join_lse<32>(a, c0, c1, (p0 + n) / heads, heads_of_chunk, (p0 + n) % heads, nullptr);
-            if (lane == 0) finish(p0 + n, z);
-            for (int c = lane; c < parts; c += 32) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(a.part_ml[index(c0 + c, p0 + n)].x - z);
-        }
-    }
+    if (parts <= 8)
+        for (int n = tid; n < pairs; n += KV_JOIN_THREADS) weigh(n, KvCount<1>());
+    else
+        for (int n = warp; n < pairs; n += KV_JOIN_WARPS) weigh(n, KvCount<32>());
     __syncthreads();
     const int tasks = (u1 - u0) * 8;
-    // element 4 * (task % 8) of unit task / 8: where it lies in a part, whether it exists
-    auto place = [&](int t, int &pair, int &d) {
-        const int u = u0 + t / 8;
-        pair = u / slices;
-        d = (u - pair * slices) * 32 + t % 8 * 4;
-        return t < tasks && d < a.c.dim;
+    // task: elements 4 * (task % 8) .. + 3 of unit task / 8; where they lie in a part and in the output, and their factors
+    struct Task {
+        bool on;
+        const float *from, *factor;
+        T *to;
+        float4 acc;
     };
-    auto put = [&](int pair, int d, const float4 &v) {
-        T *to = (T *)a.out + i * a.o_seq + ((h0 + pair / heads) * a.group + g0 + pair % heads) * a.o_head + d;
-        to[0] = kv_round<T>(v.x);
-        to[1] = kv_round<T>(v.y);
-        to[2] = kv_round<T>(v.z);
-        to[3] = kv_round<T>(v.w);
+    auto task = [&](int t) {
+        Task x;
+        const int u = u0 + t / 8, pair = u / slices, d = (u - pair * slices) * 32 + t % 8 * 4, hw = pair / heads, g = pair - hw * heads;
+        x.on = t < tasks && d < a.c.dim;
+        x.from = a.part_o + (hw * heads_of_chunk + g) * a.c.dim + d;
+        x.factor = factor + (pair - p0) * parts;
+        x.to = (T *)a.out + i * a.o_seq + ((h0 + hw) * a.group + g0 + g) * a.o_head + d;
+        x.acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        return x;
     };
-    auto add = [&](float4 &acc, int c, int pair, int d) {
-        const float4 v = *(const float4 *)(a.part_o + (long long)index(c0 + c, pair) * a.c.dim + d);
-        const float f = factor[(pair - p0) * parts + c];
-        // a factor of 0 leaves out what a part without any weight holds
-        if (f != 0.f) acc = make_float4(acc.x + f * v.x, acc.y + f * v.y, acc.z + f * v.z, acc.w + f * v.w);
+    auto add = [&](Task &x, int c) {
+        const float4 v = *(const float4 *)(x.from + (long long)slot(c0 + c) * a.c.dim);
+        const float f = x.factor[c];
+        // a factor of 0 leaves out whatever a part without any weight holds
+        if (f != 0.f) x.acc = make_float4(x.acc.x + f * v.x, x.acc.y + f * v.y, x.acc.z + f * v.z, x.acc.w + f * v.w);
     };
-    if (tasks > KV_JOIN_THREADS / 2) {           // few parts: four outputs per thread at once
-        for (int t0 = tid; t0 < tasks; t0 += 4 * KV_JOIN_THREADS) {
-            float4 acc[4];
-            int pair[4], d[4];
-            bool on[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                on[j] = place(t0 + j * KV_JOIN_THREADS, pair[j], d[j]);
-            }
+    auto put = [&](const Task &x) {
+        x.to[0] = kv_round<T>(x.acc.x);
+        x.to[1] = kv_round<T>(x.acc.y);
+        x.to[2] = kv_round<T>(x.acc.z);
+        x.to[3] = kv_round<T>(x.acc.w);
+    };
+    if (tasks > KV_JOIN_THREADS / 2) {           // few parts: two outputs per thread at once
+        for (int t = tid; t < tasks; t += 2 * KV_JOIN_THREADS) {
+            Task x = task(t), y = task(t + KV_JOIN_THREADS);
 #pragma unroll 2
-            for (int c = 0; c < parts; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (on[j]) add(acc[j], c, pair[j], d[j]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (on[j]) put(pair[j], d[j], acc[j]);
+            for (int c = 0; c < parts; ++c) {
+                if (x.on) add(x, c);
+                if (y.on) add(y, c);
+            }
+            if (x.on) put(x);
+            if (y.on) put(y);
         }
     } else if (tasks > 0) {                      // many parts: several threads to an output
         int ways = 2;
         while (ways * 2 * tasks <= KV_JOIN_THREADS) ways *= 2;
         const int t = tid % tasks, way = tid / tasks;
-        int pair, d;
-        const bool on = place(t, pair, d) && way < ways;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), *box = (float4 *)smem;
-        if (on)
+        Task x = task(t);
+        x.on = x.on && way < ways;
+        float4 *box = (float4 *)smem;
+        if (x.on)
 #pragma unroll 8
-            for (int c = way; c < parts; c += ways) add(acc, c, pair, d);
-        box[tid] = acc;
+            for (int c = way; c < parts; c += ways) add(x, c);
+        box[tid] = x.acc;
         __syncthreads();
-        if (way == 0 && on) {
+        if (way == 0 && x.on) {
             for (int w = 1; w < ways; ++w) {
                 const float4 v = box[w * tasks + t];
-                acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+                x.acc = make_float4(x.acc.x + v.x, x.acc.y + v.y, x.acc.z + v.z, x.acc.w + v.w);
             }
-            put(pair, d, acc);
+            put(x);
         }
     }
 }
 
-// steps s .. s + todo - 1 of the line, which begin at step k of the sequence's row; `share` of `shares` for the rest
-__device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int s, int todo, int piece, int i, int row, int k, int share, int shares,
-                                                float *lse2)
+// slots t0 .. of chunk `hx` of the KV heads of sequence i
+__device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int i, int hx, int t0, float *lse2)
 {
-    const int tid = threadIdx.x, warp = tid >> 5;
-    kv_join_wait();
-    while (todo > 0) {
-        const KvSpan sp(a, i);
-        const int steps = sp.steps(a), n = min(steps - k, todo);
-        if (n > 0 && row % a.group_chunks == 0) {
-            // this row's sums, and those of the further query-head chunks of the same KV heads, which follow it in the line
-            const int pairs = a.hc * a.group;
-            auto lse_of = [&](int p, auto lanes) {
-                const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk, first = s - k + gc * steps;
-                return kv_join_lse<decltype(lanes)::value>(a, first / piece, (first + steps - 1) / piece, hw, heads_of_chunk, g - gc * heads_of_chunk,
-                                                           a.row_lse + (long long)i * a.q_heads + (row / a.group_chunks * a.hc + hw) * a.group + g);
-            };
-            // few parts: a thread for every pair of KV and query head; many: a warp
-            if (steps <= 8 * piece)
-                for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = lse_of(p, KvCount<1>());
-            else
-                for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
-                    const float z = lse_of(p, KvCount<32>());
-                    if ((tid & 31) == 0) lse2[p] = z;
-                }
-            __syncthreads();
-            const int t0 = sp.base + k * a.tw * 16, count = min(sp.base + (k + n) * a.tw * 16, sp.n) - t0, h0 = row / a.group_chunks * a.hc;
-            // one warp per KV head, or several
-            const int lanes = KV_JOIN_THREADS / a.hc / 32 * 32, hw = tid / lanes;
-            if (hw < a.hc) {
-                const float *from = a.scores + (((long long)i * a.c.heads + h0 + hw) * a.c.max_len + t0) * a.group, *z = lse2 + hw * a.group;
-                const long long w = i * a.w_seq + (h0 + hw) * a.w_head + t0;
-#pragma unroll 4
-                for (int t = tid - hw * lanes; t < count; t += lanes) {
-                    const float had = a.w_in ? a.w_in[w + t] : 0.f;
-                    float add = 0.f;
-                    if (t0 + t >= sp.first) {
-                        if ((a.group & 3) == 0) {
-                            for (int g = 0; g < a.group; g += 4) {
-                                const float4 x = *(const float4 *)(from + (long long)t * a.group + g);
-                                const float part[4] = {x.x, x.y, x.z, x.w};
+    const int tid = threadIdx.x, warp = tid >> 5, pairs = a.hc * a.group, h0 = hx * a.hc;
+    const KvSpan sp(a, i);
+    if (t0 >= sp.n) return;
+    const int4 *row = a.row_of + ((long long)i * a.head_chunks + hx) * a.group_chunks;
+    auto sum_of = [&](int p, auto lanes) {
+        const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk;
+        const int4 line = row[gc];
+        const float z = line.w ? a.row_lse[(long long)i * a.q_heads + h0 * a.group + p]
+                               : kv_join_lse<decltype(lanes)::value>(a, line.x / line.z, (line.x + line.y - 1) / line.z, hw, heads_of_chunk, g - gc * heads_of_chunk);
+        return z == -INFINITY ? INFINITY : z;    // a row without any weight has scores of -inf: less +inf they give 0
+    };
+    // few parts: a thread for every pair of KV and query head; many: a warp
+    if (row[0].y <= 8 * row[0].z)
+        for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = sum_of(p, KvCount<1>());
+    else
+        for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
+            const float z = sum_of(p, KvCount<32>());
+            if ((tid & 31) == 0) lse2[p] = z;
+        }
+    __syncthreads();
+    const int lanes = KV_JOIN_THREADS / a.hc / 32 * 32, hw = tid / lanes, count = min(KV_JOIN_SLOTS / a.hc, sp.n - t0);
+    if (hw >= a.hc) return;
+    const float *from = a.scores + (((long long)i * a.c.heads + h0 + hw) * a.c.max_len + t0) * a.group, *z = lse2 + hw * a.group;
+    const long long w = i * a.w_seq + (h0 + hw) * a.w_head + t0;
+    for (int t = tid - hw * lanes; t < count; t += 4 * lanes) {          // four slots at once
+        float v[4], add[4];
+        bool on[4];                  // slots before the window keep their weight
 #pragma unroll
-                                for (int d = 0; d < 4; ++d)
-                                    if (z[g + d] != -INFINITY) add += kv_exp2(part[d] - z[g + d]);
-                            }
-                        } else {
-                            for (int g = 0; g < a.group; ++g)
-                                if (z[g] != -INFINITY) add += kv_exp2(from[(long long)t * a.group + g] - z[g]);
-                        }
-                    }
-                    a.w_out[w + t] = had + add;
-                }
+        for (int e = 0; e < 4; ++e) {
+            const int u = t + e * lanes;
+            v[e] = a.w_in && u < count ? a.w_in[w + u] : 0.f;
+            on[e] = u < count && t0 + u >= sp.first;
+            add[e] = 0.f;
+        }
+        const float *at = from + (long long)t * a.group;
+        if ((a.group & 3) == 0) {
+            for (int g = 0; g < a.group; g += 4) {
+                float4 x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] = on[e] ? *(const float4 *)(at + e * lanes * a.group + g) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    add[e] += (kv_exp2(x[e].x - z[g]) + kv_exp2(x[e].y - z[g + 1])) + (kv_exp2(x[e].z - z[g + 2]) + kv_exp2(x[e].w - z[g + 3]));
             }
-            __syncthreads();
+        } else {
+            for (int g = 0; g < a.group; ++g) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = on[e] ? at[e * lanes * a.group + g] : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) add[e] += kv_exp2(x[e] - z[g]);
+            }
         }
-        s += n;
-        todo -= n;
-        k = 0;
-        if (n == 0) ++i;             // a sequence without slots
-        else if (++row == a.head_chunks * a.group_chunks) {
-            row = 0;
-            ++i;
-        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t + e * lanes < count) a.w_out[w + t + e * lanes] = v[e] + (on[e] ? add[e] : 0.f);
     }
-    // slots before the window keep their weight
-    if (a.window > 0 && a.w_out != a.w_in)
-        for (int r = 0; r < a.seqs * a.c.heads; ++r) {
-            const KvSpan sp(a, r / a.c.heads);
-            const long long w = r / a.c.heads * a.w_seq + r % a.c.heads * a.w_head;
-            for (int t = share * KV_JOIN_THREADS + tid; t < sp.base; t += shares * KV_JOIN_THREADS) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
-        }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(KV_JOIN_THREADS, 4) kv_attend_join(const __grid_constant__ KvAttend a, int heads_of_chunk)
 {
     extern __shared__ __align__(16) float join_smem[];
-    __shared__ int red[KV_JOIN_WARPS], at[2];
-    const KvLine line(a, red);
-    const int per = a.scores ? KV_JOIN_CTAS : 1, c = blockIdx.x / per, role = blockIdx.x % per, piece = kv_attend_piece(a, line.total);
-    // the piece's steps, or this CTA's share of them
-    const long long at0 = (long long)c * piece;
-    int n = at0 < line.total ? min(line.total - (int)at0, piece) : 0, s = n ? (int)at0 : 0;
-    if (role > 0) {
-        const int lo = (int)((long long)n * (role - 1) / (per - 1)), hi = (int)((long long)n * role / (per - 1));
-        s += lo;
-        n = hi - lo;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int joins = a.pieces * KV_JOIN_ROWS, b = blockIdx.x;
+    if (b < joins) {
+        kv_join_rows<T>(a, heads_of_chunk, b / KV_JOIN_ROWS, b % KV_JOIN_ROWS, join_smem);
+    } else {                         // first the first slots of every sequence, then the next: short sequences' idle CTAs come last
+        const int rows = a.seqs * a.head_chunks, r = (b - joins) % rows;
+        kv_join_weights(a, heads_of_chunk, r / a.head_chunks, r % a.head_chunks, (b - joins) / rows * (KV_JOIN_SLOTS / a.hc), join_smem);
     }
-    int i = 0, row = 0, k = 0;
-    if (n > 0) line.find(a, s, at, i, row, k);
-    if (role > 0) kv_join_weights(a, heads_of_chunk, s, n, piece, i, row, k, c * (per - 1) + role - 1, a.pieces * (per - 1), join_smem);
-    else if (n > 0) kv_join_rows<T>(a, heads_of_chunk, c, piece, i, row, k, join_smem);
-    else kv_join_wait();
 }

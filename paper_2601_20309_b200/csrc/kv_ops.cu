@@ -117,7 +117,7 @@ int32_t launched(kv_ops *o, const char *what)
 struct AttendPlan {
     int dp, nt, warps;                       // kernel shape: padded head dimension, tiles of 8 query heads, warps per CTA
     size_t smem;
-    int64_t lse, part_ml, part_o, total;     // workspace offsets (the scores lie at 0)
+    int64_t lse, row_of, part_of, part_ml, part_o, total;   // workspace offsets (the scores lie at 0)
 };
 
 constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, less the kernel's static share
@@ -138,30 +138,39 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     p.dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     p.nt = k.group <= 8 ? 1 : 2;
     const int most = p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
-    k.hc = 1;
-    for (int d = 2; d <= most; ++d)
-        if (c->kv_heads % d == 0) k.hc = d;
-    k.tw = 1;
-    while (k.hc * k.tw * 2 <= most) k.tw *= 2;
-    p.warps = k.hc * k.tw;
-    k.head_chunks = c->kv_heads / k.hc;
+    // KV heads per CTA: as many as there are warps, so that a CTA reads whole rows of the cache.  Short rows that no CTA
+    // shares (no second kernel) rather go one head to a CTA while there are SMs for it, with more warps along the row.
+    auto shape = [&](int heads_wanted) {
+        k.hc = 1;
+        for (int d = 2; d <= heads_wanted; ++d)
+            if (c->kv_heads % d == 0) k.hc = d;
+        k.tw = 1;
+        while (k.hc * k.tw * 2 <= most) k.tw *= 2;
+        p.warps = k.hc * k.tw;
+        return ceil_div(a->max_len + 15, 16 * k.tw);     // steps of the longest row
+    };
     k.group_chunks = (int)ceil_div(k.group, 8 * p.nt);
+    const bool one_head = (int64_t)a->num_seqs * c->kv_heads * k.group_chunks <= o->sms;
+    int64_t longest = shape(one_head ? 1 : most);
+    // query-head chunks of one KV head all add to the same weights: those go through the second kernel
+    const bool split = longest > ATTEND_ALONE_STEPS || (a->weights_out && k.group_chunks > 1);
+    if (split && one_head) longest = shape(most);
+    k.head_chunks = c->kv_heads / k.hc;
     const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * p.nt * (p.dp / 16 + 1) * 4 * 32 * 4 : 0;
     const int64_t stage = (int64_t)p.warps * 64 * p.dp;
     k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
-    // rows of few steps are not worth a second kernel; several query-head chunks would all add to the same weights
-    const int64_t longest = ceil_div(a->max_len + 15, 16 * k.tw);
-    const bool split = longest > ATTEND_ALONE_STEPS || (a->weights_out && k.group_chunks > 1);
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
-    if (ceil_div(a->max_len + 15, 16 * k.tw) * a->num_seqs * k.head_chunks * k.group_chunks > INT32_MAX)
+    if (longest * a->num_seqs * k.head_chunks * k.group_chunks > INT32_MAX)
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
     k.whole_tiles = c->block_size % 16 == 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
-    p.part_ml = p.lse + align256((int64_t)a->num_seqs * a->q_heads * 4);
+    p.row_of = p.lse + align256(split ? (int64_t)a->num_seqs * a->q_heads * 4 : 0);
+    p.part_of = p.row_of + align256(split ? (int64_t)a->num_seqs * k.head_chunks * k.group_chunks * 16 : 0);
+    p.part_ml = p.part_of + align256((int64_t)k.pieces * 16);
     p.part_o = p.part_ml + align256(parts * 8);
     p.total = p.part_o + parts * c->head_dim * 4;
     return KV_OK;
@@ -280,6 +289,8 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.w_head = a->w_head_stride;
     k.scores = a->weights_out ? (float *)o->ws : nullptr;
     k.row_lse = (float *)(o->ws + p.lse);
+    k.row_of = (int4 *)(o->ws + p.row_of);
+    k.part_of = (int4 *)(o->ws + p.part_of);
     k.part_ml = (float2 *)(o->ws + p.part_ml);
     k.part_o = (float *)(o->ws + p.part_o);
 
@@ -301,7 +312,8 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
         early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         early.val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(k.pieces * (k.scores ? KV_JOIN_CTAS : 1));
+        const int64_t joins = (int64_t)k.pieces * KV_JOIN_ROWS, rows_of_weights = k.scores ? (int64_t)k.seqs * k.head_chunks : 0;
+        cfg.gridDim = dim3((unsigned)(joins + rows_of_weights * ceil_div(a->max_len, KV_JOIN_SLOTS / k.hc)));
         cfg.dynamicSmemBytes = std::max((size_t)kv_join_floats(k.hc, 8 * p.nt, k.pieces), (size_t)k.hc * k.group) * 4;
         cfg.blockDim = dim3(KV_JOIN_THREADS);
         cfg.stream = o->stream;
