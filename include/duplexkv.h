@@ -633,7 +633,8 @@ int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t
  * evicted slots below it, also ascending; the others stay where they are.  (Attention does not mind the order of
  * the slots, so nothing else needs to move.)  K and V rows move in place; weights and ages of the kept slots go to
  * weights_out / order_out, or move in place.  Rows from `keep` on stay as they were.  New lengths: min(lens[i], keep).
- * The blocks from ceil(keep/block_size) on are no longer used; kv_req_shrink tells the block table.
+ * The blocks from ceil(keep/block_size) on are no longer used; kv_req_shrink tells the block table.  Sequences that are
+ * evicted in one call must not share blocks.
  */
 typedef struct {
     int32_t first_layer, num_layers, num_seqs, keep;

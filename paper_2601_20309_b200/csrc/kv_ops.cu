@@ -384,8 +384,12 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
 namespace {
 
 struct EvictPlan {
-    int64_t problems, cap, count, holes, srcs, total;
+    int64_t problems, slots, cap, count, holes, srcs, total;
+    int threads, cluster;
+    bool regs, fused;
 };
+
+constexpr int64_t EVICT_LISTS = 256 << 20;      // bytes of lists that are worth having for every problem at once
 
 int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvEvict &k, EvictPlan &p)
 {
@@ -399,11 +403,20 @@ int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvE
     if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
     p.problems = (int64_t)a->num_layers * a->num_seqs * c->kv_heads;
     p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
+    // 256 threads hold 4096 keys, a cluster of eight such CTAs 32768; longer problems take 1024 threads per CTA, and beyond
+    // 131072 slots the keys are read again in every round
+    p.threads = a->max_len <= 256 * EV_KEYS * EV_CLUSTER ? 256 : 1024;
+    p.regs = a->max_len <= (int64_t)p.threads * EV_KEYS * EV_CLUSTER;
+    p.cluster = 1;
+    while (p.cluster < EV_CLUSTER && (int64_t)p.cluster * p.threads * EV_KEYS < a->max_len) p.cluster *= 2;
+    // with a CTA for every SM, or next to nothing to move, one kernel does it all
+    p.fused = p.problems * p.cluster >= o->sms || p.cap <= 256;
+    p.slots = p.fused && p.cap ? std::max<int64_t>(std::min(p.problems, EVICT_LISTS / (p.cap * 8)), std::min<int64_t>(p.problems, o->sms)) : p.problems;
     p.count = 0;
-    p.holes = align256(p.problems * 4);
-    p.srcs = p.holes + align256(p.problems * p.cap * 4);
-    p.total = p.srcs + p.problems * p.cap * 4;
-    if (p.problems > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
+    p.holes = align256(p.slots * 4);
+    p.srcs = p.holes + align256(p.slots * p.cap * 4);
+    p.total = p.srcs + p.slots * p.cap * 4;
+    if (p.problems * EV_CLUSTER > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
     return KV_OK;
 }
 
@@ -460,9 +473,35 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     k.holes = (int *)(o->ws + p.holes);
     k.srcs = (int *)(o->ws + p.srcs);
     k.cap = (int)p.cap;
-    kv_evict_select<<<dim3(cache->kv_heads, a->num_seqs, a->num_layers), EV_THREADS, 0, o->stream>>>(k);
-    if (p.cap > 0) kv_evict_move<<<dim3((unsigned)p.problems, (unsigned)std::min<int64_t>(ceil_div(p.cap, 32), 64)), 256, 0, o->stream>>>(k);
-    return launched(o, "kv_evict");
+    k.problems = (int)p.problems;
+    k.slots = (int)p.slots;
+    k.fused = p.fused;
+    const int units = cache->head_dim / 4;
+    k.units_shift = units & (units - 1) ? -1 : __builtin_ctz(units);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = p.cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.slots * p.cluster));
+    cfg.blockDim = dim3(p.threads);
+    cfg.stream = o->stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = p.threads == 256 ? cudaLaunchKernelEx(&cfg, kv_evict_select<256, true>, k)
+                    : p.regs         ? cudaLaunchKernelEx(&cfg, kv_evict_select<1024, true>, k)
+                                     : cudaLaunchKernelEx(&cfg, kv_evict_select<1024, false>, k);
+    if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
+    if (!p.fused) {
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        const int64_t parts = std::min(ceil_div(p.cap, EV_MOVE_ROWS), ceil_div(4 * o->sms, p.problems));
+        cfg.gridDim = dim3((unsigned)p.problems, (unsigned)parts);
+        cfg.blockDim = dim3(EV_MOVE_THREADS);
+        e = cudaLaunchKernelEx(&cfg, kv_evict_move, k);
+        if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
+    }
+    return KV_OK;
 }
 
 }  // extern "C"

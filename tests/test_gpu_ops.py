@@ -452,6 +452,33 @@ EVICT = [
 ]
 
 
+# lengths past what one CTA, a cluster of small CTAs and a cluster of large ones hold as keys; a loose bound of the length
+LONG = [([4097, 5], 2, 8, 16, 4000, 40, 4, 0), ([40000, 300, 20000], 1, 8, 16, 15000, 0, 0, 0), ([140001], 1, 8, 64, 70000, 128, 4, 0),
+        ([140001], 1, 8, 64, 300, 0, 0, 0), ([300, 200], 3, 64, 16, 120, 7, 3, 40000), ([300], 1, 64, 16, 290, 7, 3, 200000), ([9000] * 40, 4, 8, 16, 8900, 0, 1, 0)]
+
+
+@pytest.mark.parametrize("kind", ["plain", "ties", "special"])
+@pytest.mark.parametrize("lens,heads,dim,bs,keep,recent,sink,bound", LONG)
+def test_evict_long(ops, lens, heads, dim, bs, keep, recent, sink, bound, kind):
+    c = R.Cache(lens, heads, dim, bs, layers=1, seed=keep, width=-(-max(bound, max(lens)) // bs))
+    w, order = metadata(c, kind, c.g)
+    w, order = (torch.nn.functional.pad(x, (0, max(0, bound - x.shape[-1]))) for x in (w, order))
+    seen = [n + 2 for n in lens]
+    pool, w2, o2 = expect_evict(c, w, order, keep, recent, sink, seen)
+    wd, od = w.cuda(), order.cuda()
+    w_out = torch.full((1, len(lens), heads, keep), -5.0, device="cuda")
+    o_out = torch.full(w_out.shape, -5, dtype=torch.int32, device="cuda")
+    ops.kv_evict(c.handle(B), c.tables, c.lens, bound or c.longest, keep=keep, recent=recent, sink=sink, weights=wd, order=od,
+                 seen=torch.tensor(seen, dtype=torch.int32).cuda(), weights_out=w_out, order_out=o_out)
+    ops.kv_ops_sync()
+    assert torch.equal(c.pool.view(torch.int16), pool.view(torch.int16))
+    for i, n in enumerate(lens):
+        m = min(n, keep)
+        assert torch.equal(w_out[:, i, :, :m].cpu().view(torch.int32), w2[:, i, :, :m].contiguous().view(torch.int32))
+        assert torch.equal(o_out[:, i, :, :m].cpu(), o2[:, i, :, :m])
+        assert (w_out[:, i, :, m:] == -5).all()
+
+
 def metadata(c, kind, g):
     shape = (c.layers, len(c.lens_list), c.heads, c.longest + 3)
     w = torch.rand(shape, generator=g)
