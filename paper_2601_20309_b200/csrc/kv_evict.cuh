@@ -2,15 +2,17 @@
 // the evicted ones leave below it.  Sources (>= keep) and holes (< keep) never meet, so the moves need no order, and
 // in a steady state (keep + d slots) at most d rows move, where closing the gaps would move nearly all.
 //
-// A problem is one (layer, sequence, KV head).  kv_evict_select reads weight and age of every slot once, as one 32-bit key
-// in a register (16 per thread; a cluster of up to eight CTAs shares a long problem), and finds the key of rank `keep`
-// two bits at a time: three candidates are counted per round (one packed warp reduction, one barrier; in a cluster one
-// exchange through distributed shared memory), until exactly `keep` keys reach the candidate or at most EV_CANDS keys
-// agree with it so far; among those one warp finds the rest.  No histogram: the keys of positive weights share their upper bits, and atomics on one bin would queue.
-// Ballots then number the holes and the sources in slot order, and the pairs meet through two short lists.
+// A problem is one (layer, sequence, KV head).  Weight and age of every slot are read once and become one 32-bit key.  The key
+// of rank `keep` is found by digits of ten bits from above: the keys that agree so far are counted by their next digit
+// in shared memory, one warp picks the digit, and as soon as at most EV_CANDS keys are left it finds the rest among
+// them alone.  Ballots then number the holes and the sources in slot order, and the pairs meet through two short lists.
+//   kv_evict_warp     one warp per problem, keys in shared memory: nothing waits at a barrier, and what the warps of a CTA
+//                     would all do is done once.  For short problems, and for many.
+//   kv_evict_select   one CTA per problem, keys in registers, or a cluster of up to eight that exchange their counts
+//                     through distributed shared memory.
+//   kv_evict_move     the rows, spread over the GPU: 32 pairs per warp, eight 16-byte loads per lane in flight.
 //
-// What bounds it: the rows that move, 4*dim bytes read and written each.  With problems for all SMs the same CTA moves its
-// rows, while others select; with few, a second kernel spreads them over the GPU.
+// What bounds it: the rows that move, 4*dim bytes read and written each; for few short problems the chain of loads.
 #pragma once
 #include "kv_ops.cuh"
 
@@ -25,11 +27,12 @@ struct KvEvict {
     int *order_out;
     long long o_layer, o_seq, o_head;
     int *lens_out;
-    int problems, slots;     // slots: how many problems' lists the workspace holds
-    int fused;               // kv_evict_select moves the rows itself
+    int problems;
+    int fused;               // kv_evict_warp moves the rows itself
+    int quads;               // weights and ages may be read and written four at a time
     int units_shift;         // log2 of a row's 16-byte units in K and V together, or -1
-    int *count;              // [slot]: rows that move
-    int *holes, *srcs;       // [slot][cap]
+    int *count;              // [problem]: rows that move
+    int *holes, *srcs;       // [problem][cap]
     int cap;
 };
 
@@ -42,7 +45,7 @@ __device__ __forceinline__ unsigned kv_evict_key(float w, bool held)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_MOVE_THREADS = 256, EV_MOVE_ROWS = 64;
+constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_BINS = 1024 + 32, EV_WARP_SLOTS = 8192, EV_MOVE_WARPS = 4;
 
 struct KvProblem {
     int h, i, l, n;
@@ -65,94 +68,109 @@ __device__ __forceinline__ void kv_cluster_sync()
 
 // sums over a CTA and over its cluster; `before` = over the cluster's lower CTAs
 template <int THREADS> struct KvSums {
-    int (*red)[THREADS / 32];        // [2 * 3]: by turn and value
-    int4 (*table)[EV_CLUSTER];       // [2]
+    int (*red)[THREADS / 32];        // [2 * 2]: by turn and value
+    int2 (*table)[EV_CLUSTER];       // [2]
     int rank, size, turn;
-    // `warps`: every lane already has its warp's sums
-    __device__ __forceinline__ void add(int &x, int &y, int &z, int *before_x, int *before_y, bool warps)
+    __device__ __forceinline__ void add(int &x, int &y, int *before_x, int *before_y)
     {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, buf = turn & 1;
         ++turn;
-        if (!warps) {
-            x = __reduce_add_sync(~0u, x);
-            y = __reduce_add_sync(~0u, y);
-            z = __reduce_add_sync(~0u, z);
-        }
+        x = __reduce_add_sync(~0u, x);
+        y = __reduce_add_sync(~0u, y);
         if (lane == 0) {
-            red[buf * 3][warp] = x;
-            red[buf * 3 + 1][warp] = y;
-            red[buf * 3 + 2][warp] = z;
+            red[buf * 2][warp] = x;
+            red[buf * 2 + 1][warp] = y;
         }
         __syncthreads();
         const bool on = lane < THREADS / 32;
-        x = __reduce_add_sync(~0u, on ? red[buf * 3][lane] : 0);
-        y = __reduce_add_sync(~0u, on ? red[buf * 3 + 1][lane] : 0);
-        z = __reduce_add_sync(~0u, on ? red[buf * 3 + 2][lane] : 0);
-        if (before_x) *before_x = *before_y = 0;
+        x = __reduce_add_sync(~0u, on ? red[buf * 2][lane] : 0);
+        y = __reduce_add_sync(~0u, on ? red[buf * 2 + 1][lane] : 0);
+        *before_x = *before_y = 0;
         if (size == 1) return;
         if ((int)threadIdx.x < size) {
             const unsigned mine = (unsigned)__cvta_generic_to_shared(&table[buf][rank]);
             unsigned there;
             asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(threadIdx.x));
-            asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there), "r"(x), "r"(y), "r"(z), "r"(0) : "memory");
+            asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(there), "r"(x), "r"(y) : "memory");
         }
         kv_cluster_sync();
-        x = y = z = 0;
+        x = y = 0;
         for (int r = 0; r < size; ++r) {
-            const int4 v = table[buf][r];
-            if (before_x && r < rank) {
+            const int2 v = table[buf][r];
+            if (r < rank) {
                 *before_x += v.x;
                 *before_y += v.y;
             }
             x += v.x;
             y += v.y;
-            z += v.z;
         }
     }
 };
 
-// a problem's list from row j0 on, BATCH rows and then `step` further
-template <int THREADS, int BATCH>
-__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int slot, int n, int j0, int step, ulonglong2 *way)
+// Rows of up to 32 pairs, by one warp: lane q has the q-th pair (slot d < keep, slot s >= keep).
+__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int m, int d, int s, ulonglong2 *way)
 {
-    const int tid = threadIdx.x, half = a.c.dim / 8, units = 2 * half;
-    const long long plane = (a.first_layer + p.l) * 2 * a.c.plane_stride + (long long)p.h * a.c.head_stride;
-    auto unit = [&](int u) { return u < half ? u * 16ll : a.c.plane_stride + (u - half) * 16; };
-    const long long own = unit(tid & (units - 1));       // a power of two of units: a thread always has the same
-    for (int j = j0; j < n; j += step) {
-        const int m = min(n - j, BATCH);
-        if (tid < m) {
-            const int d = a.holes[(long long)slot * a.cap + j + tid], s = a.srcs[(long long)slot * a.cap + j + tid];
-            a.w_out[p.to + d] = a.w[p.at + s];
-            if (a.order_out) a.order_out[p.to + d] = a.order[p.at + s];
-            const uint8_t *from = a.c.slot(p.i, s, 0), *into = a.c.slot(p.i, d, 0);
-            const bool ok = from && into;        // a bad block id: the row stays where it is
-            way[tid] = make_ulonglong2(ok ? (unsigned long long)from + plane : 0, (unsigned long long)into + plane);
-        }
-        __syncthreads();
-        // 16 bytes per thread and load, four loads in flight before their stores
-        for (int e = tid; e < m * units; e += 4 * THREADS) {
-            uint4 v[4];
-            uint8_t *to[4];
+    const int lane = threadIdx.x & 31, half = a.c.dim / 8, units = 2 * half;
+    if (lane < m) {
+        a.w_out[p.to + d] = a.w[p.at + s];
+        if (a.order_out) a.order_out[p.to + d] = a.order[p.at + s];
+        const uint8_t *from = a.c.slot(p.i, s, 0), *into = a.c.slot(p.i, d, 0);
+        const long long plane = (a.first_layer + p.l) * 2 * a.c.plane_stride + (long long)p.h * a.c.head_stride;
+        way[lane] = make_ulonglong2(from && into ? (unsigned long long)from + plane : 0, (unsigned long long)into + plane);
+    }
+    __syncwarp();
+    for (int e = lane; e < m * units; e += 32 * 8) {
+        uint4 v[8];
+        uint8_t *to[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int f = e + q * THREADS, r = a.units_shift >= 0 ? f >> a.units_shift : f / units;
-                const long long off = a.units_shift >= 0 ? own : unit(f - r * units);
-                to[q] = nullptr;
-                if (f < m * units) {
-                    const ulonglong2 w = way[r];
-                    if (w.x) {
-                        v[q] = __ldcs((const uint4 *)(w.x + off));
-                        to[q] = (uint8_t *)(w.y + off);
-                    }
+        for (int q = 0; q < 8; ++q) {
+            const int f = e + q * 32, r = a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
+            to[q] = nullptr;
+            if (f < m * units) {
+                const ulonglong2 w = way[r];
+                const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
+                if (w.x) {           // a bad block id: the row stays where it is
+                    v[q] = __ldcs((const uint4 *)(w.x + off));
+                    to[q] = (uint8_t *)(w.y + off);
                 }
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (to[q]) *(uint4 *)to[q] = v[q];
         }
-        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (to[q]) *(uint4 *)to[q] = v[q];
     }
+    __syncwarp();
+}
+
+// Counts by digit: 32 digits per lane, each lane's shifted by one bank.
+__device__ __forceinline__ int kv_evict_bin(int digit) { return digit + (digit >> 5); }
+
+// The digit that the key of rank `want` from above has, by one warp: how many keys have a larger one, how many have it.
+__device__ __forceinline__ int kv_evict_pick(const int *bins, int want, int &larger, int &equal)
+{
+    const int lane = threadIdx.x & 31;
+    // first which 32 digits, then which of them
+    int s = 0;
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) s += bins[lane * 33 + k];
+    int x = s;                       // of this lane and those above it
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_down_sync(~0u, x, o);
+        if (lane + o < 32) x += y;
+    }
+    const int block = __ffs(__ballot_sync(~0u, x - s < want && want <= x)) - 1, above = __shfl_sync(~0u, x - s, block);
+    const int c = bins[block * 33 + lane];
+    x = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_down_sync(~0u, x, o);
+        if (lane + o < 32) x += y;
+    }
+    const int one = __ffs(__ballot_sync(~0u, above + x - c < want && want <= above + x)) - 1;
+    larger = above + __shfl_sync(~0u, x - c, one);
+    equal = __shfl_sync(~0u, c, one);
+    return block * 32 + one;
 }
 
 // The key of rank `want` from above among m <= EV_CANDS keys that agree in the bits above `shift`, found by one warp; `top` has
@@ -185,12 +203,12 @@ template <int THREADS, bool REGS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_select(const __grid_constant__ KvEvict a)
 {
     constexpr int WARPS = THREADS / 32;
-    __shared__ int red[6][WARPS];
-    __shared__ int4 table[2][EV_CLUSTER];
+    __shared__ int red[4][WARPS];
+    __shared__ int2 table[2][EV_CLUSTER];
     __shared__ int place[EV_KEYS * WARPS];
-    __shared__ ulonglong2 way[THREADS];
     __shared__ unsigned cand[EV_CANDS], s_top;
-    __shared__ int s_base, s_count;
+    __shared__ int s_base, s_count, bins[EV_BINS], all_bins[THREADS == 1024 ? EV_BINS : 1];
+    __shared__ int3 s_pick;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned rank, size;
     asm("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
@@ -199,8 +217,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
     if (size > 1) kv_cluster_sync();             // every CTA of the cluster is there before anyone writes into its memory
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int slot = blockIdx.x / size;
-    for (int pi = slot; pi < a.problems; pi += a.slots) {
-        const KvProblem p(a, pi);
+    const KvProblem p(a, slot);
+    {
         const bool apart = a.w_out != a.w;
         if (p.l == 0 && p.h == 0 && rank == 0 && tid == 0 && a.lens_out) a.lens_out[p.i] = min(p.n, a.keep);
         if (p.n <= a.keep) {
@@ -210,7 +228,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
                     if (a.order_out) a.order_out[p.to + t] = a.order[p.at + t];
                 }
             if (rank == 0 && tid == 0) a.count[slot] = 0;
-            continue;
+            return;
         }
         // ---- this CTA's slots: `rounds` times THREADS, side by side
         const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent;
@@ -243,32 +261,51 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
         else if (apart)
             for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) load(r0, true);
 
-        // ---- the largest key that at least `keep` keys reach; `over` keys lie above all that agree with it so far
+        // ---- the key of rank `keep`: `top` as far as it is known, above `shift`; `over` keys are larger, `reach` at least as large
         unsigned top = 0;
         int reach = p.n, over = 0, shift = 32;
         while (shift > 0 && reach != a.keep && reach - over > EV_CANDS) {
-            shift -= 2;
-            int x = 0, y = 0, z = 0;
+            const int width = min(10, shift);
+            for (int d = tid; d < EV_BINS; d += THREADS) bins[d] = 0;
+            __syncthreads();
             for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
                 if (!REGS) load(r0, false);
-                unsigned packed = 0;             // at most 16 keys a thread, 512 a warp: ten bits each
 #pragma unroll
                 for (int r = 0; r < EV_KEYS; ++r)
                     if (r0 + r < rounds) {
-                        packed += key[r] >= (top | 1u << shift) ? 1u : 0u;
-                        packed += key[r] >= (top | 2u << shift) ? 1u << 10 : 0u;
-                        packed += key[r] >= (top | 3u << shift) ? 1u << 20 : 0u;
+                        const bool in = base + (r0 + r) * THREADS + tid < p.n && (shift == 32 || (key[r] ^ top) >> shift == 0);
+                        if (in) atomicAdd(&bins[kv_evict_bin(key[r] >> (shift - width) & ((1 << width) - 1))], 1);
                     }
-                if (REGS) packed = __reduce_add_sync(~0u, packed);
-                x += packed & 1023;
-                y += packed >> 10 & 1023;
-                z += packed >> 20;
             }
-            sums.add(x, y, z, nullptr, nullptr, REGS);
-            if (z >= a.keep) top |= 3u << shift, reach = z;
-            else if (y >= a.keep) top |= 2u << shift, reach = y, over = z;
-            else if (x >= a.keep) top |= 1u << shift, reach = x, over = y;
-            else over = x;
+            int *counts = bins;
+            if (size > 1) {                      // the whole cluster's: every CTA adds all of them up for itself
+                kv_cluster_sync();
+                for (int d = tid; d < EV_BINS; d += THREADS) {
+                    int sum = 0;
+                    for (unsigned r = 0; r < size; ++r) {
+                        unsigned there;
+                        int v;
+                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&bins[d])), "r"(r));
+                        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+                        sum += v;
+                    }
+                    all_bins[d] = sum;
+                }
+                kv_cluster_sync();               // nobody clears counts that others still read
+                counts = all_bins;
+            } else {
+                __syncthreads();
+            }
+            if (warp == 0) {
+                int larger, equal;
+                const int digit = kv_evict_pick(counts, a.keep - over, larger, equal);
+                if (lane == 0) s_pick = make_int3(digit, larger, equal);
+            }
+            __syncthreads();
+            shift -= width;
+            top |= (unsigned)s_pick.x << shift;
+            over += s_pick.y;
+            reach = over + s_pick.z;
         }
         if (shift > 0 && reach != a.keep) {      // few keys are left: one warp finds the rest among them alone
             if (tid == 0) s_count = 0;
@@ -286,9 +323,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
             __syncthreads();
             const int m = reach - over;
             if (size > 1) {                      // every CTA gets the others' too
-                int mine = s_count, none = 0, zero = 0, before, b;
+                int mine = s_count, none = 0, before, b;
                 if (tid) mine = 0;
-                sums.add(mine, none, zero, &before, &b, false);
+                sums.add(mine, none, &before, &b);
                 const int own = s_count;
                 const unsigned x = tid < own ? cand[tid] : 0u;
                 kv_cluster_sync();               // all have read their own
@@ -315,13 +352,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
         const int spare = reach - a.keep;
         int ties = 0, ties_run = 0;
         if (spare > 0) {
-            int none = 0, zero = 0, b;
+            int none = 0, b;
             for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
                 if (!REGS) load(r0, false);
 #pragma unroll
                 for (int r = 0; r < EV_KEYS; ++r) ties += r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top;
             }
-            sums.add(ties, none, zero, &ties_run, &b, false);
+            sums.add(ties, none, &ties_run, &b);
         }
         const int stay_ties = ties - spare;      // of the equals, in slot order
         // ---- lists, numbered in slot order: the slots of a group of 16 rounds by round, warp and lane
@@ -380,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
         int holes_run = 0, srcs_run = 0, moves = 0;
         if (!REGS && size > 1) {                 // every CTA counts its own first, to know where its numbers begin
             const int ties_from = ties_run;
-            int holes = 0, srcs = 0, zero = 0;
+            int holes = 0, srcs = 0;
             for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
                 load(r0, false);
                 const unsigned gone = leavers(r0);
@@ -393,7 +430,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
                         srcs += v & ~low & 1u << lane ? 1 : 0;
                     }
             }
-            sums.add(holes, srcs, zero, &holes_run, &srcs_run, false);
+            sums.add(holes, srcs, &holes_run, &srcs_run);
             moves = holes;
             ties_run = ties_from;
         }
@@ -408,8 +445,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
             }
             number();
             if (REGS && size > 1) {
-                int holes = tid == 0 ? s_base & 0xffff : 0, srcs = tid == 0 ? (int)((unsigned)s_base >> 16) : 0, zero = 0;
-                sums.add(holes, srcs, zero, &holes_run, &srcs_run, false);
+                int holes = tid == 0 ? s_base & 0xffff : 0, srcs = tid == 0 ? (int)((unsigned)s_base >> 16) : 0;
+                sums.add(holes, srcs, &holes_run, &srcs_run);
                 moves = holes;
             }
 #pragma unroll
@@ -430,21 +467,177 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
         }
         if (size == 1) moves = holes_run;
         if (rank == 0 && tid == 0) a.count[slot] = moves;
-        if (a.fused) {
-            if (size > 1) kv_cluster_sync();     // the lists are whole
-            else __syncthreads();
-            kv_evict_rows<THREADS, THREADS>(a, p, slot, moves, rank * THREADS, size * THREADS, way);
-            if (size > 1) kv_cluster_sync();     // and no longer read
-        }
     }
     if (size > 1) kv_cluster_sync();             // nobody leaves while others may still write into its memory
 }
 
-// few problems: their rows spread over the GPU.  CTA (problem, part of its list)
-__global__ void __launch_bounds__(EV_MOVE_THREADS) kv_evict_move(const __grid_constant__ KvEvict a)
+__global__ void __launch_bounds__(32) kv_evict_warp(const __grid_constant__ KvEvict a)
 {
-    __shared__ ulonglong2 way[EV_MOVE_ROWS];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    extern __shared__ __align__(16) unsigned keys[];     // [max_len rounded up to 128], then lists
+    __shared__ unsigned cand[EV_CANDS];
+    __shared__ int bins[EV_BINS];
+    __shared__ ulonglong2 way[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x;
     const KvProblem p(a, blockIdx.x);
-    kv_evict_rows<EV_MOVE_THREADS, EV_MOVE_ROWS>(a, p, blockIdx.x, a.count[blockIdx.x], blockIdx.y * EV_MOVE_ROWS, gridDim.y * EV_MOVE_ROWS, way);
+    const bool apart = a.w_out != a.w, stay = p.n <= a.keep;
+    if (lane == 0) {
+        if (p.l == 0 && p.h == 0 && a.lens_out) a.lens_out[p.i] = min(p.n, a.keep);
+        if (stay && !a.fused) a.count[blockIdx.x] = 0;
+    }
+    const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent, padded = (p.n + 127) & ~127;
+    if (stay && !apart) return;
+    // four slots at a time where the arrays are aligned; sixteen slots per lane in flight
+    if (a.quads) {
+        for (int t0 = lane * 4; t0 < padded; t0 += 128 * 4) {
+            float4 w[4];
+            int4 age[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = t0 + r * 128;              // rows are whole quads: the last may reach past the length
+                w[r] = t < p.n ? *(const float4 *)(a.w + p.at + t) : make_float4(0.f, 0.f, 0.f, 0.f);
+                age[r] = t < p.n && a.order ? *(const int4 *)(a.order + p.at + t) : make_int4(t, t + 1, t + 2, t + 3);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = t0 + r * 128;
+                if (t >= padded) continue;
+                auto key = [&](int e, float x, int y) { return t + e < p.n ? kv_evict_key(x, y >= newest || y < a.sink) : 0u; };
+                *(uint4 *)(keys + t) = make_uint4(key(0, w[r].x, age[r].x), key(1, w[r].y, age[r].y), key(2, w[r].z, age[r].z), key(3, w[r].w, age[r].w));
+                if (!apart) continue;
+                if (t + 3 < min(p.n, a.keep)) {          // holes are overwritten by what moves there
+                    *(float4 *)(a.w_out + p.to + t) = w[r];
+                    if (a.order_out) *(int4 *)(a.order_out + p.to + t) = age[r];
+                } else {
+                    const float x[4] = {w[r].x, w[r].y, w[r].z, w[r].w};
+                    const int y[4] = {age[r].x, age[r].y, age[r].z, age[r].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (t + e < min(p.n, a.keep)) {
+                            a.w_out[p.to + t + e] = x[e];
+                            if (a.order_out) a.order_out[p.to + t + e] = y[e];
+                        }
+                }
+            }
+        }
+    } else {
+        for (int t0 = lane; t0 < padded; t0 += 32 * 16) {
+            float w[16];
+            int age[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = t0 + r * 32;
+                w[r] = t < p.n ? a.w[p.at + t] : 0.f;
+                age[r] = t < p.n ? a.order ? a.order[p.at + t] : t : 0;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = t0 + r * 32;
+                if (t < padded) keys[t] = t < p.n ? kv_evict_key(w[r], age[r] >= newest || age[r] < a.sink) : 0u;
+                if (apart && t < min(p.n, a.keep)) {
+                    a.w_out[p.to + t] = w[r];
+                    if (a.order_out) a.order_out[p.to + t] = age[r];
+                }
+            }
+        }
+    }
+    if (stay) return;
+    __syncwarp();
+    const unsigned below = (1u << lane) - 1;
+    // ---- the key of rank `keep`, as kv_evict_select finds it
+    unsigned top = 0;
+    int reach = p.n, over = 0, shift = 32;
+    while (shift > 0 && reach != a.keep && reach - over > EV_CANDS) {
+        const int width = min(10, shift);
+        for (int d = lane; d < EV_BINS; d += 32) bins[d] = 0;
+        __syncwarp();
+#pragma unroll 4
+        for (int t = lane; t < padded; t += 32) {
+            const unsigned k = keys[t];
+            if (t < p.n && (shift == 32 || (k ^ top) >> shift == 0)) atomicAdd(&bins[kv_evict_bin(k >> (shift - width) & ((1 << width) - 1))], 1);
+        }
+        __syncwarp();
+        int larger, equal;
+        const int digit = kv_evict_pick(bins, a.keep - over, larger, equal);
+        shift -= width;
+        top |= (unsigned)digit << shift;
+        over += larger;
+        reach = over + equal;
+        __syncwarp();
+    }
+    if (shift > 0 && reach != a.keep) {
+        int m = 0;
+#pragma unroll 4
+        for (int t = lane; t < padded; t += 32) {
+            const unsigned k = keys[t];
+            const bool in = t < p.n && (shift == 32 || (k ^ top) >> shift == 0);
+            const unsigned v = __ballot_sync(~0u, in);
+            if (in) cand[m + __popc(v & below)] = k;
+            m += __popc(v);
+        }
+        __syncwarp();
+        reach = over + kv_evict_among(cand, m, a.keep - over, shift, top);
+    }
+    // ---- equals that do not stay; lists in the keys' place: the number of holes found so far never exceeds the slots seen,
+    // and the m-th hole's partner lies at or above slot keep + m
+    int stay_ties = 0;
+    const int spare = reach - a.keep;
+    if (spare > 0) {
+        int ties = 0;
+        for (int t = lane; t < p.n; t += 32) ties += keys[t] == top;
+        stay_ties = __reduce_add_sync(~0u, ties) - spare;
+    }
+    int holes = 0, sources = 0, ties = 0;
+    for (int t0 = 0; t0 < padded; t0 += 128) {           // four rounds of 32 slots, read before anything is written over them
+        unsigned k[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) k[r] = keys[t0 + r * 32 + lane];
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = t0 + r * 32 + lane;
+            bool stays = k[r] >= top;
+            if (spare > 0) {
+                const bool tie = t < p.n && k[r] == top;
+                const unsigned v = __ballot_sync(~0u, tie);
+                if (tie && ties + __popc(v & below) >= stay_ties) stays = false;
+                ties += __popc(v);
+            }
+            const int c = a.keep - (t - lane);           // lanes of this round below `keep`: they can only be holes
+            const unsigned low = c >= 32 ? ~0u : c <= 0 ? 0u : (1u << c) - 1;
+            const unsigned v = __ballot_sync(~0u, t < p.n && (t < a.keep) != stays);
+            const int hole_at = holes, source_at = sources;
+            holes += __popc(v & low);
+            sources += __popc(v & ~low);
+            if (v >> lane & 1) keys[low >> lane & 1 ? hole_at + __popc(v & low & below) : holes + source_at + __popc(v & ~low & below)] = t;
+        }
+        __syncwarp();
+    }
+    if (a.fused) {
+        for (int j = 0; j < holes; j += 32) {
+            const int at = min(j + lane, holes - 1);
+            kv_evict_rows(a, p, min(holes - j, 32), keys[at], keys[holes + at], way);
+        }
+        return;
+    }
+    for (int m = lane; m < holes; m += 32) {
+        a.holes[(long long)blockIdx.x * a.cap + m] = keys[m];
+        a.srcs[(long long)blockIdx.x * a.cap + m] = keys[holes + m];
+    }
+    if (lane == 0) a.count[blockIdx.x] = holes;
+}
+
+// rows (x * EV_MOVE_WARPS + warp) * 32 .. of problem y
+__global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid_constant__ KvEvict a)
+{
+    __shared__ ulonglong2 way[EV_MOVE_WARPS][32];
+    const int warp = threadIdx.x >> 5, j = (blockIdx.x * EV_MOVE_WARPS + warp) * 32, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int y = blockIdx.y; y < a.problems; y += gridDim.y) {
+        const int n = a.count[y];
+        if (j >= n) continue;
+        const KvProblem p(a, y);
+        const int at = min(j + lane, n - 1);
+        kv_evict_rows(a, p, min(n - j, 32), a.holes[(long long)y * a.cap + at], a.srcs[(long long)y * a.cap + at], way[warp]);
+    }
 }

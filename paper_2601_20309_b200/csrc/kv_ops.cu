@@ -384,12 +384,13 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
 namespace {
 
 struct EvictPlan {
-    int64_t problems, slots, cap, count, holes, srcs, total;
-    int threads, cluster;
+    int64_t problems, cap, count, holes, srcs, total;
+    int threads, cluster;                       // threads 32: a warp per problem
     bool regs, fused;
 };
 
-constexpr int64_t EVICT_LISTS = 256 << 20;      // bytes of lists that are worth having for every problem at once
+constexpr int EVICT_WARP_SHORT = 1024;          // up to here a warp per problem has the lowest latency
+constexpr int EVICT_FUSED_ROWS = 64;            // up to here it moves the rows itself
 
 int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvEvict &k, EvictPlan &p)
 {
@@ -402,21 +403,19 @@ int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvE
     if ((int64_t)a->recent + a->sink > a->keep) return fail(o, KV_ERR_INVALID_ARG, "recent + sink exceeds keep");
     if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
     p.problems = (int64_t)a->num_layers * a->num_seqs * c->kv_heads;
-    p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
-    // 256 threads hold 4096 keys, a cluster of eight such CTAs 32768; longer problems take 1024 threads per CTA, and beyond
-    // 131072 slots the keys are read again in every round
-    p.threads = a->max_len <= 256 * EV_KEYS * EV_CLUSTER ? 256 : 1024;
-    p.regs = a->max_len <= (int64_t)p.threads * EV_KEYS * EV_CLUSTER;
-    p.cluster = 1;
-    while (p.cluster < EV_CLUSTER && (int64_t)p.cluster * p.threads * EV_KEYS < a->max_len) p.cluster *= 2;
-    // with a CTA for every SM, or next to nothing to move, one kernel does it all
-    p.fused = p.problems * p.cluster >= o->sms || p.cap <= 256;
-    p.slots = p.fused && p.cap ? std::max<int64_t>(std::min(p.problems, EVICT_LISTS / (p.cap * 8)), std::min<int64_t>(p.problems, o->sms)) : p.problems;
-    p.count = 0;
-    p.holes = align256(p.slots * 4);
-    p.srcs = p.holes + align256(p.slots * p.cap * 4);
-    p.total = p.srcs + p.slots * p.cap * 4;
     if (p.problems * EV_CLUSTER > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
+    p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
+    // A warp per problem where problems are short, or enough to fill the GPU with warps.  Else 256 threads hold 4096 keys and
+    // 1024 threads 16384; a cluster of eight such CTAs holds 131072, and beyond that the keys are read again in every round
+    p.threads = a->max_len <= EVICT_WARP_SHORT || (a->max_len <= EV_WARP_SLOTS && p.problems >= 4 * o->sms) ? 32 : a->max_len <= 256 * EV_KEYS ? 256 : 1024;
+    p.cluster = 1;
+    while (p.threads == 1024 && p.cluster < EV_CLUSTER && (int64_t)p.cluster * p.threads * EV_KEYS < a->max_len) p.cluster *= 2;
+    p.regs = a->max_len <= (int64_t)p.cluster * p.threads * EV_KEYS;
+    p.fused = p.threads == 32 && p.cap <= EVICT_FUSED_ROWS;
+    p.count = 0;
+    p.holes = align256(p.problems * 4);
+    p.srcs = p.holes + align256(p.problems * p.cap * 4);
+    p.total = p.srcs + p.problems * p.cap * 4;
     return KV_OK;
 }
 
@@ -474,30 +473,42 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     k.srcs = (int *)(o->ws + p.srcs);
     k.cap = (int)p.cap;
     k.problems = (int)p.problems;
-    k.slots = (int)p.slots;
     k.fused = p.fused;
+    const auto quad = [](const void *q, int64_t x, int64_t y, int64_t z) { return (uintptr_t)q % 16 == 0 && x % 4 == 0 && y % 4 == 0 && z % 4 == 0; };
+    // a quad that begins below the length must end inside its row: the last row of the array has max_len entries at least
+    k.quads = a->max_len % 4 == 0 && quad(k.w, k.m_layer, k.m_seq, k.m_head) && quad(k.order, 0, 0, 0) && quad(k.w_out, k.o_layer, k.o_seq, k.o_head) &&
+              quad(k.order_out, 0, 0, 0);
     const int units = cache->head_dim / 4;
     k.units_shift = units & (units - 1) ? -1 : __builtin_ctz(units);
     cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = p.cluster;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.slots * p.cluster));
-    cfg.blockDim = dim3(p.threads);
     cfg.stream = o->stream;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = p.threads == 256 ? cudaLaunchKernelEx(&cfg, kv_evict_select<256, true>, k)
-                    : p.regs         ? cudaLaunchKernelEx(&cfg, kv_evict_select<1024, true>, k)
-                                     : cudaLaunchKernelEx(&cfg, kv_evict_select<1024, false>, k);
+    cudaError_t e;
+    if (p.threads == 32) {
+        cfg.gridDim = dim3((unsigned)p.problems);
+        cfg.blockDim = dim3(32);
+        cfg.dynamicSmemBytes = align256(a->max_len * 4) + 256;
+        e = cudaLaunchKernelEx(&cfg, kv_evict_warp, k);
+    } else {
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = p.cluster;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+        cfg.gridDim = dim3((unsigned)(p.problems * p.cluster));
+        cfg.blockDim = dim3(p.threads);
+        e = p.threads == 256 ? cudaLaunchKernelEx(&cfg, kv_evict_select<256, true>, k)
+            : p.regs         ? cudaLaunchKernelEx(&cfg, kv_evict_select<1024, true>, k)
+                             : cudaLaunchKernelEx(&cfg, kv_evict_select<1024, false>, k);
+    }
     if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
-    if (!p.fused) {
+    if (!p.fused && p.cap > 0) {
         attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr.val.programmaticStreamSerializationAllowed = 1;
-        const int64_t parts = std::min(ceil_div(p.cap, EV_MOVE_ROWS), ceil_div(4 * o->sms, p.problems));
-        cfg.gridDim = dim3((unsigned)p.problems, (unsigned)parts);
-        cfg.blockDim = dim3(EV_MOVE_THREADS);
+        cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = 0;
+        cfg.gridDim = dim3((unsigned)ceil_div(p.cap, EV_MOVE_WARPS * 32), (unsigned)std::min<int64_t>(p.problems, 65535));
+        cfg.blockDim = dim3(EV_MOVE_WARPS * 32);
         e = cudaLaunchKernelEx(&cfg, kv_evict_move, k);
         if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
     }
