@@ -215,7 +215,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
     asm("mov.u32 %0, %cluster_nctaid.x;" : "=r"(size));
     KvSums<THREADS> sums{red, table, (int)rank, (int)size, 0};
     if (size > 1) kv_cluster_sync();             // every CTA of the cluster is there before anyone writes into its memory
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int slot = blockIdx.x / size;
     const KvProblem p(a, slot);
     {
@@ -477,7 +476,6 @@ __global__ void __launch_bounds__(32) kv_evict_warp(const __grid_constant__ KvEv
     __shared__ unsigned cand[EV_CANDS];
     __shared__ int bins[EV_BINS];
     __shared__ ulonglong2 way[32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x;
     const KvProblem p(a, blockIdx.x);
     const bool apart = a.w_out != a.w, stay = p.n <= a.keep;
@@ -632,7 +630,6 @@ __global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid
 {
     __shared__ ulonglong2 way[EV_MOVE_WARPS][32];
     const int warp = threadIdx.x >> 5, j = (blockIdx.x * EV_MOVE_WARPS + warp) * 32, lane = threadIdx.x & 31;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int y = blockIdx.y; y < a.problems; y += gridDim.y) {
         const int n = a.count[y];
         if (j >= n) continue;

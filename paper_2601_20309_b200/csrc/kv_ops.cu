@@ -374,8 +374,29 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     k.m_head = a->m_head_stride;
     k.token_order = a->token_order;
     memcpy(k.axis_of, a->axis_of, sizeof(k.axis_of));
-    if (cache->dtype == KV_DT_BF16) kv_append_tokens<__nv_bfloat16><<<(unsigned)a->num_tokens, 128, 0, o->stream>>>(k);
-    else kv_append_tokens<__half><<<(unsigned)a->num_tokens, 128, 0, o->stream>>>(k);
+    k.num_tokens = a->num_tokens;
+    // 16 bytes at a time where every row begins on 16 bytes and the pairs that turn together are whole packs of eight
+    const auto packs = [](const void *q, int64_t x, int64_t y) { return (uintptr_t)q % 16 == 0 && x % 8 == 0 && y % 8 == 0; };
+    const bool wide = (a->pair_style ? a->rotary_dim : a->rotary_dim / 2) % 8 == 0 && packs(a->k, a->k_token_stride, a->k_head_stride) &&
+                      packs(a->v, a->v_token_stride, a->v_head_stride) &&
+                      (!a->q || (packs(a->q, a->q_token_stride, a->q_head_stride) && packs(a->q_out, a->qo_token_stride, a->qo_head_stride)));
+    const int v = wide ? 8 : 1;
+    k.units = (wide && a->pair_style ? a->rotary_dim / 8 : a->rotary_dim / 2 / v) + (cache->head_dim - a->rotary_dim) / v;
+    // one token per CTA while all of them have room at once, else several, which share what is done once per CTA
+    const int64_t row_items = (int64_t)((a->q ? a->q_heads : 0) + 2 * cache->kv_heads) * k.units;
+    if (row_items > 1 << 20) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
+    k.per = row_items > 1 << 14 ? 1 : (int)std::min<int64_t>(AP_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
+    k.by_units = (unsigned)ceil_div(int64_t(1) << 32, k.units);
+    k.by_token = (unsigned)ceil_div(int64_t(1) << 32, row_items);
+    const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
+    const size_t smem = (size_t)k.per * (a->rotary_dim / 2) * sizeof(float2);
+    if (cache->dtype == KV_DT_BF16) {
+        if (wide) kv_append_tokens<__nv_bfloat16, 8><<<grid, AP_THREADS, smem, o->stream>>>(k);
+        else kv_append_tokens<__nv_bfloat16, 1><<<grid, AP_THREADS, smem, o->stream>>>(k);
+    } else {
+        if (wide) kv_append_tokens<__half, 8><<<grid, AP_THREADS, smem, o->stream>>>(k);
+        else kv_append_tokens<__half, 1><<<grid, AP_THREADS, smem, o->stream>>>(k);
+    }
     return launched(o, "kv_append");
 }
 
@@ -503,9 +524,9 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     }
     if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
     if (!p.fused && p.cap > 0) {
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        cfg.numAttrs = 1;
+        // an ordinary launch: its CTAs waiting on the SMs beside the first kernel's cost more than the gap (137 against 123 us
+        // in a steady state of 32 layers and 8 sequences)
+        cfg.numAttrs = 0;
         cfg.dynamicSmemBytes = 0;
         cfg.gridDim = dim3((unsigned)ceil_div(p.cap, EV_MOVE_WARPS * 32), (unsigned)std::min<int64_t>(p.problems, 65535));
         cfg.blockDim = dim3(EV_MOVE_WARPS * 32);

@@ -291,6 +291,9 @@ APPEND = [
     ([0], [40], 10, 5, 8, 3, "bf16", 0, 2, True, 1),
     ([4, 4], [3, 4], 4, 4, 96, 16, "f16", 0, 0, True, 1),
     ([0] * 150, [1] * 150, 4, 2, 64, 16, "bf16", 0, 64, True, 3),
+    ([0, 9], [5, 3], 3, 1, 8, 16, "bf16", 0, 0, True, 1),
+    ([0, 9], [5, 3], 3, 1, 8, 16, "f16", 0, 8, False, 1),
+    ([20, 0], [3000, 900], 6, 3, 128, 16, "bf16", 0, 96, False, 2),
     ([3] * 70, [i % 5 + 1 for i in range(70)], 7, 7, 112, 16, "bf16", 0, 112, True, 3),
 ]
 
