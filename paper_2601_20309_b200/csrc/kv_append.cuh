@@ -28,9 +28,9 @@ struct KvAppend {
     long long m_seq, m_head;
     const int *token_order;
     int vec;             // elements a thread moves at once: 8, or 1 where rows are not 16-byte aligned or odd in size
-    int units;           // work items of a row: packs of `vec` elements with those they turn with, then packs that pass
+    int units;           // threads of a row: packs of `vec` elements with those they turn with, then packs that pass
     int per;             // tokens per CTA
-    unsigned by_units, by_token;     // 2^32 / d, rounded up (0 for d = 1), for d = units and d = units * rows
+    unsigned by_rows;    // 2^32 / rows of a token, rounded up
     uint8_t axis_of[128];
 };
 
@@ -49,55 +49,69 @@ __device__ __forceinline__ int kv_seq_of(const int *starts, int num_seqs, long l
     return lo;
 }
 
-constexpr int AP_THREADS = 256, AP_ITEMS = 2, AP_TOKENS = 16;
+constexpr int AP_THREADS = 256, AP_ROWS = 2, AP_TOKENS = 16;
 
-// e / d by the rounded-up reciprocal (0 for d = 1): exact for e < 2^32 / d
-__device__ __forceinline__ int kv_divide(int e, unsigned reciprocal) { return reciprocal ? (int)__umulhi((unsigned)e, reciprocal) : e; }
-
+// what a thread moves at once: eight elements as four pairs, or one element
 template <typename T, int V> struct KvPack;
-template <typename T> struct __align__(16) KvPack<T, 8> { T e[8]; };
-template <typename T> struct KvPack<T, 1> { T e[1]; };
+template <typename T> struct __align__(16) KvPack<T, 8> { unsigned w[4]; };
+template <typename T> struct KvPack<T, 1> { T e; };
+
+__device__ __forceinline__ float2 kv_unpair(unsigned w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 kv_unpair(unsigned w, __half) { return __half22float2(*(const __half2 *)&w); }
+__device__ __forceinline__ unsigned kv_pair(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *(const unsigned *)&v;
+}
+__device__ __forceinline__ unsigned kv_pair(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *(const unsigned *)&v;
+}
 
 template <typename T, int V>
 __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_constant__ KvAppend a)
 {
     using Pack = KvPack<T, V>;
-    extern __shared__ float2 turn[];             // [token][frequency]: cosine and sine
-    __shared__ uint8_t *kv_row[AP_TOKENS];       // K of the token's slot, or nullptr
+    extern __shared__ __align__(16) float2 turn[];       // [token][frequency]: cosine and sine
+    __shared__ uint8_t *kv_row[AP_TOKENS];               // K of the token's slot, or nullptr
     __shared__ long long meta[AP_TOKENS];
-    const int tid = threadIdx.x, dim = a.c.dim, half = a.rotary >> 1, heads = a.c.heads, q_heads = a.q ? a.q_heads : 0;
-    // a row: `turns` items that turn (in the halves style a pack and its partners, else a pack of pairs), then packs that pass
+    const int tid = threadIdx.x, dim = a.c.dim, half = a.rotary >> 1, heads = a.c.heads, q_heads = a.q ? a.q_heads : 0, rows = q_heads + 2 * heads;
     const bool halves = a.pairs_style == 0;
-    const int turns = halves ? half / V : V == 1 ? half : a.rotary / V, units = a.units, rows = q_heads + 2 * heads;
+    // A thread has the same place in every row it works on: unit u.  The first `turns` units turn: a pack and its partners
+    // (halves style), a pack of pairs, or a single pair; the others pass.
+    const int turns = halves ? half / V : V == 1 ? half : a.rotary / V, lanes = AP_THREADS / a.units, u = tid % a.units, mine = tid / a.units;
+    const bool turned = u < turns;
+    const int lo = turned ? halves || V > 1 ? u * V : 2 * u : a.rotary + (u - turns) * V, hi = !turned ? -1 : halves ? lo + half : V == 1 ? lo + 1 : -1;
+    // frequencies of a unit lie two by two, side by side with the other units': a warp's reads of them do not collide
+    const int per_unit = V == 1 ? 1 : halves ? 8 : 4;
     const long long first = (long long)blockIdx.x * a.per;
-    const int tokens = (int)min((long long)a.per, a.num_tokens - first), items = tokens * rows * units;
-    for (int e0 = tid; e0 - tid < items; e0 += AP_THREADS * AP_ITEMS) {
-        Pack x[AP_ITEMS], y[AP_ITEMS];
-        int token[AP_ITEMS], row[AP_ITEMS], lo[AP_ITEMS], hi[AP_ITEMS];
+    const int tokens = (int)min((long long)a.per, a.num_tokens - first), total = tokens * rows;
+    for (int r0 = mine; r0 - mine < total; r0 += lanes * AP_ROWS) {
+        Pack x[AP_ROWS], y[AP_ROWS];
+        int token[AP_ROWS], row[AP_ROWS];
 #pragma unroll
-        for (int n = 0; n < AP_ITEMS; ++n) {
-            const int e = e0 + n * AP_THREADS;
+        for (int n = 0; n < AP_ROWS; ++n) {
+            const int r = r0 + n * lanes;
             row[n] = -1;
-            if (e < items) {
-                token[n] = a.per == 1 ? 0 : kv_divide(e, a.by_token);
-                const int f = e - token[n] * rows * units, u = f - kv_divide(f, a.by_units) * units;
-                row[n] = kv_divide(f, a.by_units);
-                const bool pair = u < turns;
-                lo[n] = pair ? halves || V > 1 ? u * V : 2 * u : a.rotary + (u - turns) * V;
-                hi[n] = pair ? halves ? lo[n] + half : V == 1 ? lo[n] + 1 : -1 : -1;
+            if (r < total && mine < lanes) {
+                token[n] = (int)__umulhi((unsigned)r, a.by_rows);
+                row[n] = r - token[n] * rows;
                 const long long t = first + token[n];
                 const T *from = row[n] < q_heads           ? (const T *)a.q + t * a.q_tok + row[n] * a.q_head
                                 : row[n] < q_heads + heads ? (const T *)a.k + t * a.k_tok + (row[n] - q_heads) * a.k_head
                                                            : (const T *)a.v + t * a.v_tok + (row[n] - q_heads - heads) * a.v_head;
-                x[n] = *(const Pack *)(from + lo[n]);
-                if (hi[n] >= 0) y[n] = *(const Pack *)(from + hi[n]);
+                x[n] = *(const Pack *)(from + lo);
+                if (hi >= 0) y[n] = *(const Pack *)(from + hi);
             }
         }
-        if (e0 == tid) {             // the first time: angles and slots
+        if (r0 == mine) {            // the first time: angles and slots
             for (int f = tid; f < tokens * half; f += AP_THREADS) {
                 const int k = f / half, q = f - k * half;
                 const double cycles = (double)a.positions[a.axis_of[q] * a.axis_stride + first + k] * (double)a.inv_freq[q] * 0.15915494309189533577;
-                sincospif((float)(2.0 * (cycles - rint(cycles))), &turn[f].y, &turn[f].x);
+                float2 cs;
+                sincospif((float)(2.0 * (cycles - rint(cycles))), &cs.y, &cs.x);
+                turn[k * half + (V == 1 ? q : (q % per_unit / 2 * turns + q / per_unit) * 2 + q % 2)] = cs;
             }
             for (int k = tid >> 5; k < tokens; k += AP_THREADS / 32) {
                 const long long t = first + k;
@@ -115,33 +129,40 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
             __syncthreads();
         }
 #pragma unroll
-        for (int n = 0; n < AP_ITEMS; ++n) {
+        for (int n = 0; n < AP_ROWS; ++n) {
             if (row[n] < 0) continue;
             const bool is_v = row[n] >= q_heads + heads;
             T *to;
             if (row[n] < q_heads) to = (T *)a.q_out + (first + token[n]) * a.qo_tok + row[n] * a.qo_head;
             else if (kv_row[token[n]]) to = (T *)(kv_row[token[n]] + (is_v ? a.c.plane_stride : 0)) + (row[n] - q_heads - (is_v ? heads : 0)) * dim;
             else continue;
-            if (!is_v && lo[n] < a.rotary) {
-                const float2 *cs = turn + token[n] * half + (halves ? lo[n] : lo[n] >> 1);
-                if (halves || V == 1) {
+            if (!is_v && turned) {
+                const float2 *cs = turn + token[n] * half;
+                if constexpr (V == 1) {
+                    const float2 c = cs[u];
+                    const float p = kv_float(x[n].e), q = kv_float(y[n].e);
+                    x[n].e = kv_round<T>(p * c.x - q * c.y);
+                    y[n].e = kv_round<T>(p * c.y + q * c.x);
+                } else if (halves) {
 #pragma unroll
-                    for (int d = 0; d < V; ++d) {
-                        const float u = kv_float(x[n].e[d]), w = kv_float(y[n].e[d]);
-                        x[n].e[d] = kv_round<T>(u * cs[d].x - w * cs[d].y);
-                        y[n].e[d] = kv_round<T>(u * cs[d].y + w * cs[d].x);
+                    for (int j = 0; j < 4; ++j) {        // two frequencies
+                        const float4 c = *(const float4 *)(cs + (j * turns + u) * 2);
+                        const float2 p = kv_unpair(x[n].w[j], T()), q = kv_unpair(y[n].w[j], T());
+                        x[n].w[j] = kv_pair(p.x * c.x - q.x * c.y, p.y * c.z - q.y * c.w, T());
+                        y[n].w[j] = kv_pair(p.x * c.y + q.x * c.x, p.y * c.w + q.y * c.z, T());
                     }
                 } else {
 #pragma unroll
-                    for (int d = 0; d < V / 2; ++d) {
-                        const float u = kv_float(x[n].e[2 * d]), w = kv_float(x[n].e[2 * d + 1]);
-                        x[n].e[2 * d] = kv_round<T>(u * cs[d].x - w * cs[d].y);
-                        x[n].e[2 * d + 1] = kv_round<T>(u * cs[d].y + w * cs[d].x);
+                    for (int j = 0; j < 2; ++j) {
+                        const float4 c = *(const float4 *)(cs + (j * turns + u) * 2);
+                        const float2 p = kv_unpair(x[n].w[2 * j], T()), q = kv_unpair(x[n].w[2 * j + 1], T());
+                        x[n].w[2 * j] = kv_pair(p.x * c.x - p.y * c.y, p.x * c.y + p.y * c.x, T());
+                        x[n].w[2 * j + 1] = kv_pair(q.x * c.z - q.y * c.w, q.x * c.w + q.y * c.z, T());
                     }
                 }
             }
-            *(Pack *)(to + lo[n]) = x[n];
-            if (hi[n] >= 0) *(Pack *)(to + hi[n]) = y[n];
+            *(Pack *)(to + lo) = x[n];
+            if (hi >= 0) *(Pack *)(to + hi) = y[n];
         }
     }
     if (a.weights || a.order)

@@ -383,11 +383,11 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     const int v = wide ? 8 : 1;
     k.units = (wide && a->pair_style ? a->rotary_dim / 8 : a->rotary_dim / 2 / v) + (cache->head_dim - a->rotary_dim) / v;
     // one token per CTA while all of them have room at once, else several, which share what is done once per CTA
-    const int64_t row_items = (int64_t)((a->q ? a->q_heads : 0) + 2 * cache->kv_heads) * k.units;
-    if (row_items > 1 << 20) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
-    k.per = row_items > 1 << 14 ? 1 : (int)std::min<int64_t>(AP_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
-    k.by_units = (unsigned)ceil_div(int64_t(1) << 32, k.units);
-    k.by_token = (unsigned)ceil_div(int64_t(1) << 32, row_items);
+    // a row number below 2^32 / rows is divided by rows exactly with the reciprocal
+    const int64_t rows = (int64_t)(a->q ? a->q_heads : 0) + 2 * cache->kv_heads;
+    if (rows > 4096) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
+    k.per = (int)std::min<int64_t>(AP_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
+    k.by_rows = (unsigned)ceil_div(int64_t(1) << 32, rows);
     const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
     const size_t smem = (size_t)k.per * (a->rotary_dim / 2) * sizeof(float2);
     if (cache->dtype == KV_DT_BF16) {
