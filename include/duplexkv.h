@@ -616,9 +616,10 @@ typedef struct {
     const int32_t *block_tables;    /* [num_seqs][table_width]                                          */
     int64_t table_stride;
     const int32_t *lens;            /* [num_seqs], with the new tokens                                  */
-    int32_t table_width, pad_;
-    float   *weights;               /* [num_seqs][kv_heads][slots] or NULL                              */
-    int32_t *order;                 /* [num_seqs][kv_heads][slots] or NULL; both with the strides below */
+    int32_t table_width;
+    int32_t num_slots;              /* of weights and order; a token whose slot lies beyond counts as one of a bad length */
+    float   *weights;               /* [num_seqs][kv_heads][num_slots] or NULL                          */
+    int32_t *order;                 /* likewise; both with the strides below                            */
     int64_t m_seq_stride, m_head_stride;
     const int32_t *token_order;     /* [num_tokens]: what goes into order; NULL = positions of axis 0   */
     uint8_t axis_of[128];           /* HOST, by value: axis of each frequency                           */

@@ -118,7 +118,7 @@ class kv_append_args_t(C.Structure):
                 ("v_head_stride", C.c_int64), ("q_out", C.c_void_p), ("qo_token_stride", C.c_int64),
                 ("qo_head_stride", C.c_int64), ("positions", C.c_void_p), ("axis_stride", C.c_int64),
                 ("inv_freq", C.c_void_p), ("seq_starts", C.c_void_p), ("block_tables", C.c_void_p),
-                ("table_stride", C.c_int64), ("lens", C.c_void_p), ("table_width", C.c_int32), ("pad_", C.c_int32),
+                ("table_stride", C.c_int64), ("lens", C.c_void_p), ("table_width", C.c_int32), ("num_slots", C.c_int32),
                 ("weights", C.c_void_p), ("order", C.c_void_p), ("m_seq_stride", C.c_int64), ("m_head_stride", C.c_int64),
                 ("token_order", C.c_void_p), ("axis_of", C.c_uint8 * 128)]
 
@@ -603,14 +603,20 @@ class KVTable:
 KV_DT_BF16 = 0
 KV_DT_F16 = 1
 KV_DTYPES = {"bf16": KV_DT_BF16, "f16": KV_DT_F16}
-_TORCH_TYPES: dict = {}     # torch dtype object -> its name, filled as dtypes turn up
+_ops_ext = None
 
 
-def _dtype(t) -> str:
-    d = t.dtype
-    if d not in _TORCH_TYPES:
-        _TORCH_TYPES[d] = {"torch.bfloat16": "bf16", "torch.float16": "f16"}.get(str(d), str(d))
-    return _TORCH_TYPES[d]
+def ops_ext():
+    """Load (building first if needed) the extension that marshals tensors for ``KVOps``.  Raises if it cannot be had."""
+    global _ops_ext
+    if _ops_ext is None:
+        lib()
+        import importlib.util
+        import torch  # noqa: F401  (the extension links against it)
+        spec = importlib.util.spec_from_file_location("paper_2601_20309_b200._kvops", _build.build_ops_ext())
+        _ops_ext = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_ops_ext)
+    return _ops_ext
 
 
 class KVCache:
@@ -630,23 +636,26 @@ class KVCache:
 
 
 class KVOps:
-    """Operators on the device cache, on one stream (a ``cudaStream_t`` as an int; None or 0 = the default stream): argument
-    marshalling of ``kv_append``, ``kv_attend`` and ``kv_evict``.  Arrays are CUDA tensors (anything with ``data_ptr``,
-    ``dtype``, ``shape``, ``stride`` and ``get_device``); rows may lie at any stride, the elements of a row side by side.
-    Tensors of another stream have to be ordered by the caller, and kept until the stream is done with them."""
+    """Operators on the device cache, on one stream (a ``cudaStream_t`` as an int; None or 0 = the default stream).  Arrays are
+    CUDA tensors; rows may lie at any stride, the elements of a row side by side.  Wrong types, shapes and devices raise
+    ``ValueError``; the C status comes back, or raises ``KVError`` with ``check``.  Tensors of another stream have to be
+    ordered by the caller, and kept until this stream is done with them."""
 
     def __init__(self, device_id: int = 0, stream: Optional[int] = None):
         self._h = C.c_void_p()
         self.device_id = device_id
+        ext = ops_ext()
+        self._ext_attend, self._ext_append, self._ext_evict = ext.attend, ext.append, ext.evict
         rc = lib().kv_ops_create(device_id, stream or None, C.byref(self._h))
         if rc != KV_OK:
             raise KVError(rc, lib().kv_ops_last_error(None).decode())
-        self._attend, self._append, self._evict = kv_attend_args_t(), kv_append_args_t(), kv_evict_args_t()
+        self._address = self._h.value
 
     def destroy(self) -> None:
         if self._h:
             lib().kv_ops_destroy(self._h)
             self._h = C.c_void_p()
+            self._address = 0
 
     def __del__(self):
         try:
@@ -674,49 +683,12 @@ class KVOps:
     def kv_ops_reserve(self, nbytes: int, check: bool = True) -> int:
         return self._ret(lib().kv_ops_reserve(self._h, nbytes), check)
 
-    def _ptr(self, t, dtype: str, what: str) -> int:
-        if _dtype(t) != dtype:
-            raise ValueError(f"{what} must be {dtype}, not {_dtype(t)}")
-        if t.get_device() != self.device_id:
-            raise ValueError(f"{what} must be on cuda:{self.device_id}")
-        return t.data_ptr()
-
-    def _rows(self, t, dtype: str, shape: tuple, what: str) -> tuple:
-        """Address and outer strides of a tensor whose leading dimensions are ``shape`` (None: any size)."""
-        p, st = self._ptr(t, dtype, what), t.stride()
-        have = t.shape
-        if len(have) != len(shape) or any(b is not None and a != b for a, b in zip(have, shape)):
-            raise ValueError(f"{what} must have shape {shape}, not {tuple(have)}")
-        if st[-1] != 1 and have[-1] > 1:
-            raise ValueError(f"{what}: the last dimension must be contiguous")
-        return (p,) + st[:-1]
-
     def kv_attend(self, cache: KVCache, layer: int, q, block_tables, lens, max_len: int, *, out, lse=None, window: int = 0,
                   scale: float = 0.0, weights_in=None, weights_out=None, check: bool = True) -> int:
         """q, out [seqs, q_heads, dim]; block_tables int32 [seqs, width]; lens int32 [seqs] (with the new token); max_len: a
         bound of lens known on the host; lse float32 [seqs, q_heads]; weights float32 [seqs, kv_heads, >= max_len]."""
-        a = self._attend
-        n, heads = len(q), q.shape[1]
-        a.layer, a.num_seqs, a.q_heads, a.window, a.max_len, a.scale = layer, n, heads, window, max_len, scale
-        shape = (n, heads, cache.dim)
-        a.q, a.q_seq_stride, a.q_head_stride = self._rows(q, cache.dtype, shape, "q")
-        a.out, a.out_seq_stride, a.out_head_stride = self._rows(out, cache.dtype, shape, "out")
-        self._tables(a, block_tables, lens, n)
-        if lse is None:
-            a.lse = None
-        else:
-            a.lse, stride = self._rows(lse, "torch.float32", (n, heads), "lse")
-            if stride != heads and n > 1:
-                raise ValueError("lse must be contiguous")
-        a.weights_in = a.weights_out = None
-        if weights_out is not None:
-            a.weights_out, a.w_seq_stride, a.w_head_stride = self._weights(weights_out, "torch.float32", (n, cache.heads), max_len, "weights_out")
-        if weights_in is not None:
-            p, s0, s1 = self._weights(weights_in, "torch.float32", (n, cache.heads), max_len, "weights_in")
-            if weights_out is not None and (s0, s1) != (a.w_seq_stride, a.w_head_stride):
-                raise ValueError("weights_in and weights_out differ in strides")
-            a.weights_in = p
-        return self._ret(lib().kv_attend(self._h, cache.address, C.addressof(a)), check)
+        return self._ret(self._ext_attend(self._address, self.device_id, cache.address, layer, q, block_tables, lens, max_len, out,
+                                          lse, window, scale, weights_in, weights_out), check)
 
     def kv_attend_workspace(self, cache: KVCache, num_seqs: int, q_heads: int, max_len: int, weights: bool = True) -> int:
         """Bytes of workspace a ``kv_attend`` of these sizes uses (for ``kv_ops_reserve``)."""
@@ -724,17 +696,6 @@ class KVOps:
         a.num_seqs, a.q_heads, a.max_len, a.weights_out = num_seqs, q_heads, max_len, int(weights) or None
         self._ret(lib().kv_attend_workspace(self._h, cache.address, C.addressof(a), C.byref(n)), True)
         return n.value
-
-    def _tables(self, a, block_tables, lens, n: int) -> None:
-        a.block_tables, a.table_stride = self._rows(block_tables, "torch.int32", (n, None), "block_tables")
-        a.table_width = block_tables.shape[1]
-        a.lens, = self._rows(lens, "torch.int32", (n,), "lens")
-
-    def _weights(self, t, dtype: str, shape: tuple, slots: int, what: str) -> tuple:
-        r = self._rows(t, dtype, shape + (None,), what)
-        if t.shape[-1] < slots:
-            raise ValueError(f"{what} needs {slots} slots")
-        return r
 
     def kv_append(self, cache: KVCache, layer: int, q, k, v, block_tables, lens, *, positions, inv_freq, axis_of=None,
                   halves: bool = True, q_out=None, seq_starts=None, weights=None, order=None, token_order=None,
@@ -744,73 +705,16 @@ class KVOps:
         (f, f + rotary_dim/2), else (2f, 2f + 1); seq_starts int32 [seqs + 1], None = one token per sequence; block_tables int32
         [seqs, width]; lens int32 [seqs], with the new tokens; weights float32 and order int32 [seqs, kv_heads, slots];
         token_order int32 [tokens]."""
-        a = self._append
-        t, n, heads = len(k), len(lens), cache.heads
-        a.layer, a.num_seqs, a.num_tokens, a.pair_style = layer, n, t, 0 if halves else 1
-        a.q = a.q_out = None
-        a.q_heads = 0
-        if q is not None:
-            a.q_heads = q.shape[1]
-            shape = (t, a.q_heads, cache.dim)
-            a.q, a.q_token_stride, a.q_head_stride = self._rows(q, cache.dtype, shape, "q")
-            if q_out is not None:
-                a.q_out, a.qo_token_stride, a.qo_head_stride = self._rows(q_out, cache.dtype, shape, "q_out")
-        a.k, a.k_token_stride, a.k_head_stride = self._rows(k, cache.dtype, (t, heads, cache.dim), "k")
-        a.v, a.v_token_stride, a.v_head_stride = self._rows(v, cache.dtype, (t, heads, cache.dim), "v")
-        a.positions, a.axis_stride = self._rows(positions, "torch.int32", (None, t), "positions")
-        a.num_axes = len(positions)
-        a.inv_freq, = self._rows(inv_freq, "torch.float32", (None,), "inv_freq")
-        half = len(inv_freq)
-        a.rotary_dim = 2 * half
-        of = bytes(axis_of) if axis_of is not None else bytes(half)
-        if len(of) != half or half > 128:
-            raise ValueError("axis_of must name an axis for each of at most 128 frequencies")
-        C.memmove(a.axis_of, of, half)
-        a.seq_starts = None
-        if seq_starts is not None:
-            a.seq_starts, = self._rows(seq_starts, "torch.int32", (n + 1,), "seq_starts")
-        self._tables(a, block_tables, lens, n)
-        a.weights = a.order = a.token_order = None
-        if weights is not None:
-            a.weights, a.m_seq_stride, a.m_head_stride = self._rows(weights, "torch.float32", (n, heads, None), "weights")
-        if order is not None:
-            p, s0, s1 = self._rows(order, "torch.int32", (n, heads, None), "order")
-            if weights is not None and ((s0, s1) != (a.m_seq_stride, a.m_head_stride) or order.shape != weights.shape):
-                raise ValueError("weights and order differ in shape or strides")
-            a.order, a.m_seq_stride, a.m_head_stride = p, s0, s1
-            if token_order is not None:
-                a.token_order, = self._rows(token_order, "torch.int32", (t,), "token_order")
-        return self._ret(lib().kv_append(self._h, cache.address, C.addressof(a)), check)
+        return self._ret(self._ext_append(self._address, self.device_id, cache.address, layer, q, k, v, block_tables, lens, positions,
+                                          inv_freq, axis_of, halves, q_out, seq_starts, weights, order, token_order), check)
 
     def kv_evict(self, cache: KVCache, block_tables, lens, max_len: int, *, keep: int, weights, order=None, seen=None,
                  recent: int = 0, sink: int = 0, weights_out=None, order_out=None, lens_out=None, first_layer: int = 0,
                  check: bool = True) -> int:
         """weights float32 and order int32 [layers, seqs, kv_heads, >= max_len]; weights_out and order_out likewise with >= keep
         slots, or None: in place; seen, lens_out int32 [seqs]."""
-        a = self._evict
-        n, layers = len(lens), len(weights)
-        a.first_layer, a.num_layers, a.num_seqs, a.keep, a.recent, a.sink, a.max_len = first_layer, layers, n, keep, recent, sink, max_len
-        self._tables(a, block_tables, lens, n)
-        shape = (layers, n, cache.heads)
-        a.weights, a.m_layer_stride, a.m_seq_stride, a.m_head_stride = strides = self._weights(weights, "torch.float32", shape, max_len, "weights")
-        a.order = a.seen = a.weights_out = a.order_out = a.lens_out = None
-        if order is not None:
-            own = self._weights(order, "torch.int32", shape, max_len, "order")
-            if own[1:] != strides[1:]:
-                raise ValueError("weights and order differ in strides")
-            a.order = own[0]
-        if weights_out is not None:
-            a.weights_out, a.o_layer_stride, a.o_seq_stride, a.o_head_stride = strides = self._weights(weights_out, "torch.float32", shape, min(keep, max_len), "weights_out")
-        if order_out is not None:
-            own = self._weights(order_out, "torch.int32", shape, min(keep, max_len), "order_out")
-            if weights_out is not None and own[1:] != strides[1:]:
-                raise ValueError("weights_out and order_out differ in strides")
-            a.order_out = own[0]
-        if seen is not None:
-            a.seen, = self._rows(seen, "torch.int32", (n,), "seen")
-        if lens_out is not None:
-            a.lens_out, = self._rows(lens_out, "torch.int32", (n,), "lens_out")
-        return self._ret(lib().kv_evict(self._h, cache.address, C.addressof(a)), check)
+        return self._ret(self._ext_evict(self._address, self.device_id, cache.address, block_tables, lens, max_len, keep, weights, order,
+                                         seen, recent, sink, weights_out, order_out, lens_out, first_layer), check)
 
     def kv_evict_workspace(self, cache: KVCache, num_layers: int, num_seqs: int, max_len: int, keep: int) -> int:
         """Bytes of workspace a ``kv_evict`` of these sizes uses (for ``kv_ops_reserve``)."""

@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libduplexkv.so")
 TESTUTIL_LIB = os.path.join(HERE, "libkvtestutil.so")
+OPS_EXT = os.path.join(HERE, "_kvops.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
@@ -56,5 +57,28 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_ops_ext(force: bool = False) -> str:
+    """``_kvops.so`` from ``csrc/kv_ops_py.cpp``: the Python extension (host code, links torch and ``libduplexkv.so``) that
+    marshals tensors for the operators on the device cache."""
+    source = os.path.join(CSRC, "kv_ops_py.cpp")
+    if not force and not _stale(OPS_EXT, [source, os.path.join(os.path.dirname(HERE), "include", "duplexkv.h")]):
+        return OPS_EXT
+    build()
+    import sysconfig
+    import torch
+    home = os.path.dirname(torch.__file__)
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_path("include"), "/usr/local/cuda/include"]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += ["-I" + d for d in include] + ["-o", OPS_EXT, source, "-L" + HERE, "-l:libduplexkv.so",
+                                          "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu",
+                                          "-lc10", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(home, "lib")]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+    return OPS_EXT
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose="-v" in sys.argv))
+    print(build_ops_ext(force=True))

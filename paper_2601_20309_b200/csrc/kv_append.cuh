@@ -27,7 +27,7 @@ struct KvAppend {
     int *order;
     long long m_seq, m_head;
     const int *token_order;
-    int vec;             // elements a thread moves at once: 8, or 1 where rows are not 16-byte aligned or odd in size
+    int num_slots;       // of weights and order
     int units;           // threads of a row: packs of `vec` elements with those they turn with, then packs that pass
     int per;             // tokens per CTA
     unsigned by_rows;    // 2^32 / rows of a token, rounded up
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
                 const long long left = a.starts ? a.starts[i + 1] - t : 1;       // this token and those behind it
                 const int n = a.c.len(i);
                 const long long s = n - left;
-                const bool ok = left > 0 && s >= 0;
+                const bool ok = left > 0 && s >= 0 && (!(a.weights || a.order) || s < a.num_slots);
                 if ((tid & 31) == 0) {
                     if (!ok && n > 0) atomicOr(a.c.status, KV_OPS_BAD_LEN);
                     kv_row[k] = ok ? a.c.slot(i, (int)s, a.layer * 2) : nullptr;

@@ -373,6 +373,7 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     k.m_seq = a->m_seq_stride;
     k.m_head = a->m_head_stride;
     k.token_order = a->token_order;
+    k.num_slots = a->num_slots;
     memcpy(k.axis_of, a->axis_of, sizeof(k.axis_of));
     k.num_tokens = a->num_tokens;
     // 16 bytes at a time where every row begins on 16 bytes and the pairs that turn together are whole packs of eight

@@ -628,7 +628,6 @@ def test_refusals_launch_nothing(ops):
     attend(0, num_seqs=0, q=None)
     assert L.kv_attend(None, h.address, 0) == B.KV_ERR_INVALID_ARG and L.kv_attend(ops._h, None, 0) == B.KV_ERR_INVALID_ARG
     assert L.kv_attend(ops._h, h.address, 0) == B.KV_ERR_INVALID_ARG
-    args = (1, q, c.tables, c.lens, 40)
     base = c.pool.data_ptr()
     for code, kw in ((B.KV_ERR_UNSUPPORTED, dict(head_dim=60)), (B.KV_ERR_UNSUPPORTED, dict(head_dim=264)), (B.KV_ERR_INVALID_ARG, dict(device_base=base + 8)),
                      (B.KV_ERR_INVALID_ARG, dict(device_base=None)), (B.KV_ERR_INVALID_ARG, dict(block_size=0)), (B.KV_ERR_INVALID_ARG, dict(num_gpu_blocks=0)),
@@ -636,7 +635,8 @@ def test_refusals_launch_nothing(ops):
         bad = c.handle(B)
         for k, v in kw.items():
             setattr(bad.c, k, v)
-        assert ops.kv_attend(bad, *args, out=out, check=False) == code
+        full = B.kv_attend_args_t(num_seqs=2, q_heads=4, max_len=40)
+        assert L.kv_attend(ops._h, bad.address, C.addressof(full)) == code
         a = B.kv_append_args_t(num_seqs=1, num_tokens=1, num_axes=1)
         assert L.kv_append(ops._h, bad.address, C.addressof(a)) == code
         e = B.kv_evict_args_t(num_layers=1, num_seqs=1, keep=4)
