@@ -51,9 +51,8 @@ __device__ __forceinline__ int kv_seq_of(const int *starts, int num_seqs, long l
 
 constexpr int AP_THREADS = 256, AP_ROWS = 2, AP_TOKENS = 16;
 
-// what a thread moves at once: eight elements as four pairs, or one element
-template <typename T, int V> struct KvPack;
-template <typename T> struct __align__(16) KvPack<T, 8> { unsigned w[4]; };
+// what a thread moves at once: eight or four elements as pairs, or one element
+template <typename T, int V> struct __align__(V * 2) KvPack { unsigned w[V / 2]; };
 template <typename T> struct KvPack<T, 1> { T e; };
 
 __device__ __forceinline__ float2 kv_unpair(unsigned w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
@@ -84,7 +83,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
     const bool turned = u < turns;
     const int lo = turned ? halves || V > 1 ? u * V : 2 * u : a.rotary + (u - turns) * V, hi = !turned ? -1 : halves ? lo + half : V == 1 ? lo + 1 : -1;
     // frequencies of a unit lie two by two, side by side with the other units': a warp's reads of them do not collide
-    const int per_unit = V == 1 ? 1 : halves ? 8 : 4;
+    const int per_unit = V == 1 ? 1 : halves ? V : V / 2;
     const long long first = (long long)blockIdx.x * a.per;
     const int tokens = (int)min((long long)a.per, a.num_tokens - first), total = tokens * rows;
     for (int r0 = mine; r0 - mine < total; r0 += lanes * AP_ROWS) {
@@ -145,7 +144,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
                     y[n].e = kv_round<T>(p * c.y + q * c.x);
                 } else if (halves) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {        // two frequencies
+                    for (int j = 0; j < V / 2; ++j) {    // two frequencies
                         const float4 c = *(const float4 *)(cs + (j * turns + u) * 2);
                         const float2 p = kv_unpair(x[n].w[j], T()), q = kv_unpair(y[n].w[j], T());
                         x[n].w[j] = kv_pair(p.x * c.x - q.x * c.y, p.y * c.z - q.y * c.w, T());
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
+                    for (int j = 0; j < V / 4; ++j) {
                         const float4 c = *(const float4 *)(cs + (j * turns + u) * 2);
                         const float2 p = kv_unpair(x[n].w[2 * j], T()), q = kv_unpair(x[n].w[2 * j + 1], T());
                         x[n].w[2 * j] = kv_pair(p.x * c.x - p.y * c.y, p.x * c.y + p.y * c.x, T());

@@ -45,7 +45,7 @@ struct KvAttend {
     float *scores;       // [seq][kv_head][max_len][group], base 2; nullptr: no weights wanted
     float2 *part_ml;     // [piece][2][hc][8*NT]: maximum and sum
     float *part_o;       // [piece][2][hc][8*NT][dim]
-    int4 *part_of;       // [piece]: the sequence and row that the piece begins inside of, the row's place in the line and its steps (0: none)
+    int4 *part_of;       // [piece]: the row (of all) that the piece begins inside of, its place in the line, its steps (0: none), the length of a piece
     int4 *row_of;        // [seq][row]: its place in the line, its steps, the length of a piece, whether one CTA has all of it
     float *row_lse;      // [seq][q_head], base 2, of rows that one CTA has
 };
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                 const long long part = ((long long)blockIdx.x * 2 + (began ? 1 : 0)) * a.hc + hw;
                 if (a.pieces && tid == 0) {
                     if (began) a.row_of[(long long)tile.z * rows_of_seq + tile.w] = make_int4(s0 + n0, KvSpan(a, tile.z).steps(a), piece, whole);
-                    else a.part_of[blockIdx.x] = make_int4(tile.z, tile.w, s0 - k0, KvSpan(a, tile.z).steps(a));
+                    else a.part_of[blockIdx.x] = make_int4(tile.z * rows_of_seq + tile.w, s0 - k0, KvSpan(a, tile.z).steps(a), piece);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -614,9 +614,9 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int4 of = a.part_of[b];
-    if (of.w == 0) return;
-    const int i = of.x, row = of.y, piece = a.row_of[(long long)i * a.head_chunks * a.group_chunks + row].z;
-    const int c0 = of.z / piece, c1 = (of.z + of.w - 1) / piece, parts = c1 - c0 + 1;
+    if (of.z == 0) return;
+    const int i = of.x / (a.head_chunks * a.group_chunks), row = of.x - i * (a.head_chunks * a.group_chunks);
+    const int c0 = of.y / of.w, c1 = (of.y + of.z - 1) / of.w, parts = c1 - c0 + 1;
     const int g0 = row % a.group_chunks * heads_of_chunk, heads = min(heads_of_chunk, a.group - g0), h0 = row / a.group_chunks * a.hc;
     // units (KV head, query head, 32 elements) of this piece, one of the parts - 1 that cut the row
     const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = (b - c0 - 1) * KV_JOIN_ROWS + sub, turns = (parts - 1) * KV_JOIN_ROWS;
@@ -706,18 +706,19 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
 __device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int i, int hx, int t0, float *lse2)
 {
     const int tid = threadIdx.x, warp = tid >> 5, pairs = a.hc * a.group, h0 = hx * a.hc;
+    const int4 *row = a.row_of + ((long long)i * a.head_chunks + hx) * a.group_chunks;
+    const int4 own = row[0];         // nothing yet where the sequence has no slots
     const KvSpan sp(a, i);
     if (t0 >= sp.n) return;
-    const int4 *row = a.row_of + ((long long)i * a.head_chunks + hx) * a.group_chunks;
     auto sum_of = [&](int p, auto lanes) {
         const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk;
-        const int4 line = row[gc];
+        const int4 line = gc ? row[gc] : own;
         const float z = line.w ? a.row_lse[(long long)i * a.q_heads + h0 * a.group + p]
                                : kv_join_lse<decltype(lanes)::value>(a, line.x / line.z, (line.x + line.y - 1) / line.z, hw, heads_of_chunk, g - gc * heads_of_chunk);
         return z == -INFINITY ? INFINITY : z;    // a row without any weight has scores of -inf: less +inf they give 0
     };
     // few parts: a thread for every pair of KV and query head; many: a warp
-    if (row[0].y <= 8 * row[0].z)
+    if (own.y <= 8 * own.z)
         for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = sum_of(p, KvCount<1>());
     else
         for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
@@ -770,11 +771,13 @@ __global__ void __launch_bounds__(KV_JOIN_THREADS, 4) kv_attend_join(const __gri
 {
     extern __shared__ __align__(16) float join_smem[];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int joins = a.pieces * KV_JOIN_ROWS, b = blockIdx.x;
-    if (b < joins) {
-        kv_join_rows<T>(a, heads_of_chunk, b / KV_JOIN_ROWS, b % KV_JOIN_ROWS, join_smem);
-    } else {                         // first the first slots of every sequence, then the next: short sequences' idle CTAs come last
-        const int rows = a.seqs * a.head_chunks, r = (b - joins) % rows;
-        kv_join_weights(a, heads_of_chunk, r / a.head_chunks, r % a.head_chunks, (b - joins) / rows * (KV_JOIN_SLOTS / a.hc), join_smem);
+    // weights first: the first slots of every sequence, then the next, so that short sequences' idle CTAs come last; among
+    // them, after the first round, the rows
+    const int joins = a.pieces * KV_JOIN_ROWS, rows = a.scores ? a.seqs * a.head_chunks : 0, b = blockIdx.x;
+    if (b >= rows && b < rows + joins) {
+        kv_join_rows<T>(a, heads_of_chunk, (b - rows) / KV_JOIN_ROWS, (b - rows) % KV_JOIN_ROWS, join_smem);
+    } else {
+        const int n = b < rows ? b : b - joins, r = n % rows;
+        kv_join_weights(a, heads_of_chunk, r / a.head_chunks, r % a.head_chunks, n / rows * (KV_JOIN_SLOTS / a.hc), join_smem);
     }
 }

@@ -376,14 +376,17 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     k.num_slots = a->num_slots;
     memcpy(k.axis_of, a->axis_of, sizeof(k.axis_of));
     k.num_tokens = a->num_tokens;
-    // 16 bytes at a time where every row begins on 16 bytes and the pairs that turn together are whole packs of eight
-    const auto packs = [](const void *q, int64_t x, int64_t y) { return (uintptr_t)q % 16 == 0 && x % 8 == 0 && y % 8 == 0; };
-    const bool wide = (a->pair_style ? a->rotary_dim : a->rotary_dim / 2) % 8 == 0 && packs(a->k, a->k_token_stride, a->k_head_stride) &&
-                      packs(a->v, a->v_token_stride, a->v_head_stride) &&
-                      (!a->q || (packs(a->q, a->q_token_stride, a->q_head_stride) && packs(a->q_out, a->qo_token_stride, a->qo_head_stride)));
-    const int v = wide ? 8 : 1;
-    k.units = (wide && a->pair_style ? a->rotary_dim / 8 : a->rotary_dim / 2 / v) + (cache->head_dim - a->rotary_dim) / v;
-    // one token per CTA while all of them have room at once, else several, which share what is done once per CTA
+    // 16 bytes at a time where every row begins on 16 bytes and the pairs that turn together are whole packs of eight, 8 bytes
+    // likewise (a rotation of 40 of 80 elements turns halves of 20), else element by element
+    const int turning = a->pair_style ? a->rotary_dim : a->rotary_dim / 2;
+    const auto packs = [&](int64_t v) {
+        const auto fits = [v](const void *q, int64_t x, int64_t y) { return (uintptr_t)q % (2 * v) == 0 && x % v == 0 && y % v == 0; };
+        return turning % v == 0 && (cache->head_dim - a->rotary_dim) % v == 0 && fits(a->k, a->k_token_stride, a->k_head_stride) &&
+               fits(a->v, a->v_token_stride, a->v_head_stride) &&
+               (!a->q || (fits(a->q, a->q_token_stride, a->q_head_stride) && fits(a->q_out, a->qo_token_stride, a->qo_head_stride)));
+    };
+    const int v = packs(8) ? 8 : packs(4) ? 4 : 1;
+    k.units = (v > 1 && a->pair_style ? a->rotary_dim / v : a->rotary_dim / 2 / v) + (cache->head_dim - a->rotary_dim) / v;
     // a row number below 2^32 / rows is divided by rows exactly with the reciprocal
     const int64_t rows = (int64_t)(a->q ? a->q_heads : 0) + 2 * cache->kv_heads;
     if (rows > 4096) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
@@ -391,13 +394,12 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     k.by_rows = (unsigned)ceil_div(int64_t(1) << 32, rows);
     const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
     const size_t smem = (size_t)k.per * (a->rotary_dim / 2) * sizeof(float2);
-    if (cache->dtype == KV_DT_BF16) {
-        if (wide) kv_append_tokens<__nv_bfloat16, 8><<<grid, AP_THREADS, smem, o->stream>>>(k);
-        else kv_append_tokens<__nv_bfloat16, 1><<<grid, AP_THREADS, smem, o->stream>>>(k);
-    } else {
-        if (wide) kv_append_tokens<__half, 8><<<grid, AP_THREADS, smem, o->stream>>>(k);
-        else kv_append_tokens<__half, 1><<<grid, AP_THREADS, smem, o->stream>>>(k);
-    }
+    const bool bf16 = cache->dtype == KV_DT_BF16;
+    const auto kernel = bf16 ? (v == 8   ? kv_append_tokens<__nv_bfloat16, 8>
+                                : v == 4 ? kv_append_tokens<__nv_bfloat16, 4>
+                                         : kv_append_tokens<__nv_bfloat16, 1>)
+                             : (v == 8 ? kv_append_tokens<__half, 8> : v == 4 ? kv_append_tokens<__half, 4> : kv_append_tokens<__half, 1>);
+    kernel<<<grid, AP_THREADS, smem, o->stream>>>(k);
     return launched(o, "kv_append");
 }
 
