@@ -6,9 +6,9 @@
 // of rank `keep` is found by digits of ten bits from above: the keys that agree so far are counted by their next digit
 // in shared memory, one warp picks the digit, and as soon as at most EV_CANDS keys are left it finds the rest among
 // them alone.  Ballots then number the holes and the sources in slot order, and the pairs meet through two short lists.
-//   kv_evict_warp     one warp per problem, keys in shared memory: nothing waits at a barrier, and what the warps of a CTA
-//                     would all do is done once.  For short problems, and for many.
-//   kv_evict_select   one CTA per problem, keys in registers, or a cluster of up to eight that exchange their counts
+//   kv_evict_small    four warps per problem, keys in shared memory: many problems on an SM at once.  For short problems, and
+//                     for many; next to no rows it moves itself.
+//   kv_evict_select   one CTA of 256 or 1024 threads per problem, keys in registers, or a cluster of up to eight that exchange their counts
 //                     through distributed shared memory.
 //   kv_evict_move     the rows, spread over the GPU: 32 pairs per warp, eight 16-byte loads per lane in flight.
 //
@@ -28,7 +28,7 @@ struct KvEvict {
     long long o_layer, o_seq, o_head;
     int *lens_out;
     int problems;
-    int fused;               // kv_evict_warp moves the rows itself
+    int fused;               // kv_evict_small moves the rows itself
     int quads;               // weights and ages may be read and written four at a time
     int units_shift;         // log2 of a row's 16-byte units in K and V together, or -1
     int *count;              // [problem]: rows that move
@@ -45,7 +45,8 @@ __device__ __forceinline__ unsigned kv_evict_key(float w, bool held)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_BINS = 1024 + 32, EV_WARP_SLOTS = 8192, EV_MOVE_WARPS = 4;
+constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_BINS = 1024 + 32, EV_MOVE_WARPS = 4,
+              EV_SMALL_THREADS = 128, EV_SMALL_SLOTS = 8192, EV_FUSED_ROWS = 64;
 
 struct KvProblem {
     int h, i, l, n;
@@ -470,35 +471,40 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
     if (size > 1) kv_cluster_sync();             // nobody leaves while others may still write into its memory
 }
 
-__global__ void __launch_bounds__(32) kv_evict_warp(const __grid_constant__ KvEvict a)
+__global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_constant__ KvEvict a)
 {
-    extern __shared__ __align__(16) unsigned keys[];     // [max_len rounded up to 128], then lists
-    __shared__ unsigned cand[EV_CANDS];
-    __shared__ int bins[EV_BINS];
-    __shared__ ulonglong2 way[32];
-    const int lane = threadIdx.x;
+    constexpr int THREADS = EV_SMALL_THREADS, WARPS = THREADS / 32;
+    extern __shared__ __align__(16) unsigned keys[];     // [max_len rounded up to 4 * THREADS]
+    __shared__ unsigned cand[EV_CANDS], s_top;
+    __shared__ int bins[EV_BINS], s_count, s_ties[WARPS], s_lists[2 * EV_FUSED_ROWS];
+    __shared__ int2 s_moves[WARPS];
+    __shared__ int3 s_pick;
+    __shared__ ulonglong2 way[WARPS][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvProblem p(a, blockIdx.x);
     const bool apart = a.w_out != a.w, stay = p.n <= a.keep;
-    if (lane == 0) {
+    if (tid == 0) {
         if (p.l == 0 && p.h == 0 && a.lens_out) a.lens_out[p.i] = min(p.n, a.keep);
         if (stay && !a.fused) a.count[blockIdx.x] = 0;
+        s_count = 0;
     }
-    const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent, padded = (p.n + 127) & ~127;
+    const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent, padded = (p.n + 4 * THREADS - 1) / (4 * THREADS) * (4 * THREADS);
     if (stay && !apart) return;
-    // four slots at a time where the arrays are aligned; sixteen slots per lane in flight
+    for (int d = tid; d < EV_BINS; d += THREADS) bins[d] = 0;
+    // four slots at a time where the arrays are aligned; eight per thread in flight
     if (a.quads) {
-        for (int t0 = lane * 4; t0 < padded; t0 += 128 * 4) {
-            float4 w[4];
-            int4 age[4];
+        for (int t0 = tid * 4; t0 < padded; t0 += THREADS * 4 * 2) {
+            float4 w[2];
+            int4 age[2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = t0 + r * 128;              // rows are whole quads: the last may reach past the length
+            for (int r = 0; r < 2; ++r) {
+                const int t = t0 + r * THREADS * 4;      // rows are whole quads: the last may reach past the length
                 w[r] = t < p.n ? *(const float4 *)(a.w + p.at + t) : make_float4(0.f, 0.f, 0.f, 0.f);
                 age[r] = t < p.n && a.order ? *(const int4 *)(a.order + p.at + t) : make_int4(t, t + 1, t + 2, t + 3);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = t0 + r * 128;
+            for (int r = 0; r < 2; ++r) {
+                const int t = t0 + r * THREADS * 4;
                 if (t >= padded) continue;
                 auto key = [&](int e, float x, int y) { return t + e < p.n ? kv_evict_key(x, y >= newest || y < a.sink) : 0u; };
                 *(uint4 *)(keys + t) = make_uint4(key(0, w[r].x, age[r].x), key(1, w[r].y, age[r].y), key(2, w[r].z, age[r].z), key(3, w[r].w, age[r].w));
@@ -519,18 +525,18 @@ __global__ void __launch_bounds__(32) kv_evict_warp(const __grid_constant__ KvEv
             }
         }
     } else {
-        for (int t0 = lane; t0 < padded; t0 += 32 * 16) {
-            float w[16];
-            int age[16];
+        for (int t0 = tid; t0 < padded; t0 += THREADS * 8) {
+            float w[8];
+            int age[8];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = t0 + r * 32;
+            for (int r = 0; r < 8; ++r) {
+                const int t = t0 + r * THREADS;
                 w[r] = t < p.n ? a.w[p.at + t] : 0.f;
                 age[r] = t < p.n ? a.order ? a.order[p.at + t] : t : 0;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = t0 + r * 32;
+            for (int r = 0; r < 8; ++r) {
+                const int t = t0 + r * THREADS;
                 if (t < padded) keys[t] = t < p.n ? kv_evict_key(w[r], age[r] >= newest || age[r] < a.sink) : 0u;
                 if (apart && t < min(p.n, a.keep)) {
                     a.w_out[p.to + t] = w[r];
@@ -540,89 +546,139 @@ __global__ void __launch_bounds__(32) kv_evict_warp(const __grid_constant__ KvEv
         }
     }
     if (stay) return;
-    __syncwarp();
+    __syncthreads();
     const unsigned below = (1u << lane) - 1;
     // ---- the key of rank `keep`, as kv_evict_select finds it
     unsigned top = 0;
     int reach = p.n, over = 0, shift = 32;
     while (shift > 0 && reach != a.keep && reach - over > EV_CANDS) {
         const int width = min(10, shift);
-        for (int d = lane; d < EV_BINS; d += 32) bins[d] = 0;
-        __syncwarp();
+        if (shift < 32) {
+            for (int d = tid; d < EV_BINS; d += THREADS) bins[d] = 0;
+            __syncthreads();
+        }
 #pragma unroll 4
-        for (int t = lane; t < padded; t += 32) {
+        for (int t = tid; t < padded; t += THREADS) {
             const unsigned k = keys[t];
             if (t < p.n && (shift == 32 || (k ^ top) >> shift == 0)) atomicAdd(&bins[kv_evict_bin(k >> (shift - width) & ((1 << width) - 1))], 1);
         }
-        __syncwarp();
-        int larger, equal;
-        const int digit = kv_evict_pick(bins, a.keep - over, larger, equal);
+        __syncthreads();
+        if (warp == 0) {
+            int larger, equal;
+            const int digit = kv_evict_pick(bins, a.keep - over, larger, equal);
+            if (lane == 0) s_pick = make_int3(digit, larger, equal);
+        }
+        __syncthreads();
         shift -= width;
-        top |= (unsigned)digit << shift;
-        over += larger;
-        reach = over + equal;
-        __syncwarp();
+        top |= (unsigned)s_pick.x << shift;
+        over += s_pick.y;
+        reach = over + s_pick.z;
     }
     if (shift > 0 && reach != a.keep) {
-        int m = 0;
 #pragma unroll 4
-        for (int t = lane; t < padded; t += 32) {
+        for (int t = tid; t < padded; t += THREADS) {
             const unsigned k = keys[t];
-            const bool in = t < p.n && (shift == 32 || (k ^ top) >> shift == 0);
-            const unsigned v = __ballot_sync(~0u, in);
-            if (in) cand[m + __popc(v & below)] = k;
-            m += __popc(v);
+            if (t < p.n && (shift == 32 || (k ^ top) >> shift == 0)) cand[atomicAdd(&s_count, 1)] = k;
         }
-        __syncwarp();
-        reach = over + kv_evict_among(cand, m, a.keep - over, shift, top);
+        __syncthreads();
+        if (warp == 0) {
+            const int n = kv_evict_among(cand, reach - over, a.keep - over, shift, top);
+            if (lane == 0) {
+                s_top = top;
+                s_count = n;
+            }
+        }
+        __syncthreads();
+        top = s_top;
+        reach = over + s_count;
     }
-    // ---- equals that do not stay; lists in the keys' place: the number of holes found so far never exceeds the slots seen,
-    // and the m-th hole's partner lies at or above slot keep + m
-    int stay_ties = 0;
-    const int spare = reach - a.keep;
+    // ---- lists, numbered in slot order.  Every warp has a run of slots; 32 of them vote at a time (a hole or a source, which
+    // of the two goes by `keep`), and lane r keeps the vote of round r, to number and write down its slots later
+    const int spare = reach - a.keep, run = padded / WARPS, from = warp * run;
+    int ties = 0, stay_ties = 0;     // equals of the last key in front of this warp's run; how many of all stay
     if (spare > 0) {
-        int ties = 0;
-        for (int t = lane; t < p.n; t += 32) ties += keys[t] == top;
-        stay_ties = __reduce_add_sync(~0u, ties) - spare;
+        int mine = 0, all = 0;
+        for (int t = from + lane; t < from + run; t += 32) mine += t < p.n && keys[t] == top;
+        mine = __reduce_add_sync(~0u, mine);
+        if (lane == 0) s_ties[warp] = mine;
+        __syncthreads();
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) ties += s_ties[w];
+            all += s_ties[w];
+        }
+        stay_ties = all - spare;
     }
-    int holes = 0, sources = 0, ties = 0;
-    for (int t0 = 0; t0 < padded; t0 += 128) {           // four rounds of 32 slots, read before anything is written over them
-        unsigned k[4];
+    constexpr int GROUPS = EV_SMALL_SLOTS / WARPS / 1024;        // of 32 rounds
+    unsigned votes[GROUPS];
+    int2 mine = make_int2(0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) k[r] = keys[t0 + r * 32 + lane];
-        __syncwarp();
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = t0 + r * 32 + lane;
-            bool stays = k[r] >= top;
+    for (int g = 0; g < GROUPS; ++g) {
+        votes[g] = 0;
+        const int rounds = min(32, run / 32 - g * 32);
+#pragma unroll 4
+        for (int r = 0; r < rounds; ++r) {
+            const int t = from + g * 1024 + r * 32 + lane;
+            const unsigned k = keys[t];
+            bool stays = k >= top;
             if (spare > 0) {
-                const bool tie = t < p.n && k[r] == top;
+                const bool tie = t < p.n && k == top;
                 const unsigned v = __ballot_sync(~0u, tie);
                 if (tie && ties + __popc(v & below) >= stay_ties) stays = false;
                 ties += __popc(v);
             }
-            const int c = a.keep - (t - lane);           // lanes of this round below `keep`: they can only be holes
-            const unsigned low = c >= 32 ? ~0u : c <= 0 ? 0u : (1u << c) - 1;
             const unsigned v = __ballot_sync(~0u, t < p.n && (t < a.keep) != stays);
-            const int hole_at = holes, source_at = sources;
-            holes += __popc(v & low);
-            sources += __popc(v & ~low);
-            if (v >> lane & 1) keys[low >> lane & 1 ? hole_at + __popc(v & low & below) : holes + source_at + __popc(v & ~low & below)] = t;
+            if (lane == r) votes[g] = v;
         }
-        __syncwarp();
     }
-    if (a.fused) {
-        for (int j = 0; j < holes; j += 32) {
-            const int at = min(j + lane, holes - 1);
-            kv_evict_rows(a, p, min(holes - j, 32), keys[at], keys[holes + at], way);
+    auto low = [&](int g) {          // which of the round's slots lie below `keep`
+        const int c = a.keep - (from + g * 1024 + lane * 32);
+        return c >= 32 ? ~0u : c <= 0 ? 0u : (1u << c) - 1;
+    };
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        mine.x += __popc(votes[g] & low(g));
+        mine.y += __popc(votes[g] & ~low(g));
+    }
+    mine.x = __reduce_add_sync(~0u, mine.x);
+    mine.y = __reduce_add_sync(~0u, mine.y);
+    if (lane == 0) s_moves[warp] = mine;
+    __syncthreads();
+    int holes = 0, sources = 0, moves = 0;
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) {
+            holes += s_moves[w].x;
+            sources += s_moves[w].y;
         }
+        moves += s_moves[w].x;
+    }
+    int *hole_list = a.fused ? s_lists : a.holes + (long long)blockIdx.x * a.cap, *source_list = a.fused ? s_lists + EV_FUSED_ROWS : a.srcs + (long long)blockIdx.x * a.cap;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        if (g * 1024 >= run) break;
+        unsigned h = votes[g] & low(g), s = votes[g] & ~low(g);
+        int x = __popc(h) | __popc(s) << 16;             // of this round and those in front of it: at most 1024 of each
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o) x += y;
+        }
+        const int total = __shfl_sync(~0u, x, 31), t0 = from + g * 1024 + lane * 32;
+        int *to = hole_list + holes + (x & 0xffff) - __popc(h);
+        for (; h; h &= h - 1) *to++ = t0 + __ffs(h) - 1;
+        to = source_list + sources + (x >> 16) - __popc(s);
+        for (; s; s &= s - 1) *to++ = t0 + __ffs(s) - 1;
+        holes += total & 0xffff;
+        sources += total >> 16;
+    }
+    if (!a.fused) {
+        if (tid == 0) a.count[blockIdx.x] = moves;
         return;
     }
-    for (int m = lane; m < holes; m += 32) {
-        a.holes[(long long)blockIdx.x * a.cap + m] = keys[m];
-        a.srcs[(long long)blockIdx.x * a.cap + m] = keys[holes + m];
+    __syncthreads();
+    for (int j = warp * 8; j < moves; j += WARPS * 8) {  // eight rows per warp: few as they are, all warps have some
+        const int at = min(j + lane, moves - 1);
+        kv_evict_rows(a, p, min(moves - j, 8), s_lists[at], s_lists[EV_FUSED_ROWS + at], way[warp]);
     }
-    if (lane == 0) a.count[blockIdx.x] = holes;
 }
 
 // rows (x * EV_MOVE_WARPS + warp) * 32 .. of problem y

@@ -409,12 +409,11 @@ namespace {
 
 struct EvictPlan {
     int64_t problems, cap, count, holes, srcs, total;
-    int threads, cluster;                       // threads 32: a warp per problem
+    int threads, cluster;                       // EV_SMALL_THREADS: kv_evict_small
     bool regs, fused;
 };
 
-constexpr int EVICT_WARP_SHORT = 1024;          // up to here a warp per problem has the lowest latency
-constexpr int EVICT_FUSED_ROWS = 64;            // up to here it moves the rows itself
+constexpr int EVICT_SHORT = 1024;               // up to here kv_evict_small has the lowest latency
 
 int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvEvict &k, EvictPlan &p)
 {
@@ -429,13 +428,15 @@ int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvE
     p.problems = (int64_t)a->num_layers * a->num_seqs * c->kv_heads;
     if (p.problems * EV_CLUSTER > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
     p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
-    // A warp per problem where problems are short, or enough to fill the GPU with warps.  Else 256 threads hold 4096 keys and
+    // Four warps per problem where problems are short, or enough of them to fill the GPU.  Else 256 threads hold 4096 keys and
     // 1024 threads 16384; a cluster of eight such CTAs holds 131072, and beyond that the keys are read again in every round
-    p.threads = a->max_len <= EVICT_WARP_SHORT || (a->max_len <= EV_WARP_SLOTS && p.problems >= 4 * o->sms) ? 32 : a->max_len <= 256 * EV_KEYS ? 256 : 1024;
+    p.threads = a->max_len <= EVICT_SHORT || (a->max_len <= EV_SMALL_SLOTS && p.problems >= 4 * o->sms) ? EV_SMALL_THREADS
+                : a->max_len <= 256 * EV_KEYS                                                       ? 256
+                                                                                                      : 1024;
     p.cluster = 1;
     while (p.threads == 1024 && p.cluster < EV_CLUSTER && (int64_t)p.cluster * p.threads * EV_KEYS < a->max_len) p.cluster *= 2;
     p.regs = a->max_len <= (int64_t)p.cluster * p.threads * EV_KEYS;
-    p.fused = p.threads == 32 && p.cap <= EVICT_FUSED_ROWS;
+    p.fused = p.threads == EV_SMALL_THREADS && p.cap <= EV_FUSED_ROWS;
     p.count = 0;
     p.holes = align256(p.problems * 4);
     p.srcs = p.holes + align256(p.problems * p.cap * 4);
@@ -509,11 +510,11 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     cfg.stream = o->stream;
     cfg.attrs = &attr;
     cudaError_t e;
-    if (p.threads == 32) {
+    if (p.threads == EV_SMALL_THREADS) {
         cfg.gridDim = dim3((unsigned)p.problems);
-        cfg.blockDim = dim3(32);
-        cfg.dynamicSmemBytes = align256(a->max_len * 4) + 256;
-        e = cudaLaunchKernelEx(&cfg, kv_evict_warp, k);
+        cfg.blockDim = dim3(EV_SMALL_THREADS);
+        cfg.dynamicSmemBytes = ceil_div(a->max_len, 4 * EV_SMALL_THREADS) * 16 * EV_SMALL_THREADS;
+        e = cudaLaunchKernelEx(&cfg, kv_evict_small, k);
     } else {
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = p.cluster;
