@@ -46,7 +46,6 @@ struct KvAttend {
     float2 *part_ml;     // [piece][2][hc][8*NT]: maximum and sum
     float *part_o;       // [piece][2][hc][8*NT][dim]
     int4 *part_of;       // [piece]: the row (of all) that the piece begins inside of, its place in the line, its steps (0: none), the length of a piece
-    int4 *row_of;        // [seq][row]: its place in the line, its steps, the length of a piece, whether one CTA has all of it
     float *row_lse;      // [seq][q_head], base 2, of rows that one CTA has
 };
 
@@ -316,7 +315,6 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
     float o[NT][KS][4], m[NT][2], l[NT][2];
     int take = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
-    int n0 = 0;                      // its first tile
     for (int n = 0; n < todo; ++n) {
         __syncwarp();                // the stage about to be filled is no longer read
         issue();
@@ -327,7 +325,6 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
         const int heads = min(HEADS, a.group - g0);
         if (tile.x & 1 << 16) {
             began = tile.x & 1 << 18;
-            n0 = n;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int g = nt * 8 + (lane >> 2);
@@ -489,10 +486,8 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
             }
             if (way == 0) {
                 const long long part = ((long long)blockIdx.x * 2 + (began ? 1 : 0)) * a.hc + hw;
-                if (a.pieces && tid == 0) {
-                    if (began) a.row_of[(long long)tile.z * rows_of_seq + tile.w] = make_int4(s0 + n0, KvSpan(a, tile.z).steps(a), piece, whole);
-                    else a.part_of[blockIdx.x] = make_int4(tile.z * rows_of_seq + tile.w, s0 - k0, KvSpan(a, tile.z).steps(a), piece);
-                }
+                if (a.pieces && tid == 0 && !began)
+                    a.part_of[blockIdx.x] = make_int4(tile.z * rows_of_seq + tile.w, s0 - k0, KvSpan(a, tile.z).steps(a), piece);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -567,13 +562,13 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 
 // ---- join: what is left when rows were split.
 //
-// KV_JOIN_ROWS CTAs per piece join output rows: where the piece begins inside a row, the pieces that cut that row share
-// its output, in units of 32 elements of a head, among them.  Behind them come CTAs that add up the weights, each for
-// KV_JOIN_SLOTS weights of one sequence and chunk of KV heads, with the sums of all parts of the row.  What such a kernel
-// takes is the number of loads that wait for one another, each close to a microsecond: the first kernel leaves
-// what lies where, so there are three in a chain (what, the row's sums, the data), and every load that can be in
-// flight together is.
-constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_ROWS = 4, KV_JOIN_SLOTS = 2048, KV_MAX_GROUP = 256;
+// The first KV_JOIN_SHARES * pieces CTAs add up the weights, each over its equal share of the line of steps, with the sums of
+// all parts of its rows.  They fit beside the first kernel and find their place in the line before it ends.  Then come
+// `row_ctas` per piece that join output rows: where the piece begins inside a row, the pieces that cut that row share
+// its output, in units of 32 elements of a head, among them.  What such a kernel takes is the number of loads that
+// wait for one another, each close to a microsecond, times the waves of CTAs: there are three in a chain (what, the row's
+// sums, the data), every load that can be in flight together is, and four CTAs per SM are all there are.
+constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_SHARES = 3, KV_MAX_GROUP = 256;
 
 // maximum and sum of two sets of slots together
 __device__ __forceinline__ void kv_meet(float &top, float &sum, float top2, float sum2)
@@ -610,7 +605,7 @@ __host__ __device__ constexpr int kv_join_floats(int hc, int heads_of_chunk, int
 }
 
 template <typename T>
-__device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chunk, int b, int sub, float *smem)
+__device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chunk, int b, int sub, int subs, float *smem)
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int4 of = a.part_of[b];
@@ -619,7 +614,7 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
     const int c0 = of.y / of.w, c1 = (of.y + of.z - 1) / of.w, parts = c1 - c0 + 1;
     const int g0 = row % a.group_chunks * heads_of_chunk, heads = min(heads_of_chunk, a.group - g0), h0 = row / a.group_chunks * a.hc;
     // units (KV head, query head, 32 elements) of this piece, one of the parts - 1 that cut the row
-    const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = (b - c0 - 1) * KV_JOIN_ROWS + sub, turns = (parts - 1) * KV_JOIN_ROWS;
+    const int slices = (a.c.dim + 31) / 32, all = a.hc * heads * slices, turn = (b - c0 - 1) * subs + sub, turns = (parts - 1) * subs;
     const int u0 = all * turn / turns, u1 = all * (turn + 1) / turns, p0 = u0 / slices, pairs = u1 > u0 ? (u1 - 1) / slices - p0 + 1 : 0;
     float *factor = smem + 4 * KV_JOIN_THREADS;
     const int stride = a.hc * heads_of_chunk;            // entries of a part
@@ -702,82 +697,110 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
     }
 }
 
-// slots t0 .. of chunk `hx` of the KV heads of sequence i
-__device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int i, int hx, int t0, float *lse2)
+// `todo` steps of the line from step s on, which is step k of a row of sequence i
+__device__ __forceinline__ void kv_join_weights(const KvAttend &a, int heads_of_chunk, int s, int todo, int piece, int i, int row, int k, float *lse2)
 {
-    const int tid = threadIdx.x, warp = tid >> 5, pairs = a.hc * a.group, h0 = hx * a.hc;
-    const int4 *row = a.row_of + ((long long)i * a.head_chunks + hx) * a.group_chunks;
-    const int4 own = row[0];         // nothing yet where the sequence has no slots
-    const KvSpan sp(a, i);
-    if (t0 >= sp.n) return;
-    auto sum_of = [&](int p, auto lanes) {
-        const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk;
-        const int4 line = gc ? row[gc] : own;
-        const float z = line.w ? a.row_lse[(long long)i * a.q_heads + h0 * a.group + p]
-                               : kv_join_lse<decltype(lanes)::value>(a, line.x / line.z, (line.x + line.y - 1) / line.z, hw, heads_of_chunk, g - gc * heads_of_chunk);
-        return z == -INFINITY ? INFINITY : z;    // a row without any weight has scores of -inf: less +inf they give 0
-    };
-    // few parts: a thread for every pair of KV and query head; many: a warp
-    if (own.y <= 8 * own.z)
-        for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = sum_of(p, KvCount<1>());
-    else
-        for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
-            const float z = sum_of(p, KvCount<32>());
-            if ((tid & 31) == 0) lse2[p] = z;
-        }
-    __syncthreads();
-    const int lanes = KV_JOIN_THREADS / a.hc / 32 * 32, hw = tid / lanes, count = min(KV_JOIN_SLOTS / a.hc, sp.n - t0);
-    if (hw >= a.hc) return;
-    const float *from = a.scores + (((long long)i * a.c.heads + h0 + hw) * a.c.max_len + t0) * a.group, *z = lse2 + hw * a.group;
-    const long long w = i * a.w_seq + (h0 + hw) * a.w_head + t0;
-    for (int t = tid - hw * lanes; t < count; t += 4 * lanes) {          // four slots at once
-        float v[4], add[4];
-        bool on[4];                  // slots before the window keep their weight
+    const int tid = threadIdx.x, warp = tid >> 5, pairs = a.hc * a.group;
+    while (todo > 0) {
+        const KvSpan sp(a, i);
+        const int steps = sp.steps(a), n = min(steps - k, todo), hx = row / a.group_chunks;
+        if (n > 0 && row == hx * a.group_chunks) {       // the row of the KV heads' first query heads does it for all of them
+            const int first = s - k;
+            auto sum_of = [&](int p, auto lanes) {
+                const int hw = p / a.group, g = p - hw * a.group, gc = g / heads_of_chunk, at = first + gc * steps;      // further query heads follow in the line
+                const int c0 = at / piece, c1 = (at + steps - 1) / piece;
+                const float z = c0 == c1 ? a.row_lse[(long long)i * a.q_heads + hx * pairs + p]
+                                         : kv_join_lse<decltype(lanes)::value>(a, c0, c1, hw, heads_of_chunk, g - gc * heads_of_chunk);
+                return z == -INFINITY ? INFINITY : z;    // a row without any weight has scores of -inf: less +inf they give 0
+            };
+            // few parts: a thread for every pair of KV and query head; many: a warp
+            if (steps <= 8 * piece)
+                for (int p = tid; p < pairs; p += KV_JOIN_THREADS) lse2[p] = sum_of(p, KvCount<1>());
+            else
+                for (int p = warp; p < pairs; p += KV_JOIN_WARPS) {
+                    const float z = sum_of(p, KvCount<32>());
+                    if ((tid & 31) == 0) lse2[p] = z;
+                }
+            __syncthreads();
+            const int t0 = sp.base + k * a.tw * 16, count = min(sp.base + (k + n) * a.tw * 16, sp.n) - t0;
+            const int lanes = KV_JOIN_THREADS / a.hc / 32 * 32, hw = tid / lanes;        // one warp per KV head, or several
+            if (hw < a.hc) {
+                const float *from = a.scores + (((long long)i * a.c.heads + hx * a.hc + hw) * a.c.max_len + t0) * a.group, *z = lse2 + hw * a.group;
+                const long long w = i * a.w_seq + (hx * a.hc + hw) * a.w_head + t0;
+                for (int t = tid - hw * lanes; t < count; t += 4 * lanes) {              // four slots at once
+                    float v[4], add[4];
+                    bool on[4];      // slots before the window keep their weight
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int u = t + e * lanes;
-            v[e] = a.w_in && u < count ? a.w_in[w + u] : 0.f;
-            on[e] = u < count && t0 + u >= sp.first;
-            add[e] = 0.f;
-        }
-        const float *at = from + (long long)t * a.group;
-        if ((a.group & 3) == 0) {
-            for (int g = 0; g < a.group; g += 4) {
-                float4 x[4];
+                    for (int e = 0; e < 4; ++e) {
+                        const int u = t + e * lanes;
+                        v[e] = a.w_in && u < count ? a.w_in[w + u] : 0.f;
+                        on[e] = u < count && t0 + u >= sp.first;
+                        add[e] = 0.f;
+                    }
+                    const float *at = from + (long long)t * a.group;
+                    if ((a.group & 3) == 0) {
+                        for (int g = 0; g < a.group; g += 4) {
+                            float4 x[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] = on[e] ? *(const float4 *)(at + e * lanes * a.group + g) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                            for (int e = 0; e < 4; ++e)
+                                x[e] = on[e] ? *(const float4 *)(at + e * lanes * a.group + g) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    add[e] += (kv_exp2(x[e].x - z[g]) + kv_exp2(x[e].y - z[g + 1])) + (kv_exp2(x[e].z - z[g + 2]) + kv_exp2(x[e].w - z[g + 3]));
+                            for (int e = 0; e < 4; ++e)
+                                add[e] += (kv_exp2(x[e].x - z[g]) + kv_exp2(x[e].y - z[g + 1])) + (kv_exp2(x[e].z - z[g + 2]) + kv_exp2(x[e].w - z[g + 3]));
+                        }
+                    } else {
+                        for (int g = 0; g < a.group; ++g) {
+                            float x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[e] = on[e] ? at[e * lanes * a.group + g] : -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) add[e] += kv_exp2(x[e] - z[g]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (t + e * lanes < count) a.w_out[w + t + e * lanes] = v[e] + (on[e] ? add[e] : 0.f);
+                }
             }
-        } else {
-            for (int g = 0; g < a.group; ++g) {
-                float x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = on[e] ? at[e * lanes * a.group + g] : -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) add[e] += kv_exp2(x[e] - z[g]);
-            }
+            __syncthreads();         // the next row's sums take the place of these
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (t + e * lanes < count) a.w_out[w + t + e * lanes] = v[e] + (on[e] ? add[e] : 0.f);
+        s += n;
+        todo -= n;
+        k = 0;
+        if (n == 0) ++i;             // a sequence without slots
+        else if (++row == a.head_chunks * a.group_chunks) {
+            row = 0;
+            ++i;
+        }
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(KV_JOIN_THREADS, 4) kv_attend_join(const __grid_constant__ KvAttend a, int heads_of_chunk)
+__global__ void __launch_bounds__(KV_JOIN_THREADS, 4) kv_attend_join(const __grid_constant__ KvAttend a, int heads_of_chunk, int row_ctas)
 {
     extern __shared__ __align__(16) float join_smem[];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    // weights first: the first slots of every sequence, then the next, so that short sequences' idle CTAs come last; among
-    // them, after the first round, the rows
-    const int joins = a.pieces * KV_JOIN_ROWS, rows = a.scores ? a.seqs * a.head_chunks : 0, b = blockIdx.x;
-    if (b >= rows && b < rows + joins) {
-        kv_join_rows<T>(a, heads_of_chunk, (b - rows) / KV_JOIN_ROWS, (b - rows) % KV_JOIN_ROWS, join_smem);
+    __shared__ int red[KV_JOIN_WARPS], at[2];
+    const int shares = a.scores ? a.pieces * KV_JOIN_SHARES : 0, b = blockIdx.x - shares;
+    if (b < 0) {
+        const KvLine line(a, red);
+        const int each = (line.total + shares - 1) / shares, s = (int)min((long long)blockIdx.x * each, (long long)line.total), n = min(line.total - s, each);
+        int i = 0, row = 0, k = 0;
+        if (n > 0) line.find(a, s, at, i, row, k);
+        const int piece = kv_attend_piece(a, line.total);
+        if (a.window > 0 && a.w_out != a.w_in) {         // slots in front of the window keep their weight: nothing to wait for
+            const int rows = a.seqs * a.c.heads, split = max(1, shares / rows);
+            for (int r = blockIdx.x; r < rows * split; r += shares) {
+                const int j = r % rows / a.c.heads;
+                const KvSpan sp(a, j);
+                const long long w = j * a.w_seq + r % a.c.heads * a.w_head;
+#pragma unroll 4
+                for (int t = r / rows * KV_JOIN_THREADS + threadIdx.x; t < sp.base; t += split * KV_JOIN_THREADS) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
+            }
+        }
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        kv_join_weights(a, heads_of_chunk, s, n, piece, i, row, k, join_smem);
     } else {
-        const int n = b < rows ? b : b - joins, r = n % rows;
-        kv_join_weights(a, heads_of_chunk, r / a.head_chunks, r % a.head_chunks, n / rows * (KV_JOIN_SLOTS / a.hc), join_smem);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        kv_join_rows<T>(a, heads_of_chunk, b / row_ctas, b % row_ctas, row_ctas, join_smem);
     }
 }

@@ -131,7 +131,7 @@ __device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem 
                 const ulonglong2 w = way[r];
                 const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
                 if (w.x) {           // a bad block id: the row stays where it is
-                    v[q] = __ldcs((const uint4 *)(w.x + off));
+                    v[q] = __ldcg((const uint4 *)(w.x + off));
                     to[q] = (uint8_t *)(w.y + off);
                 }
             }

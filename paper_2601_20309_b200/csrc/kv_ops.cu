@@ -117,12 +117,13 @@ int32_t launched(kv_ops *o, const char *what)
 struct AttendPlan {
     int dp, nt, warps;                       // kernel shape: padded head dimension, tiles of 8 query heads, warps per CTA
     size_t smem;
-    int64_t lse, row_of, part_of, part_ml, part_o, total;   // workspace offsets (the scores lie at 0)
+    int64_t lse, part_of, part_ml, part_o, total;   // workspace offsets (the scores lie at 0)
 };
 
 constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, less the kernel's static share
 constexpr int ATTEND_ALONE_STEPS = 8;                // rows of up to this many steps are never split
 constexpr int ATTEND_MIN_STEPS = 4;
+constexpr int ATTEND_ROW_CTAS = 1;                   // of the join, per piece, beside those that add up weights
 
 int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, KvAttend &k, AttendPlan &p)
 {
@@ -168,8 +169,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     k.whole_tiles = c->block_size % 16 == 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
-    p.row_of = p.lse + align256(split ? (int64_t)a->num_seqs * a->q_heads * 4 : 0);
-    p.part_of = p.row_of + align256(split ? (int64_t)a->num_seqs * k.head_chunks * k.group_chunks * 16 : 0);
+    p.part_of = p.lse + align256(split ? (int64_t)a->num_seqs * a->q_heads * 4 : 0);
     p.part_ml = p.part_of + align256((int64_t)k.pieces * 16);
     p.part_o = p.part_ml + align256(parts * 8);
     p.total = p.part_o + parts * c->head_dim * 4;
@@ -289,7 +289,6 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.w_head = a->w_head_stride;
     k.scores = a->weights_out ? (float *)o->ws : nullptr;
     k.row_lse = (float *)(o->ws + p.lse);
-    k.row_of = (int4 *)(o->ws + p.row_of);
     k.part_of = (int4 *)(o->ws + p.part_of);
     k.part_ml = (float2 *)(o->ws + p.part_ml);
     k.part_o = (float *)(o->ws + p.part_o);
@@ -312,14 +311,14 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
         early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         early.val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t cfg = {};
-        const int64_t joins = (int64_t)k.pieces * KV_JOIN_ROWS, rows_of_weights = k.scores ? (int64_t)k.seqs * k.head_chunks : 0;
-        cfg.gridDim = dim3((unsigned)(joins + rows_of_weights * ceil_div(a->max_len, KV_JOIN_SLOTS / k.hc)));
+        const int row_ctas = k.scores ? ATTEND_ROW_CTAS : 4;
+        cfg.gridDim = dim3(k.pieces * (row_ctas + (k.scores ? KV_JOIN_SHARES : 0)));
         cfg.dynamicSmemBytes = std::max((size_t)kv_join_floats(k.hc, 8 * p.nt, k.pieces), (size_t)k.hc * k.group) * 4;
         cfg.blockDim = dim3(KV_JOIN_THREADS);
         cfg.stream = o->stream;
         cfg.attrs = &early;
         cfg.numAttrs = 1;
-        e = bf16 ? cudaLaunchKernelEx(&cfg, kv_attend_join<__nv_bfloat16>, k, 8 * p.nt) : cudaLaunchKernelEx(&cfg, kv_attend_join<__half>, k, 8 * p.nt);
+        e = bf16 ? cudaLaunchKernelEx(&cfg, kv_attend_join<__nv_bfloat16>, k, 8 * p.nt, row_ctas) : cudaLaunchKernelEx(&cfg, kv_attend_join<__half>, k, 8 * p.nt, row_ctas);
         if (e != cudaSuccess) return fail_cuda(o, e, "kv_attend");
     }
     return KV_OK;
