@@ -121,8 +121,11 @@ struct AttendPlan {
 };
 
 constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, less the kernel's static share
-constexpr int ATTEND_ALONE_STEPS = 8;                // rows of up to this many steps are never split
-constexpr int ATTEND_MIN_STEPS = 4;
+// Rows of up to this many steps are never split.  A step of one warp takes about 0.9 us, the second kernel 4 to 7 (the more
+// with weights to add up): 4 sequences of 500 slots with weights 13.5 us whole, 17.6 split; 1 of 900 without 14.7 whole, 12.1 split
+constexpr int ATTEND_ALONE_STEPS = 4, ATTEND_ALONE_STEPS_WEIGHTS = 8;
+// No piece is shorter: with 1 step one sequence of 2000 slots takes 22.5 us, with 2 18.8, with 4 18.8; seven windows of 333 12.8, 14.9, 17.9
+constexpr int ATTEND_MIN_STEPS = 2;
 constexpr int ATTEND_ROW_CTAS = 1;                   // of the join, per piece, beside those that add up weights
 
 int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, KvAttend &k, AttendPlan &p)
@@ -154,7 +157,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     const bool one_head = (int64_t)a->num_seqs * c->kv_heads * k.group_chunks <= o->sms;
     int64_t longest = shape(one_head ? 1 : most);
     // query-head chunks of one KV head all add to the same weights: those go through the second kernel
-    const bool split = longest > ATTEND_ALONE_STEPS || (a->weights_out && k.group_chunks > 1);
+    const bool split = longest > (a->weights_out ? ATTEND_ALONE_STEPS_WEIGHTS : ATTEND_ALONE_STEPS) || (a->weights_out && k.group_chunks > 1);
     if (split && one_head) longest = shape(most);
     k.head_chunks = c->kv_heads / k.hc;
     const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * p.nt * (p.dp / 16 + 1) * 4 * 32 * 4 : 0;
