@@ -521,8 +521,8 @@ int32_t kv_table_fail_pool_call(kv_table_t *table, int64_t after_calls, int32_t 
  * Conventions
  *   - All array arguments are DEVICE pointers unless a comment says HOST; strides count elements.  Nothing is
  *     copied to or from the host, nothing is allocated except the context's workspace (see kv_ops_reserve).
- *   - Every call runs on the context's stream, asynchronously, and may be captured into a CUDA graph (reserve
- *     the workspace first).  A call without sequences, tokens or layers is a no-op.
+ *   - Every call runs on the context's device and stream whatever device is current, asynchronously, and may be
+ *     captured into a CUDA graph (reserve the workspace first).  A call without sequences, tokens or layers is a no-op.
  *   - The context knows nothing of the pool's transfers: order the stream after swap-ins with kv_stream_wait,
  *     and finish the stream (kv_ops_sync) before blocks it still reads or writes are rotated out, released
  *     (kv_req_shrink, kv_req_preempt, kv_req_finish) or handed to another stream.
@@ -545,12 +545,12 @@ typedef struct {
     int32_t dtype;                  /* KV_DT_*: of the cache, q and the outputs                         */
 } kv_cache_t;
 
-/* A context for `stream` (a cudaStream_t of device_id that outlives it; NULL = the default stream).  Sets the
- * current device.  One caller thread. */
+/* A context for `stream` (a cudaStream_t of device_id that outlives it; NULL = the default stream).  One caller
+ * thread. */
 int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out);
 /* Waits for the stream, then frees the context and its workspace. */
 int32_t kv_ops_destroy(kv_ops_t *ops);
-/* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA / KV_ERR_TIMEOUT of earlier calls. */
+/* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA of earlier calls. */
 int32_t kv_ops_sync(kv_ops_t *ops);
 /* Makes the workspace at least `bytes` large.  A call that needs more than there is does this itself, with a
  * cudaMalloc (not possible during stream capture: KV_ERR_NOMEM).  Outgrown workspaces stay allocated until

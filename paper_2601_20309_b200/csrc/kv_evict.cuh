@@ -12,7 +12,14 @@
 //                     through distributed shared memory.
 //   kv_evict_move     the rows, spread over the GPU: 32 pairs per warp, eight 16-byte loads per lane in flight.
 //
-// What bounds it: the rows that move, 4*dim bytes read and written each; for few short problems the chain of loads.
+// What bounds it: the rows that move, 4*dim bytes read and written each, in pieces of 256 bytes at random places (5.3 to 6
+// TB/s); beside them the instructions of the selection, which no longer depend on how many bits the weights share; for few
+// short problems the chain of loads.
+//
+// Measured: 32 layers x 8 sequences x 8 heads of 128, 2304 -> 2048 slots, 452 MB: 110 us (selection 36, rows 70), 63 % of the
+// floor; moving the rows in the selecting CTA, 256 threads each, took 125, two bits a round without digits 130, one kernel
+// after the other in the first form 284.  4 x 3 x 8 heads, 16384 -> 4096: 77 us (22 + 51; counting in clusters 99).  One problem of
+// 131072 slots: 34 us.  16 problems of 100 slots: 7.7 us.
 #pragma once
 #include "kv_ops.cuh"
 
@@ -45,7 +52,7 @@ __device__ __forceinline__ unsigned kv_evict_key(float w, bool held)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_BINS = 1024 + 32, EV_MOVE_WARPS = 4,
+constexpr int EV_KEYS = 16, EV_CLUSTER = 8, EV_CANDS = 256, EV_BINS = 1024 + 32, EV_MOVE_WARPS = 8,
               EV_SMALL_THREADS = 128, EV_SMALL_SLOTS = 8192, EV_FUSED_ROWS = 64;
 
 struct KvProblem {
@@ -681,12 +688,12 @@ __global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_
     }
 }
 
-// rows (x * EV_MOVE_WARPS + warp) * 32 .. of problem y
+// rows x * 32 .. of problems y * EV_MOVE_WARPS .., a warp each: neighbouring KV heads move neighbouring slots together
 __global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid_constant__ KvEvict a)
 {
     __shared__ ulonglong2 way[EV_MOVE_WARPS][32];
-    const int warp = threadIdx.x >> 5, j = (blockIdx.x * EV_MOVE_WARPS + warp) * 32, lane = threadIdx.x & 31;
-    for (int y = blockIdx.y; y < a.problems; y += gridDim.y) {
+    const int warp = threadIdx.x >> 5, j = blockIdx.x * 32, lane = threadIdx.x & 31;
+    for (int y = blockIdx.y * EV_MOVE_WARPS + warp; y < a.problems; y += gridDim.y * EV_MOVE_WARPS) {
         const int n = a.count[y];
         if (j >= n) continue;
         const KvProblem p(a, y);

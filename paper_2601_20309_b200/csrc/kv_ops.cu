@@ -41,6 +41,20 @@ int32_t fail_cuda(kv_ops *o, cudaError_t e, const char *what)
     return KV_ERR_CUDA;
 }
 
+// the context's device is current while one of these lives
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(int device)
+    {
+        int now = -1;
+        if (cudaGetDevice(&now) == cudaSuccess && now != device && cudaSetDevice(device) == cudaSuccess) before = now;
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) (void)cudaSetDevice(before);
+    }
+};
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t align256(int64_t a) { return (a + 255) / 256 * 256; }
 
@@ -196,8 +210,11 @@ int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out)
 {
     if (!out) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
     *out = nullptr;
-    cudaError_t e = cudaSetDevice(device_id);
-    if (e != cudaSuccess) return fail_cuda(nullptr, e, "cudaSetDevice");
+    int devices = 0;
+    cudaError_t e = cudaGetDeviceCount(&devices);
+    if (e != cudaSuccess) return fail_cuda(nullptr, e, "cudaGetDeviceCount");
+    if (device_id < 0 || device_id >= devices) return fail(nullptr, KV_ERR_INVALID_ARG, "no such device");
+    const OnDevice on(device_id);
     kv_ops *o = new (std::nothrow) kv_ops();
     if (!o) return fail(nullptr, KV_ERR_NOMEM, "out of host memory");
     o->device = device_id;
@@ -222,6 +239,7 @@ int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out)
 int32_t kv_ops_destroy(kv_ops_t *o)
 {
     if (!o) return KV_ERR_INVALID_ARG;
+    const OnDevice on(o->device);
     (void)cudaStreamSynchronize(o->stream);
     if (o->ws) cudaFree(o->ws);
     for (void *p : o->outgrown) cudaFree(p);
@@ -234,12 +252,14 @@ int32_t kv_ops_destroy(kv_ops_t *o)
 int32_t kv_ops_reserve(kv_ops_t *o, int64_t bytes)
 {
     if (!o) return KV_ERR_INVALID_ARG;
+    const OnDevice on(o->device);
     return grow_workspace(o, bytes);
 }
 
 int32_t kv_ops_sync(kv_ops_t *o)
 {
     if (!o) return KV_ERR_INVALID_ARG;
+    const OnDevice on(o->device);
     const cudaError_t e = cudaStreamSynchronize(o->stream);
     if (e != cudaSuccess) return fail_cuda(o, e, "cudaStreamSynchronize");
     const unsigned st = *(volatile unsigned *)o->status_host;
@@ -269,6 +289,7 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     int32_t rc = plan_attend(o, cache, a, k, p);
     if (rc != KV_OK) return rc;
     if (a->num_seqs == 0) return KV_OK;
+    const OnDevice on(o->device);
     if (!a->q || !a->out) return fail(o, KV_ERR_INVALID_ARG, "q and out are needed");
     if (a->weights_in && !a->weights_out) return fail(o, KV_ERR_INVALID_ARG, "weights_in without weights_out");
     if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens, a->max_len)) != KV_OK) return rc;
@@ -342,6 +363,7 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     for (int f = 0; f < a->rotary_dim / 2; ++f)
         if (a->axis_of[f] >= a->num_axes) return fail(o, KV_ERR_RANGE, "axis_of names an axis that positions does not have");
     if (a->num_tokens == 0 || a->num_seqs == 0) return KV_OK;
+    const OnDevice on(o->device);
     if (!a->seq_starts && a->num_tokens != a->num_seqs) return fail(o, KV_ERR_INVALID_ARG, "without seq_starts every sequence has one token");
     if (!a->k || !a->v) return fail(o, KV_ERR_INVALID_ARG, "k and v are needed");
     if (a->q && !a->q_out) return fail(o, KV_ERR_INVALID_ARG, "q without q_out");
@@ -468,6 +490,7 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     int32_t rc = plan_evict(o, cache, a, k, p);
     if (rc != KV_OK) return rc;
     if (p.problems == 0) return KV_OK;
+    const OnDevice on(o->device);
     if (!a->weights) return fail(o, KV_ERR_INVALID_ARG, "weights are needed");
     if (a->order_out && !a->order) return fail(o, KV_ERR_INVALID_ARG, "order_out without order");
     if (a->order && !a->order_out != !a->weights_out) return fail(o, KV_ERR_INVALID_ARG, "weights and order go to outputs both, or are both changed in place");
@@ -534,7 +557,7 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
         // in a steady state of 32 layers and 8 sequences)
         cfg.numAttrs = 0;
         cfg.dynamicSmemBytes = 0;
-        cfg.gridDim = dim3((unsigned)ceil_div(p.cap, EV_MOVE_WARPS * 32), (unsigned)std::min<int64_t>(p.problems, 65535));
+        cfg.gridDim = dim3((unsigned)ceil_div(p.cap, 32), (unsigned)std::min<int64_t>(ceil_div(p.problems, EV_MOVE_WARPS), 65535));
         cfg.blockDim = dim3(EV_MOVE_WARPS * 32);
         e = cudaLaunchKernelEx(&cfg, kv_evict_move, k);
         if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
