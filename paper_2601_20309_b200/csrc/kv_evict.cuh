@@ -71,7 +71,7 @@ struct KvProblem {
 
 __device__ __forceinline__ void kv_cluster_sync()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // sums over a CTA and over its cluster; `before` = over the cluster's lower CTAs
@@ -120,11 +120,14 @@ __device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem 
 {
     const int lane = threadIdx.x & 31, half = a.c.dim / 8, units = 2 * half;
     if (lane < m) {
-        a.w_out[p.to + d] = a.w[p.at + s];
-        if (a.order_out) a.order_out[p.to + d] = a.order[p.at + s];
         const uint8_t *from = a.c.slot(p.i, s, 0), *into = a.c.slot(p.i, d, 0);
         const long long plane = (a.first_layer + p.l) * 2 * a.c.plane_stride + (long long)p.h * a.c.head_stride;
-        way[lane] = make_ulonglong2(from && into ? (unsigned long long)from + plane : 0, (unsigned long long)into + plane);
+        const bool ok = from && into;            // a bad block id: the row stays where it is
+        way[lane] = make_ulonglong2(ok ? (unsigned long long)from + plane : 0, ok ? (unsigned long long)into + plane : 0);
+        if (ok) {
+            a.w_out[p.to + d] = a.w[p.at + s];
+            if (a.order_out) a.order_out[p.to + d] = a.order[p.at + s];
+        }
     }
     __syncwarp();
     for (int e = lane; e < m * units; e += 32 * 8) {
@@ -137,7 +140,7 @@ __device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem 
             if (f < m * units) {
                 const ulonglong2 w = way[r];
                 const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
-                if (w.x) {           // a bad block id: the row stays where it is
+                if (w.x) {
                     v[q] = __ldcg((const uint4 *)(w.x + off));
                     to[q] = (uint8_t *)(w.y + off);
                 }
@@ -225,256 +228,254 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
     if (size > 1) kv_cluster_sync();             // every CTA of the cluster is there before anyone writes into its memory
     const int slot = blockIdx.x / size;
     const KvProblem p(a, slot);
-    {
-        const bool apart = a.w_out != a.w;
-        if (p.l == 0 && p.h == 0 && rank == 0 && tid == 0 && a.lens_out) a.lens_out[p.i] = min(p.n, a.keep);
-        if (p.n <= a.keep) {
-            if (apart)
-                for (int t = rank * THREADS + tid; t < p.n; t += size * THREADS) {
-                    a.w_out[p.to + t] = a.w[p.at + t];
-                    if (a.order_out) a.order_out[p.to + t] = a.order[p.at + t];
-                }
-            if (rank == 0 && tid == 0) a.count[slot] = 0;
-            return;
+    const bool apart = a.w_out != a.w;
+    if (p.l == 0 && p.h == 0 && rank == 0 && tid == 0 && a.lens_out) a.lens_out[p.i] = min(p.n, a.keep);
+    if (p.n <= a.keep) {
+        if (apart)
+            for (int t = rank * THREADS + tid; t < p.n; t += size * THREADS) {
+                a.w_out[p.to + t] = a.w[p.at + t];
+                if (a.order_out) a.order_out[p.to + t] = a.order[p.at + t];
+            }
+        if (rank == 0 && tid == 0) a.count[slot] = 0;
+        return;
+    }
+    // ---- this CTA's slots: `rounds` times THREADS, side by side
+    const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent;
+    const int base = rank * (REGS ? EV_KEYS : (p.n + size * THREADS - 1) / (size * THREADS)) * THREADS;
+    const int rounds = max(0, min(REGS ? EV_KEYS : (p.n + (int)size * THREADS - 1) / ((int)size * THREADS), (p.n - base + THREADS - 1) / THREADS));
+    unsigned key[EV_KEYS];
+    // the keys of rounds r0 .. r0 + 15; a slot beyond the length gets 0, which no candidate reaches
+    auto load = [&](int r0, bool copy) {
+        float w[EV_KEYS];
+        int age[EV_KEYS];
+#pragma unroll
+        for (int r = 0; r < EV_KEYS; ++r) {
+            const int t = base + (r0 + r) * THREADS + tid;
+            const bool on = r0 + r < rounds && t < p.n;
+            w[r] = on ? a.w[p.at + t] : 0.f;
+            age[r] = on ? a.order ? a.order[p.at + t] : t : 0;
         }
-        // ---- this CTA's slots: `rounds` times THREADS, side by side
-        const int newest = (a.seen ? a.seen[p.i] : p.n) - a.recent;
-        const int base = rank * (REGS ? EV_KEYS : (p.n + size * THREADS - 1) / (size * THREADS)) * THREADS;
-        const int rounds = max(0, min(REGS ? EV_KEYS : (p.n + (int)size * THREADS - 1) / ((int)size * THREADS), (p.n - base + THREADS - 1) / THREADS));
-        unsigned key[EV_KEYS];
-        // the keys of rounds r0 .. r0 + 15; a slot beyond the length gets 0, which no candidate reaches
-        auto load = [&](int r0, bool copy) {
-            float w[EV_KEYS];
-            int age[EV_KEYS];
 #pragma unroll
-            for (int r = 0; r < EV_KEYS; ++r) {
-                const int t = base + (r0 + r) * THREADS + tid;
-                const bool on = r0 + r < rounds && t < p.n;
-                w[r] = on ? a.w[p.at + t] : 0.f;
-                age[r] = on ? a.order ? a.order[p.at + t] : t : 0;
+        for (int r = 0; r < EV_KEYS; ++r) {
+            const int t = base + (r0 + r) * THREADS + tid;
+            const bool on = r0 + r < rounds && t < p.n;
+            key[r] = on ? kv_evict_key(w[r], age[r] >= newest || age[r] < a.sink) : 0u;
+            if (copy && on && t < a.keep) {  // holes are overwritten by what moves there
+                a.w_out[p.to + t] = w[r];
+                if (a.order_out) a.order_out[p.to + t] = age[r];
             }
-#pragma unroll
-            for (int r = 0; r < EV_KEYS; ++r) {
-                const int t = base + (r0 + r) * THREADS + tid;
-                const bool on = r0 + r < rounds && t < p.n;
-                key[r] = on ? kv_evict_key(w[r], age[r] >= newest || age[r] < a.sink) : 0u;
-                if (copy && on && t < a.keep) {  // holes are overwritten by what moves there
-                    a.w_out[p.to + t] = w[r];
-                    if (a.order_out) a.order_out[p.to + t] = age[r];
-                }
-            }
-        };
-        if (REGS) load(0, apart);
-        else if (apart)
-            for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) load(r0, true);
+        }
+    };
+    if (REGS) load(0, apart);
+    else if (apart)
+        for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) load(r0, true);
 
-        // ---- the key of rank `keep`: `top` as far as it is known, above `shift`; `over` keys are larger, `reach` at least as large
-        unsigned top = 0;
-        int reach = p.n, over = 0, shift = 32;
-        while (shift > 0 && reach != a.keep && reach - over > EV_CANDS) {
-            const int width = min(10, shift);
-            for (int d = tid; d < EV_BINS; d += THREADS) bins[d] = 0;
-            __syncthreads();
-            for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
-                if (!REGS) load(r0, false);
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r)
-                    if (r0 + r < rounds) {
-                        const bool in = base + (r0 + r) * THREADS + tid < p.n && (shift == 32 || (key[r] ^ top) >> shift == 0);
-                        if (in) atomicAdd(&bins[kv_evict_bin(key[r] >> (shift - width) & ((1 << width) - 1))], 1);
-                    }
-            }
-            int *counts = bins;
-            if (size > 1) {                      // the whole cluster's: every CTA adds all of them up for itself
-                kv_cluster_sync();
-                for (int d = tid; d < EV_BINS; d += THREADS) {
-                    int sum = 0;
-                    for (unsigned r = 0; r < size; ++r) {
-                        unsigned there;
-                        int v;
-                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&bins[d])), "r"(r));
-                        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
-                        sum += v;
-                    }
-                    all_bins[d] = sum;
-                }
-                kv_cluster_sync();               // nobody clears counts that others still read
-                counts = all_bins;
-            } else {
-                __syncthreads();
-            }
-            if (warp == 0) {
-                int larger, equal;
-                const int digit = kv_evict_pick(counts, a.keep - over, larger, equal);
-                if (lane == 0) s_pick = make_int3(digit, larger, equal);
-            }
-            __syncthreads();
-            shift -= width;
-            top |= (unsigned)s_pick.x << shift;
-            over += s_pick.y;
-            reach = over + s_pick.z;
-        }
-        if (shift > 0 && reach != a.keep) {      // few keys are left: one warp finds the rest among them alone
-            if (tid == 0) s_count = 0;
-            __syncthreads();
-            for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
-                if (!REGS) load(r0, false);
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r)
-                    if (r0 + r < rounds) {
-                        // a full shift only where nothing was counted yet: all keys agree
-                        const bool in = base + (r0 + r) * THREADS + tid < p.n && (shift == 32 || (key[r] ^ top) >> shift == 0);
-                        if (in) cand[atomicAdd(&s_count, 1)] = key[r];
-                    }
-            }
-            __syncthreads();
-            const int m = reach - over;
-            if (size > 1) {                      // every CTA gets the others' too
-                int mine = s_count, none = 0, before, b;
-                if (tid) mine = 0;
-                sums.add(mine, none, &before, &b);
-                const int own = s_count;
-                const unsigned x = tid < own ? cand[tid] : 0u;
-                kv_cluster_sync();               // all have read their own
-                if (tid < own)
-                    for (unsigned r = 0; r < size; ++r) {
-                        unsigned there;
-                        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&cand[before + tid])), "r"(r));
-                        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(there), "r"(x) : "memory");
-                    }
-                kv_cluster_sync();
-            }
-            if (warp == 0) {
-                const int n = kv_evict_among(cand, m, a.keep - over, shift, top);
-                if (lane == 0) {
-                    s_top = top;
-                    s_count = n;
-                }
-            }
-            __syncthreads();
-            top = s_top;
-            reach = over + s_count;
-        }
-        // ---- equals of the last one: the lowest slots stay.  `spare` of them do not; equals are numbered only where some go
-        const int spare = reach - a.keep;
-        int ties = 0, ties_run = 0;
-        if (spare > 0) {
-            int none = 0, b;
-            for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
-                if (!REGS) load(r0, false);
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r) ties += r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top;
-            }
-            sums.add(ties, none, &ties_run, &b);
-        }
-        const int stay_ties = ties - spare;      // of the equals, in slot order
-        // ---- lists, numbered in slot order: the slots of a group of 16 rounds by round, warp and lane
-        // `place`: counts by round and warp become the sums in front of them; their total goes to s_base
-        auto number = [&]() {
-            __syncthreads();
-            if (warp == 0) {
-                constexpr int PER = EV_KEYS * WARPS / 32;
-                int v[PER], s = 0;
-#pragma unroll
-                for (int q = 0; q < PER; ++q) {
-                    v[q] = s;
-                    s += place[lane * PER + q];
-                }
-                int x = s;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int y = __shfl_up_sync(~0u, x, o);
-                    if (lane >= o) x += y;
-                }
-#pragma unroll
-                for (int q = 0; q < PER; ++q) place[lane * PER + q] = x - s + v[q];
-                if (lane == 31) s_base = x;
-            }
-            __syncthreads();
-        };
-        const unsigned below = (1u << lane) - 1;
-        // the equals of rounds r0 .. that do not stay, as a bit per round
-        auto leavers = [&](int r0) {
-            unsigned gone = 0;
-            if (spare > 0) {
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r) {
-                    const unsigned vote = __ballot_sync(~0u, r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top);
-                    if (lane == 0) place[r * WARPS + warp] = __popc(vote);
-                }
-                number();
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r) {
-                    const bool tie = r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top;
-                    const unsigned vote = __ballot_sync(~0u, tie);
-                    if (tie && ties_run + place[r * WARPS + warp] + __popc(vote & below) >= stay_ties) gone |= 1u << r;
-                }
-                ties_run += s_base;
-                __syncthreads();
-            }
-            return gone;
-        };
-        // whether the slot of round r is a hole or a source, as the warp's vote; its lanes below `keep` (`low`) can only be holes
-        auto vote = [&](int r, int t, unsigned gone, unsigned &low) {
-            const int k = a.keep - (t - lane);
-            low = k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
-            const bool stays = key[r] >= top && !(gone >> r & 1);
-            return __ballot_sync(~0u, t < p.n && (t < a.keep) != stays);
-        };
-        int holes_run = 0, srcs_run = 0, moves = 0;
-        if (!REGS && size > 1) {                 // every CTA counts its own first, to know where its numbers begin
-            const int ties_from = ties_run;
-            int holes = 0, srcs = 0;
-            for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
-                load(r0, false);
-                const unsigned gone = leavers(r0);
-#pragma unroll
-                for (int r = 0; r < EV_KEYS; ++r)
-                    if (r0 + r < rounds) {
-                        unsigned low;
-                        const unsigned v = vote(r, base + (r0 + r) * THREADS + tid, gone, low);
-                        holes += v & low & 1u << lane ? 1 : 0;
-                        srcs += v & ~low & 1u << lane ? 1 : 0;
-                    }
-            }
-            sums.add(holes, srcs, &holes_run, &srcs_run);
-            moves = holes;
-            ties_run = ties_from;
-        }
-        for (int r0 = 0; r0 < rounds || (REGS && r0 == 0); r0 += EV_KEYS) {
+    // ---- the key of rank `keep`: `top` as far as it is known, above `shift`; `over` keys are larger, `reach` at least as large
+    unsigned top = 0;
+    int reach = p.n, over = 0, shift = 32;
+    while (shift > 0 && reach != a.keep && reach - over > EV_CANDS) {
+        const int width = min(10, shift);
+        for (int d = tid; d < EV_BINS; d += THREADS) bins[d] = 0;
+        __syncthreads();
+        for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
             if (!REGS) load(r0, false);
-            const unsigned gone = leavers(r0);
-#pragma unroll
-            for (int r = 0; r < EV_KEYS; ++r) {
-                unsigned v = 0, low = 0;
-                if (r0 + r < rounds) v = vote(r, base + (r0 + r) * THREADS + tid, gone, low);
-                if (lane == 0) place[r * WARPS + warp] = __popc(v & low) | __popc(v & ~low) << 16;    // at most 16 * THREADS of each
-            }
-            number();
-            if (REGS && size > 1) {
-                int holes = tid == 0 ? s_base & 0xffff : 0, srcs = tid == 0 ? (int)((unsigned)s_base >> 16) : 0;
-                sums.add(holes, srcs, &holes_run, &srcs_run);
-                moves = holes;
-            }
 #pragma unroll
             for (int r = 0; r < EV_KEYS; ++r)
                 if (r0 + r < rounds) {
-                    const int t = base + (r0 + r) * THREADS + tid;
-                    unsigned low;
-                    const unsigned v = vote(r, t, gone, low), at = place[r * WARPS + warp];
-                    if (v >> lane & 1) {
-                        int *list = low >> lane & 1 ? a.holes + holes_run + (at & 0xffff) + __popc(v & low & below)
-                                                    : a.srcs + srcs_run + (at >> 16) + __popc(v & ~low & below);
-                        list[(long long)slot * a.cap] = t;
-                    }
+                    const bool in = base + (r0 + r) * THREADS + tid < p.n && (shift == 32 || (key[r] ^ top) >> shift == 0);
+                    if (in) atomicAdd(&bins[kv_evict_bin(key[r] >> (shift - width) & ((1 << width) - 1))], 1);
                 }
-            holes_run += s_base & 0xffff;
-            srcs_run += (unsigned)s_base >> 16;
+        }
+        int *counts = bins;
+        if (size > 1) {                      // the whole cluster's: every CTA adds all of them up for itself
+            kv_cluster_sync();
+            for (int d = tid; d < EV_BINS; d += THREADS) {
+                int sum = 0;
+                for (unsigned r = 0; r < size; ++r) {
+                    unsigned there;
+                    int v;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&bins[d])), "r"(r));
+                    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+                    sum += v;
+                }
+                all_bins[d] = sum;
+            }
+            kv_cluster_sync();               // nobody clears counts that others still read
+            counts = all_bins;
+        } else {
             __syncthreads();
         }
-        if (size == 1) moves = holes_run;
-        if (rank == 0 && tid == 0) a.count[slot] = moves;
+        if (warp == 0) {
+            int larger, equal;
+            const int digit = kv_evict_pick(counts, a.keep - over, larger, equal);
+            if (lane == 0) s_pick = make_int3(digit, larger, equal);
+        }
+        __syncthreads();
+        shift -= width;
+        top |= (unsigned)s_pick.x << shift;
+        over += s_pick.y;
+        reach = over + s_pick.z;
     }
+    if (shift > 0 && reach != a.keep) {      // few keys are left: one warp finds the rest among them alone
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
+            if (!REGS) load(r0, false);
+#pragma unroll
+            for (int r = 0; r < EV_KEYS; ++r)
+                if (r0 + r < rounds) {
+                    // a full shift only where nothing was counted yet: all keys agree
+                    const bool in = base + (r0 + r) * THREADS + tid < p.n && (shift == 32 || (key[r] ^ top) >> shift == 0);
+                    if (in) cand[atomicAdd(&s_count, 1)] = key[r];
+                }
+        }
+        __syncthreads();
+        const int m = reach - over;
+        if (size > 1) {                      // every CTA gets the others' too
+            int mine = s_count, none = 0, before, b;
+            if (tid) mine = 0;
+            sums.add(mine, none, &before, &b);
+            const int own = s_count;
+            const unsigned x = tid < own ? cand[tid] : 0u;
+            kv_cluster_sync();               // all have read their own
+            if (tid < own)
+                for (unsigned r = 0; r < size; ++r) {
+                    unsigned there;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&cand[before + tid])), "r"(r));
+                    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(there), "r"(x) : "memory");
+                }
+            kv_cluster_sync();
+        }
+        if (warp == 0) {
+            const int n = kv_evict_among(cand, m, a.keep - over, shift, top);
+            if (lane == 0) {
+                s_top = top;
+                s_count = n;
+            }
+        }
+        __syncthreads();
+        top = s_top;
+        reach = over + s_count;
+    }
+    // ---- equals of the last one: the lowest slots stay.  `spare` of them do not; equals are numbered only where some go
+    const int spare = reach - a.keep;
+    int ties = 0, ties_run = 0;
+    if (spare > 0) {
+        int none = 0, b;
+        for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
+            if (!REGS) load(r0, false);
+#pragma unroll
+            for (int r = 0; r < EV_KEYS; ++r) ties += r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top;
+        }
+        sums.add(ties, none, &ties_run, &b);
+    }
+    const int stay_ties = ties - spare;      // of the equals, in slot order
+    // ---- lists, numbered in slot order: the slots of a group of 16 rounds by round, warp and lane
+    // `place`: counts by round and warp become the sums in front of them; their total goes to s_base
+    auto number = [&]() {
+        __syncthreads();
+        if (warp == 0) {
+            constexpr int PER = EV_KEYS * WARPS / 32;
+            int v[PER], s = 0;
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                v[q] = s;
+                s += place[lane * PER + q];
+            }
+            int x = s;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(~0u, x, o);
+                if (lane >= o) x += y;
+            }
+#pragma unroll
+            for (int q = 0; q < PER; ++q) place[lane * PER + q] = x - s + v[q];
+            if (lane == 31) s_base = x;
+        }
+        __syncthreads();
+    };
+    const unsigned below = (1u << lane) - 1;
+    // the equals of rounds r0 .. that do not stay, as a bit per round
+    auto leavers = [&](int r0) {
+        unsigned gone = 0;
+        if (spare > 0) {
+#pragma unroll
+            for (int r = 0; r < EV_KEYS; ++r) {
+                const unsigned vote = __ballot_sync(~0u, r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top);
+                if (lane == 0) place[r * WARPS + warp] = __popc(vote);
+            }
+            number();
+#pragma unroll
+            for (int r = 0; r < EV_KEYS; ++r) {
+                const bool tie = r0 + r < rounds && base + (r0 + r) * THREADS + tid < p.n && key[r] == top;
+                const unsigned vote = __ballot_sync(~0u, tie);
+                if (tie && ties_run + place[r * WARPS + warp] + __popc(vote & below) >= stay_ties) gone |= 1u << r;
+            }
+            ties_run += s_base;
+            __syncthreads();
+        }
+        return gone;
+    };
+    // whether the slot of round r is a hole or a source, as the warp's vote; its lanes below `keep` (`low`) can only be holes
+    auto vote = [&](int r, int t, unsigned gone, unsigned &low) {
+        const int k = a.keep - (t - lane);
+        low = k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1;
+        const bool stays = key[r] >= top && !(gone >> r & 1);
+        return __ballot_sync(~0u, t < p.n && (t < a.keep) != stays);
+    };
+    int holes_run = 0, srcs_run = 0, moves = 0;
+    if (!REGS && size > 1) {                 // every CTA counts its own first, to know where its numbers begin
+        const int ties_from = ties_run;
+        int holes = 0, srcs = 0;
+        for (int r0 = 0; r0 < rounds; r0 += EV_KEYS) {
+            load(r0, false);
+            const unsigned gone = leavers(r0);
+#pragma unroll
+            for (int r = 0; r < EV_KEYS; ++r)
+                if (r0 + r < rounds) {
+                    unsigned low;
+                    const unsigned v = vote(r, base + (r0 + r) * THREADS + tid, gone, low);
+                    holes += v & low & 1u << lane ? 1 : 0;
+                    srcs += v & ~low & 1u << lane ? 1 : 0;
+                }
+        }
+        sums.add(holes, srcs, &holes_run, &srcs_run);
+        moves = holes;
+        ties_run = ties_from;
+    }
+    for (int r0 = 0; r0 < rounds || (REGS && r0 == 0); r0 += EV_KEYS) {
+        if (!REGS) load(r0, false);
+        const unsigned gone = leavers(r0);
+#pragma unroll
+        for (int r = 0; r < EV_KEYS; ++r) {
+            unsigned v = 0, low = 0;
+            if (r0 + r < rounds) v = vote(r, base + (r0 + r) * THREADS + tid, gone, low);
+            if (lane == 0) place[r * WARPS + warp] = __popc(v & low) | __popc(v & ~low) << 16;    // at most 16 * THREADS of each
+        }
+        number();
+        if (REGS && size > 1) {
+            int holes = tid == 0 ? s_base & 0xffff : 0, srcs = tid == 0 ? (int)((unsigned)s_base >> 16) : 0;
+            sums.add(holes, srcs, &holes_run, &srcs_run);
+            moves = holes;
+        }
+#pragma unroll
+        for (int r = 0; r < EV_KEYS; ++r)
+            if (r0 + r < rounds) {
+                const int t = base + (r0 + r) * THREADS + tid;
+                unsigned low;
+                const unsigned v = vote(r, t, gone, low), at = place[r * WARPS + warp];
+                if (v >> lane & 1) {
+                    int *list = low >> lane & 1 ? a.holes + holes_run + (at & 0xffff) + __popc(v & low & below)
+                                                : a.srcs + srcs_run + (at >> 16) + __popc(v & ~low & below);
+                    list[(long long)slot * a.cap] = t;
+                }
+            }
+        holes_run += s_base & 0xffff;
+        srcs_run += (unsigned)s_base >> 16;
+        __syncthreads();
+    }
+    if (size == 1) moves = holes_run;
+    if (rank == 0 && tid == 0) a.count[slot] = moves;
     if (size > 1) kv_cluster_sync();             // nobody leaves while others may still write into its memory
 }
 

@@ -424,6 +424,19 @@ def test_append_without_q_idle_places_and_bad_ids():
         assert (q_out[2] != 0).any()
 
 
+def test_append_does_not_write_past_the_rows_of_weights_and_order():
+    c, a = append_case([3, 16, 20], [1, 1, 1], 4, 2, 64, 16, "bf16", 0, 64, 1)
+    qkv, start = a["qkv"], c.pool.clone()
+    big = torch.full((3, 2, 40), 5.0, device="cuda")
+    with B.KVOps(0) as o:
+        o.kv_append(c.handle(B), 1, None, qkv[:, 4:6], qkv[:, 6:], c.tables, c.lens, positions=a["positions"], inv_freq=a["inv_freq"], weights=big[:, :, :17])
+        assert o.kv_ops_sync(check=False) == B.KV_ERR_RANGE             # slots 3 and 16 fit, slot 20 does not
+    assert (big[0, :, 3] == 0).all() and (big[1, :, 16] == 0).all()
+    assert (big[2] == 5).all() and (big[:, :, 17:] == 5).all()
+    b, r = c.where(2, torch.tensor([20]))
+    assert torch.equal(c.pool.view(torch.int16)[1, :, b, r], start.view(torch.int16)[1, :, b, r])
+
+
 def test_append_offsets_beyond_32_bits(ops):
     blocks = (5 << 30) // (4 * 64 * 4 * 128 * 2) + 1
     for layout in (0, 1):
@@ -543,6 +556,29 @@ def test_evict(ops, lens, heads, dim, bs, dtype, layout, layers, keep, recent, s
     ops.kv_ops_sync()
     assert torch.equal(c.pool.view(torch.int16), pool.view(torch.int16))
     assert torch.equal(wd.cpu().view(torch.int32), w2.view(torch.int32)) and torch.equal(od.cpu(), o2)
+
+
+@pytest.mark.parametrize("lens,keep,layers,heads", [([101, 98, 37, 3], 50, 2, 3), ([1000, 999, 997], 601, 1, 2), ([130, 257, 61, 256] * 10, 99, 4, 4)])
+def test_evict_rows_of_whole_quads(ops, lens, keep, layers, heads):
+    """Weights and ages whose rows are 16-byte aligned (read four at a time), lengths and numbers to keep that end inside a quad."""
+    c = R.Cache(lens, heads, 64, 16, layers=layers, seed=keep)
+    bound = -(-c.longest // 4) * 4
+    w, order = (torch.nn.functional.pad(x[..., :c.longest], (0, bound + 4 - c.longest)).contiguous() for x in metadata(c, "ties", c.g))
+    seen = [n + 1 for n in lens]
+    pool, w2, o2 = expect_evict(c, w, order, keep, 7, 2, seen)
+    wd, od = w.cuda(), order.cuda()
+    c.tables = torch.nn.functional.pad(c.tables, (0, 1), value=-1)       # wide enough for the rounded bound
+    w_out = torch.full((layers, len(lens), heads, -(-keep // 4) * 4), -5.0, device="cuda")
+    o_out = torch.full(w_out.shape, -5, dtype=torch.int32, device="cuda")
+    ops.kv_evict(c.handle(B), c.tables, c.lens, bound, keep=keep, recent=7, sink=2, weights=wd, order=od, seen=torch.tensor(seen, dtype=torch.int32).cuda(),
+                 weights_out=w_out, order_out=o_out)
+    ops.kv_ops_sync()
+    assert torch.equal(c.pool.view(torch.int16), pool.view(torch.int16))
+    for i, n in enumerate(lens):
+        m = min(n, keep)
+        assert torch.equal(w_out[:, i, :, :m].cpu().view(torch.int32), w2[:, i, :, :m].contiguous().view(torch.int32))
+        assert torch.equal(o_out[:, i, :, :m].cpu(), o2[:, i, :, :m])
+        assert (w_out[:, i, :, m:] == -5).all() and (o_out[:, i, :, m:] == -5).all()
 
 
 def test_evict_some_layers_without_order(ops):
