@@ -25,7 +25,8 @@
 // Mathematics of a tile, on mma.m16n8k16 with the cache as the left operand, so that the few query heads fill the narrow
 // side:  S^T[16 slots, 8 heads] = K Q^T;  m, p = exp2(S - m), l in float32 (scale and log2 e are applied to the sums);
 // O^T[dim, 8 heads] = alpha O^T + V^T P^T, V^T by transposing ldmatrix, P^T by movmatrix from the score fragment.  P is
-// rounded to the cache's type, the only rounding besides the output's; l sums the unrounded p.  (tcgen05 would take the cache
+// rounded to the cache's type, the only rounding besides the output's; l sums the unrounded p, with compensation, since in a long
+// row the small ones would vanish beside one large.  (tcgen05 would take the cache
 // as its left operand just the same, 128 slots at a time, but a decode step has no use for its rate: the tensor pipe is 8 %
 // busy as it is, and the running maximum would have to travel between tensor memory and registers for every tile.)
 // Masked slots (beyond the length, before the window, in a bad block) are never loaded: their K and V are zero-filled, so
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 
     // ---- consumer
     unsigned qf[NT][KS][2];
-    float o[NT][KS][4], m[NT][2], l[NT][2];
+    float o[NT][KS][4], m[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
     int take = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
     for (int n = 0; n < todo; ++n) {
@@ -354,7 +355,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[nt][ks][e] = 0.f;
                 m[nt][0] = m[nt][1] = -INFINITY;
-                l[nt][0] = l[nt][1] = 0.f;
+                l[nt][0] = l[nt][1] = rest[nt][0] = rest[nt][1] = 0.f;
             }
         }
         // the tile that is computed now was committed stages - 1 groups ago
@@ -418,15 +419,26 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                     m[nt][e] = x;
                     s[nt][e] = kv_exp2(s[nt][e] - ref);
                     s[nt][e + 2] = kv_exp2(s[nt][e + 2] - ref);
-                    l[nt][e] = l[nt][e] * alpha[e] + (s[nt][e] + s[nt][e + 2]);
                 }
                 pf[nt][0] = kv_movmatrix_t(KvMma<T>::pack(s[nt][0], s[nt][1]));
                 pf[nt][1] = kv_movmatrix_t(KvMma<T>::pack(s[nt][2], s[nt][3]));
-                if (__any_sync(~0u, alpha[0] != 1.f || alpha[1] != 1.f))
+                if (__any_sync(~0u, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        l[nt][e] *= alpha[e];
+                        rest[nt][e] *= alpha[e];
+                    }
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[nt][ks][e] *= alpha[e & 1];
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {            // compensated: weights of 2^-25 of the largest would vanish one by one
+                    const float x = s[nt][e] + s[nt][e + 2] + rest[nt][e], sum = l[nt][e] + x;
+                    rest[nt][e] = x - (sum - l[nt][e]);
+                    l[nt][e] = sum;
+                }
             }
             const unsigned vrow = stage + TILE + ((lane & 7) + (lane >> 4) * 8) * ROW + ((lane >> 3 & 1 ^ lane & 7) << 4);
 #pragma unroll
