@@ -25,8 +25,9 @@
 // Mathematics of a tile, on mma.m16n8k16 with the cache as the left operand, so that the few query heads fill the narrow
 // side:  S^T[16 slots, 8 heads] = K Q^T;  m, p = exp2(S - m), l in float32 (scale and log2 e are applied to the sums);
 // O^T[dim, 8 heads] = alpha O^T + V^T P^T, V^T by transposing ldmatrix, P^T by movmatrix from the score fragment.  P is
-// rounded to the cache's type, the only rounding besides the output's; l sums the unrounded p, with compensation, since in a long
-// row the small ones would vanish beside one large.  (tcgen05 would take the cache
+// rounded to the cache's type (f16: times 2^14, taken back at the end), the only rounding besides the output's: it is what lets the second product run on
+// the tensor pipe at the cache's width, and its error averages out over the slots below the output's own.  l sums the
+// unrounded p, with compensation, since in a long row the small ones would vanish beside one large.  (tcgen05 would take the cache
 // as its left operand just the same, 128 slots at a time, but a decode step has no use for its rate: the tensor pipe is 8 %
 // busy as it is, and the running maximum would have to travel between tensor memory and registers for every tile.)
 // Masked slots (beyond the length, before the window, in a bad block) are never loaded: their K and V are zero-filled, so
@@ -75,6 +76,7 @@ __device__ __forceinline__ float kv_ref(float m) { return m == -INFINITY ? 0.f :
 
 template <typename T> struct KvMma;
 template <> struct KvMma<__nv_bfloat16> {
+    static constexpr float LIFT = 1.f;
     static __device__ __forceinline__ void mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1)
     {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -87,6 +89,9 @@ template <> struct KvMma<__nv_bfloat16> {
     }
 };
 template <> struct KvMma<__half> {
+    // the weights of the second product go up to this: f16 has no numbers below 2^-24, and many small weights count together, so
+    // only those below 2^-28 of the row's largest lose bits, and those below 2^-39 vanish
+    static constexpr float LIFT = 16384.f;
     static __device__ __forceinline__ void mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1)
     {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -189,6 +194,7 @@ __device__ __forceinline__ int kv_attend_piece(const KvAttend &a, int total) { r
 template <typename T, int DP, int NT>
 __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP * NT <= 128 ? 2 : 1) kv_attend_stream(const __grid_constant__ KvAttend a)
 {
+    constexpr float LIFT = KvMma<T>::LIFT;
     constexpr int ROW = DP * 2, TILE = 16 * ROW, KS = DP / 16, LANES = DP / 8, PASS = 32 / LANES, HEADS = 8 * NT;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int red[KV_ATTEND_WARPS], s_at[2];
@@ -420,8 +426,8 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                     s[nt][e] = kv_exp2(s[nt][e] - ref);
                     s[nt][e + 2] = kv_exp2(s[nt][e + 2] - ref);
                 }
-                pf[nt][0] = kv_movmatrix_t(KvMma<T>::pack(s[nt][0], s[nt][1]));
-                pf[nt][1] = kv_movmatrix_t(KvMma<T>::pack(s[nt][2], s[nt][3]));
+                pf[nt][0] = kv_movmatrix_t(KvMma<T>::pack(s[nt][0] * LIFT, s[nt][1] * LIFT));
+                pf[nt][1] = kv_movmatrix_t(KvMma<T>::pack(s[nt][2] * LIFT, s[nt][3] * LIFT));
                 if (__any_sync(~0u, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
@@ -518,7 +524,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                         if (g >= heads) continue;
                         const int gq = h * a.group + g0 + g;
                         if (whole) {
-                            const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e];
+                            const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e] * (1.f / LIFT);
                             const float lse2 = l[nt][e] == 0.f ? -INFINITY : m[nt][e] + log2f(l[nt][e]);
                             T *to = (T *)a.out + tile.z * a.o_seq + gq * a.o_head;
 #pragma unroll
@@ -541,7 +547,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 #pragma unroll
                                 for (int b = 0; b < 2; ++b) {
                                     const int d = ks * 16 + b * 8 + (lane >> 2);
-                                    if (d < a.c.dim) to[d] = o[nt][ks][2 * b + e];
+                                    if (d < a.c.dim) to[d] = o[nt][ks][2 * b + e] * (1.f / LIFT);
                                 }
                             if (lane < 4) a.part_ml[part * HEADS + g] = make_float2(m[nt][e], l[nt][e]);
                         }

@@ -52,3 +52,13 @@ def test_the_sum_of_a_row_keeps_many_small_weights(ops, dtype, seqs, heads, n):
     """lse = 18 + log(1 + x), to the bound of all lse tests: an uncompensated sum of a long row is off by twice as much."""
     _, lse, x = one_peak(ops, dtype, seqs, heads, n)
     assert (lse - (18.0 + math.log1p(x))).abs().max().item() <= 2.0 ** -20 * 19
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("seqs,heads,n", PEAKS)
+def test_the_output_keeps_many_small_weights(ops, dtype, seqs, heads, n):
+    """out = 1000 x / (1 + x).  Bound: the weights' rounding and the output's, u each, the exponential's and the sums' error
+    2^-18, and half of the smallest f16 number."""
+    out, _, x = one_peak(ops, dtype, seqs, heads, n)
+    want = 1000.0 * x / (1 + x)
+    assert (out - want).abs().max().item() <= (2 * R.UNIT[dtype] + 2.0 ** -18) * want + 2.0 ** -25
