@@ -566,7 +566,8 @@ int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
  * over the slots t in [max(0, lens[i] - window), lens[i]) (window 0: all):
  *     s_t = scale * q . K_t,  p_t = exp(s_t) / sum exp(s),  out = sum p_t V_t,  lse = log sum exp(s)
  *     weights_out[i][h][t] = weights_in[i][h][t] + sum over h's query heads of p_t      (t < lens[i])
- * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing.
+ * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing, whatever V holds.  Else every
+ * slot counts, one of weight 0 too: an infinite or NaN element of its V makes that element of out infinite or NaN.
  */
 typedef struct {
     int32_t layer, num_seqs, q_heads, window;

@@ -524,15 +524,16 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                         if (g >= heads) continue;
                         const int gq = h * a.group + g0 + g;
                         if (whole) {
-                            const float inv = l[nt][e] == 0.f ? 0.f : 1.f / l[nt][e] * (1.f / LIFT);
-                            const float lse2 = l[nt][e] == 0.f ? -INFINITY : m[nt][e] + log2f(l[nt][e]);
+                            const bool none = l[nt][e] == 0.f;           // the sums may be 0 * inf then
+                            const float inv = none ? 0.f : 1.f / l[nt][e] * (1.f / LIFT);
+                            const float lse2 = none ? -INFINITY : m[nt][e] + log2f(l[nt][e]);
                             T *to = (T *)a.out + tile.z * a.o_seq + gq * a.o_head;
 #pragma unroll
                             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                                 for (int b = 0; b < 2; ++b) {
                                     const int d = ks * 16 + b * 8 + (lane >> 2);
-                                    if (d < a.c.dim) to[d] = kv_round<T>(o[nt][ks][2 * b + e] * inv);
+                                    if (d < a.c.dim) to[d] = kv_round<T>(none ? 0.f : o[nt][ks][2 * b + e] * inv);
                                 }
                             if (lane < 4) {
                                 if (a.lse) a.lse[(long long)tile.z * a.q_heads + gq] = lse2 * KV_LN2;
@@ -655,7 +656,7 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
         const int own = step == 1 ? 0 : lane;
         if (a.lse && own == 0 && pair * slices >= u0) a.lse[(long long)i * a.q_heads + (h0 + hw) * a.group + g0 + g] = z * KV_LN2;
 #pragma unroll 4
-        for (int c = own; c < parts; c += step) factor[n * parts + c] = z == -INFINITY ? 0.f : kv_exp2(ml[slot(c0 + c)].x - z);
+        for (int c = own; c < parts; c += step) factor[n * parts + c] = z == -INFINITY ? -1.f : kv_exp2(ml[slot(c0 + c)].x - z);
     };
     if (parts <= 8)
         for (int n = tid; n < pairs; n += KV_JOIN_THREADS) weigh(n, KvCount<1>());
@@ -683,8 +684,8 @@ __device__ __forceinline__ void kv_join_rows(const KvAttend &a, int heads_of_chu
     auto add = [&](Task &x, int c) {
         const float4 v = *(const float4 *)(x.from + (long long)slot(c0 + c) * a.c.dim);
         const float f = x.factor[c];
-        // a factor of 0 leaves out whatever a part without any weight holds
-        if (f != 0.f) x.acc = make_float4(x.acc.x + f * v.x, x.acc.y + f * v.y, x.acc.z + f * v.z, x.acc.w + f * v.w);
+        // a part without weight counts as 0 times what it holds, as its slots would in one sum; of a row without any (-1) nothing does
+        if (!(f < 0.f)) x.acc = make_float4(x.acc.x + f * v.x, x.acc.y + f * v.y, x.acc.z + f * v.z, x.acc.w + f * v.w);
     };
     auto put = [&](const Task &x) {
         x.to[0] = kv_round<T>(x.acc.x);

@@ -62,3 +62,54 @@ def test_the_output_keeps_many_small_weights(ops, dtype, seqs, heads, n):
     out, _, x = one_peak(ops, dtype, seqs, heads, n)
     want = 1000.0 * x / (1 + x)
     assert (out - want).abs().max().item() <= (2 * R.UNIT[dtype] + 2.0 ** -18) * want + 2.0 ** -25
+
+
+# ---- values that are not finite -------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n,others", [(40, 0), (40, 3), (300, 200), (6000, 0), (6000, 40)])
+@pytest.mark.parametrize("weights", [True, False])
+def test_no_score_left_gives_zero_whatever_v_holds(ops, n, others, weights):
+    """All scores of head 0 are -inf and its V rows hold infinities and NaN: out 0, lse -inf, weights as they were."""
+    c = R.Cache([n] + [50] * others, 2, 64, 16, seed=n)
+    k, v = c.read(0, 1, 0).cpu(), c.read(0, 1, 1).cpu()
+    k[:, 0] = -INF
+    v[3, 0, 5], v[n // 2, 0, 6], v[n - 1, 0, 63] = INF, NAN, -INF
+    c.write(0, 1, 0, k)
+    c.write(0, 1, 1, v)
+    q = randn(c.g, 1 + others, 4, 64).abs() + 0.5
+    out, lse = torch.full_like(q, 7.0), torch.full((1 + others, 4), 7.0, device="cuda")
+    w = torch.rand(1 + others, 2, c.longest, device="cuda") if weights else None
+    w_out = torch.full_like(w, -3.0) if weights else None
+    ops.kv_attend(c.handle(B), 1, q, c.tables, c.lens, c.longest, out=out, lse=lse, weights_in=w, weights_out=w_out)
+    ops.kv_ops_sync()
+    assert (out[0, :2] == 0).all() and (lse[0, :2] == -INF).all()
+    assert out[0, 2:].isfinite().all() and lse[0, 2:].isfinite().all() and out[1:].isfinite().all()
+    if weights:
+        assert torch.equal(w_out[0, 0, :n], w[0, 0, :n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,run,others", [(100, 30, 0), (900, 500, 0), (6000, 3000, 0), (6000, 3000, 150)])
+def test_v_of_a_slot_without_weight_counts_wherever_the_row_is_cut(ops, dtype, n, run, others):
+    """A run of slots of score -inf, weight 0, with one infinity and one NaN in their V: 0 * inf makes those two elements NaN, in
+    rows that one CTA has and in rows that are cut (inside the run as well) alike; all other elements are as ever."""
+    c = R.Cache([n] + [60] * others, 1, 64, 16, dtype, seed=run)
+    k, v = c.read(0, 1, 0).cpu(), c.read(0, 1, 1).cpu()
+    first = n // 4
+    k[first:first + run] = -INF
+    v[first + run // 2, 0, 5], v[first + run // 3, 0, 40] = INF, NAN
+    c.write(0, 1, 0, k)
+    c.write(0, 1, 1, v)
+    q = randn(c.g, 1 + others, 2, 64, dtype=dtype).abs() + 0.5
+    out = torch.full_like(q, 7.0)
+    ops.kv_attend(c.handle(B), 1, q, c.tables, c.lens, n, out=out)
+    ops.kv_ops_sync()
+    rest = [d for d in range(64) if d not in (5, 40)]
+    assert out[0][:, [5, 40]].isnan().all()
+    v[first + run // 2, 0, 5] = v[first + run // 3, 0, 40] = 0.0        # for the statement in 64 bits
+    c.write(0, 1, 1, v)
+    for i, row in enumerate(R.attend(c, 1, q)):
+        for g, (o, _, _, _, bound, _) in enumerate(row):
+            d = rest if i == 0 else list(range(64))
+            assert ((out[i, g].double().cpu() - o)[d].abs() <= bound[d]).all(), (i, g)
