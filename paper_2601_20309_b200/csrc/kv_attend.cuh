@@ -579,7 +579,8 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
                         add[b] += __shfl_xor_sync(~0u, add[b], 1);
                         add[b] += __shfl_xor_sync(~0u, add[b], 2);
                         const int t = t0 + b * 8 + (lane >> 2);
-                        if ((lane & 3) == 0 && t < sp.n) a.w_out[w + t] = (a.w_in ? a.w_in[w + t] : 0.f) + add[b];
+                        // slots of the tile that lie before the window keep their weight, even where the sum is NaN
+                        if ((lane & 3) == 0 && t < sp.n) a.w_out[w + t] = (a.w_in ? a.w_in[w + t] : 0.f) + (t >= sp.first ? add[b] : 0.f);
                     }
                 }
                 if (a.tw > 1) __syncthreads();           // the next row's sums take the place of these

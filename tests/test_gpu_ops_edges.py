@@ -113,3 +113,22 @@ def test_v_of_a_slot_without_weight_counts_wherever_the_row_is_cut(ops, dtype, n
         for g, (o, _, _, _, bound, _) in enumerate(row):
             d = rest if i == 0 else list(range(64))
             assert ((out[i, g].double().cpu() - o)[d].abs() <= bound[d]).all(), (i, g)
+
+
+@pytest.mark.parametrize("n,window", [(40, 10), (700, 333), (6000, 333)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_slots_before_the_window_keep_their_weight_when_the_sum_is_nan(ops, n, window, in_place):
+    """A NaN in K makes the row's sum NaN, and with it the weights inside the window; in front of it nothing changes."""
+    c = R.Cache([n], 1, 64, 16, seed=n)
+    k = c.read(0, 1, 0).cpu()
+    k[n - 3, 0, 9] = NAN
+    c.write(0, 1, 0, k)
+    q = randn(c.g, 1, 2, 64)
+    w = torch.rand(1, 1, n, device="cuda")
+    had = w.clone()
+    w_out = w if in_place else torch.full_like(w, -3.0)
+    out = torch.zeros_like(q)
+    ops.kv_attend(c.handle(B), 1, q, c.tables, c.lens, n, out=out, window=window, weights_in=w, weights_out=w_out)
+    ops.kv_ops_sync()
+    assert torch.equal(w_out[..., :n - window], had[..., :n - window])
+    assert w_out[..., n - window:].isnan().all() and out.isnan().all()
