@@ -597,7 +597,8 @@ int32_t kv_attend_workspace(kv_ops_t *ops, const kv_cache_t *cache, const kv_att
  *     (x, y) -> (x cos - y sin, x sin + y cos),   x, y = elements f and f + rotary_dim/2, or 2f and 2f + 1
  * for every head of q and k; elements from rotary_dim on pass unchanged.  q_out = turned q, K = turned k, V = v.
  * weights[i][h][slot] = 0 and order[i][h][slot] = the token's number, where given.  A sequence of length 0 (an idle
- * place of a batch of fixed size) gets its q turned and nothing written.
+ * place of a batch of fixed size) gets its q turned and nothing written; so does a token of no sequence (in front of
+ * seq_starts[0], or from seq_starts[num_seqs] on), which counts as one of a bad length unless the sequence beside it is idle.
  */
 typedef struct {
     int32_t layer, num_seqs, q_heads;

@@ -121,9 +121,10 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_cons
                 const long long t = first + k;
                 const int i = a.starts ? kv_seq_of(a.starts, a.num_seqs, t) : (int)t;
                 const long long left = a.starts ? a.starts[i + 1] - t : 1;       // this token and those behind it
+                const bool member = !a.starts || a.starts[i] <= t;               // not one in front of the first start
                 const int n = a.c.len(i);
                 const long long s = n - left;
-                const bool ok = left > 0 && s >= 0 && (!(a.weights || a.order) || s < a.num_slots);
+                const bool ok = member && left > 0 && s >= 0 && (!(a.weights || a.order) || s < a.num_slots);
                 if ((tid & 31) == 0) {
                     if (!ok && n > 0) atomicOr(a.c.status, KV_OPS_BAD_LEN);
                     kv_row[k] = ok ? a.c.slot(i, (int)s, a.layer * 2) : nullptr;

@@ -132,3 +132,24 @@ def test_slots_before_the_window_keep_their_weight_when_the_sum_is_nan(ops, n, w
     ops.kv_ops_sync()
     assert torch.equal(w_out[..., :n - window], had[..., :n - window])
     assert w_out[..., n - window:].isnan().all() and out.isnan().all()
+
+
+# ---- tokens of no sequence ------------------------------------------------------------------------------------------
+
+
+def test_tokens_in_front_of_the_first_start_are_not_written():
+    """seq_starts = [2, 5]: tokens 0 and 1 belong to no sequence.  They are skipped and reported; 2, 3 and 4 go to the last slots."""
+    c = R.Cache([20], 2, 64, 16, seed=1)
+    kv = randn(c.g, 5, 4, 64)
+    start = c.pool.clone()
+    w = torch.full((1, 2, 20), 5.0, device="cuda")
+    with B.KVOps(0) as o:
+        o.kv_append(c.handle(B), 1, None, kv[:, :2], kv[:, 2:], c.tables, c.lens, positions=torch.zeros(1, 5, dtype=torch.int32, device="cuda"),
+                    inv_freq=torch.ones(32, device="cuda"), seq_starts=torch.tensor([2, 5], dtype=torch.int32).cuda(), weights=w)
+        assert o.kv_ops_sync(check=False) == B.KV_ERR_RANGE
+    assert torch.equal(c.read(0, 1, 0)[17:], kv[2:, :2]) and torch.equal(c.read(0, 1, 1)[17:], kv[2:, 2:])
+    assert (w[..., :17] == 5).all() and (w[..., 17:] == 0).all()
+    b, r = c.where(0, torch.arange(17, 20))
+    for side in range(2):
+        c.plane(1, side)[b, r] = start[1, side][b, r]
+    assert torch.equal(c.pool.view(torch.int16), start.view(torch.int16))
