@@ -50,7 +50,7 @@ struct Call {
         }
         if (st.back() != 1 && have.back() > 1) throw Bad{std::string(what) + ": the last dimension must be contiguous"};
         *p = t.data_ptr();
-        for (size_t k = 0; strides && k + 1 < st.size(); ++k) strides[k] = st[k];
+        for (size_t k = 0; strides && k + 1 < st.size(); ++k) strides[k] = have[k] > 1 ? st[k] : 0;      // nothing steps along a dimension of size 1
         return t;
     }
     const at::Tensor &slots(PyObject *o, at::ScalarType want, std::initializer_list<int64_t> shape, int64_t least, const char *what, const void **p, int64_t *strides) const

@@ -153,3 +153,41 @@ def test_tokens_in_front_of_the_first_start_are_not_written():
     for side in range(2):
         c.plane(1, side)[b, r] = start[1, side][b, r]
     assert torch.equal(c.pool.view(torch.int16), start.view(torch.int16))
+
+
+# ---- strides that are never used ------------------------------------------------------------------------------------
+
+
+def test_strides_of_dimensions_of_size_one_do_not_count(ops):
+    """One sequence (one layer) cut out of a larger array beside a fresh one: their strides differ where nothing steps."""
+    c = R.Cache([40], 2, 64, 16, seed=2)
+    q = randn(c.g, 1, 4, 64)
+    out = torch.zeros_like(q)
+    big = torch.rand(6, 2, 40, device="cuda")
+    had, fresh = big[::3][1:], torch.zeros(1, 2, 40, device="cuda")
+    assert had.stride() != fresh.stride() and had.shape == fresh.shape
+    ops.kv_attend(c.handle(B), 1, q, c.tables, c.lens, 40, out=out, weights_in=had, weights_out=fresh)
+    ops.kv_ops_sync()
+    p = [row[2] for row in R.attend(c, 1, q)[0]]
+    want = had[0].double().cpu() + torch.stack([p[0] + p[1], p[2] + p[3]])
+    assert torch.allclose(fresh[0].double().cpu(), want, rtol=1e-4, atol=1e-6)
+
+    order = torch.full((1, 2, 40), -9, dtype=torch.int32, device="cuda")
+    kv = randn(c.g, 1, 4, 64)
+    ops.kv_append(c.handle(B), 1, None, kv[:, :2], kv[:, 2:], c.tables, c.lens, positions=torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
+                  inv_freq=torch.ones(32, device="cuda"), weights=had, order=order, token_order=torch.tensor([77], dtype=torch.int32).cuda())
+    ops.kv_ops_sync()
+    assert (had[0, :, 39] == 0).all() and (order[0, :, 39] == 77).all() and (order[0, :, :39] == -9).all()
+
+    layers = torch.rand(4, 1, 2, 40, device="cuda")
+    w, ages = layers[2:3], torch.arange(40, dtype=torch.int32, device="cuda").expand(3, 2, 1, 2, 40).contiguous()[1:2, 1]
+    w_out, o_out = torch.zeros(3, 5, 2, 24, device="cuda")[1:2, 4:], torch.zeros(1, 1, 2, 24, dtype=torch.int32, device="cuda")
+    assert w.stride() != ages.stride() and w_out.stride() != o_out.stride()
+    before = w.clone()
+    ops.kv_evict(c.handle(B), c.tables, c.lens, 40, keep=24, recent=4, sink=2, weights=w, order=ages, weights_out=w_out, order_out=o_out, first_layer=1)
+    ops.kv_ops_sync()
+    for h in range(2):
+        want = list(range(24))
+        for d, s in R.evict(before[0, 0, h].cpu(), torch.arange(40), 40, 24, 4, 2, 40):
+            want[d] = s
+        assert o_out[0, 0, h].tolist() == want and torch.equal(w_out[0, 0, h], before[0, 0, h, want])
