@@ -637,9 +637,9 @@ class KVCache:
 
 class KVOps:
     """Operators on the device cache, on one stream (a ``cudaStream_t`` as an int; None or 0 = the default stream).  Arrays are
-    CUDA tensors; rows may lie at any stride, the elements of a row side by side.  Wrong types, shapes and devices raise
-    ``ValueError``; the C status comes back, or raises ``KVError`` with ``check``.  Tensors of another stream have to be
-    ordered by the caller, and kept until this stream is done with them."""
+    CUDA tensors; rows may lie at any stride, the elements of a row side by side.  Wrong types, shapes and devices, and tensors
+    that require gradients while those are recorded, raise ``ValueError``; the C status comes back, or raises ``KVError`` with
+    ``check``.  Tensors of another stream have to be ordered by the caller, and kept until this stream is done with them."""
 
     def __init__(self, device_id: int = 0, stream: Optional[int] = None):
         self._h = C.c_void_p()

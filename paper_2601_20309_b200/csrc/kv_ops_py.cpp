@@ -2,6 +2,7 @@
 // calls these a few times per layer; read through Python attributes, a call's dozen tensors took 13 to 30 us, several
 // times what the kernels of a small call need.
 #include <Python.h>
+#include <ATen/core/grad_mode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -32,6 +33,8 @@ struct Call {
         if (!THPVariable_Check(o)) throw Bad{std::string(what) + " must be a tensor"};
         const at::Tensor &t = THPVariable_Unpack(o);
         if (t.scalar_type() != want) throw Bad{std::string(what) + " must be " + name_of(want) + ", not " + name_of(t.scalar_type())};
+        if (t.requires_grad() && at::GradMode::is_enabled())
+            throw Bad{std::string(what) + " requires grad, and the operators have no backward pass: call them under torch.no_grad()"};
         if (!t.is_cuda() || t.get_device() != device) throw Bad{std::string(what) + " must be on cuda:" + std::to_string(device)};
         const auto have = t.sizes(), st = t.strides();
         bool ok = have.size() == shape.size();

@@ -191,3 +191,39 @@ def test_strides_of_dimensions_of_size_one_do_not_count(ops):
         for d, s in R.evict(before[0, 0, h].cpu(), torch.arange(40), 40, 24, 4, 2, 40):
             want[d] = s
         assert o_out[0, 0, h].tolist() == want and torch.equal(w_out[0, 0, h], before[0, 0, h, want])
+
+
+# ---- tensors that want gradients ------------------------------------------------------------------------------------
+
+
+def test_tensors_that_want_gradients_are_refused_where_they_would_be_recorded(ops):
+    """The operators have no backward pass: with gradients on, such a tensor would leave the graph without a word."""
+    c = R.Cache([40, 7], 2, 64, 16, seed=3)
+    q, kv = randn(c.g, 2, 4, 64), randn(c.g, 2, 4, 64)
+    out = torch.full_like(q, 3.0)
+    start = c.pool.clone()
+    pos, freq = torch.zeros(1, 2, dtype=torch.int32, device="cuda"), torch.ones(32, device="cuda")
+    leaf, kv_leaf, freq_leaf = (x.clone().requires_grad_() for x in (q, kv, freq))
+    h = c.handle(B)
+    for bad in (dict(q=leaf), dict(q=leaf * 2), dict(out=leaf)):
+        a = {"q": q, "out": out, **bad}
+        with pytest.raises(ValueError, match="grad"):
+            ops.kv_attend(h, 1, a["q"], c.tables, c.lens, 40, out=a["out"])
+    for k, v, f in ((kv_leaf[:, :2], kv[:, 2:], freq), (kv[:, :2], kv_leaf[:, 2:], freq), (kv[:, :2], kv[:, 2:], freq_leaf)):
+        with pytest.raises(ValueError, match="grad"):
+            ops.kv_append(h, 1, None, k, v, c.tables, c.lens, positions=pos, inv_freq=f)
+    with pytest.raises(ValueError, match="grad"):
+        ops.kv_evict(h, c.tables, c.lens, 40, keep=10, weights=torch.rand(2, 2, 2, 40, device="cuda", requires_grad=True))
+    ops.kv_ops_sync()
+    assert (out == 3).all() and torch.equal(c.pool.view(torch.int16), start.view(torch.int16))
+    ops.kv_attend(h, 1, q, c.tables, c.lens, 40, out=out)
+    for guard in (torch.no_grad, torch.inference_mode):
+        with guard():
+            got = torch.zeros_like(q)
+            ops.kv_attend(h, 1, leaf, c.tables, c.lens, 40, out=got)
+            ops.kv_ops_sync()
+            assert torch.equal(got, out)
+    got = torch.zeros_like(q)
+    ops.kv_attend(h, 1, leaf.detach(), c.tables, c.lens, 40, out=got)
+    ops.kv_ops_sync()
+    assert torch.equal(got, out)
