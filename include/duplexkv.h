@@ -573,7 +573,8 @@ typedef struct {
     int32_t layer, num_seqs, q_heads, window;
     int64_t max_len;                /* HOST bound of lens: sizes the launch and the workspace           */
     float   scale;                  /* 0 = 1 / sqrt(head_dim)                                           */
-    int32_t table_width;            /* entries per row of block_tables; table_width*block_size >= max_len */
+    int32_t table_width;            /* entries per row of block_tables; table_width*block_size >= max_len (0: no
+                                       block yet, all lengths are 0)                                    */
     const void *q;                  /* [num_seqs][q_heads][head_dim]                                    */
     int64_t q_seq_stride, q_head_stride;
     void   *out;                    /* same shape; may be q                                             */

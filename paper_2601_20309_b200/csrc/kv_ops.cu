@@ -109,8 +109,9 @@ int32_t make_view(kv_ops *o, const kv_cache_t *c, KvView &v)
 
 int32_t set_tables(kv_ops *o, KvView &v, const int32_t *tables, int64_t stride, int32_t width, const int32_t *lens, int64_t max_len)
 {
-    if (!tables || !lens) return fail(o, KV_ERR_INVALID_ARG, "block_tables and lens are needed");
-    if (width <= 0 || stride < 0) return fail(o, KV_ERR_INVALID_ARG, "bad block table shape");
+    // before any token there is a batch without blocks: tables of no entries
+    if ((!tables && (width || max_len)) || !lens) return fail(o, KV_ERR_INVALID_ARG, "block_tables and lens are needed");
+    if (width < 0 || stride < 0) return fail(o, KV_ERR_INVALID_ARG, "bad block table shape");
     if (max_len < 0 || max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
     if (max_len > (int64_t)width * v.bs) return fail(o, KV_ERR_INVALID_ARG, "the block tables are too narrow for max_len");
     v.tables = tables;

@@ -227,3 +227,23 @@ def test_tensors_that_want_gradients_are_refused_where_they_would_be_recorded(op
     ops.kv_attend(h, 1, leaf.detach(), c.tables, c.lens, 40, out=got)
     ops.kv_ops_sync()
     assert torch.equal(got, out)
+
+
+# ---- nothing in the cache yet ---------------------------------------------------------------------------------------
+
+
+def test_tables_without_entries_for_a_batch_without_tokens(ops):
+    """All places of the batch are idle and no block has been handed out: tables of width 0, max_len 0."""
+    c = R.Cache([5], 2, 64, 16, seed=4)
+    tables, lens = torch.empty(3, 0, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    q, kv = randn(c.g, 3, 4, 64), randn(c.g, 3, 4, 64)
+    out, lse = torch.full_like(q, 3.0), torch.zeros(3, 4, device="cuda")
+    start = c.pool.clone()
+    ops.kv_attend(c.handle(B), 1, q, tables, lens, 0, out=out, lse=lse)
+    assert (out == 0).all() and (lse == -INF).all()
+    turned = torch.zeros_like(q)
+    ops.kv_append(c.handle(B), 1, q, kv[:, :2], kv[:, 2:], tables, lens, positions=torch.zeros(1, 3, dtype=torch.int32, device="cuda"),
+                  inv_freq=torch.ones(32, device="cuda"), q_out=turned)
+    assert ops.kv_ops_sync() == 0
+    assert torch.equal(turned, q) and torch.equal(c.pool.view(torch.int16), start.view(torch.int16))
+    assert ops.kv_attend(c.handle(B), 1, q, tables, lens, 1, out=out, check=False) == B.KV_ERR_INVALID_ARG
