@@ -247,3 +247,48 @@ def test_tables_without_entries_for_a_batch_without_tokens(ops):
     assert ops.kv_ops_sync() == 0
     assert torch.equal(turned, q) and torch.equal(c.pool.view(torch.int16), start.view(torch.int16))
     assert ops.kv_attend(c.handle(B), 1, q, tables, lens, 1, out=out, check=False) == B.KV_ERR_INVALID_ARG
+
+
+# ---- bad block ids --------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("n,keep,quads", [(100, 50, False), (100, 52, True), (400, 150, False), (3000, 2000, False), (5000, 700, False)])
+def test_evict_drops_exactly_the_pairs_of_a_bad_block(n, keep, quads, layout):
+    """Bad ids in a block of holes and in a block of sources: their rows, weights and ages stay, all other pairs move.  Up to 64
+    rows move in the selecting kernel, more in a second one; lengths for each kind of selection."""
+    c = R.Cache([n, n - 1], 2, 64, 16, layout=layout, layers=2, seed=n)
+    g, width = c.g, n if quads else n + 3
+    w = torch.rand(2, 2, 2, width, generator=g)
+    order = torch.rand(2, 2, 2, width, generator=g).argsort(-1).to(torch.int32)
+    lost = {1, (keep + n) // 32}                # of sequence 1: a block of holes, a block of sources
+    bad = c.tables.clone()
+    bad[1, 1], bad[1, (keep + n) // 32] = c.nb, -3
+    want, w2, o2 = c.pool.clone(), w.clone(), order.clone()
+    planed, source = (p if layout else p.permute(2, 0, 1, 3, 4, 5) for p in (want, c.pool))
+    dropped = 0
+    for l in range(2):
+        for i in range(2):
+            for h in range(2):
+                pairs = R.evict(w[l, i, h], order[l, i, h], c.lens_list[i], keep, 5, 2, n + 1)
+                fine = [(d, s) for d, s in pairs if i == 0 or not {d // 16, s // 16} & lost]
+                dropped += len(pairs) - len(fine)
+                d, s = (torch.tensor(x) for x in zip(*fine))
+                (db, dr), (sb, sr) = c.where(i, d), c.where(i, s)
+                planed[db, l, :, dr, h] = source[sb, l, :, sr, h]
+                w2[l, i, h, d], o2[l, i, h, d] = w[l, i, h, s], order[l, i, h, s]
+    assert dropped > 0
+    wd, od = w.cuda(), order.cuda()
+    w_out, o_out = torch.full((2, 2, 2, keep), -5.0, device="cuda"), torch.full((2, 2, 2, keep), -5, dtype=torch.int32, device="cuda")
+    seen = torch.full((2,), n + 1, dtype=torch.int32, device="cuda")
+    start = c.pool.clone()
+    args = dict(keep=keep, recent=5, sink=2, weights=wd, order=od, seen=seen)
+    with B.KVOps(0) as o:
+        for outputs in (dict(weights_out=w_out, order_out=o_out), {}):
+            c.pool.copy_(start)
+            o.kv_evict(c.handle(B), bad, c.lens, n, **args, **outputs)
+            assert o.kv_ops_sync(check=False) == B.KV_ERR_RANGE
+            assert torch.equal(c.pool.view(torch.int16), want.view(torch.int16))
+            got_w, got_o = (w_out, o_out) if outputs else (wd, od)
+            m = keep if outputs else width
+            assert torch.equal(got_w.cpu(), w2[..., :m]) and torch.equal(got_o.cpu(), o2[..., :m])
