@@ -567,10 +567,11 @@ int32_t kv_req_shrink(kv_table_t *t, int64_t req, int64_t tokens)
     if (tokens < 1 || tokens > r->tokens) return tfail(t, KV_ERR_INVALID_ARG, "a request shrinks to between one token and its present number");
     const TPending seq = now(t);                    // an eager copy of its blocks may still be in flight
     const size_t want = (size_t)blocks_for(t, tokens);
+    // rows have moved: what the host holds is no longer any block's content.  First, so that it holds if memory runs out below
+    for (auto &b : r->blocks) b.host_valid = false;
     try {
         while (r->blocks.size() > want) {           // from the back, so that running out of memory leaves a shorter, whole request
             TBlock &b = r->blocks.back();
-            b.host_valid = false;
             if (b.h >= 0) t->host_free.give(b.h);
             b.h = -1;
             release_gpu(t, b.g, seq);
@@ -581,7 +582,6 @@ int32_t kv_req_shrink(kv_table_t *t, int64_t req, int64_t tokens)
         return tfail(t, KV_ERR_NOMEM, "out of host memory");
     }
     r->tokens = tokens;
-    for (auto &b : r->blocks) b.host_valid = false; // rows moved: what the host holds is no longer the block's content
     return KV_OK;
 }
 

@@ -1,0 +1,107 @@
+"""Host side of the operators on the device cache at its edges, without a GPU: the block table when host memory runs out inside a
+shrink."""
+import os
+import subprocess
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+# The table's source with a pool that does nothing and an operator new that fails on demand: the n-th allocation from now on.
+PROGRAM = r"""
+#include "paper_2601_20309_b200/csrc/kv_table.cu"
+#include <cstdlib>
+
+static long fail_in = -1;
+static int64_t done = 0;             // 1: the pool's transfers have finished
+void *operator new(size_t n)
+{
+    if (fail_in >= 0 && fail_in-- == 0) throw std::bad_alloc();
+    if (void *p = malloc(n)) return p;
+    throw std::bad_alloc();
+}
+void operator delete(void *p) noexcept { free(p); }
+void operator delete(void *p, size_t) noexcept { free(p); }
+
+extern "C" {
+int32_t kv_pool_progress(kv_pool_t *, int64_t *a, int64_t *b, int64_t *c, int64_t *d)
+{
+    if (a) *a = 1;               // a swap-out was issued and has not finished: released blocks are pending ones
+    if (b) *b = done;
+    if (c) *c = 0;
+    if (d) *d = 0;
+    return KV_OK;
+}
+int32_t kv_pool_shape(kv_pool_t *, kv_pool_shape_t *s)
+{
+    s->num_gpu_blocks = 200;
+    s->num_host_blocks = 300;
+    s->block_size = 16;
+    return KV_OK;
+}
+int32_t kv_sync(kv_pool_t *)
+{
+    done = 1;
+    return KV_OK;
+}
+int32_t kv_swap_out(kv_pool_t *, const int32_t *, const int32_t *, int64_t) { return KV_OK; }
+int32_t kv_rotate(kv_pool_t *, const int32_t *, const int32_t *, int64_t, const int32_t *, const int32_t *, int64_t) { return KV_OK; }
+const char *kv_last_error(kv_pool_t *) { return ""; }
+}
+
+static bool check(bool ok, const char *what, long at)
+{
+    if (!ok) printf("%s (allocation %ld)\n", what, at);
+    return ok;
+}
+
+int main()
+{
+    bool ok = true, failed = false;
+    int dummy;
+    for (long at = 0; at < 200; ++at) {
+        kv_table_t *t = nullptr;
+        done = 0;
+        ok &= kv_table_create((kv_pool_t *)&dummy, &t) == KV_OK;
+        // request 1 between others whose host blocks come back, so that its own merge with free ones or stand alone
+        int64_t n = 0;
+        for (int r = 0; r < 5; ++r) {
+            ok &= kv_req_add(t, r, 16 * 20) == KV_OK;
+            ok &= kv_eager_rotate(t, 7, &n) == KV_OK && n == 7;
+        }
+        for (int k = 0; k < 10; ++k) kv_eager_rotate(t, 6, &n);
+        kv_req_finish(t, 0);
+        kv_req_finish(t, 3);
+        kv_table_stats_t before, after;
+        kv_table_get_stats(t, &before);
+        kv_req_info_t info;
+        kv_req_info(t, 1, &info);
+        ok &= check(info.synced_blocks > 5, "the request has copies", at);
+        fail_in = at;
+        const int32_t rc = kv_req_shrink(t, 1, 40);
+        fail_in = -1;
+        kv_req_info(t, 1, &info);
+        kv_table_get_stats(t, &after);
+        ok &= check(info.synced_blocks == 0, "a stale copy counts as valid", at);
+        ok &= check(after.free_gpu_blocks + info.num_blocks == before.free_gpu_blocks + 20, "device blocks are lost", at);
+        if (rc != KV_OK) {
+            failed = true;
+            ok &= check(rc == KV_ERR_NOMEM && info.num_blocks >= 3 && info.tokens >= 40, "not a whole request", at);
+            ok &= check(kv_req_shrink(t, 1, 40) == KV_OK, "a second try", at);
+        }
+        kv_req_info(t, 1, &info);
+        ok &= check(info.tokens == 40 && info.num_blocks == 3 && info.synced_blocks == 0, "shrunk", at);
+        kv_table_destroy(t);
+        if (rc == KV_OK) break;
+    }
+    ok &= check(failed, "an allocation failed", -1);
+    return ok ? 0 : 1;
+}
+"""
+
+
+def test_a_shrink_without_memory_leaves_no_stale_copy(tmp_path):
+    source, exe = tmp_path / "shrink.cpp", tmp_path / "shrink"
+    source.write_text(PROGRAM)
+    built = subprocess.run(["g++", "-O1", "-std=c++17", "-x", "c++", f"-I{ROOT}", "-o", exe, source], capture_output=True, text=True)
+    assert built.returncode == 0, built.stderr
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout
