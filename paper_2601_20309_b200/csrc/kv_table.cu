@@ -81,23 +81,23 @@ class ExtentAllocator {
         }
         return true;
     }
+    // may run out of memory only where the block touches no free extent, and then changes nothing
     void give(int32_t id)
     {
-        int64_t start = id, len = 1;
-        auto nxt = free_.lower_bound(start);
-        if (nxt != free_.end() && nxt->first == start + 1) {              // merge with the extent after
-            len += nxt->second;
-            nxt = free_.erase(nxt);
+        const auto after = free_.lower_bound(id);
+        const bool joins_after = after != free_.end() && after->first == (int64_t)id + 1;
+        const auto before = after == free_.begin() ? free_.end() : std::prev(after);
+        if (before != free_.end() && before->first + before->second == id) {
+            before->second += 1 + (joins_after ? after->second : 0);
+            if (joins_after) free_.erase(after);
+        } else if (joins_after) {
+            auto node = free_.extract(after);
+            node.key() = id;
+            node.mapped()++;
+            free_.insert(std::move(node));
+        } else {
+            free_.emplace_hint(after, id, 1);
         }
-        if (nxt != free_.begin()) {                                       // merge with the extent before
-            auto prv = std::prev(nxt);
-            if (prv->first + prv->second == start) {
-                start = prv->first;
-                len += prv->second;
-                free_.erase(prv);
-            }
-        }
-        free_[start] = len;
         nfree_++;
     }
     int64_t extents() const { return (int64_t)free_.size(); }

@@ -74,6 +74,7 @@ int main()
         kv_table_get_stats(t, &before);
         kv_req_info_t info;
         kv_req_info(t, 1, &info);
+        const int64_t host = info.host_blocks;
         ok &= check(info.synced_blocks > 5, "the request has copies", at);
         fail_in = at;
         const int32_t rc = kv_req_shrink(t, 1, 40);
@@ -82,6 +83,7 @@ int main()
         kv_table_get_stats(t, &after);
         ok &= check(info.synced_blocks == 0, "a stale copy counts as valid", at);
         ok &= check(after.free_gpu_blocks + info.num_blocks == before.free_gpu_blocks + 20, "device blocks are lost", at);
+        ok &= check(after.free_host_blocks + info.host_blocks == before.free_host_blocks + host, "host blocks are lost", at);
         if (rc != KV_OK) {
             failed = true;
             ok &= check(rc == KV_ERR_NOMEM && info.num_blocks >= 3 && info.tokens >= 40, "not a whole request", at);
@@ -89,6 +91,11 @@ int main()
         }
         kv_req_info(t, 1, &info);
         ok &= check(info.tokens == 40 && info.num_blocks == 3 && info.synced_blocks == 0, "shrunk", at);
+        for (int r : {1, 2, 4}) kv_req_finish(t, r);
+        kv_table_get_stats(t, &after);
+        ok &= check(after.free_gpu_blocks == 200 && after.free_host_blocks == 300 && after.free_host_extents == 1, "all blocks are back, in one run", at);
+        // the free host blocks that are counted are there: one request takes them all
+        ok &= check(kv_req_add(t, 9, 16 * 200) == KV_OK && kv_eager_rotate(t, 200, &n) == KV_OK && n == 200, "taken again", at);
         kv_table_destroy(t);
         if (rc == KV_OK) break;
     }
@@ -98,7 +105,7 @@ int main()
 """
 
 
-def test_a_shrink_without_memory_leaves_no_stale_copy(tmp_path):
+def test_a_shrink_without_memory_loses_nothing_and_leaves_no_stale_copy(tmp_path):
     source, exe = tmp_path / "shrink.cpp", tmp_path / "shrink"
     source.write_text(PROGRAM)
     built = subprocess.run(["g++", "-O1", "-std=c++17", "-x", "c++", f"-I{ROOT}", "-o", exe, source], capture_output=True, text=True)
