@@ -556,7 +556,8 @@ int32_t kv_ops_sync(kv_ops_t *ops);
  * cudaMalloc (not possible during stream capture: KV_ERR_NOMEM).  Outgrown workspaces stay allocated until
  * kv_ops_destroy, so graphs captured with them keep working. */
 int32_t kv_ops_reserve(kv_ops_t *ops, int64_t bytes);
-/* Text of the latest error of this context (never NULL); with NULL: of the latest kv_ops_create failure. */
+/* Text of the latest error of this context (never NULL); with NULL: of this thread's
+ * latest kv_ops_create failure. */
 const char *kv_ops_last_error(kv_ops_t *ops);
 /* The pool's device side as a kv_cache_t. */
 int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);

@@ -25,7 +25,7 @@ struct kv_ops {
 
 namespace {
 
-char g_ops_err[256] = "no error";
+thread_local char g_ops_err[256] = "no error";
 
 int32_t fail(kv_ops *o, int32_t code, const char *msg)
 {

@@ -1,7 +1,11 @@
 """Host side of the operators on the device cache at its edges, without a GPU: the block table when host memory runs out inside a
-shrink."""
+shrink, error texts of several threads."""
+import ctypes as C
 import os
 import subprocess
+import threading
+
+from paper_2601_20309_b200 import binding as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -112,3 +116,23 @@ def test_a_shrink_without_memory_loses_nothing_and_leaves_no_stale_copy(tmp_path
     assert built.returncode == 0, built.stderr
     run = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert run.returncode == 0, run.stdout
+
+
+def test_the_error_text_of_a_failed_create_belongs_to_its_thread():
+    """One context per device is often made by one thread per device: what went wrong in one is not told to another."""
+    L = B.lib()
+    texts = {}
+
+    def other():
+        texts["before"] = L.kv_ops_last_error(None)
+        assert L.kv_ops_create(0, None, None) == B.KV_ERR_INVALID_ARG
+        texts["after"] = L.kv_ops_last_error(None)
+
+    handle = C.c_void_p()
+    assert L.kv_ops_create(1 << 20, None, C.byref(handle)) != B.KV_OK and not handle
+    mine = L.kv_ops_last_error(None)
+    t = threading.Thread(target=other)
+    t.start()
+    t.join()
+    assert texts == {"before": b"no error", "after": b"null argument"}
+    assert L.kv_ops_last_error(None) == mine != b"null argument"
