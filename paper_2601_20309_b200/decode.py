@@ -16,8 +16,8 @@ from . import binding as B
 
 
 class Decoder:
-    """Requests in `places` rows of a batch of fixed size; a row without a request on the GPU is idle (length 0).  Weights and ages
-    of the slots are kept per layer and place; block tables and lengths go to the device once per change."""
+    """Requests in `places` rows of a batch of fixed size, of up to max_tokens tokens each; a row without a request on the GPU is idle
+    (length 0).  Weights and ages of the slots are kept per layer and place; block tables and lengths go to the device once per call."""
 
     def __init__(self, num_layers, block_size, q_heads, kv_heads, head_dim, num_gpu_blocks, num_host_blocks, places, max_tokens, *, keep=0,
                  slack=0, recent=0, sink=0, sections=None, theta=10000.0, device=0):
@@ -34,7 +34,7 @@ class Decoder:
         half = head_dim // 2
         self.inv_freq = (theta ** (-torch.arange(half, dtype=torch.float64) / half)).float().to(self.device)
         self.axis_of = [a for a, n in enumerate(sections) for _ in range(n)] if sections else [0] * half
-        self.width = -(-max_tokens // block_size)
+        self.max_tokens, self.width = max_tokens, -(-max_tokens // block_size)
         self.weights = torch.zeros(num_layers, places, kv_heads, max_tokens, device=self.device)
         self.order = torch.zeros(num_layers, places, kv_heads, max_tokens, dtype=torch.int32, device=self.device)
         self.place_of: dict = {}                # request -> row, whether on the GPU or not
@@ -61,42 +61,84 @@ class Decoder:
                 lens[row] = self.held[row]
         return tables.to(self.device), lens.to(self.device)
 
+    def _check(self, qkv, positions, n):
+        """Tensors of n tokens, before anything is booked for them."""
+        t, shape = self.torch, (self.layers, n, self.q_heads + 2 * self.kv_heads, self.dim)
+        if tuple(qkv.shape) != shape or qkv.dtype != t.bfloat16 or qkv.device != self.device:
+            raise ValueError(f"qkv must be bf16 {shape} on {self.device}")
+        if positions.dim() != 2 or positions.shape[0] <= max(self.axis_of) or positions.shape[1] != n or positions.dtype != t.int32 \
+                or positions.device != self.device:
+            raise ValueError(f"positions must be int32 ({max(self.axis_of) + 1} or more, {n}) on {self.device}")
+
     def add(self, req, qkv, positions):
-        """A request with its prompt: qkv [layers, tokens, q_heads + 2 kv_heads, dim], positions int32 [axes, tokens]."""
+        """A request with its prompt: qkv [layers, tokens, q_heads + 2 kv_heads, dim], positions int32 [axes, tokens].  What does not
+        fit (no place, more than max_tokens tokens: ``ValueError``; no blocks: ``KVError``) leaves everything as it was."""
         t, h, k = self.torch, self.q_heads, self.kv_heads
         n = qkv.shape[1]
-        row = next(r for r in range(len(self.held)) if r not in self.place_of.values())
+        self._check(qkv, positions, n)
+        if n > self.max_tokens:
+            raise ValueError(f"a request of {n} tokens, max_tokens is {self.max_tokens}")
+        row = next((r for r in range(len(self.held)) if r not in self.place_of.values()), None)
+        if row is None:
+            raise ValueError(f"all {len(self.held)} places are taken")
         self.table.kv_req_add(req, n)
-        self.pool.kv_stream_wait(self.stream)
-        self.place_of[req], self.held[row], self.seen[row], self.running[row] = row, n, n, True
-        tables, lens = self._upload({row})
-        starts = t.tensor([0, n], dtype=t.int32, device=self.device)
-        numbers = t.arange(n, dtype=t.int32, device=self.device)
-        one = slice(row, row + 1)
-        for layer in range(self.layers):
-            x = qkv[layer]
-            self.ops.kv_append(self.cache, layer, None, x[:, h:h + k], x[:, h + k:], tables[one], lens[one], positions=positions, inv_freq=self.inv_freq,
-                               axis_of=self.axis_of, seq_starts=starts, weights=self.weights[layer, one], order=self.order[layer, one],
-                               token_order=numbers)
+        try:
+            self.pool.kv_stream_wait(self.stream)
+            self.place_of[req], self.held[row], self.seen[row], self.running[row] = row, n, n, True
+            tables, lens = self._upload({row})
+            starts = t.tensor([0, n], dtype=t.int32, device=self.device)
+            numbers = t.arange(n, dtype=t.int32, device=self.device)
+            one = slice(row, row + 1)
+            for layer in range(self.layers):
+                x = qkv[layer]
+                self.ops.kv_append(self.cache, layer, None, x[:, h:h + k], x[:, h + k:], tables[one], lens[one], positions=positions,
+                                   inv_freq=self.inv_freq, axis_of=self.axis_of, seq_starts=starts, weights=self.weights[layer, one],
+                                   order=self.order[layer, one], token_order=numbers)
+        except BaseException:
+            self.ops.kv_ops_sync(check=False)   # kernels of earlier layers may still write the blocks that go back
+            self.table.kv_req_finish(req, check=False)
+            self.place_of.pop(req, None)
+            self.held[row], self.seen[row], self.running[row] = 0, 0, False
+            raise
 
     def step(self, qkv, positions):
         """One token for every running row: qkv [layers, places, q_heads + 2 kv_heads, dim], positions int32 [axes, places].
-        Returns the attention's outputs [layers, places, q_heads, dim] (idle rows: zeros)."""
+        Returns the attention's outputs [layers, places, q_heads, dim] (idle rows: zeros), in a buffer that the next step overwrites.
+        A step that a running row has no room for (it holds max_tokens: ``ValueError``), or that there are not enough blocks for
+        (``KVError`` with KV_ERR_NOMEM: preempt something and repeat it), changes nothing."""
         t, h, k = self.torch, self.q_heads, self.kv_heads
-        for req, row in self.place_of.items():
-            if self.running[row]:
+        self._check(qkv, positions, len(self.held))
+        rows = [(req, row) for req, row in self.place_of.items() if self.running[row]]
+        for req, row in rows:
+            if self.held[row] >= self.max_tokens:
+                raise ValueError(f"request {req} holds max_tokens = {self.max_tokens} tokens")
+        need, free = sum(self.held[row] % self.bs == 0 for _, row in rows), self.table.kv_table_get_stats()["free_gpu_blocks"]
+        if need > free:
+            raise B.KVError(B.KV_ERR_NOMEM, f"the step needs {need} blocks, {free} are free")
+        done = []
+        try:
+            for req, row in rows:
                 self.table.kv_req_append(req, 1)
+                done.append((req, row))
                 self.held[row] += 1
                 self.seen[row] += 1
-        tables, lens = self._upload()
-        numbers = t.tensor([max(0, s - 1) for s in self.seen], dtype=t.int32, device=self.device)
-        longest = max(self.held)
-        for layer in range(self.layers):
-            x = qkv[layer]
-            self.ops.kv_append(self.cache, layer, x[:, :h], x[:, h:h + k], x[:, h + k:], tables, lens, positions=positions, inv_freq=self.inv_freq,
-                               axis_of=self.axis_of, q_out=self.turned, weights=self.weights[layer], order=self.order[layer], token_order=numbers)
-            self.ops.kv_attend(self.cache, layer, self.turned, tables, lens, longest, out=self.out[layer], weights_in=self.weights[layer],
-                               weights_out=self.weights[layer])
+            tables, lens = self._upload()
+            numbers = t.tensor([max(0, s - 1) for s in self.seen], dtype=t.int32, device=self.device)
+            longest = max(self.held)
+            for layer in range(self.layers):
+                x = qkv[layer]
+                self.ops.kv_append(self.cache, layer, x[:, :h], x[:, h:h + k], x[:, h + k:], tables, lens, positions=positions,
+                                   inv_freq=self.inv_freq, axis_of=self.axis_of, q_out=self.turned, weights=self.weights[layer],
+                                   order=self.order[layer], token_order=numbers)
+                self.ops.kv_attend(self.cache, layer, self.turned, tables, lens, longest, out=self.out[layer], weights_in=self.weights[layer],
+                                   weights_out=self.weights[layer])
+        except BaseException:               # no row keeps a token that was not written in every layer
+            self.ops.kv_ops_sync(check=False)
+            for req, row in done:
+                self.held[row] -= 1
+                self.seen[row] -= 1
+                self.table.kv_req_shrink(req, self.held[row], check=False)
+            raise
         full = {row for row in range(len(self.held)) if self.running[row] and self.keep and self.held[row] >= self.keep + self.slack}
         if full:
             self._evict(full)
