@@ -10,6 +10,7 @@
 from __future__ import annotations
 
 import argparse
+import contextlib
 import sys
 
 from . import binding as B
@@ -17,7 +18,8 @@ from . import binding as B
 
 class Decoder:
     """Requests in `places` rows of a batch of fixed size, of up to max_tokens tokens each; a row without a request on the GPU is idle
-    (length 0).  Weights and ages of the slots are kept per layer and place; block tables and lengths go to the device once per call."""
+    (length 0).  Weights and ages of the slots are kept per layer and place; block tables and lengths go to the device once per call.
+    Kernels and copies run on the stream that is current when the decoder is made, in order with the stream a method is called under."""
 
     def __init__(self, num_layers, block_size, q_heads, kv_heads, head_dim, num_gpu_blocks, num_host_blocks, places, max_tokens, *, keep=0,
                  slack=0, recent=0, sink=0, sections=None, theta=10000.0, device=0):
@@ -28,7 +30,8 @@ class Decoder:
         self.store = torch.zeros(num_layers, 2, num_gpu_blocks, block_size, kv_heads, head_dim, dtype=torch.bfloat16, device=self.device)
         self.pool = B.KVPool(num_layers, block_size, kv_heads, head_dim, num_gpu_blocks, num_host_blocks, self.store.data_ptr(), device_id=device)
         self.table = B.KVTable(self.pool)
-        self.stream = torch.cuda.current_stream(self.device).cuda_stream
+        self.own = torch.cuda.current_stream(self.device)
+        self.stream = self.own.cuda_stream
         self.ops = B.KVOps(device, self.stream)
         self.cache = self.pool.kv_pool_cache("bf16")
         half = head_dim // 2
@@ -49,6 +52,21 @@ class Decoder:
         self.ops.destroy()
         self.table.destroy()
         self.pool.destroy()
+
+    @contextlib.contextmanager
+    def _on_own_stream(self):
+        """All work of a call goes to the stream the decoder was made on: after what the caller's current stream holds so far (the
+        call's inputs), and before what comes next there (who reads the results or gives the inputs' memory to something else)."""
+        caller = self.torch.cuda.current_stream(self.device)
+        if caller == self.own:
+            yield
+            return
+        self.own.wait_stream(caller)
+        try:
+            with self.torch.cuda.stream(self.own):
+                yield
+        finally:
+            caller.wait_stream(self.own)
 
     def _upload(self, rows=None):
         """Block tables and lengths of the given rows (others count as idle)."""
@@ -83,17 +101,18 @@ class Decoder:
             raise ValueError(f"all {len(self.held)} places are taken")
         self.table.kv_req_add(req, n)
         try:
-            self.pool.kv_stream_wait(self.stream)
-            self.place_of[req], self.held[row], self.seen[row], self.running[row] = row, n, n, True
-            tables, lens = self._upload({row})
-            starts = t.tensor([0, n], dtype=t.int32, device=self.device)
-            numbers = t.arange(n, dtype=t.int32, device=self.device)
-            one = slice(row, row + 1)
-            for layer in range(self.layers):
-                x = qkv[layer]
-                self.ops.kv_append(self.cache, layer, None, x[:, h:h + k], x[:, h + k:], tables[one], lens[one], positions=positions,
-                                   inv_freq=self.inv_freq, axis_of=self.axis_of, seq_starts=starts, weights=self.weights[layer, one],
-                                   order=self.order[layer, one], token_order=numbers)
+            with self._on_own_stream():
+                self.pool.kv_stream_wait(self.stream)
+                self.place_of[req], self.held[row], self.seen[row], self.running[row] = row, n, n, True
+                tables, lens = self._upload({row})
+                starts = t.tensor([0, n], dtype=t.int32, device=self.device)
+                numbers = t.arange(n, dtype=t.int32, device=self.device)
+                one = slice(row, row + 1)
+                for layer in range(self.layers):
+                    x = qkv[layer]
+                    self.ops.kv_append(self.cache, layer, None, x[:, h:h + k], x[:, h + k:], tables[one], lens[one], positions=positions,
+                                       inv_freq=self.inv_freq, axis_of=self.axis_of, seq_starts=starts, weights=self.weights[layer, one],
+                                       order=self.order[layer, one], token_order=numbers)
         except BaseException:
             self.ops.kv_ops_sync(check=False)   # kernels of earlier layers may still write the blocks that go back
             self.table.kv_req_finish(req, check=False)
@@ -122,16 +141,17 @@ class Decoder:
                 done.append((req, row))
                 self.held[row] += 1
                 self.seen[row] += 1
-            tables, lens = self._upload()
-            numbers = t.tensor([max(0, s - 1) for s in self.seen], dtype=t.int32, device=self.device)
-            longest = max(self.held)
-            for layer in range(self.layers):
-                x = qkv[layer]
-                self.ops.kv_append(self.cache, layer, x[:, :h], x[:, h:h + k], x[:, h + k:], tables, lens, positions=positions,
-                                   inv_freq=self.inv_freq, axis_of=self.axis_of, q_out=self.turned, weights=self.weights[layer],
-                                   order=self.order[layer], token_order=numbers)
-                self.ops.kv_attend(self.cache, layer, self.turned, tables, lens, longest, out=self.out[layer], weights_in=self.weights[layer],
-                                   weights_out=self.weights[layer])
+            with self._on_own_stream():
+                tables, lens = self._upload()
+                numbers = t.tensor([max(0, s - 1) for s in self.seen], dtype=t.int32, device=self.device)
+                longest = max(self.held)
+                for layer in range(self.layers):
+                    x = qkv[layer]
+                    self.ops.kv_append(self.cache, layer, x[:, :h], x[:, h:h + k], x[:, h + k:], tables, lens, positions=positions,
+                                       inv_freq=self.inv_freq, axis_of=self.axis_of, q_out=self.turned, weights=self.weights[layer],
+                                       order=self.order[layer], token_order=numbers)
+                    self.ops.kv_attend(self.cache, layer, self.turned, tables, lens, longest, out=self.out[layer],
+                                       weights_in=self.weights[layer], weights_out=self.weights[layer])
         except BaseException:               # no row keeps a token that was not written in every layer
             self.ops.kv_ops_sync(check=False)
             for req, row in done:
@@ -141,7 +161,8 @@ class Decoder:
             raise
         full = {row for row in range(len(self.held)) if self.running[row] and self.keep and self.held[row] >= self.keep + self.slack}
         if full:
-            self._evict(full)
+            with self._on_own_stream():
+                self._evict(full)
         return self.out
 
     def _evict(self, rows):

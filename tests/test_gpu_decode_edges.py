@@ -121,3 +121,43 @@ def test_a_request_that_does_not_fit_is_not_added():
         assert same(before, state(d))
     finally:
         d.close()
+
+
+@pytest.mark.parametrize("busy", ["caller", "own"])
+def test_calls_under_another_stream(busy):
+    """Made on one stream, fed and read under another, with one of the two a few milliseconds behind: what the caller made is there
+    before the kernels read it, tables and lengths are there and stay, results are there when the caller's stream goes on."""
+    s, own = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(own):
+        d, m, g = make(24, 3, 64, {1: 30, 2: 7}, 4, keep=32, slack=4, recent=4, sink=2)
+    m.keep, m.slack, m.recent, m.sink = 32, 4, 4, 2
+    torch.cuda.synchronize()
+    try:
+        for step in range(8):
+            x, pos = token(g, 3)
+            with torch.cuda.stream(s if busy == "caller" else own):
+                torch.cuda._sleep(10_000_000)
+            with torch.cuda.stream(s):
+                xd, pd = x.cuda(), pos.cuda()
+                got = d.step(xd, pd).clone()
+                del xd, pd
+                torch.full((1 << 20,), 0x7FFFFFFF, dtype=torch.int32, device="cuda")       # takes what the allocator has back
+            s.synchronize()
+            compare(d, m, got.double().cpu(), x, pos)
+            for req in [r for r, row in d.place_of.items() if len(m.w[(0, r, 0)]) >= 36]:
+                m.evict(req)
+            assert all(d.held[row] == len(m.w[(0, req, 0)]) for req, row in d.place_of.items())
+        with torch.cuda.stream(s):
+            x, pos = torch.randn(LAYERS, 20, HQ + 2 * HK, DIM, generator=g).to(torch.bfloat16), torch.randint(0, 50, (3, 20), generator=g, dtype=torch.int32)
+            d.add(5, x.cuda(), pos.cuda())
+        for layer in range(LAYERS):
+            m.append(5, layer, x[layer], pos)
+        m.seen[5] = 20
+        with torch.cuda.stream(s):
+            d.rotate([1], [])
+            x, pos = token(g, 3)
+            got = d.step(x.cuda(), pos.cuda()).clone()
+        s.synchronize()
+        compare(d, m, got.double().cpu(), x, pos, away=[1])
+    finally:
+        d.close()
