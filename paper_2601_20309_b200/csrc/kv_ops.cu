@@ -180,7 +180,8 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
-    if (longest * a->num_seqs * k.head_chunks * k.group_chunks > INT32_MAX)
+    // the kernels round the number of steps up to their numbers of CTAs in 32 bits
+    if (longest * a->num_seqs * k.head_chunks * k.group_chunks > INT32_MAX - KV_JOIN_SHARES * o->sms)
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;

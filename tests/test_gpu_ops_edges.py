@@ -292,3 +292,15 @@ def test_evict_drops_exactly_the_pairs_of_a_bad_block(n, keep, quads, layout):
             got_w, got_o = (w_out, o_out) if outputs else (wd, od)
             m = keep if outputs else width
             assert torch.equal(got_w.cpu(), w2[..., :m]) and torch.equal(got_o.cpu(), o2[..., :m])
+
+
+# ---- sizes at the limit of 32 bits ----------------------------------------------------------------------------------
+
+
+def test_a_call_whose_steps_do_not_round_up_within_32_bits_is_refused(ops):
+    """42966 sequences of 49981 steps (128 slots each, one KV head) are 2^31 - 2 steps: rounded up to whole pieces they would wrap."""
+    cache = B.KVCache(1 << 20, 1, 1 << 14, 1, 64, 1 << 20)
+    with pytest.raises(B.KVError) as e:
+        ops.kv_attend_workspace(cache, 42966, 1, 49981 * 128 - 15, weights=False)
+    assert e.value.code == B.KV_ERR_UNSUPPORTED
+    assert ops.kv_attend_workspace(cache, 42966, 1, 49970 * 128 - 15, weights=False) > 0
