@@ -523,6 +523,9 @@ int32_t kv_table_fail_pool_call(kv_table_t *table, int64_t after_calls, int32_t 
  *     copied to or from the host, nothing is allocated except the context's workspace (see kv_ops_reserve).
  *   - Every call runs on the context's device and stream whatever device is current, asynchronously, and may be
  *     captured into a CUDA graph (reserve the workspace first).  A call without sequences, tokens or layers is a no-op.
+ *   - A context has one workspace.  Its calls, and the graphs captured from them, must run one after the other: a graph
+ *     replayed on another stream beside a call or a graph of the same context would share it.  What runs at the same
+ *     time needs a context each.
  *   - The context knows nothing of the pool's transfers: order the stream after swap-ins with kv_stream_wait,
  *     and finish the stream (kv_ops_sync) before blocks it still reads or writes are rotated out, released
  *     (kv_req_shrink, kv_req_preempt, kv_req_finish) or handed to another stream.
@@ -567,6 +570,8 @@ int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
  * over the slots t in [max(0, lens[i] - window), lens[i]) (window 0: all):
  *     s_t = scale * q . K_t,  p_t = exp(s_t) / sum exp(s),  out = sum p_t V_t,  lse = log sum exp(s)
  *     weights_out[i][h][t] = weights_in[i][h][t] + sum over h's query heads of p_t      (t < lens[i])
+ * The window counts slots.  These are the newest tokens as long as slots are in the tokens' order; kv_evict moves new tokens to
+ * low slots, so a request that has been evicted from is read without a window.
  * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing, whatever V holds.  Else every
  * slot counts, one of weight 0 too: an infinite or NaN element of its V makes that element of out infinite or NaN.
  */
@@ -636,7 +641,7 @@ int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t
  * seen[i] - recent: the newest, or order[s] < sink: the first), then those with the largest weights; equals go to
  * the lower slot, NaN counts less than any number.  Kept slots at or above `keep` move, in ascending order, into the
  * evicted slots below it, also ascending; the others stay where they are.  (Attention does not mind the order of
- * the slots, so nothing else needs to move.)  K and V rows move in place; weights and ages of the kept slots go to
+ * the slots, so nothing else needs to move; a window of kv_attend does, and must not be used afterwards.)  K and V rows move in place; weights and ages of the kept slots go to
  * weights_out / order_out, or move in place.  Rows from `keep` on stay as they were.  New lengths: min(lens[i], keep).
  * The blocks from ceil(keep/block_size) on are no longer used; kv_req_shrink tells the block table.  Sequences that are
  * evicted in one call must not share blocks.

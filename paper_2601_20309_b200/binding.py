@@ -636,7 +636,8 @@ class KVCache:
 
 
 class KVOps:
-    """Operators on the device cache, on one stream (a ``cudaStream_t`` as an int; None or 0 = the default stream).  Arrays are
+    """Operators on the device cache, on one stream (a ``cudaStream_t`` as an int; None or 0 = the default stream), with one workspace:
+    what runs at the same time, graphs captured from the calls included, needs an object each.  Arrays are
     CUDA tensors; rows may lie at any stride, the elements of a row side by side.  Wrong types, shapes and devices, and tensors
     that require gradients while those are recorded, raise ``ValueError``; the C status comes back, or raises ``KVError`` with
     ``check``.  Tensors of another stream have to be ordered by the caller, and kept until this stream is done with them."""
@@ -686,7 +687,8 @@ class KVOps:
     def kv_attend(self, cache: KVCache, layer: int, q, block_tables, lens, max_len: int, *, out, lse=None, window: int = 0,
                   scale: float = 0.0, weights_in=None, weights_out=None, check: bool = True) -> int:
         """q, out [seqs, q_heads, dim]; block_tables int32 [seqs, width]; lens int32 [seqs] (with the new token); max_len: a
-        bound of lens known on the host; lse float32 [seqs, q_heads]; weights float32 [seqs, kv_heads, >= max_len]."""
+        bound of lens known on the host; window: so many slots at the end, 0 = all (not after ``kv_evict``, which moves new tokens to
+        low slots); lse float32 [seqs, q_heads]; weights float32 [seqs, kv_heads, >= max_len]."""
         return self._ret(self._ext_attend(self._address, self.device_id, cache.address, layer, q, block_tables, lens, max_len, out,
                                           lse, window, scale, weights_in, weights_out), check)
 
