@@ -17,10 +17,10 @@
 // several ways share.  With eight KV heads the warps of a CTA read whole rows of the cache, 2 KiB each, side by side.
 //
 // Measured (B200, 148 SMs): 32 sequences around 2k up to 16k slots, 64 query and 8 KV heads of 128, 424 MB: 58 us from the first
-// tile to the median CTA's last, 7.3 TB/s; the whole call 80 us (5.3 TB/s, 81 % of the floor): 4 us until loads are under way,
+// tile to the median CTA's last, 7.3 TB/s; the whole call 81 us (5.2 TB/s, 80 % of the floor): 4 us until loads are under way,
 // 6 between the median and the slowest SM, 8 for the second kernel.  64 sequences around 1k up to 8k with weights, 415 MB:
-// 89 us.  What was counted on the way there: 730 instructions per tile and warp at 4.4 cycles each kept it at 88 us; one
-// address per tile instead of one per row, xor addressing and two score chains brought that to 460.
+// 90 us.  What was counted on the way there: 730 instructions per tile and warp at 4.4 cycles each kept it at 88 us; one
+// address per tile instead of one per row, xor addressing and two score chains brought that to 460 (the compensated sum adds 17).
 //
 // Mathematics of a tile, on mma.m16n8k16 with the cache as the left operand, so that the few query heads fill the narrow
 // side:  S^T[16 slots, 8 heads] = K Q^T;  m, p = exp2(S - m), l in float32 (scale and log2 e are applied to the sums);
@@ -598,6 +598,7 @@ __global__ void __launch_bounds__(KV_ATTEND_WARPS * 32 / (DP == 256 ? 2 : 1), DP
 // its output, in units of 32 elements of a head, among them.  What such a kernel takes is the number of loads that
 // wait for one another, each close to a microsecond, times the waves of CTAs: there are three in a chain (what, the row's
 // sums, the data), every load that can be in flight together is, and four CTAs per SM are all there are.
+// With 2 / 3 / 4 shares 64 sequences take 91.4 / 90.0 / 89.3 us, one of 131072 slots 27.8 / 27.8 / 29.3.
 constexpr int KV_JOIN_THREADS = 256, KV_JOIN_WARPS = KV_JOIN_THREADS / 32, KV_JOIN_SHARES = 3, KV_MAX_GROUP = 256;
 
 // maximum and sum of two sets of slots together

@@ -137,11 +137,15 @@ struct AttendPlan {
 
 constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, less the kernel's static share
 // Rows of up to this many steps are never split.  A step of one warp takes about 0.9 us, the second kernel 4 to 7 (the more
-// with weights to add up): 4 sequences of 500 slots with weights 13.5 us whole, 17.6 split; 1 of 900 without 14.7 whole, 12.1 split
+// with weights to add up): 4 sequences of 500 slots with weights 13.5 us whole, 17.6 split; 1 of 900 without 14.7 whole, 12.1 split.
+// Near the limit with weights few whole rows lose already: of 900 slots one takes 21.6 us whole and 16.7 split, 16 take 26.8 and 29.1
 constexpr int ATTEND_ALONE_STEPS = 4, ATTEND_ALONE_STEPS_WEIGHTS = 8;
 // No piece is shorter: with 1 step one sequence of 2000 slots takes 22.5 us, with 2 18.8, with 4 18.8; seven windows of 333 12.8, 14.9, 17.9
 constexpr int ATTEND_MIN_STEPS = 2;
-constexpr int ATTEND_ROW_CTAS = 1;                   // of the join, per piece, beside those that add up weights
+// CTAs of the join per piece that put rows together.  With weights there are KV_JOIN_SHARES others beside them: 64 sequences 90.6 us
+// with 1, 90.2 with 2, 90.0 with 4; one of 131072 slots 27.8, 28.0, 29.0.  Without: 32 sequences of the 70B shape 86.0, 82.8, 81.2
+// (8: 84.5); 64 sequences 80.0, 78.6, 78.1 (82.2); one of 131072 slots 25.0, 25.3, 25.3 (27.0)
+constexpr int ATTEND_ROW_CTAS_WEIGHTS = 1, ATTEND_ROW_CTAS = 4;
 
 int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, KvAttend &k, AttendPlan &p)
 {
@@ -155,10 +159,15 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     if (a->max_len < 0 || a->max_len > INT32_MAX / 2) return fail(o, KV_ERR_INVALID_ARG, "bad max_len");
     k.group = a->q_heads / c->kv_heads;
     p.dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    // One tile of 8 query heads or two at once; more than 16 walk the cache again for each 16.  32 sequences around 8k slots, 2 KV
+    // heads, 377 MB: groups of 8 72 us with one tile and 81 with two, 9 123 and 82, 16 124 and 84; 17 to 32 147, 64 268 us
+    // (with weights 8 86, 16 110, 32 235, 64 598)
     p.nt = k.group <= 8 ? 1 : 2;
     const int most = p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
     // KV heads per CTA: as many as there are warps, so that a CTA reads whole rows of the cache.  Short rows that no CTA
-    // shares (no second kernel) rather go one head to a CTA while there are SMs for it, with more warps along the row.
+    // shares (no second kernel) rather go one head to a CTA while there are SMs for it, with more warps along the row: 1 (16)
+    // sequences of 37 slots and 8 KV heads 6.9 (7.2) us, all heads in one CTA 10.6 (10.8); of 130 8.9 (9.3) against 12.3 (15.5); of 16,
+    // where one step is all there is, 6.9 (7.2) against 6.7 (6.8).
     auto shape = [&](int heads_wanted) {
         k.hc = 1;
         for (int d = 2; d <= heads_wanted; ++d)
@@ -185,6 +194,8 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
+    // one address per tile where a block holds whole tiles, else one per row: 70B shape 80.4 against 89.2 us, 64 sequences with
+    // weights 90.3 against 100.5, one of 131072 slots 27.9 against 28.9
     k.whole_tiles = c->block_size % 16 == 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
@@ -337,7 +348,7 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
         early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         early.val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t cfg = {};
-        const int row_ctas = k.scores ? ATTEND_ROW_CTAS : 4;
+        const int row_ctas = k.scores ? ATTEND_ROW_CTAS_WEIGHTS : ATTEND_ROW_CTAS;
         cfg.gridDim = dim3(k.pieces * (row_ctas + (k.scores ? KV_JOIN_SHARES : 0)));
         cfg.dynamicSmemBytes = std::max((size_t)kv_join_floats(k.hc, 8 * p.nt, k.pieces), (size_t)k.hc * k.group) * 4;
         cfg.blockDim = dim3(KV_JOIN_THREADS);
@@ -403,7 +414,8 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     memcpy(k.axis_of, a->axis_of, sizeof(k.axis_of));
     k.num_tokens = a->num_tokens;
     // 16 bytes at a time where every row begins on 16 bytes and the pairs that turn together are whole packs of eight, 8 bytes
-    // likewise (a rotation of 40 of 80 elements turns halves of 20), else element by element
+    // likewise (a rotation of 40 of 80 elements turns halves of 20), else element by element: 14.3k prompt tokens 65, 80 and 204 us,
+    // 64 tokens of a decode step 4.9, 5.6 and 10.0
     const int turning = a->pair_style ? a->rotary_dim : a->rotary_dim / 2;
     const auto packs = [&](int64_t v) {
         const auto fits = [v](const void *q, int64_t x, int64_t y) { return (uintptr_t)q % (2 * v) == 0 && x % v == 0 && y % v == 0; };
@@ -416,6 +428,8 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     // a row number below 2^32 / rows is divided by rows exactly with the reciprocal
     const int64_t rows = (int64_t)(a->q ? a->q_heads : 0) + 2 * cache->kv_heads;
     if (rows > 4096) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
+    // tokens per CTA: up to eight CTAs per SM, then more tokens.  With 4 / 8 / 16 CTAs per SM 2000 tokens of 32 + 8 + 8 heads take
+    // 12.2 / 14.1 / 17.9 us, 3500 18.9 / 20.1 / 21.3, 6900 36.5 / 35.2 / 36.0, 14.3k 67.1 / 65.0 / 63.5; up to 500 all the same
     k.per = (int)std::min<int64_t>(AP_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
     k.by_rows = (unsigned)ceil_div(int64_t(1) << 32, rows);
     const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
@@ -439,7 +453,9 @@ struct EvictPlan {
     bool regs, fused;
 };
 
-constexpr int EVICT_SHORT = 1024;               // up to here kv_evict_small has the lowest latency
+// Up to here kv_evict_small has the lowest latency.  16 problems with four warps each / 256 threads / 1024: of 300 slots 9.1 / 15.3 /
+// 19.1 us (its rows in the same kernel), 600 15.3 / 15.8 / 19.1, 1000 15.2 / 15.9 / 19.1, 2000 17.6 / 17.1 / 19.7, 4000 21.9 / 19.5 / 20.9
+constexpr int EVICT_SHORT = 1024;
 
 int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvEvict &k, EvictPlan &p)
 {
@@ -454,14 +470,20 @@ int32_t plan_evict(kv_ops *o, const kv_cache_t *c, const kv_evict_args_t *a, KvE
     p.problems = (int64_t)a->num_layers * a->num_seqs * c->kv_heads;
     if (p.problems * EV_CLUSTER > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "too many (layer, sequence, head) problems in one call");
     p.cap = std::max<int64_t>(0, std::min<int64_t>(a->keep, a->max_len - a->keep));
-    // Four warps per problem where problems are short, or enough of them to fill the GPU.  Else 256 threads hold 4096 keys and
-    // 1024 threads 16384; a cluster of eight such CTAs holds 131072, and beyond that the keys are read again in every round
+    // Four warps per problem where problems are short, or enough of them to fill the GPU: of 2304 slots 64 take 18.8 us so and 17.5 with
+    // 256 threads, 256 28.9 / 27.6, 512 42.9 / 44.9, 592 45.7 / 47.4, 2048 110 / 132; of 8000 slots 64 take 52.6 and 40.6 with 1024
+    // threads, 256 111 / 111, 592 200 / 221, 1024 270 / 302.  Else 256 threads hold 4096 keys and 1024 threads 16384 (16 problems of 4000
+    // slots 19.5 us with 256 and 20.9 with 1024, 256 of them 54.5 / 64.4).  A cluster of eight such CTAs holds 131072, and beyond that the
+    // keys are read again in every round: one problem of 40000 slots 79 us in one CTA that reads again, 66 in two, 32 in four that
+    // hold them; of 131072 247, 165, 98, and 45 in eight; of 140000 86 in eight that read again
     p.threads = a->max_len <= EVICT_SHORT || (a->max_len <= EV_SMALL_SLOTS && p.problems >= 4 * o->sms) ? EV_SMALL_THREADS
                 : a->max_len <= 256 * EV_KEYS                                                       ? 256
                                                                                                       : 1024;
     p.cluster = 1;
     while (p.threads == 1024 && p.cluster < EV_CLUSTER && (int64_t)p.cluster * p.threads * EV_KEYS < a->max_len) p.cluster *= 2;
     p.regs = a->max_len <= (int64_t)p.cluster * p.threads * EV_KEYS;
+    // Rows in the same kernel, or in a second one: 16 problems of 500 slots and 40 rows 11.3 / 16.2 us, 100 rows 11.5 / 14.9, 200 14.9 / 15.0,
+    // 400 18.6 / 14.9; 2048 problems of 2048 slots and 64 rows 54.9 / 61.4, 256 101 / 110.  The limit keeps the lists at 512 bytes per CTA
     p.fused = p.threads == EV_SMALL_THREADS && p.cap <= EV_FUSED_ROWS;
     p.count = 0;
     p.holes = align256(p.problems * 4);
@@ -527,7 +549,8 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
     k.problems = (int)p.problems;
     k.fused = p.fused;
     const auto quad = [](const void *q, int64_t x, int64_t y, int64_t z) { return (uintptr_t)q % 16 == 0 && x % 4 == 0 && y % 4 == 0 && z % 4 == 0; };
-    // a quad that begins below the length must end inside its row: the last row of the array has max_len entries at least
+    // a quad that begins below the length must end inside its row: the last row of the array has max_len entries at least.  2048 problems
+    // of 2304 slots 109.8 us by quads, 111.0 one by one
     k.quads = a->max_len % 4 == 0 && quad(k.w, k.m_layer, k.m_seq, k.m_head) && quad(k.order, 0, 0, 0) && quad(k.w_out, k.o_layer, k.o_seq, k.o_head) &&
               quad(k.order_out, 0, 0, 0);
     const int units = cache->head_dim / 4;
