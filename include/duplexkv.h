@@ -641,8 +641,9 @@ int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t
  * seen[i] - recent: the newest, or order[s] < sink: the first), then those with the largest weights; equals go to
  * the lower slot, NaN counts less than any number.  Kept slots at or above `keep` move, in ascending order, into the
  * evicted slots below it, also ascending; the others stay where they are.  (Attention does not mind the order of
- * the slots, so nothing else needs to move; a window of kv_attend does, and must not be used afterwards.)  K and V rows move in place; weights and ages of the kept slots go to
- * weights_out / order_out, or move in place.  Rows from `keep` on stay as they were.  New lengths: min(lens[i], keep).
+ * the slots, so nothing else needs to move; a window of kv_attend does, and must not be used afterwards.)  K and V
+ * rows move in place; weights and ages of the kept slots go to weights_out / order_out, or move in place.  Rows from
+ * `keep` on stay as they were.  New lengths: min(lens[i], keep).
  * The blocks from ceil(keep/block_size) on are no longer used; kv_req_shrink tells the block table.  Sequences that are
  * evicted in one call must not share blocks.
  */

@@ -25,10 +25,10 @@
 // Mathematics of a tile, on mma.m16n8k16 with the cache as the left operand, so that the few query heads fill the narrow
 // side:  S^T[16 slots, 8 heads] = K Q^T;  m, p = exp2(S - m), l in float32 (scale and log2 e are applied to the sums);
 // O^T[dim, 8 heads] = alpha O^T + V^T P^T, V^T by transposing ldmatrix, P^T by movmatrix from the score fragment.  P is
-// rounded to the cache's type (f16: times 2^14, taken back at the end), the only rounding besides the output's: it is what lets the second product run on
-// the tensor pipe at the cache's width, and its error averages out over the slots below the output's own.  l sums the
-// unrounded p, with compensation, since in a long row the small ones would vanish beside one large.  (tcgen05 would take the cache
-// as its left operand just the same, 128 slots at a time, but a decode step has no use for its rate: the tensor pipe is 8 %
+// rounded to the cache's type (f16: times 2^14, taken back at the end), the only rounding besides the output's: it lets the
+// second product run on the tensor pipe at the cache's width, and over many slots its error averages out below the output's
+// own.  l sums the unrounded p, with compensation, since in a long row the small ones would vanish beside one large.  (tcgen05
+// would take the cache as its left operand just the same, 128 slots at a time, but a decode step has no use for its rate: the tensor pipe is 8 %
 // busy as it is, and the running maximum would have to travel between tensor memory and registers for every tile.)
 // Masked slots (beyond the length, before the window, in a bad block) are never loaded: their K and V are zero-filled, so
 // whatever the block holds there cannot reach a sum, and their score is -inf.
