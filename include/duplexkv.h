@@ -510,13 +510,25 @@ int32_t kv_table_fail_pool_call(kv_table_t *table, int64_t after_calls, int32_t 
  * sits beside a model runner that has these; they are operators of this library.)
  *
  *   kv_append   writes new tokens into the cache: rotary positions (several axes) on q and k, then k and v
- *               into their slots
+ *               into their slots; kv_append_normed with norms of q and k per head in front of that
  *   kv_attend   attention of one new token per sequence over its cache, with the slots' attention weights
  *               added up on request
  *   kv_evict    keeps the slots with the largest added-up weights and frees the rest of the cache
+ *   kv_read     copies rows of the cache out, side by side and in 16 bits
  *
  * Slot s of a sequence lies in row s % block_size of device block table[s / block_size], for every layer, K
  * and V plane and KV head.  Elements are bf16 or f16; sums, softmax statistics and weights are float32.
+ *
+ * The cache may be held in 4 bits (KV_DT_BF16_Q4, KV_DT_F16_Q4: q, k, v and the outputs are bf16 or f16).  Heads are padded to
+ * 64, 128 or 256 elements, which are G = 2, 4 or 8 groups of 32.  Each group of a row has a lowest value lo and a step s, and
+ * an element is lo + s * code, code = 0 .. 15:
+ *     lo = min, s = max((max - min) / 15, |lo| 2^-20) rounded to bf16, code = min(floor((x - lo) / s + 1/2), 15)   (0 where s is 0),
+ * with the differences, the quotient by 15 and the maximum in float32 and the code exact; K is what the 16-bit cache would hold,
+ * rounded to its type.  A group with an element that is not finite, or whose range is not, reads as NaN.  A row of one plane and
+ * head is 20 G bytes (80 instead of 256 for heads of 128), so a pool for it is made with head_dim = kv_cache_row_units(...) and moves
+ * its blocks as any other.  A plane of a block is, for each head, block_size rows of 16 G bytes of codes, then block_size
+ * rows of G 32-bit words: lo in the lower half, s in the upper.  K's code word a G + g (a < 4) of a row has elements
+ * 32 g + 8 a + (0 .. 7) of the head, V's half word i G + g (i < 8) elements 32 g + 4 i + (0 .. 3), lowest bits first.
  *
  * Conventions
  *   - All array arguments are DEVICE pointers unless a comment says HOST; strides count elements.  Nothing is
@@ -538,6 +550,8 @@ typedef struct kv_ops kv_ops_t;     /* operator context of one stream; opaque, o
 
 #define KV_DT_BF16 0
 #define KV_DT_F16  1
+#define KV_DT_BF16_Q4 2             /* 4-bit cache; q, k, v, outputs and lowest values bf16                    */
+#define KV_DT_F16_Q4  3             /* 4-bit cache; ... f16                                                    */
 
 /* Where and how the cache lies in device memory: a pool's device side, or any memory of that layout. */
 typedef struct {
@@ -545,8 +559,11 @@ typedef struct {
     int32_t num_layers, block_size, kv_heads, head_dim;   /* head_dim: a multiple of 8, at most 256     */
     int64_t num_gpu_blocks;
     int32_t device_layout;          /* KV_DEV_LAYER_FIRST or KV_DEV_BLOCK_FIRST                         */
-    int32_t dtype;                  /* KV_DT_*: of the cache, q and the outputs                         */
+    int32_t dtype;                  /* KV_DT_*: of the cache, q and the outputs.  4 bits: block_size is a multiple of 4 */
 } kv_cache_t;
+/* Elements of 16 bits that a row of one plane and head takes: head_dim, or 10 G in 4 bits; 0 where there is no such cache.  What a
+ * pool's head_dim has to be. */
+int32_t kv_cache_row_units(int32_t dtype, int32_t head_dim);
 
 /* A context for `stream` (a cudaStream_t of device_id that outlives it; NULL = the default stream).  One caller
  * thread. */
@@ -562,7 +579,8 @@ int32_t kv_ops_reserve(kv_ops_t *ops, int64_t bytes);
 /* Text of the latest error of this context (never NULL); with NULL: of this thread's
  * latest kv_ops_create failure. */
 const char *kv_ops_last_error(kv_ops_t *ops);
-/* The pool's device side as a kv_cache_t. */
+/* The pool's device side as a kv_cache_t.  In 4 bits head_dim comes out padded (64, 128 or 256, by the pool's 20, 40 or 80): the
+ * caller may set it to the model's own. */
 int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
 
 /*
@@ -573,7 +591,8 @@ int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
  * The window counts slots.  These are the newest tokens as long as slots are in the tokens' order; kv_evict moves new tokens to
  * low slots, so a request that has been evicted from is read without a window.
  * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing, whatever V holds.  Else every
- * slot counts, one of weight 0 too: an infinite or NaN element of its V makes that element of out infinite or NaN.
+ * slot counts, one of weight 0 too: an infinite or NaN element of its V makes that element of out infinite or NaN.  (Of a cache in
+ * 4 bits a query head with an element that is not finite gives NaN; |K| has to stay below 2^100.)
  */
 typedef struct {
     int32_t layer, num_seqs, q_heads, window;
@@ -634,6 +653,38 @@ typedef struct {
     uint8_t axis_of[128];           /* HOST, by value: axis of each frequency                           */
 } kv_append_args_t;
 int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t *args);
+
+/*
+ * kv_append with norms of q and k over the elements of each head, in front of the rotation and in the same pass:
+ *     x_d -> x_d / sqrt(sum_d x_d^2 / head_dim + eps) * weight_d
+ * in float32 (keys of a 4-bit cache in float64, so that their codes are those of the formula), rounded once, after the rotation.  norms
+ * NULL, or both weights NULL: kv_append.
+ */
+typedef struct {
+    const void *q_weight, *k_weight;        /* [heads][head_dim]; NULL: q (k) is not normed                  */
+    int64_t q_head_stride, k_head_stride;   /* elements from a head's weights to the next head's; 0: all heads share them */
+    int32_t weight_float;                   /* 1: the weights are float32, 0: of the type of q, k and v      */
+    float   eps;                            /* not negative                                                  */
+} kv_norm_args_t;
+int32_t kv_append_normed(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t *args, const kv_norm_args_t *norms);
+
+/*
+ * Rows of the cache, side by side and in 16 bits (of a 4-bit cache the values its codes stand for, rounded once).  The tokens are
+ * those of a kv_append with the same seq_starts and lens: token j of sequence i's n_i comes from slot lens[i] - n_i + j.  A token
+ * of no sequence, of an idle one, of a bad length or block is left as it was in k and v (and reported as there).
+ */
+typedef struct {
+    int32_t layer, num_seqs;
+    int64_t num_tokens;             /* of all sequences together                                        */
+    void   *k, *v;                  /* [num_tokens][kv_heads][head_dim]; one of them may be NULL        */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int32_t *seq_starts;      /* [num_seqs + 1], or NULL: the last token of each (num_tokens = num_seqs) */
+    const int32_t *block_tables;    /* [num_seqs][table_width]                                          */
+    int64_t table_stride;
+    const int32_t *lens;            /* [num_seqs]                                                       */
+    int32_t table_width, pad_;
+} kv_read_args_t;
+int32_t kv_read(kv_ops_t *ops, const kv_cache_t *cache, const kv_read_args_t *args);
 
 /*
  * Eviction by accumulated attention weight, in all layers first_layer .. first_layer + num_layers - 1 at once.  Each

@@ -123,6 +123,18 @@ class kv_append_args_t(C.Structure):
                 ("token_order", C.c_void_p), ("axis_of", C.c_uint8 * 128)]
 
 
+class kv_norm_args_t(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_head_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("weight_float", C.c_int32), ("eps", C.c_float)]
+
+
+class kv_read_args_t(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("num_seqs", C.c_int32), ("num_tokens", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64),
+                ("v_head_stride", C.c_int64), ("seq_starts", C.c_void_p), ("block_tables", C.c_void_p),
+                ("table_stride", C.c_int64), ("lens", C.c_void_p), ("table_width", C.c_int32), ("pad_", C.c_int32)]
+
+
 class kv_evict_args_t(C.Structure):
     _fields_ = [("first_layer", C.c_int32), ("num_layers", C.c_int32), ("num_seqs", C.c_int32), ("keep", C.c_int32),
                 ("recent", C.c_int32), ("sink", C.c_int32), ("max_len", C.c_int64), ("block_tables", C.c_void_p),
@@ -149,7 +161,8 @@ EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_set_path", "kv_swap_out
            "kv_pool_set_wait_limit", "kv_pool_set_call_timing", "kv_completion_event", "kv_pool_set_ctas",
            "kv_debug_pair_in_bounds", "kv_rotate_req", "kv_debug_ring_shape",
            "kv_ops_create", "kv_ops_destroy", "kv_ops_sync", "kv_ops_reserve", "kv_ops_last_error", "kv_pool_cache",
-           "kv_attend", "kv_attend_workspace", "kv_append", "kv_evict", "kv_evict_workspace", "kv_req_shrink"]
+           "kv_attend", "kv_attend_workspace", "kv_append", "kv_append_normed", "kv_read", "kv_evict", "kv_evict_workspace",
+           "kv_cache_row_units", "kv_req_shrink"]
 
 _lib = None
 
@@ -259,9 +272,13 @@ def lib() -> C.CDLL:
     L.kv_ops_last_error.argtypes = [vp]
     L.kv_pool_cache.restype = C.c_int32
     L.kv_pool_cache.argtypes = [vp, C.c_int32, C.POINTER(kv_cache_t)]
-    for name in ("kv_attend", "kv_append", "kv_evict"):       # handle, address of a kv_cache_t, address of the argument struct
+    for name in ("kv_attend", "kv_append", "kv_evict", "kv_read"):       # handle, address of a kv_cache_t, address of the argument struct
         getattr(L, name).restype = C.c_int32
         getattr(L, name).argtypes = [vp, vp, vp]
+    L.kv_append_normed.restype = C.c_int32
+    L.kv_append_normed.argtypes = [vp, vp, vp, vp]
+    L.kv_cache_row_units.restype = C.c_int32
+    L.kv_cache_row_units.argtypes = [C.c_int32, C.c_int32]
     for name in ("kv_attend_workspace", "kv_evict_workspace"):
         getattr(L, name).restype = C.c_int32
         getattr(L, name).argtypes = [vp, vp, vp, i64p]
@@ -465,11 +482,16 @@ class KVPool:
     def kv_pool_set_wait_limit(self, polls: int, ns: int, check: bool = True) -> int:
         return self._ret(lib().kv_pool_set_wait_limit(self._h, polls, ns), check)
 
-    def kv_pool_cache(self, dtype: str = "bf16") -> "KVCache":
-        """The pool's device side as the operators (``KVOps``) take it."""
+    def kv_pool_cache(self, dtype: str = "bf16", head_dim: Optional[int] = None) -> "KVCache":
+        """The pool's device side as the operators (``KVOps``) take it.  A cache in 4 bits (``"bf16_q4"``, ``"f16_q4"``) needs a pool
+        made with ``head_dim=kv_cache_row_units(dtype, head_dim)``; head_dim: the model's, where heads are padded (None: 64, 128 or 256)."""
         out = KVCache.__new__(KVCache)
         out.c = kv_cache_t()
         self._ret(lib().kv_pool_cache(self._h, KV_DTYPES[dtype], C.byref(out.c)), True)
+        if head_dim is not None and head_dim != out.c.head_dim:
+            if kv_cache_row_units(dtype, head_dim) != kv_cache_row_units(dtype, out.c.head_dim):
+                raise ValueError(f"the pool's rows do not hold heads of {head_dim}")
+            out.c.head_dim = head_dim
         out._settle()
         return out
 
@@ -602,8 +624,15 @@ class KVTable:
 
 KV_DT_BF16 = 0
 KV_DT_F16 = 1
-KV_DTYPES = {"bf16": KV_DT_BF16, "f16": KV_DT_F16}
+KV_DT_BF16_Q4 = 2
+KV_DT_F16_Q4 = 3
+KV_DTYPES = {"bf16": KV_DT_BF16, "f16": KV_DT_F16, "bf16_q4": KV_DT_BF16_Q4, "f16_q4": KV_DT_F16_Q4}
 _ops_ext = None
+
+
+def kv_cache_row_units(dtype: str, head_dim: int) -> int:
+    """Elements of 16 bits that a row of one plane and head takes in a pool: its ``head_dim``; 0 where there is no such cache."""
+    return lib().kv_cache_row_units(KV_DTYPES[dtype], head_dim)
 
 
 def ops_ext():
@@ -630,7 +659,7 @@ class KVCache:
         self._settle()
 
     def _settle(self) -> None:
-        self.dtype = "f16" if self.c.dtype == KV_DT_F16 else "bf16"
+        self.dtype = next(name for name, number in KV_DTYPES.items() if number == self.c.dtype)
         self.heads, self.dim = self.c.kv_heads, self.c.head_dim
         self.address = C.addressof(self.c)
 
@@ -646,7 +675,7 @@ class KVOps:
         self._h = C.c_void_p()
         self.device_id = device_id
         ext = ops_ext()
-        self._ext_attend, self._ext_append, self._ext_evict = ext.attend, ext.append, ext.evict
+        self._ext_attend, self._ext_append, self._ext_evict, self._ext_read = ext.attend, ext.append, ext.evict, ext.read
         rc = lib().kv_ops_create(device_id, stream or None, C.byref(self._h))
         if rc != KV_OK:
             raise KVError(rc, lib().kv_ops_last_error(None).decode())
@@ -701,14 +730,21 @@ class KVOps:
 
     def kv_append(self, cache: KVCache, layer: int, q, k, v, block_tables, lens, *, positions, inv_freq, axis_of=None,
                   halves: bool = True, q_out=None, seq_starts=None, weights=None, order=None, token_order=None,
-                  check: bool = True) -> int:
+                  q_norm=None, k_norm=None, norm_eps: float = 1e-6, check: bool = True) -> int:
         """q, q_out [tokens, q_heads, dim] (None: k and v only), k, v [tokens, kv_heads, dim]; positions int32 [axes, tokens];
         inv_freq float32 [rotary_dim / 2]; axis_of: the axis of every frequency (a sequence of ints, None = all 0); halves: pairs
         (f, f + rotary_dim/2), else (2f, 2f + 1); seq_starts int32 [seqs + 1], None = one token per sequence; block_tables int32
         [seqs, width]; lens int32 [seqs], with the new tokens; weights float32 and order int32 [seqs, kv_heads, slots];
-        token_order int32 [tokens]."""
+        token_order int32 [tokens]; q_norm, k_norm: weights of a norm over each head's elements in front of the rotation, [dim] for all
+        heads or [heads, dim], both float32 or both of q's type (None: no norm), with norm_eps."""
         return self._ret(self._ext_append(self._address, self.device_id, cache.address, layer, q, k, v, block_tables, lens, positions,
-                                          inv_freq, axis_of, halves, q_out, seq_starts, weights, order, token_order), check)
+                                          inv_freq, axis_of, halves, q_out, seq_starts, weights, order, token_order, q_norm, k_norm,
+                                          norm_eps), check)
+
+    def kv_read(self, cache: KVCache, layer: int, block_tables, lens, *, k_out=None, v_out=None, seq_starts=None, check: bool = True) -> int:
+        """Rows of the cache into k_out, v_out [tokens, kv_heads, dim] (either may be None), in 16 bits: the tokens that a ``kv_append``
+        with the same seq_starts (None: the last token of each sequence) and lens writes; block_tables int32 [seqs, width]."""
+        return self._ret(self._ext_read(self._address, self.device_id, cache.address, layer, block_tables, lens, k_out, v_out, seq_starts), check)
 
     def kv_evict(self, cache: KVCache, block_tables, lens, max_len: int, *, keep: int, weights, order=None, seen=None,
                  recent: int = 0, sink: int = 0, weights_out=None, order_out=None, lens_out=None, first_layer: int = 0,

@@ -2,7 +2,7 @@
 
 ``build()`` produces ``paper_2601_20309_b200/libduplexkv.so`` from ``csrc/duplexkv.cu``
 (kernels in ``csrc/kv_kernels.cuh``), ``csrc/kv_table.cu`` (block table, host code) and ``csrc/kv_ops.cu``
-(operators on the device cache; kernels in ``csrc/kv_{attend,append,evict}.cuh``), and ``libkvtestutil.so`` from ``csrc/kv_testutil.cu``
+(operators on the device cache; kernels in ``csrc/kv_{attend,attend_q4,append,append_rows,evict,read}.cuh``), and ``libkvtestutil.so`` from ``csrc/kv_testutil.cu``
 (pool fill / checksum helpers used by tests and the bench to make and check inputs; not
 part of the rotation path).  nvcc cross-compiles without a GPU.
 """
@@ -39,7 +39,8 @@ def _stale(target: str, sources) -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     # (target, files to compile, further files the target depends on)
     main_src = [os.path.join(CSRC, "duplexkv.cu"), os.path.join(CSRC, "kv_table.cu"), os.path.join(CSRC, "kv_ops.cu")]
-    main_dep = [os.path.join(CSRC, f) for f in ("kv_kernels.cuh", "kv_ops.cuh", "kv_attend.cuh", "kv_append.cuh", "kv_evict.cuh")]
+    main_dep = [os.path.join(CSRC, f) for f in ("kv_kernels.cuh", "kv_ops.cuh", "kv_attend.cuh", "kv_attend_q4.cuh", "kv_append.cuh",
+                                                "kv_append_rows.cuh", "kv_evict.cuh", "kv_read.cuh")]
     main_dep += [os.path.join(os.path.dirname(HERE), "include", "duplexkv.h")]
     jobs = [(LIB, main_src, main_dep)]
     util_src = os.path.join(CSRC, "kv_testutil.cu")

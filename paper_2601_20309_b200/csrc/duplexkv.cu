@@ -1944,8 +1944,13 @@ int32_t kv_pool_shape(kv_pool_t *p, kv_pool_shape_t *out)
 int32_t kv_pool_cache(kv_pool_t *p, int32_t dtype, kv_cache_t *out)
 {
     if (!p || !out) return KV_ERR_INVALID_ARG;
-    if (dtype != KV_DT_BF16 && dtype != KV_DT_F16) return fail(p, KV_ERR_INVALID_ARG, "unknown element type");
-    *out = kv_cache_t{p->dev, p->cfg.num_layers, p->cfg.block_size, p->cfg.kv_heads, p->cfg.head_dim, p->cfg.num_gpu_blocks,
+    int32_t head_dim = p->cfg.head_dim;
+    if (dtype == KV_DT_BF16_Q4 || dtype == KV_DT_F16_Q4) {
+        for (head_dim = 64; head_dim <= 256 && kv_cache_row_units(dtype, head_dim) != p->cfg.head_dim; head_dim *= 2) {}
+        if (head_dim > 256) return fail(p, KV_ERR_INVALID_ARG, "the pool's rows are not those of a cache in 4 bits: make it with kv_cache_row_units");
+    } else if (dtype != KV_DT_BF16 && dtype != KV_DT_F16)
+        return fail(p, KV_ERR_INVALID_ARG, "unknown element type");
+    *out = kv_cache_t{p->dev, p->cfg.num_layers, p->cfg.block_size, p->cfg.kv_heads, head_dim, p->cfg.num_gpu_blocks,
                       p->cfg.device_layout, dtype};
     return KV_OK;
 }

@@ -39,39 +39,11 @@ struct KvAppend {
     uint8_t axis_of[128];
 };
 
-// the sequence that token t belongs to: the last one that starts at or before it.  A warp looks at 32 places at once
-__device__ __forceinline__ int kv_seq_of(const int *starts, int num_seqs, long long t)
-{
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = num_seqs;        // the answer lies in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + 31) / 32, at = lo + lane * step;
-        const unsigned v = __ballot_sync(~0u, lane * step < n && starts[at] <= t);
-        const int last = v ? 31 - __clz(v) : 0;
-        lo += last * step;
-        n = min(step, n - last * step);
-    }
-    return lo;
-}
-
 constexpr int AP_THREADS = 256, AP_ROWS = 2, AP_TOKENS = 16;
 
 // what a thread moves at once: eight or four elements as pairs, or one element
 template <typename T, int V> struct __align__(V * 2) KvPack { unsigned w[V / 2]; };
 template <typename T> struct KvPack<T, 1> { T e; };
-
-__device__ __forceinline__ float2 kv_unpair(unsigned w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ float2 kv_unpair(unsigned w, __half) { return __half22float2(*(const __half2 *)&w); }
-__device__ __forceinline__ unsigned kv_pair(float lo, float hi, __nv_bfloat16)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *(const unsigned *)&v;
-}
-__device__ __forceinline__ unsigned kv_pair(float lo, float hi, __half)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *(const unsigned *)&v;
-}
 
 template <typename T, int V>
 __global__ void __launch_bounds__(AP_THREADS) kv_append_tokens(const __grid_constant__ KvAppend a)

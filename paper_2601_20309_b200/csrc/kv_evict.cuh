@@ -116,40 +116,67 @@ template <int THREADS> struct KvSums {
 };
 
 // Rows of up to 32 pairs, by one warp: lane q has the q-th pair (slot d < keep, slot s >= keep).
-__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int m, int d, int s, ulonglong2 *way)
+struct KvWays {
+    ulonglong2 row[32];      // K of the source and of the hole, or 0
+    int2 words[32];          // in 4 bits: from there to the rows' words
+};
+
+template <typename U, bool Q4> __device__ __forceinline__ void kv_evict_units(const KvEvict &a, int m, const KvWays &way)
 {
-    const int lane = threadIdx.x & 31, half = a.c.dim / 8, units = 2 * half;
+    // units of K, then as many of V; in 4 bits a plane's are those of the codes, then of the words
+    const int lane = threadIdx.x & 31, codes = Q4 ? a.c.groups * 16 / (int)sizeof(U) : 0;
+    const int half = Q4 ? a.c.groups * 20 / (int)sizeof(U) : a.c.dim / 8, units = 2 * half;
+    for (int e = lane; e < m * units; e += 32 * 8) {
+        U v[8];
+        uint8_t *to[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int f = e + q * 32, r = !Q4 && a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
+            to[q] = nullptr;
+            if (f < m * units) {
+                const ulonglong2 w = way.row[r];
+                if constexpr (Q4) {
+                    const int in = u < half ? u : u - half;
+                    const int2 words = in < codes ? make_int2(in * (int)sizeof(U), in * (int)sizeof(U))
+                                                  : make_int2(way.words[r].x + (in - codes) * (int)sizeof(U), way.words[r].y + (in - codes) * (int)sizeof(U));
+                    const long long plane = u < half ? 0 : a.c.plane_stride;
+                    if (w.x) {
+                        v[q] = __ldcg((const U *)(w.x + plane + words.x));
+                        to[q] = (uint8_t *)(w.y + plane + words.y);
+                    }
+                } else {
+                    const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
+                    if (w.x) {
+                        v[q] = __ldcg((const U *)(w.x + off));
+                        to[q] = (uint8_t *)(w.y + off);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (to[q]) *(U *)to[q] = v[q];
+    }
+}
+
+template <bool Q4>
+__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int m, int d, int s, KvWays &way)
+{
+    const int lane = threadIdx.x & 31;
     if (lane < m) {
         const uint8_t *from = a.c.slot(p.i, s, 0), *into = a.c.slot(p.i, d, 0);
         const long long plane = (a.first_layer + p.l) * 2 * a.c.plane_stride + (long long)p.h * a.c.head_stride;
         const bool ok = from && into;            // a bad block id: the row stays where it is
-        way[lane] = make_ulonglong2(ok ? (unsigned long long)from + plane : 0, ok ? (unsigned long long)into + plane : 0);
+        way.row[lane] = make_ulonglong2(ok ? (unsigned long long)from + plane : 0, ok ? (unsigned long long)into + plane : 0);
+        if (Q4) way.words[lane] = make_int2(a.c.to_words(s), a.c.to_words(d));
         if (ok) {
             a.w_out[p.to + d] = a.w[p.at + s];
             if (a.order_out) a.order_out[p.to + d] = a.order[p.at + s];
         }
     }
     __syncwarp();
-    for (int e = lane; e < m * units; e += 32 * 8) {
-        uint4 v[8];
-        uint8_t *to[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int f = e + q * 32, r = a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
-            to[q] = nullptr;
-            if (f < m * units) {
-                const ulonglong2 w = way[r];
-                const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
-                if (w.x) {
-                    v[q] = __ldcg((const uint4 *)(w.x + off));
-                    to[q] = (uint8_t *)(w.y + off);
-                }
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (to[q]) *(uint4 *)to[q] = v[q];
-    }
+    if (Q4 && a.c.groups == 2) kv_evict_units<uint2, Q4>(a, m, way);     // words of two groups: 8 bytes
+    else kv_evict_units<uint4, Q4>(a, m, way);
     __syncwarp();
 }
 
@@ -479,7 +506,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) kv_evict_sele
     if (size > 1) kv_cluster_sync();             // nobody leaves while others may still write into its memory
 }
 
-__global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_constant__ KvEvict a)
+template <bool Q4> __global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_constant__ KvEvict a)
 {
     constexpr int THREADS = EV_SMALL_THREADS, WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned keys[];     // [max_len rounded up to 4 * THREADS]
@@ -487,7 +514,7 @@ __global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_
     __shared__ int bins[EV_BINS], s_count, s_ties[WARPS], s_lists[2 * EV_FUSED_ROWS];
     __shared__ int2 s_moves[WARPS];
     __shared__ int3 s_pick;
-    __shared__ ulonglong2 way[WARPS][32];
+    __shared__ KvWays way[WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const KvProblem p(a, blockIdx.x);
     const bool apart = a.w_out != a.w, stay = p.n <= a.keep;
@@ -685,20 +712,20 @@ __global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_small(const __grid_
     __syncthreads();
     for (int j = warp * 8; j < moves; j += WARPS * 8) {  // eight rows per warp: few as they are, all warps have some
         const int at = min(j + lane, moves - 1);
-        kv_evict_rows(a, p, min(moves - j, 8), s_lists[at], s_lists[EV_FUSED_ROWS + at], way[warp]);
+        kv_evict_rows<Q4>(a, p, min(moves - j, 8), s_lists[at], s_lists[EV_FUSED_ROWS + at], way[warp]);
     }
 }
 
 // rows x * 32 .. of problems y * EV_MOVE_WARPS .., a warp each: neighbouring KV heads move neighbouring slots together
-__global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid_constant__ KvEvict a)
+template <bool Q4> __global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid_constant__ KvEvict a)
 {
-    __shared__ ulonglong2 way[EV_MOVE_WARPS][32];
+    __shared__ KvWays way[EV_MOVE_WARPS];
     const int warp = threadIdx.x >> 5, j = blockIdx.x * 32, lane = threadIdx.x & 31;
     for (int y = blockIdx.y * EV_MOVE_WARPS + warp; y < a.problems; y += gridDim.y * EV_MOVE_WARPS) {
         const int n = a.count[y];
         if (j >= n) continue;
         const KvProblem p(a, y);
         const int at = min(j + lane, n - 1);
-        kv_evict_rows(a, p, min(n - j, 32), a.holes[(long long)y * a.cap + at], a.srcs[(long long)y * a.cap + at], way[warp]);
+        kv_evict_rows<Q4>(a, p, min(n - j, 32), a.holes[(long long)y * a.cap + at], a.srcs[(long long)y * a.cap + at], way[warp]);
     }
 }

@@ -8,8 +8,11 @@
 #include <vector>
 
 #include "kv_append.cuh"
+#include "kv_append_rows.cuh"
 #include "kv_attend.cuh"
+#include "kv_attend_q4.cuh"
 #include "kv_evict.cuh"
+#include "kv_read.cuh"
 
 struct kv_ops {
     int device = 0, sms = 0;
@@ -19,7 +22,7 @@ struct kv_ops {
     std::vector<void *> outgrown;    // earlier workspaces: captured graphs may hold them
     unsigned *status_host = nullptr, *status_dev = nullptr;
     int32_t sticky = KV_OK;
-    bool attend_ready[2][3][2] = {};   // [bf16][head dimension][query tiles]: shared-memory limit raised
+    bool attend_ready[2][2][3][2] = {};   // [4 bits][bf16][head dimension][query tiles]: shared-memory limit raised
     char err[256];
 };
 
@@ -56,6 +59,9 @@ struct OnDevice {
 };
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline bool is_bf16(const kv_cache_t *c) { return c->dtype == KV_DT_BF16 || c->dtype == KV_DT_BF16_Q4; }
+inline bool is_q4(int32_t dtype) { return dtype == KV_DT_BF16_Q4 || dtype == KV_DT_F16_Q4; }
+inline int q4_groups(int head_dim) { return head_dim <= 64 ? 2 : head_dim <= 128 ? 4 : 8; }
 inline int64_t align256(int64_t a) { return (a + 255) / 256 * 256; }
 
 int32_t grow_workspace(kv_ops *o, int64_t bytes)
@@ -89,16 +95,18 @@ int32_t make_view(kv_ops *o, const kv_cache_t *c, KvView &v)
     if (c->num_layers <= 0 || c->block_size <= 0 || c->kv_heads <= 0 || c->head_dim <= 0 || c->num_gpu_blocks <= 0 || c->num_gpu_blocks > INT32_MAX)
         return fail(o, KV_ERR_INVALID_ARG, "bad cache shape");
     if (c->device_layout != KV_DEV_LAYER_FIRST && c->device_layout != KV_DEV_BLOCK_FIRST) return fail(o, KV_ERR_INVALID_ARG, "unknown device layout");
-    if (c->dtype != KV_DT_BF16 && c->dtype != KV_DT_F16) return fail(o, KV_ERR_INVALID_ARG, "unknown element type");
+    if (c->dtype != KV_DT_BF16 && c->dtype != KV_DT_F16 && !is_q4(c->dtype)) return fail(o, KV_ERR_INVALID_ARG, "unknown element type");
     if (c->head_dim % 8 || c->head_dim > 256) return fail(o, KV_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most 256");
     if ((uintptr_t)c->device_base % 16) return fail(o, KV_ERR_INVALID_ARG, "the cache must be 16-byte aligned");
-    const int64_t row = (int64_t)c->kv_heads * c->head_dim * 2, seg = row * c->block_size;
+    if (is_q4(c->dtype) && c->block_size % 4) return fail(o, KV_ERR_UNSUPPORTED, "a cache in 4 bits needs blocks of a multiple of 4 tokens");
+    const int64_t row = (int64_t)c->kv_heads * kv_cache_row_units(c->dtype, c->head_dim) * 2, seg = row * c->block_size;
     if (seg > INT32_MAX) return fail(o, KV_ERR_UNSUPPORTED, "a plane of one block exceeds 2 GiB");
     v.base = (uint8_t *)c->device_base;
     v.blk_stride = c->device_layout == KV_DEV_BLOCK_FIRST ? seg * 2 * c->num_layers : seg;
     v.plane_stride = c->device_layout == KV_DEV_BLOCK_FIRST ? seg : seg * c->num_gpu_blocks;
-    v.row_stride = (int)row;
-    v.head_stride = c->head_dim * 2;
+    v.groups = is_q4(c->dtype) ? q4_groups(c->head_dim) : 0;
+    v.row_stride = v.groups ? 16 * v.groups : (int)row;
+    v.head_stride = v.groups ? 20 * v.groups * c->block_size : c->head_dim * 2;
     v.bs = c->block_size;
     v.nb = (int)c->num_gpu_blocks;
     v.heads = c->kv_heads;
@@ -163,14 +171,14 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     // heads, 377 MB: groups of 8 72 us with one tile and 81 with two, 9 123 and 82, 16 124 and 84; 17 to 32 147, 64 268 us
     // (with weights 8 86, 16 110, 32 235, 64 598)
     p.nt = k.group <= 8 ? 1 : 2;
-    const int most = p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
+    const int G = k.c.groups, most = G ? kv_q4_threads(G, p.nt) / 32 : p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
     // KV heads per CTA: as many as there are warps, so that a CTA reads whole rows of the cache.  Short rows that no CTA
     // shares (no second kernel) rather go one head to a CTA while there are SMs for it, with more warps along the row: 1 (16)
     // sequences of 37 slots and 8 KV heads 6.9 (7.2) us, all heads in one CTA 10.6 (10.8); of 130 8.9 (9.3) against 12.3 (15.5); of 16,
     // where one step is all there is, 6.9 (7.2) against 6.7 (6.8).
     auto shape = [&](int heads_wanted) {
         k.hc = 1;
-        for (int d = 2; d <= heads_wanted; ++d)
+        for (int d = 2; d <= std::min(heads_wanted, KV_ATTEND_WARPS); ++d)
             if (c->kv_heads % d == 0) k.hc = d;
         k.tw = 1;
         while (k.hc * k.tw * 2 <= most) k.tw *= 2;
@@ -184,8 +192,8 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     const bool split = longest > (a->weights_out ? ATTEND_ALONE_STEPS_WEIGHTS : ATTEND_ALONE_STEPS) || (a->weights_out && k.group_chunks > 1);
     if (split && one_head) longest = shape(most);
     k.head_chunks = c->kv_heads / k.hc;
-    const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * p.nt * (p.dp / 16 + 1) * 4 * 32 * 4 : 0;
-    const int64_t stage = (int64_t)p.warps * 64 * p.dp;
+    const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * (G ? kv_q4_box(G, p.nt) : p.nt * (p.dp / 16 + 1) * 4) * 32 * 4 : 0;
+    const int64_t stage = (int64_t)p.warps * (G ? kv_q4_tile(G) : 64 * p.dp);
     k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
@@ -206,8 +214,13 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     return KV_OK;
 }
 
-template <typename T> const void *attend_kernel(int dp, int nt)
+template <typename T> const void *attend_kernel(int dp, int nt, bool q4)
 {
+    if (q4) {
+        if (dp == 64) return nt == 1 ? (const void *)kv_attend_q4<T, 2, 1> : (const void *)kv_attend_q4<T, 2, 2>;
+        if (dp == 128) return nt == 1 ? (const void *)kv_attend_q4<T, 4, 1> : (const void *)kv_attend_q4<T, 4, 2>;
+        return nt == 1 ? (const void *)kv_attend_q4<T, 8, 1> : (const void *)kv_attend_q4<T, 8, 2>;
+    }
     if (dp == 64) return nt == 1 ? (const void *)kv_attend_stream<T, 64, 1> : (const void *)kv_attend_stream<T, 64, 2>;
     if (dp == 128) return nt == 1 ? (const void *)kv_attend_stream<T, 128, 1> : (const void *)kv_attend_stream<T, 128, 2>;
     return nt == 1 ? (const void *)kv_attend_stream<T, 256, 1> : (const void *)kv_attend_stream<T, 256, 2>;
@@ -216,6 +229,13 @@ template <typename T> const void *attend_kernel(int dp, int nt)
 }  // namespace
 
 extern "C" {
+
+int32_t kv_cache_row_units(int32_t dtype, int32_t head_dim)
+{
+    if (head_dim <= 0 || head_dim % 8 || head_dim > 256) return 0;
+    if (dtype == KV_DT_BF16 || dtype == KV_DT_F16) return head_dim;
+    return is_q4(dtype) ? 10 * q4_groups(head_dim) : 0;
+}
 
 const char *kv_ops_last_error(kv_ops_t *o) { return o ? o->err : g_ops_err; }
 
@@ -316,6 +336,8 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.q_seq = a->q_seq_stride;
     k.q_head = a->q_head_stride;
     k.q_pairs = (uintptr_t)a->q % 4 == 0 && a->q_seq_stride % 2 == 0 && a->q_head_stride % 2 == 0;
+    k.q_vec = (uintptr_t)a->q % 16 == 0 && a->q_seq_stride % 8 == 0 && a->q_head_stride % 8 == 0;
+    k.out_vec = (uintptr_t)a->out % 8 == 0 && a->out_seq_stride % 4 == 0 && a->out_head_stride % 4 == 0;
     k.out = a->out;
     k.o_seq = a->out_seq_stride;
     k.o_head = a->out_head_stride;
@@ -330,9 +352,9 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.part_ml = (float2 *)(o->ws + p.part_ml);
     k.part_o = (float *)(o->ws + p.part_o);
 
-    const bool bf16 = cache->dtype == KV_DT_BF16;
-    const void *kernel = bf16 ? attend_kernel<__nv_bfloat16>(p.dp, p.nt) : attend_kernel<__half>(p.dp, p.nt);
-    bool &ready = o->attend_ready[bf16][p.dp / 128][p.nt - 1];
+    const bool bf16 = is_bf16(cache), q4 = k.c.groups != 0;
+    const void *kernel = bf16 ? attend_kernel<__nv_bfloat16>(p.dp, p.nt, q4) : attend_kernel<__half>(p.dp, p.nt, q4);
+    bool &ready = o->attend_ready[q4][bf16][p.dp / 128][p.nt - 1];
     if (!ready) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(227 * 1024 - 4096));
         if (e != cudaSuccess) return fail_cuda(o, e, "cudaFuncSetAttribute");
@@ -361,7 +383,9 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     return KV_OK;
 }
 
-int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *a)
+int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *a) { return kv_append_normed(o, cache, a, nullptr); }
+
+int32_t kv_append_normed(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *a, const kv_norm_args_t *norms)
 {
     if (!o) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
     if (!a) return fail(o, KV_ERR_INVALID_ARG, "no arguments");
@@ -375,6 +399,13 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     if (a->num_axes < 1 || a->num_axes > 4) return fail(o, KV_ERR_INVALID_ARG, "num_axes must be 1 to 4");
     for (int f = 0; f < a->rotary_dim / 2; ++f)
         if (a->axis_of[f] >= a->num_axes) return fail(o, KV_ERR_RANGE, "axis_of names an axis that positions does not have");
+    const bool normed = norms && (norms->q_weight || norms->k_weight);
+    if (normed) {
+        if (!(norms->eps >= 0.f) || !(norms->eps < INFINITY)) return fail(o, KV_ERR_INVALID_ARG, "eps must be a number and not negative");
+        if (norms->weight_float != 0 && norms->weight_float != 1) return fail(o, KV_ERR_INVALID_ARG, "unknown type of the norms' weights");
+        if (norms->q_head_stride < 0 || norms->k_head_stride < 0) return fail(o, KV_ERR_INVALID_ARG, "negative stride of the norms' weights");
+        if (norms->q_weight && !a->q) return fail(o, KV_ERR_INVALID_ARG, "weights of a norm of q without q");
+    }
     if (a->num_tokens == 0 || a->num_seqs == 0) return KV_OK;
     const OnDevice on(o->device);
     if (!a->seq_starts && a->num_tokens != a->num_seqs) return fail(o, KV_ERR_INVALID_ARG, "without seq_starts every sequence has one token");
@@ -432,15 +463,81 @@ int32_t kv_append(kv_ops_t *o, const kv_cache_t *cache, const kv_append_args_t *
     // 12.2 / 14.1 / 17.9 us, 3500 18.9 / 20.1 / 21.3, 6900 36.5 / 35.2 / 36.0, 14.3k 67.1 / 65.0 / 63.5; up to 500 all the same
     k.per = (int)std::min<int64_t>(AP_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
     k.by_rows = (unsigned)ceil_div(int64_t(1) << 32, rows);
+    const bool bf16 = is_bf16(cache);
+    if (normed || k.c.groups) {
+        KvAppendRows r;
+        r.q_w = normed ? norms->q_weight : nullptr;
+        r.k_w = normed ? norms->k_weight : nullptr;
+        r.q_w_head = normed ? norms->q_head_stride : 0;
+        r.k_w_head = normed ? norms->k_head_stride : 0;
+        r.w_float = normed ? norms->weight_float : 0;
+        r.eps = normed ? norms->eps : 0.f;
+        r.turns = (int)ceil_div(a->rotary_dim, 16);
+        const int lanes = std::max(r.turns + (int)ceil_div(cache->head_dim - a->rotary_dim, 16), 2 * k.c.groups);
+        r.lanes_log2 = 0;
+        while (1 << r.lanes_log2 < lanes) ++r.lanes_log2;
+        const int q4 = k.c.groups != 0, per_token = r.turns * (q4 ? 192 : 64);
+        if (per_token) k.per = std::min(k.per, 40 * 1024 / per_token);       // with the keys in passing 48 KB at most
+        r.p = k;
+        const size_t smem = (size_t)k.per * per_token + (q4 ? (size_t)(AP_THREADS >> r.lanes_log2) * k.c.groups * 64 : 0);
+        const auto pick = [&](auto t) {
+            using T = decltype(t);
+            return q4 ? v == 8 ? kv_append_rows<T, 8, true> : v == 4 ? kv_append_rows<T, 4, true> : kv_append_rows<T, 1, true>
+                      : v == 8 ? kv_append_rows<T, 8, false> : v == 4 ? kv_append_rows<T, 4, false> : kv_append_rows<T, 1, false>;
+        };
+        const auto kernel = bf16 ? pick(__nv_bfloat16()) : pick(__half());
+        kernel<<<(unsigned)ceil_div(a->num_tokens, k.per), AP_THREADS, smem, o->stream>>>(r);
+        return launched(o, "kv_append");
+    }
     const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
     const size_t smem = (size_t)k.per * (a->rotary_dim / 2) * sizeof(float2);
-    const bool bf16 = cache->dtype == KV_DT_BF16;
     const auto kernel = bf16 ? (v == 8   ? kv_append_tokens<__nv_bfloat16, 8>
                                 : v == 4 ? kv_append_tokens<__nv_bfloat16, 4>
                                          : kv_append_tokens<__nv_bfloat16, 1>)
                              : (v == 8 ? kv_append_tokens<__half, 8> : v == 4 ? kv_append_tokens<__half, 4> : kv_append_tokens<__half, 1>);
     kernel<<<grid, AP_THREADS, smem, o->stream>>>(k);
     return launched(o, "kv_append");
+}
+
+int32_t kv_read(kv_ops_t *o, const kv_cache_t *cache, const kv_read_args_t *a)
+{
+    if (!o) return fail(nullptr, KV_ERR_INVALID_ARG, "null argument");
+    if (!a) return fail(o, KV_ERR_INVALID_ARG, "no arguments");
+    KvRead k;
+    int32_t rc = make_view(o, cache, k.c);
+    if (rc != KV_OK) return rc;
+    if (a->layer < 0 || a->layer >= cache->num_layers) return fail(o, KV_ERR_RANGE, "no such layer");
+    if (a->num_seqs < 0 || a->num_tokens < 0 || a->num_tokens > INT32_MAX) return fail(o, KV_ERR_INVALID_ARG, "bad count");
+    if (cache->kv_heads > 512) return fail(o, KV_ERR_UNSUPPORTED, "too many heads");
+    if (a->num_tokens == 0 || a->num_seqs == 0) return KV_OK;
+    const OnDevice on(o->device);
+    if (!a->seq_starts && a->num_tokens != a->num_seqs) return fail(o, KV_ERR_INVALID_ARG, "without seq_starts every sequence has one token");
+    if (!a->k && !a->v) return fail(o, KV_ERR_INVALID_ARG, "k or v is needed");
+    if ((rc = set_tables(o, k.c, a->block_tables, a->table_stride, a->table_width, a->lens,
+                         std::min<int64_t>((int64_t)a->table_width * cache->block_size, INT32_MAX / 2))) != KV_OK) return rc;
+    k.layer = a->layer;
+    k.num_seqs = a->num_seqs;
+    k.num_tokens = a->num_tokens;
+    k.k = a->k;
+    k.v = a->v;
+    k.k_tok = a->k_token_stride;
+    k.k_head = a->k_head_stride;
+    k.v_tok = a->v_token_stride;
+    k.v_head = a->v_head_stride;
+    k.starts = a->seq_starts;
+    k.units = (int)ceil_div(cache->head_dim, 16);
+    const int per_token = k.units * cache->kv_heads;
+    k.by_units = (unsigned)ceil_div(int64_t(1) << 32, per_token);
+    k.per = (int)std::min<int64_t>(RD_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
+    const auto fits = [](const void *p, int64_t x, int64_t y) { return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0; };
+    const bool vec = (!a->k || fits(a->k, a->k_token_stride, a->k_head_stride)) && (!a->v || fits(a->v, a->v_token_stride, a->v_head_stride));
+    const auto pick = [&](auto t) {
+        using T = decltype(t);
+        return k.c.groups ? vec ? kv_read_rows<T, true, true> : kv_read_rows<T, false, true> : vec ? kv_read_rows<T, true, false> : kv_read_rows<T, false, false>;
+    };
+    const auto kernel = is_bf16(cache) ? pick(__nv_bfloat16()) : pick(__half());
+    kernel<<<(unsigned)ceil_div(a->num_tokens, k.per), AP_THREADS, 0, o->stream>>>(k);
+    return launched(o, "kv_read");
 }
 
 }  // extern "C"
@@ -564,7 +661,7 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
         cfg.gridDim = dim3((unsigned)p.problems);
         cfg.blockDim = dim3(EV_SMALL_THREADS);
         cfg.dynamicSmemBytes = ceil_div(a->max_len, 4 * EV_SMALL_THREADS) * 16 * EV_SMALL_THREADS;
-        e = cudaLaunchKernelEx(&cfg, kv_evict_small, k);
+        e = k.c.groups ? cudaLaunchKernelEx(&cfg, kv_evict_small<true>, k) : cudaLaunchKernelEx(&cfg, kv_evict_small<false>, k);
     } else {
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = p.cluster;
@@ -584,7 +681,7 @@ int32_t kv_evict(kv_ops_t *o, const kv_cache_t *cache, const kv_evict_args_t *a)
         cfg.dynamicSmemBytes = 0;
         cfg.gridDim = dim3((unsigned)ceil_div(p.cap, 32), (unsigned)std::min<int64_t>(ceil_div(p.problems, EV_MOVE_WARPS), 65535));
         cfg.blockDim = dim3(EV_MOVE_WARPS * 32);
-        e = cudaLaunchKernelEx(&cfg, kv_evict_move, k);
+        e = k.c.groups ? cudaLaunchKernelEx(&cfg, kv_evict_move<true>, k) : cudaLaunchKernelEx(&cfg, kv_evict_move<false>, k);
         if (e != cudaSuccess) return fail_cuda(o, e, "kv_evict");
     }
     return KV_OK;

@@ -25,7 +25,7 @@ struct Call {
     int device;
     const kv_cache_t *cache;
 
-    at::ScalarType type() const { return cache->dtype == KV_DT_F16 ? at::kHalf : at::kBFloat16; }
+    at::ScalarType type() const { return cache->dtype == KV_DT_F16 || cache->dtype == KV_DT_F16_Q4 ? at::kHalf : at::kBFloat16; }
 
     // address and outer strides of a tensor whose last dimension is contiguous; -1 in `shape`: any size
     const at::Tensor &rows(PyObject *o, at::ScalarType want, std::initializer_list<int64_t> shape, const char *what, const void **p, int64_t *strides) const
@@ -140,7 +140,7 @@ int32_t attend(PyObject *const *v)
 }
 
 // (handle, device, cache address, layer, q, k, v, block_tables, lens, positions, inv_freq, axis_of, halves, q_out, seq_starts,
-//  weights, order, token_order)
+//  weights, order, token_order, q_norm, k_norm, norm_eps)
 int32_t append(PyObject *const *v)
 {
     const Call c{(int)integer(v[1]), (const kv_cache_t *)integer(v[2])};
@@ -205,7 +205,57 @@ int32_t append(PyObject *const *v)
         if (v[17] != Py_None) c.rows(v[17], at::kInt, {t}, "token_order", (const void **)&a.token_order, nullptr);
     }
     if (slots >= 0) a.num_slots = (int32_t)std::min<int64_t>(slots, INT32_MAX);
-    return kv_append((kv_ops_t *)integer(v[0]), c.cache, &a);
+    if (v[18] == Py_None && v[19] == Py_None) return kv_append((kv_ops_t *)integer(v[0]), c.cache, &a);
+    kv_norm_args_t norms;
+    memset(&norms, 0, sizeof(norms));
+    norms.eps = (float)number(v[20]);
+    at::ScalarType kind = at::kFloat;
+    // weights of one head for all, or of each; float32 or of the cache's type, both alike
+    const auto weights = [&](PyObject *o, int64_t of_heads, const char *what, bool first, const void **p, int64_t *stride) {
+        if (!THPVariable_Check(o)) throw Bad{std::string(what) + " must be a tensor"};
+        const at::Tensor &w = THPVariable_Unpack(o);
+        if (w.scalar_type() != at::kFloat && w.scalar_type() != c.type()) throw Bad{std::string(what) + " must be float32 or " + name_of(c.type()) + ", not " + name_of(w.scalar_type())};
+        if (!first && w.scalar_type() != kind) throw Bad{"q_norm and k_norm differ in type"};
+        kind = w.scalar_type();
+        if (w.dim() == 1) c.rows(o, kind, {dim}, what, p, nullptr);
+        else c.rows(o, kind, {of_heads, dim}, what, p, stride);
+    };
+    if (v[18] != Py_None) {
+        if (v[4] == Py_None) throw Bad{"q_norm without q"};
+        weights(v[18], a.q_heads, "q_norm", true, &norms.q_weight, &norms.q_head_stride);
+    }
+    if (v[19] != Py_None) weights(v[19], heads, "k_norm", v[18] == Py_None, &norms.k_weight, &norms.k_head_stride);
+    norms.weight_float = kind == at::kFloat;
+    return kv_append_normed((kv_ops_t *)integer(v[0]), c.cache, &a, &norms);
+}
+
+// (handle, device, cache address, layer, block_tables, lens, k_out, v_out, seq_starts)
+int32_t read(PyObject *const *v)
+{
+    const Call c{(int)integer(v[1]), (const kv_cache_t *)integer(v[2])};
+    kv_read_args_t a;
+    memset(&a, 0, sizeof(a));
+    const int64_t n = size_of(v[5], 0, "lens"), heads = c.cache->kv_heads, dim = c.cache->head_dim;
+    const bool k = v[6] != Py_None, w = v[7] != Py_None;
+    if (!k && !w) throw Bad{"k_out or v_out is needed"};
+    const int64_t t = size_of(v[k ? 6 : 7], 0, k ? "k_out" : "v_out");
+    int64_t s[2];
+    a.layer = integer32(v[3]);
+    a.num_seqs = (int32_t)n;
+    a.num_tokens = t;
+    if (k) {
+        c.rows(v[6], c.type(), {t, heads, dim}, "k_out", (const void **)&a.k, s);
+        a.k_token_stride = s[0];
+        a.k_head_stride = s[1];
+    }
+    if (w) {
+        c.rows(v[7], c.type(), {t, heads, dim}, "v_out", (const void **)&a.v, s);
+        a.v_token_stride = s[0];
+        a.v_head_stride = s[1];
+    }
+    c.tables(a, v[4], v[5], n);
+    if (v[8] != Py_None) c.rows(v[8], at::kInt, {n + 1}, "seq_starts", (const void **)&a.seq_starts, nullptr);
+    return kv_read((kv_ops_t *)integer(v[0]), c.cache, &a);
 }
 
 // (handle, device, cache address, block_tables, lens, max_len, keep, weights, order, seen, recent, sink, weights_out, order_out,
@@ -266,7 +316,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 PyMethodDef methods[] = {
     {"attend", (PyCFunction)(void (*)(void))entry<attend, 14>, METH_FASTCALL, "kv_attend on tensors; its status"},
-    {"append", (PyCFunction)(void (*)(void))entry<append, 18>, METH_FASTCALL, "kv_append on tensors; its status"},
+    {"append", (PyCFunction)(void (*)(void))entry<append, 21>, METH_FASTCALL, "kv_append on tensors; its status"},
+    {"read", (PyCFunction)(void (*)(void))entry<read, 9>, METH_FASTCALL, "kv_read on tensors; its status"},
     {"evict", (PyCFunction)(void (*)(void))entry<evict, 16>, METH_FASTCALL, "kv_evict on tensors; its status"},
     {nullptr, nullptr, 0, nullptr},
 };
