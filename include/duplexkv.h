@@ -522,8 +522,8 @@ int32_t kv_table_fail_pool_call(kv_table_t *table, int64_t after_calls, int32_t 
  * The cache may be held in 4 bits (KV_DT_BF16_Q4, KV_DT_F16_Q4: q, k, v and the outputs are bf16 or f16).  Heads are padded to
  * 64, 128 or 256 elements, which are G = 2, 4 or 8 groups of 32.  Each group of a row has a lowest value lo and a step s, and
  * an element is lo + s * code, code = 0 .. 15:
- *     lo = min, s = max((max - min) / 15, |lo| 2^-20) rounded to bf16, code = min(floor((x - lo) / s + 1/2), 15)   (0 where s is 0),
- * with the differences, the quotient by 15 and the maximum in float32 and the code exact; K is what the 16-bit cache would hold,
+ *     lo = min, s = max((max - min) * r, |lo| 2^-20) rounded to bf16, code = min(floor((x - lo) / s + 1/2), 15)   (0 where s is 0),
+ * with r the float32 number next to 1/15, the differences and the products in float32 and the code exact; K is what the 16-bit cache would hold,
  * rounded to its type.  A group with an element that is not finite, or whose range is not, reads as NaN.  A row of one plane and
  * head is 20 G bytes (80 instead of 256 for heads of 128), so a pool for it is made with head_dim = kv_cache_row_units(...) and moves
  * its blocks as any other.  A plane of a block is, for each head, block_size rows of 16 G bytes of codes, then block_size
@@ -570,7 +570,8 @@ int32_t kv_cache_row_units(int32_t dtype, int32_t head_dim);
 int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out);
 /* Waits for the stream, then frees the context and its workspace. */
 int32_t kv_ops_destroy(kv_ops_t *ops);
-/* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA of earlier calls. */
+/* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA of earlier calls, or KV_ERR_TIMEOUT where a bounded
+ * wait inside a kernel ran out (its results are not to be used). */
 int32_t kv_ops_sync(kv_ops_t *ops);
 /* Makes the workspace at least `bytes` large.  A call that needs more than there is does this itself, with a
  * cudaMalloc (not possible during stream capture: KV_ERR_NOMEM).  Outgrown workspaces stay allocated until

@@ -3,7 +3,7 @@
 //
 //   norm      y_d = x_d / sqrt(mean x^2 + eps) * w_d, for the heads of q and of k whose weights are given; then the rotation of
 //             kv_append.cuh.  Float32 throughout, one rounding at the end.
-//   4 bits    per group of 32 elements: lo = the lowest, s = (highest - lo) / 15, at least |lo| 2^-20, rounded to bf16;
+//   4 bits    per group of 32 elements: lo = the lowest, s = (highest - lo) * float32(1/15), at least |lo| 2^-20, rounded to bf16;
 //             code = floor((x - lo) / s + 1/2), at most 15.  lo is an element, so it is exact; s is never 0 beside a lo that is
 //             not, which gives the attention a bound of lo by s.  A group with an element that is not finite, or whose range is not,
 //             has NaN for both and reads as NaN.
@@ -54,7 +54,7 @@ template <typename T> __device__ __forceinline__ unsigned kv_quantise(const unsi
     bad |= __shfl_xor_sync(mask, (int)bad, 1) != 0;
     codes[0] = codes[1] = 0;
     if (lo > hi && !bad) return 0;                       // a group of nothing
-    const float raw = fmaxf((hi - lo) / 15.f, fabsf(lo) * 0x1p-20f);
+    const float raw = fmaxf((hi - lo) * (1.f / 15.f), fabsf(lo) * 0x1p-20f);
     const __nv_bfloat16 rounded = __float2bfloat16(raw);
     float s = __bfloat162float(rounded);
     if (bad || !(s < INFINITY)) return kv_nan_word<T>();

@@ -22,38 +22,91 @@
 // Masked slots (beyond the length, before the window) are loaded with their tile where their block is known: codes are numbers
 // whatever they hold, scores are replaced by -inf and words by 0, so nothing of such a slot reaches a sum.
 #pragma once
+#include <type_traits>
+
 #include "kv_attend.cuh"
 
-constexpr int KV_Q4_WARPS = 16, KV_Q4_STAGES = 6;
+constexpr int KV_Q4_WARPS = 8, KV_Q4_STAGES = 6;     // warps that compute; one more loads
 constexpr float KV_Q4_SLACK = 6.f, KV_Q4_LIFT = 8.f;
 constexpr int KV_Q4_LOWEST = -80;    // exponent of a step below which it counts as this: sums of 2^31 weights stay in range
+constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
 
-__host__ __device__ constexpr int kv_q4_threads(int groups, int tiles) { return groups * tiles <= 4 ? KV_Q4_WARPS * 32 : KV_Q4_WARPS * 16; }
+// tiles of 16 slots that a warp takes at once
+__host__ __device__ constexpr int kv_q4_sub(int groups, int tiles) { return groups * tiles <= 4 ? 2 : 1; }
+// bytes of a tile: K's and V's codes and words
 __host__ __device__ constexpr int kv_q4_tile(int groups) { return 640 * groups; }
 // floats of a lane that one way hands to another
 __host__ __device__ constexpr int kv_q4_box(int groups, int tiles) { return tiles * (8 * groups + 4); }
 
-template <int N> __device__ __forceinline__ void kv_lds(unsigned (&r)[N], unsigned addr)
+__device__ __forceinline__ void kv_mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
-    if constexpr (N == 1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(addr) : "memory");
-    else if constexpr (N == 2) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
-    else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a1, unsigned b0, unsigned b1, __half) { kv_mma_f16(c, a0, a1, a0, a1, b0, b1); }
+__device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a1, unsigned b0, unsigned b1, __nv_bfloat16)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%4,%5}, {%6,%7}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ unsigned kv_transpose(unsigned x)
+{
+    unsigned y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+template <int N> __device__ __forceinline__ void kv_lds(unsigned (&r)[N], const uint8_t *at)
+{
+    if constexpr (N == 1) r[0] = *(const unsigned *)at;
+    else if constexpr (N == 2) {
+        const uint2 v = *(const uint2 *)at;
+        r[0] = v.x, r[1] = v.y;
+    } else
 #pragma unroll
-        for (int k = 0; k < N; k += 4)
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[k]), "=r"(r[k + 1]), "=r"(r[k + 2]), "=r"(r[k + 3]) : "r"(addr + k * 4) : "memory");
+        for (int k = 0; k < N; k += 4) {
+            const uint4 v = *(const uint4 *)(at + k * 4);
+            r[k] = v.x, r[k + 1] = v.y, r[k + 2] = v.z, r[k + 3] = v.w;
+        }
+}
+
+__device__ __forceinline__ void kv_mbar_init(unsigned bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void kv_mbar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void kv_mbar_expect(unsigned bar, int bytes) { asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
+__device__ __forceinline__ bool kv_mbar_try(unsigned bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
+// Nothing here waits without a limit: a wait that runs out is reported, and the kernel goes on with whatever is there, waiting no more
+__device__ __forceinline__ void kv_mbar_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned *status)
+{
+    if (kv_mbar_try(bar, parity)) return;
+    for (int polls = 0; polls < KV_Q4_POLLS && !*gave_up; ++polls)
+        if (kv_mbar_try(bar, parity)) return;
+    *gave_up = 1;
+    atomicOr(status, KV_OPS_TIMEOUT);
+}
+__device__ __forceinline__ void kv_bulk(unsigned dst, const uint8_t *src, int bytes, unsigned bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 template <typename T, int G, int NT>
-__global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const __grid_constant__ KvAttend a)
 {
-    constexpr int TILE = kv_q4_tile(G), KW = 256 * G, VC = 320 * G, VW = 576 * G, HEADS = 8 * NT, CHUNKS = 40 * G, LOADS = (CHUNKS + 31) / 32;
+    constexpr int PLANE = 320 * G, WORDS = 256 * G, HEADS = 8 * NT;     // bytes of a tile's plane, and of its codes
     constexpr int PARTS = G == 8 ? 2 : 1;        // matrix instructions for the sum over lo
+    constexpr int SUB = kv_q4_sub(G, NT);
+    constexpr bool EXACT = std::is_same<T, __half>::value;      // see R below
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int red[KV_Q4_WARPS], s_at[2];
-    __shared__ int4 info[KV_Q4_WARPS][KV_Q4_STAGES];
-    __shared__ float s_lse[KV_Q4_WARPS][HEADS];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
-    const int hw = warp % a.hc, way = warp / a.hc;
+    __shared__ int red[KV_Q4_WARPS + 1], s_at[2], gave_up;
+    __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
+    __shared__ float s_lse[KV_ATTEND_WARPS][HEADS];
+    __shared__ __align__(8) unsigned long long bars[2][KV_Q4_STAGES];    // filled, empty
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ways = a.tw / SUB, warps = a.hc * ways;
     const int rows_of_seq = a.head_chunks * a.group_chunks;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -68,8 +121,18 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                 for (int g = tid; g < a.q_heads; g += blockDim.x) a.lse[(long long)i * a.q_heads + g] = -INFINITY;
         }
 
+    const unsigned filled = (unsigned)__cvta_generic_to_shared(bars[0]), empty = (unsigned)__cvta_generic_to_shared(bars[1]);
+    if (tid == 0) {
+        gave_up = 0;
+        for (int s = 0; s < a.stages; ++s) {
+            kv_mbar_init(filled + 8 * s, 1);
+            kv_mbar_init(empty + 8 * s, warps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+
     // ---- this CTA's piece of the line of steps: the row and step it begins at, and how many steps it has
-    int pi, pch, pk;                 // sequence, row of the sequence, step: where the next tile to be loaded lies
+    int pi, pch, pk;                 // sequence, row of the sequence, step
     int todo, s0 = 0, piece = 0;
     if (a.pieces == 0) {
         pi = blockIdx.x / rows_of_seq;
@@ -85,124 +148,117 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
         line.find(a, s0, s_at, pi, pch, pk);
     }
     if (todo <= 0) return;
+    __syncthreads();                 // the barriers are there
     const int k0 = pk;
 
-    const unsigned ring = (unsigned)__cvta_generic_to_shared(smem) + warp * a.stages * TILE;
-    const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
-    int4 *my_info = info[warp];
-
-    // ---- producer: block ids of two tiles of a row are read at once, lane r for row r % 16 of tile r / 16, and used one tile later.
-    // A tile is 40 G pieces of 16 bytes: K's codes, K's words, V's codes, V's words.  With blocks of whole tiles these are four runs.
-    int unseen = todo;               // tiles whose ids have not been read
-    int id = -1, row_in = 0, ph = 0, t0 = 0, ti = 0, tch = 0, have = 0, half = 0, tk = 0, tsteps = 0;
-    unsigned masks = 0, loads = 0;
-    const uint8_t *headp = a.c.base;
-    bool live = false, exists = false, fresh = true;   // fresh: the next tile begins this CTA's run in its row
-    KvSpan span(a, pi);
-    int psteps = span.steps(a);
-    auto peek = [&]() {
-        have = min(min(2, psteps - pk), unseen);
-        half = 0;
-        if (have == 0) return;
-        t0 = span.base + (pk * a.tw + way) * 16;
-        const int t = t0 + (lane >> 4) * a.tw * 16 + (lane & 15);
-        // slots of the tile before the window are slots of the sequence: their ids are there
-        exists = (lane >> 4) < have && (a.whole_tiles ? t - (lane & 15) : t) < span.n;
-        live = (lane >> 4) < have && t >= span.first && t < span.n;
-        if (exists) {
-            const int b = t / a.c.bs;
-            id = a.c.tables[pi * a.c.table_stride + b];
-            row_in = t - b * a.c.bs;
-        }
-        ph = pch / a.group_chunks * a.hc + hw;
-        ti = pi;
-        tch = pch;
-        tk = pk;
-        tsteps = psteps;
-        unseen -= have;
-        pk += have;
-        if (pk == psteps && unseen > 0) {
-            pk = 0;
-            if (++pch == rows_of_seq) {
-                pch = 0;
-                do span = KvSpan(a, ++pi);
-                while (span.n == 0);
-                psteps = span.steps(a);
+    if (warp == warps) {
+        // ---- the loading warp.  A stage is a step: [tile][K, V][KV head][codes, words].  The block ids of the next step are read while
+        // this one's copies are issued.  A lane looks after a tile, or, where blocks do not hold whole tiles, after four rows of
+        // one (blocks are multiples of four rows).
+        const int stage_bytes = a.tw * a.hc * 2 * PLANE, quads = a.whole_tiles ? 1 : 4, per = 16 / quads, roles = a.tw * quads;
+        const unsigned ring = (unsigned)__cvta_generic_to_shared(smem);
+        const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
+        KvSpan span(a, pi);
+        int psteps = span.steps(a), id, row, put = 0;
+        bool fresh = true;           // the next step begins this CTA's run in its row
+        auto peek = [&]() {          // the lane's block id in the step the cursor is at
+            const int t = span.base + pk * a.tw * 16 + lane * per;
+            row = -1;                // no slot of the sequence
+            id = -1;
+            if (lane < roles && t < span.n) {
+                const int b = t / a.c.bs;
+                id = a.c.tables[pi * a.c.table_stride + b];
+                row = t - b * a.c.bs;
             }
-        }
-    };
-    int put = 0;
-    auto issue = [&]() {
-        if (half < have) {
-            if (half == 0) {
-                const bool known = exists && (unsigned)id < (unsigned)a.c.nb;
-                if (live && !known) atomicOr(a.c.status, KV_OPS_BAD_BLOCK);
-                masks = __ballot_sync(~0u, live && known);
-                loads = __ballot_sync(~0u, known);
-                headp = known ? kbase + id * a.c.blk_stride + (long long)ph * a.c.head_stride : a.c.base;
-            }
-            const unsigned mask = (masks >> (half * 16)) & 0xffffu, load = (loads >> (half * 16)) & 0xffffu;
-            const bool ends = tk + half == tsteps - 1;
-            if (lane == 0) {
-                const int flags = (fresh ? 1 << 16 : 0) | (ends || (unseen == 0 && half == have - 1) ? 1 << 17 : 0) | (tk + half == 0 ? 1 << 18 : 0) |
-                                  (ends ? 1 << 19 : 0);
-                my_info[put] = make_int4((int)mask | flags, t0 + half * a.tw * 16, ti, tch);
-            }
+        };
+        peek();
+        for (int n = 0; n < todo; ++n) {
+            const int t0 = span.base + pk * a.tw * 16, t = t0 + lane * per, lo = max(span.first - t, 0), hi = min(span.n - t, per);
+            const bool ends = pk == psteps - 1;
+            const int flags = (fresh ? 1 << 16 : 0) | (ends || n == todo - 1 ? 1 << 17 : 0) | (pk == 0 ? 1 << 18 : 0) | (ends ? 1 << 19 : 0);
             fresh = ends;
-            const unsigned dst = ring + put * TILE + lane * 16;
-            if (a.whole_tiles) {
-                if (load & 1) {
-                    const uint8_t *codes = (const uint8_t *)__shfl_sync(~0u, (unsigned long long)headp, half * 16);
-                    const int row = __shfl_sync(~0u, row_in, half * 16);
-                    const uint8_t *words = codes + a.c.bs * 16 * G + row * 4 * G;
-                    codes += row * 16 * G;
-#pragma unroll
-                    for (int k = 0; k < LOADS; ++k) {
-                        const int c = lane + 32 * k;
-                        if (c < CHUNKS) {
-                            const bool v = c >= 20 * G;
-                            const int in = v ? c - 20 * G : c;
-                            const uint8_t *src = (in < 16 * G ? codes + in * 16 : words + (in - 16 * G) * 16) + (v ? a.c.plane_stride : 0);
-                            kv_cp16(dst + k * 512, src, true);
-                        }
-                    }
-                }
-            } else {
-#pragma unroll 1
-                for (int k = 0; k < LOADS; ++k) {
-                    const int c = min(lane + 32 * k, CHUNKS - 1);
-                    const bool v = c >= 20 * G;
-                    const int in = v ? c - 20 * G : c, w = in - 16 * G;
-                    // a piece of words may be of two rows: blocks are multiples of four rows, so both lie in one
-                    const int r = w < 0 ? in / G : w * 4 / G;
-                    const uint8_t *src = (const uint8_t *)__shfl_sync(~0u, (unsigned long long)headp, half * 16 + r);
-                    const int row = __shfl_sync(~0u, row_in, half * 16 + r);
-                    src += (w < 0 ? row * 16 * G + in % G * 16 : a.c.bs * 16 * G + row * 4 * G + (G == 8 ? (w & 1) * 16 : 0)) + (v ? a.c.plane_stride : 0);
-                    if ((load >> r & 1) && lane + 32 * k < CHUNKS) kv_cp16(dst + k * 512, src, true);
+            const bool known = (unsigned)id < (unsigned)a.c.nb;
+            unsigned mask = row >= 0 && hi > lo ? (1u << hi) - (1u << lo) : 0u;
+            if (mask && !known) {
+                atomicOr(a.c.status, KV_OPS_BAD_BLOCK);
+                mask = 0;
+            }
+            const bool load = mask != 0;
+            const int r = row;
+            const uint8_t *from = load ? kbase + id * a.c.blk_stride + (long long)(pch / a.group_chunks * a.hc) * a.c.head_stride : a.c.base;
+            if (quads == 4) {
+                mask <<= 4 * (lane & 3);
+                mask |= __shfl_xor_sync(~0u, mask, 1);
+                mask |= __shfl_xor_sync(~0u, mask, 2);
+            }
+            const int bytes = __popc(__ballot_sync(~0u, load)) * per * 40 * G * a.hc;
+            const int4 what = make_int4((int)mask | flags, t0 + lane / quads * 16, pi, pch);
+            // the cursor moves, and the next step's ids are on their way while this one is issued
+            if (++pk == psteps && n + 1 < todo) {
+                pk = 0;
+                if (++pch == rows_of_seq) {
+                    pch = 0;
+                    do span = KvSpan(a, ++pi);
+                    while (span.n == 0);
+                    psteps = span.steps(a);
                 }
             }
+            if (n + 1 < todo) peek();
+            if (n >= a.stages) kv_mbar_wait(empty + 8 * put, (n / a.stages - 1) & 1, &gave_up, a.c.status);
+            if (lane < roles && lane % quads == 0) info[put][lane / quads] = what;
+            __syncwarp();
+            const unsigned stage = ring + put * stage_bytes, bar = filled + 8 * put;
+            if (lane == 0) kv_mbar_expect(bar, bytes);
+            __syncwarp();
+            if (a.c.bs == 16) {      // a block's heads lie side by side: one copy per tile and plane
+                const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, lane >> 1);
+                const int on = __shfl_sync(~0u, (int)load, lane >> 1);
+                if (lane < 2 * a.tw && on) kv_bulk(stage + lane * a.hc * PLANE, (const uint8_t *)p + (lane & 1 ? a.c.plane_stride : 0), a.hc * PLANE, bar);
+            } else                   // (role, head, plane, codes or words)
+                for (int c0 = 0; c0 < roles * a.hc * 4; c0 += 32) {
+                    const int c = c0 + lane, words = c & 1, plane = c >> 1 & 1, rest = c >> 2, role = rest / a.hc, h = rest - role * a.hc;
+                    const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, role & 31);
+                    const int on = __shfl_sync(~0u, (int)load, role & 31), in = __shfl_sync(~0u, r, role & 31);
+                    if (role < roles && on)
+                        kv_bulk(stage + ((role / quads * 2 + plane) * a.hc + h) * PLANE + (words ? WORDS : 0) + role % quads * per * (words ? 4 : 16) * G,
+                                (const uint8_t *)p + (plane ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride + (words ? a.c.bs * 16 * G + in * 4 * G : in * 16 * G),
+                                per * (words ? 4 : 16) * G, bar);
+                }
             put = put + 1 == a.stages ? 0 : put + 1;
-            if (++half == have) peek();
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    peek();
-    for (int s = 0; s < a.stages - 1; ++s) issue();
+        return;                      // the computing warps wait for every copy before they leave
+    }
 
-    // ---- consumer
+    // ---- a computing warp
+    const int hw = warp % a.hc, way = warp / a.hc, threads = warps * 32;
+    auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); };
     const int rho = lane >> 2, j = lane & 3, slot = (rho >> 1) + 4 * (rho & 1);
+    // where a lane reads in a plane of a tile
+    const int code_at = (slot * 4 + j) * 4 * G, word_at = WORDS + slot * 4 * G, v_at = j * 16 * G + rho * 2 * G;
     unsigned qf[NT][G][4], ql[NT][PARTS][2];
     float fb[NT][2];
-    float o[NT][G][2][4], lo[NT][G][2], m[NT][2], ref[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
+    float o[NT][G][2][4], lo[NT][G][2], m[NT][2], ref[NT][2], lim[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
+    // The rounding of p s is multiplied by a code, 0 to 15, where the element itself may lie near 0.  For f16 outputs, fine enough to
+    // show it, R = the sum of the rounded p s over the slots (row g of the fragment: group g) moves the codes to -8 to 7:
+    // sum (p s) code + sum p lo = sum (p s)' (code - 8) + sum p (lo + 8 s), with ' the rounded ones
+    float R[NT][EXACT ? 4 : 1];
     int top_step = KV_Q4_LOWEST;
     int take = 0;
+    unsigned parity = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
     for (int n = 0; n < todo; ++n) {
-        __syncwarp();                // the stage about to be filled is no longer read
-        issue();
-        __syncwarp();
-        const int4 tile = my_info[take];
-        const unsigned mask = tile.x & 0xffff, stage = ring + take * TILE;
+        kv_mbar_wait(filled + 8 * take, parity, &gave_up, a.c.status);
+        const int4 tile = info[take][way * SUB];
+        unsigned mask[SUB], some = tile.x & 0xffff, all = some;
+        mask[0] = some;
+#pragma unroll
+        for (int u = 1; u < SUB; ++u) {
+            mask[u] = info[take][way * SUB + u].x & 0xffff;
+            some |= mask[u];
+            all &= mask[u];
+        }
+        const uint8_t *kt = smem + ((take * a.tw + way * SUB) * 2 * a.hc + hw) * PLANE;
+        const int to_v = a.hc * PLANE, to_next = 2 * to_v;
         const int h = tile.w / a.group_chunks * a.hc + hw, g0 = tile.w % a.group_chunks * HEADS;   // first query head in the group
         const int heads = min(HEADS, a.group - g0);
         if (tile.x & 1 << 16) {
@@ -240,7 +296,7 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     bad |= __shfl_xor_sync(~0u, (int)bad, x) != 0;
                 }
                 const int shift = bad || top == 0.f ? 0 : min(100, 135 - (int)(__float_as_uint(top) >> 23));
-                const float by = __uint_as_float((127 + shift) << 23);
+                const float by = a.scale2 < 0.f ? -__uint_as_float((127 + shift) << 23) : __uint_as_float((127 + shift) << 23);
                 float sum[G];
 #pragma unroll
                 for (int b = 0; b < G; ++b) {
@@ -259,6 +315,7 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     qf[nt][b][3] = kv_pair(v[3] * 0.0625f, v[7] * 0.0625f, __half());
                     sum[b] += __shfl_xor_sync(~0u, sum[b], 1);
                     sum[b] += __shfl_xor_sync(~0u, sum[b], 2);
+                    if (!EXACT) sum[b] *= 0x1p-24f;      // the codes' unit; float16 has no room for that
                     if (bad) sum[b] = NAN;       // a query that is not finite: its row is NaN
                 }
                 // columns of the instruction over lo: two groups, in a part per lane (or per register, of eight groups)
@@ -284,11 +341,12 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
 #pragma unroll
                         for (int b = 0; b < 2; ++b) ql[nt][p][b] = kv_pair(part(x, 2 * p + b), part(y, 2 * p + b), T());
                 }
-                const float scale = __uint_as_float((127 - shift) << 23) * a.scale2;
+                const float scale = __uint_as_float((127 - shift) << 23) * fabsf(a.scale2) * (EXACT ? 1.f : 0x1p24f);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     fb[nt][e] = __shfl_sync(~0u, scale, (2 * j + e) * 4);
                     m[nt][e] = -INFINITY;
+                    lim[nt][e] = -INFINITY;
                     ref[nt][e] = (float)KV_Q4_LOWEST - KV_Q4_LIFT;
                     l[nt][e] = rest[nt][e] = 0.f;
                 }
@@ -298,45 +356,36 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     for (int e = 0; e < 8; ++e) o[nt][b][e >> 2][e & 3] = 0.f;
                     lo[nt][b][0] = lo[nt][b][1] = 0.f;
                 }
+                if constexpr (EXACT) R[nt][0] = R[nt][1] = R[nt][2] = R[nt][3] = 0.f;
             }
         }
-        // the tile that is computed now was committed stages - 1 groups ago
-        switch (a.stages) {
-        case 1: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-        case 2: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-        case 3: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-        case 4: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-        case 5: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-        default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-        }
-        __syncwarp();
-        if (mask) {
-            float y[NT][4];
-            {
+        if (some) {
+            float y[SUB][NT][4];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                const uint8_t *at = kt + u * to_next;
                 unsigned c0[G], c1[G], w0[G], w1[G];
-                kv_lds(c0, stage + (slot * 4 + j) * 4 * G);
-                kv_lds(c1, stage + ((slot + 8) * 4 + j) * 4 * G);
-                kv_lds(w0, stage + KW + slot * 4 * G);
-                kv_lds(w1, stage + KW + (slot + 8) * 4 * G);
+                kv_lds(c0, at + code_at);
+                kv_lds(c1, at + code_at + 128 * G);
+                kv_lds(w0, at + word_at);
+                kv_lds(w1, at + word_at + 32 * G);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[nt][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) y[u][nt][e] = 0.f;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const unsigned k0[4] = {c0[g] & 0x000f000fu, c1[g] & 0x000f000fu, c0[g] & 0x00f000f0u, c1[g] & 0x00f000f0u};
                     const unsigned h0 = c0[g] >> 8, h1 = c1[g] >> 8;
-                    const unsigned k1[4] = {h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u};
                     const float s0 = __uint_as_float(w0[g] & 0xffff0000u), s1 = __uint_as_float(w1[g] & 0xffff0000u);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float x[4] = {0.f, 0.f, 0.f, 0.f};
-                        KvMma<__half>::mma(x, k0, qf[nt][g][0], qf[nt][g][1]);
-                        KvMma<__half>::mma(x, k1, qf[nt][g][2], qf[nt][g][3]);
-                        y[nt][0] = fmaf(s0, x[0], y[nt][0]);
-                        y[nt][1] = fmaf(s0, x[1], y[nt][1]);
-                        y[nt][2] = fmaf(s1, x[2], y[nt][2]);
-                        y[nt][3] = fmaf(s1, x[3], y[nt][3]);
+                        kv_mma_f16(x, c0[g] & 0x000f000fu, c1[g] & 0x000f000fu, c0[g] & 0x00f000f0u, c1[g] & 0x00f000f0u, qf[nt][g][0], qf[nt][g][1]);
+                        kv_mma_f16(x, h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u, qf[nt][g][2], qf[nt][g][3]);
+                        y[u][nt][0] = fmaf(s0, x[0], y[u][nt][0]);
+                        y[u][nt][1] = fmaf(s0, x[1], y[u][nt][1]);
+                        y[u][nt][2] = fmaf(s1, x[2], y[u][nt][2]);
+                        y[u][nt][3] = fmaf(s1, x[3], y[u][nt][3]);
                     }
                 }
                 unsigned x0, x1, z0, z1;         // the two groups of this lane's columns
@@ -346,74 +395,103 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     x0 = j & 2 ? j & 1 ? w0[6] : w0[4] : j & 1 ? w0[2] : w0[0], z0 = j & 2 ? j & 1 ? w0[7] : w0[5] : j & 1 ? w0[3] : w0[1];
                     x1 = j & 2 ? j & 1 ? w1[6] : w1[4] : j & 1 ? w1[2] : w1[0], z1 = j & 2 ? j & 1 ? w1[7] : w1[5] : j & 1 ? w1[3] : w1[1];
                 }
-                const unsigned p0 = __byte_perm(x0, z0, 0x5410), p1 = __byte_perm(x1, z1, 0x5410), kl[4] = {p0, p1, p0, p1};
-                const bool on0 = mask >> slot & 1, on1 = mask >> (slot + 8) & 1;
+                const unsigned p0 = __byte_perm(x0, z0, 0x5410), p1 = __byte_perm(x1, z1, 0x5410);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (EXACT) {
+                        float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int p = 0; p < PARTS; ++p) KvMma<T>::mma(x, kl, ql[nt][p][0], ql[nt][p][1]);
+                        for (int p = 0; p < PARTS; ++p) kv_mma_lo(x, p0, p1, ql[nt][p][0], ql[nt][p][1], T());
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[nt][e] = (e < 2 ? on0 : on1) ? fmaf(y[nt][e], 0x1p24f, x[e]) * fb[nt][e & 1] : -INFINITY;
-                    if (a.scores) {
-                        const int g = nt * 8 + j * 2;
-                        float *to = a.scores + (((long long)tile.z * a.c.heads + h) * a.c.max_len + tile.y + slot) * a.group + g0 + g;
+                        for (int e = 0; e < 4; ++e) y[u][nt][e] = fmaf(y[u][nt][e], 0x1p24f, x[e]);
+                    } else
 #pragma unroll
-                        for (int b = 0; b < 2; ++b, to += 8 * a.group) {
-                            if (tile.y + slot + b * 8 >= a.c.max_len) continue;
-                            if ((a.group & 1) == 0 && g < heads) *(float2 *)to = make_float2(y[nt][2 * b], y[nt][2 * b + 1]);
-                            else
+                        for (int p = 0; p < PARTS; ++p) kv_mma_lo(y[u][nt], p0, p1, ql[nt][p][0], ql[nt][p][1], T());
+                }
+            }
+            unsigned w0[SUB][G], w1[SUB][G];
 #pragma unroll
-                                for (int e = 0; e < 2; ++e)
-                                    if (g + e < heads) to[e] = y[nt][2 * b + e];
-                        }
+            for (int u = 0; u < SUB; ++u) {
+                kv_lds(w0[u], kt + to_v + u * to_next + word_at);
+                kv_lds(w1[u], kt + to_v + u * to_next + word_at + 32 * G);
+            }
+            if (all != 0xffffu)
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    const bool on0 = mask[u] >> slot & 1, on1 = mask[u] >> (slot + 8) & 1;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[u][nt][e] = (e < 2 ? on0 : on1) ? y[u][nt][e] : -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        w0[u][g] = on0 ? w0[u][g] : 0u;
+                        w1[u][g] = on1 ? w1[u][g] : 0u;
                     }
                 }
-            }
-            unsigned w0[G], w1[G];
-            kv_lds(w0, stage + VW + slot * 4 * G);
-            kv_lds(w1, stage + VW + (slot + 8) * 4 * G);
-            if (mask != 0xffffu) {
-                const bool on0 = mask >> slot & 1, on1 = mask >> (slot + 8) & 1;
+            if (a.scores)
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    w0[g] = on0 ? w0[g] : 0u;
-                    w1[g] = on1 ? w1[g] : 0u;
-                }
-            }
-            // the largest step of the tile: words are in the order of their steps; those of a group that is not finite do not count
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const int g = nt * 8 + j * 2, t = tile.y + 16 * u + slot;
+                        float *to = a.scores + (((long long)tile.z * a.c.heads + h) * a.c.max_len + t) * a.group + g0 + g;
+#pragma unroll
+                        for (int b = 0; b < 2; ++b, to += 8 * a.group) {
+                            if (t + b * 8 >= a.c.max_len) continue;
+                            const float2 score = make_float2(y[u][nt][2 * b] * fb[nt][0], y[u][nt][2 * b + 1] * fb[nt][1]);
+                            if ((a.group & 1) == 0 && g < heads) *(float2 *)to = score;
+                            else {
+                                if (g < heads) to[0] = score.x;
+                                if (g + 1 < heads) to[1] = score.y;
+                            }
+                        }
+                    }
+            // the largest step of the tiles: words are in the order of their steps; those of a group that is not finite do not count
             unsigned most = 0;
 #pragma unroll
-            for (int g = 0; g < G; ++g) most = max(most, max(w0[g], w1[g]));
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int g = 0; g < G; ++g) most = max(most, max(w0[u][g], w1[u][g]));
             most = __reduce_max_sync(~0u, most);
             if (most >= 0x7f800000u) {
                 most = 0;
 #pragma unroll
-                for (int g = 0; g < G; ++g) most = max(most, max(w0[g] < 0x7f800000u ? w0[g] : 0u, w1[g] < 0x7f800000u ? w1[g] : 0u));
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) most = max(most, max(w0[u][g] < 0x7f800000u ? w0[u][g] : 0u, w1[u][g] < 0x7f800000u ? w1[u][g] : 0u));
                 most = __reduce_max_sync(~0u, most);
             }
             const int step = (int)(most >> 23) - 127;
+            float top[NT][2];
             bool moves = step > top_step;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) moves |= fmaxf(y[nt][e], y[nt][e + 2]) > m[nt][e] + KV_Q4_SLACK;
+                for (int e = 0; e < 2; ++e) {
+                    top[nt][e] = fmaxf(y[0][nt][e], y[0][nt][e + 2]);
+#pragma unroll
+                    for (int u = 1; u < SUB; ++u) top[nt][e] = fmaxf(top[nt][e], fmaxf(y[u][nt][e], y[u][nt][e + 2]));
+                    moves |= top[nt][e] > lim[nt][e];
+                }
             if (__any_sync(~0u, moves)) {
                 top_step = max(top_step, step);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float x = fmaxf(y[nt][e], y[nt][e + 2]);
+                        float x = top[nt][e];
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                        x = fmaxf(x, m[nt][e]);
+                        x = fmaxf(x * fb[nt][e], m[nt][e]);
                         const float now = kv_ref(x) + ((float)top_step - KV_Q4_LIFT), alpha = m[nt][e] == -INFINITY ? 0.f : kv_exp2(ref[nt][e] - now);
                         m[nt][e] = x;
                         ref[nt][e] = now;
+                        lim[nt][e] = (x + KV_Q4_SLACK) / fb[nt][e];
                         l[nt][e] *= alpha;
                         rest[nt][e] *= alpha;
+                        if constexpr (EXACT) R[nt][e] *= alpha;
 #pragma unroll
                         for (int g = 0; g < G; ++g) {
                             lo[nt][g][e] *= alpha;
@@ -428,41 +506,61 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[nt][e] = kv_exp2(y[nt][e] - ref[nt][e & 1]);
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][nt][e] = kv_exp2(fmaf(y[u][nt][e], fb[nt][e & 1], -ref[nt][e & 1]));
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {            // compensated: weights of 2^-25 of the largest would vanish one by one
-                    const float x = y[nt][e] + y[nt][e + 2] + rest[nt][e], sum = l[nt][e] + x;
+                    float x = y[0][nt][e] + y[0][nt][e + 2];
+#pragma unroll
+                    for (int u = 1; u < SUB; ++u) x += y[u][nt][e] + y[u][nt][e + 2];
+                    x += rest[nt][e];
+                    const float sum = l[nt][e] + x;
                     rest[nt][e] = x - (sum - l[nt][e]);
                     l[nt][e] = sum;
                 }
             }
-            unsigned v[4][G / 2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) kv_lds(v[r], stage + VC + (j + 4 * r) * 16 * G + rho * 2 * G);
+            for (int u = 0; u < SUB; ++u) {
+                unsigned v[4][G / 2];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);
-                const unsigned v0[4] = {r0 & 0x000f000fu, r0 & 0x00f000f0u, r1 & 0x000f000fu, r1 & 0x00f000f0u};
-                const unsigned h0 = r0 >> 8, h1 = r1 >> 8;
-                const unsigned v1[4] = {h0 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x000f000fu, h1 & 0x00f000f0u};
-                const float s0 = __uint_as_float(w0[g] & 0xffff0000u), s1 = __uint_as_float(w1[g] & 0xffff0000u);
-                const float z0 = kv_unpair(w0[g], T()).x, z1 = kv_unpair(w1[g], T()).x;
+                for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + r * 64 * G);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const unsigned p0 = kv_movmatrix_t(kv_pair(y[nt][0] * s0, y[nt][1] * s0, __half())), p1 = kv_movmatrix_t(kv_pair(y[nt][2] * s1, y[nt][3] * s1, __half()));
-                    KvMma<__half>::mma(o[nt][g][0], v0, p0, p1);
-                    KvMma<__half>::mma(o[nt][g][1], v1, p0, p1);
+                for (int g = 0; g < G; ++g) {
+                    const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);
+                    const unsigned h0 = r0 >> 8, h1 = r1 >> 8;
+                    const float s0 = __uint_as_float(w0[u][g] & 0xffff0000u), s1 = __uint_as_float(w1[u][g] & 0xffff0000u);
+                    float z0 = kv_unpair(w0[u][g], T()).x, z1 = kv_unpair(w1[u][g], T()).x;
+                    if constexpr (EXACT) {
+                        z0 = fmaf(8.f, s0, z0);
+                        z1 = fmaf(8.f, s1, z1);
+                    }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(y[nt][e], z0, fmaf(y[nt][e + 2], z1, lo[nt][g][e]));
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float(&p)[4] = y[u][nt];
+                        const unsigned p0 = kv_transpose(kv_pair(p[0] * s0, p[1] * s0, __half())), p1 = kv_transpose(kv_pair(p[2] * s1, p[3] * s1, __half()));
+                        kv_mma_f16(o[nt][g][0], r0 & 0x000f000fu, r0 & 0x00f000f0u, r1 & 0x000f000fu, r1 & 0x00f000f0u, p0, p1);
+                        kv_mma_f16(o[nt][g][1], h0 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x000f000fu, h1 & 0x00f000f0u, p0, p1);
+                        if constexpr (EXACT) {
+                            const unsigned one = rho == g ? 0x3c003c00u : 0u;
+                            kv_mma_f16(R[nt], one, 0u, one, 0u, p0, p1);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(p[e], z0, fmaf(p[e + 2], z1, lo[nt][g][e]));
+                    }
                 }
             }
         }
-        else if (a.scores)           // nothing of the tile counts
-            for (int e = lane; e < 16 * heads; e += 32)
+        else if (a.scores)           // nothing of the tiles counts
+            for (int e = lane; e < 16 * SUB * heads; e += 32)
                 if (tile.y + e / heads < a.c.max_len)
                     a.scores[(((long long)tile.z * a.c.heads + h) * a.c.max_len + tile.y + e / heads) * a.group + g0 + e % heads] = -INFINITY;
         __syncwarp();
-        take = take + 1 == a.stages ? 0 : take + 1;
+        if (lane == 0) kv_mbar_arrive(empty + 8 * take);
+        if (++take == a.stages) {
+            take = 0;
+            parity ^= 1;
+        }
 
         if (tile.x & 1 << 17) {      // the CTA's last step in this row
             // element 32 g + 4 rho + 2 t + b of head 2 j + e is o[g][t][2 b + e]
@@ -478,6 +576,7 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     for (int g = 0; g < G; ++g) {
 #pragma unroll
                         for (int x = 4; x <= 16; x <<= 1) lo[nt][g][e] += __shfl_xor_sync(~0u, lo[nt][g][e], x);
+                        if constexpr (EXACT) lo[nt][g][e] -= 8.f * __shfl_sync(~0u, R[nt][e], 4 * g + j);
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -485,9 +584,9 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                     }
                 }
             const bool whole = began && (tile.x & 1 << 19);
-            if (a.tw > 1) {          // the ways of a head meet in pairs
-                float *box = (float *)(smem + warps * a.stages * TILE);
-                for (int st = a.tw >> 1; st >= 1; st >>= 1) {
+            if (ways > 1) {          // the ways of a head meet in pairs
+                float *box = (float *)(smem + a.stages * a.tw * a.hc * 2 * PLANE);
+                for (int st = ways >> 1; st >= 1; st >>= 1) {
                     if (way >= st && way < 2 * st) {
                         float *to = box + ((way - st) * a.hc + hw) * kv_q4_box(G, NT) * 32 + lane;
 #pragma unroll
@@ -503,7 +602,7 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                                 for (int e = 0; e < 8; ++e) to[(NT * 4 + (nt * G + g) * 8 + e) * 32] = o[nt][g][e >> 2][e & 3];
                         }
                     }
-                    __syncthreads();
+                    meet();
                     if (way < st) {
                         const float *from = box + (way * a.hc + hw) * kv_q4_box(G, NT) * 32 + lane;
 #pragma unroll
@@ -524,7 +623,7 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
                                     o[nt][g][e >> 2][e & 3] = o[nt][g][e >> 2][e & 3] * x[e & 1] + from[(NT * 4 + (nt * G + g) * 8 + e) * 32] * z[e & 1];
                         }
                     }
-                    __syncthreads();
+                    meet();
                 }
             }
             if (way == 0) {
@@ -574,34 +673,36 @@ __global__ void __launch_bounds__(kv_q4_threads(G, NT), 1) kv_attend_q4(const __
             }
             // where there is no second kernel, the weights are added up here: every thread reads the scores it wrote itself
             if (a.pieces == 0 && a.scores) {
-                if (a.tw > 1) __syncthreads();
+                if (ways > 1) meet();
                 else __syncwarp();
                 const KvSpan sp(a, tile.z);
                 const float *from = a.scores + ((long long)tile.z * a.c.heads + h) * a.c.max_len * a.group;
                 const long long w = tile.z * a.w_seq + h * a.w_head;
-                for (int t = way * 32 + lane; t < sp.base; t += a.tw * 32) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
-                for (int first = sp.base + way * 16; first < sp.n; first += a.tw * 16) {
-                    float add[2] = {0.f, 0.f};
+                for (int t = way * 32 + lane; t < sp.base; t += ways * 32) a.w_out[w + t] = a.w_in ? a.w_in[w + t] : 0.f;
+                for (int base = sp.base + way * 16 * SUB; base < sp.n; base += a.tw * 16)
+#pragma unroll 1
+                    for (int first = base; first < base + 16 * SUB; first += 16) {
+                        float add[2] = {0.f, 0.f};
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        if (first + b * 8 + slot < sp.n)
+                        for (int b = 0; b < 2; ++b)
+                            if (first + b * 8 + slot < sp.n)
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
+                                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const int g = nt * 8 + j * 2 + e;
-                                    if (g < heads) add[b] += kv_exp2(from[(long long)(first + b * 8 + slot) * a.group + g] - s_lse[hw][g]);
-                                }
+                                    for (int e = 0; e < 2; ++e) {
+                                        const int g = nt * 8 + j * 2 + e;
+                                        if (g < heads) add[b] += kv_exp2(from[(long long)(first + b * 8 + slot) * a.group + g] - s_lse[hw][g]);
+                                    }
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        add[b] += __shfl_xor_sync(~0u, add[b], 1);
-                        add[b] += __shfl_xor_sync(~0u, add[b], 2);
-                        const int t = first + b * 8 + slot;
-                        // slots of the tile that lie before the window keep their weight, even where the sum is NaN
-                        if (j == 0 && t < sp.n) a.w_out[w + t] = (a.w_in ? a.w_in[w + t] : 0.f) + (t >= sp.first ? add[b] : 0.f);
+                        for (int b = 0; b < 2; ++b) {
+                            add[b] += __shfl_xor_sync(~0u, add[b], 1);
+                            add[b] += __shfl_xor_sync(~0u, add[b], 2);
+                            const int t = first + b * 8 + slot;
+                            // slots of the tile that lie before the window keep their weight, even where the sum is NaN
+                            if (j == 0 && t < sp.n) a.w_out[w + t] = (a.w_in ? a.w_in[w + t] : 0.f) + (t >= sp.first ? add[b] : 0.f);
+                        }
                     }
-                }
-                if (a.tw > 1) __syncthreads();           // the next row's sums take the place of these
+                if (ways > 1) meet();           // the next row's sums take the place of these
                 else __syncwarp();
             }
         }

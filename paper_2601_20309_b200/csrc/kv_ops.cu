@@ -171,7 +171,10 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     // heads, 377 MB: groups of 8 72 us with one tile and 81 with two, 9 123 and 82, 16 124 and 84; 17 to 32 147, 64 268 us
     // (with weights 8 86, 16 110, 32 235, 64 598)
     p.nt = k.group <= 8 ? 1 : 2;
-    const int G = k.c.groups, most = G ? kv_q4_threads(G, p.nt) / 32 : p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
+    const int G = k.c.groups, most = G ? KV_Q4_WARPS : p.dp == 256 ? KV_ATTEND_WARPS / 2 : KV_ATTEND_WARPS;
+    // one address per tile where a block holds whole tiles, else one per row: 70B shape 80.4 against 89.2 us, 64 sequences with
+    // weights 90.3 against 100.5, one of 131072 slots 27.9 against 28.9
+    k.whole_tiles = c->block_size % 16 == 0;
     // KV heads per CTA: as many as there are warps, so that a CTA reads whole rows of the cache.  Short rows that no CTA
     // shares (no second kernel) rather go one head to a CTA while there are SMs for it, with more warps along the row: 1 (16)
     // sequences of 37 slots and 8 KV heads 6.9 (7.2) us, all heads in one CTA 10.6 (10.8); of 130 8.9 (9.3) against 12.3 (15.5); of 16,
@@ -181,8 +184,9 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
         for (int d = 2; d <= std::min(heads_wanted, KV_ATTEND_WARPS); ++d)
             if (c->kv_heads % d == 0) k.hc = d;
         k.tw = 1;
-        while (k.hc * k.tw * 2 <= most) k.tw *= 2;
+        while (k.hc * k.tw * 2 <= most && !(G && !k.whole_tiles && k.tw * 2 * kv_q4_sub(G, p.nt) > 8)) k.tw *= 2;   // rows are looked up by a warp: 8 tiles by fours
         p.warps = k.hc * k.tw;
+        if (G) k.tw *= kv_q4_sub(G, p.nt);               // a warp takes two tiles at once
         return ceil_div(a->max_len + 15, 16 * k.tw);     // steps of the longest row
     };
     k.group_chunks = (int)ceil_div(k.group, 8 * p.nt);
@@ -192,8 +196,8 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     const bool split = longest > (a->weights_out ? ATTEND_ALONE_STEPS_WEIGHTS : ATTEND_ALONE_STEPS) || (a->weights_out && k.group_chunks > 1);
     if (split && one_head) longest = shape(most);
     k.head_chunks = c->kv_heads / k.hc;
-    const int64_t box = k.tw > 1 ? (int64_t)p.warps / 2 * (G ? kv_q4_box(G, p.nt) : p.nt * (p.dp / 16 + 1) * 4) * 32 * 4 : 0;
-    const int64_t stage = (int64_t)p.warps * (G ? kv_q4_tile(G) : 64 * p.dp);
+    const int64_t box = p.warps > k.hc ? (int64_t)p.warps / 2 * (G ? kv_q4_box(G, p.nt) : p.nt * (p.dp / 16 + 1) * 4) * 32 * 4 : 0;
+    const int64_t stage = G ? (int64_t)k.tw * k.hc * kv_q4_tile(G) : (int64_t)p.warps * 64 * p.dp;
     k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
@@ -202,9 +206,6 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
-    // one address per tile where a block holds whole tiles, else one per row: 70B shape 80.4 against 89.2 us, 64 sequences with
-    // weights 90.3 against 100.5, one of 131072 slots 27.9 against 28.9
-    k.whole_tiles = c->block_size % 16 == 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
     p.part_of = p.lse + align256(split ? (int64_t)a->num_seqs * a->q_heads * 4 : 0);
@@ -297,9 +298,11 @@ int32_t kv_ops_sync(kv_ops_t *o)
     if (e != cudaSuccess) return fail_cuda(o, e, "cudaStreamSynchronize");
     const unsigned st = *(volatile unsigned *)o->status_host;
     if (st && o->sticky == KV_OK) {
-        o->sticky = KV_ERR_RANGE;
-        snprintf(o->err, 256, "a kernel met %s and skipped it (status 0x%x)",
-                 st & KV_OPS_BAD_BLOCK ? "a block id outside the cache" : "a length outside its bounds", st);
+        o->sticky = st & KV_OPS_TIMEOUT ? KV_ERR_TIMEOUT : KV_ERR_RANGE;
+        if (st & KV_OPS_TIMEOUT) snprintf(o->err, 256, "a wait inside a kernel ran out (status 0x%x)", st);
+        else
+            snprintf(o->err, 256, "a kernel met %s and skipped it (status 0x%x)",
+                     st & KV_OPS_BAD_BLOCK ? "a block id outside the cache" : "a length outside its bounds", st);
     }
     return o->sticky;
 }
@@ -362,7 +365,7 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     }
     void *params[] = {&k};
     const unsigned rows = (unsigned)(k.seqs * k.head_chunks * k.group_chunks);
-    cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3(p.warps * 32), params, p.smem, o->stream);
+    cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3((p.warps + (q4 ? 1 : 0)) * 32), params, p.smem, o->stream);
     if (e != cudaSuccess) return fail_cuda(o, e, "kv_attend");
     if (k.pieces) {
         // programmatic dependent launch: the join's CTAs come up while the last of the stream's finish

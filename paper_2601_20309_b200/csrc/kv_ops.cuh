@@ -15,6 +15,7 @@
 #include <stdint.h>
 
 #define KV_OPS_BAD_BLOCK 1u   // a live slot's block id lies outside the pool: the slot was skipped
+#define KV_OPS_TIMEOUT   4u   // a wait inside a kernel ran out: its results are not to be used
 #define KV_OPS_BAD_LEN   2u   // a length outside [0, max_len]: the sequence was taken as empty
 
 struct KvView {

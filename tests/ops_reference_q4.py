@@ -27,7 +27,7 @@ def quantise(x):
     for a in range(0, x.shape[-1], 32):
         y = x[..., a:a + 32].float()
         low, high = y.amin(-1, keepdim=True), y.amax(-1, keepdim=True)      # NaN wherever one is
-        s = torch.maximum((high - low) / 15, low.abs() * 2.0 ** -20).to(torch.bfloat16).double()
+        s = torch.maximum((high - low) * torch.tensor(1 / 15), low.abs() * 2.0 ** -20).to(torch.bfloat16).double()
         bad = ~(torch.isfinite(y).all(-1, keepdim=True) & torch.isfinite(s))
         d = (y - low).double()
         c = torch.where(s > 0, torch.floor(d / s.masked_fill(s <= 0, 1.0) + 0.5), torch.zeros_like(d)).clamp(0, 15)
