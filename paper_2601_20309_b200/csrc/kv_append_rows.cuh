@@ -27,6 +27,7 @@ struct KvAppendRows {
     float eps;
     int lanes_log2;              // lanes of a row
     int turns;                   // lanes that hold what turns
+    int splits, per_split;       // CTAs that share a token's rows (where there are few tokens), rows of each
 };
 
 // a word of a group that is not finite
@@ -66,15 +67,17 @@ template <typename T> __device__ __forceinline__ unsigned kv_quantise(const unsi
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float2 v = kv_unpair(x[j], T());
+        unsigned pair = 0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float d = ((e ? v.y : v.x) - lo) * lift;
-            float n = floorf(fmaf(d, inv, 0.5f));
-            const float left = fmaf(-n, s, d);
-            n += (left >= border ? 1.f : 0.f) - (left < -border ? 1.f : 0.f);
-            const unsigned code = 2 * j < count ? (unsigned)fminf(fmaxf(n, 0.f), 15.f) : 0u;
-            codes[j >> 2] |= code << (4 * (2 * (j & 3) + e));
+            const float d = ((e ? v.y : v.x) - lo) * lift, t = __fadd_rd(fmaf(d, inv, 0.5f), 0x1p23f);   // 2^23 + the code, rounded down
+            const float left = fmaf(0x1p23f - t, s, d);
+            int n = __float_as_int(t) - __float_as_int(0x1p23f);
+            if (left >= border) ++n;
+            if (left < -border) --n;
+            pair |= (unsigned)min(max(n, 0), 15) << (4 * e);
         }
+        codes[j >> 2] |= (2 * j < count ? pair : 0u) << (8 * (j & 3));
     }
     return word;
 }
@@ -116,12 +119,12 @@ template <int V> __device__ __forceinline__ void kv_store_run(void *to, const un
     }
 }
 
-constexpr int AR_WEIGHTS = 256;      // elements of a head, at most
+constexpr int AR_WEIGHTS = 256 + 16;         // elements of a head, at most, and those of the last run that are none
 
 // Dynamic shared memory: [token][4][turns] float4 of cosine and sine of two frequencies each; packed caches further have
 // [token][8][turns] double2 in front, and [row of the CTA][padded dim] elements behind
 template <typename T, int V, bool Q4>
-__global__ void __launch_bounds__(AP_THREADS) kv_append_rows(const __grid_constant__ KvAppendRows b)
+__global__ void __launch_bounds__(AP_THREADS, Q4 ? 3 : 4) kv_append_rows(const __grid_constant__ KvAppendRows b)
 {
     const KvAppend &a = b.p;
     extern __shared__ __align__(16) uint8_t ar_smem[];
@@ -129,7 +132,9 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_rows(const __grid_consta
     __shared__ long long meta[AP_TOKENS];
     __shared__ int to_words[AP_TOKENS];
     __shared__ __align__(16) float weight[2][AR_WEIGHTS];
-    const int tid = threadIdx.x, dim = a.c.dim, half = a.rotary >> 1, heads = a.c.heads, q_heads = a.q ? a.q_heads : 0, rows = q_heads + 2 * heads;
+    __shared__ __align__(16) double k_weight[Q4 ? AR_WEIGHTS : 2];
+    const int tid = threadIdx.x, dim = a.c.dim, half = a.rotary >> 1, heads = a.c.heads, q_heads = a.q ? a.q_heads : 0;
+    const int split = b.splits > 1 ? blockIdx.x % b.splits : 0, row0 = split * b.per_split, rows = min(b.per_split, q_heads + 2 * heads - row0);
     const int L = 1 << b.lanes_log2, u = tid & (L - 1), mine = tid >> b.lanes_log2, lanes = AP_THREADS >> b.lanes_log2, turns = b.turns;
     const unsigned mask = (L == 32 ? ~0u : (1u << L) - 1) << (tid & 31 & ~(L - 1));      // the lanes of this row
     const bool halves = a.pairs_style == 0;
@@ -137,208 +142,231 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_rows(const __grid_consta
     float4 *turn = (float4 *)(ar_smem + (Q4 ? a.per * 8 * turns * 16 : 0));
     T *cross = (T *)(ar_smem + a.per * turns * (Q4 ? 192 : 64)) + mine * a.c.groups * 32;
 
-    // the two runs of the lane in a row of q or k, and in one of v
+    // The two runs of the lane in a row of q or k, and in one of v.  What a run has beyond its elements is zero, is worked on like them and
+    // goes nowhere
     const bool turned = u < turns;
     const int b0 = turned ? (halves ? 8 * u : 16 * u) : a.rotary + 16 * (u - turns), b1 = turned && halves ? half + 8 * u : b0 + 8;
     const int end0 = turned ? (halves ? half : a.rotary) : dim, end1 = turned ? a.rotary : dim;
     const int n0 = min(max(end0 - b0, 0), 8), n1 = min(max(end1 - b1, 0), 8);
+    const int w0 = n0 ? b0 : 0, w1 = n1 ? b1 : 0;        // where their weights are
     const int v0 = 16 * u, vn0 = min(max(dim - v0, 0), 8), vn1 = min(max(dim - v0 - 8, 0), 8);
 
-    const long long first = (long long)blockIdx.x * a.per;
+    const long long first = (long long)(blockIdx.x / b.splits) * a.per;
     const int tokens = (int)min((long long)a.per, a.num_tokens - first), total = tokens * rows;
-    for (int r0 = mine; r0 - mine < total; r0 += lanes * AP_ROWS) {
-        unsigned x[AP_ROWS][4], y[AP_ROWS][4];
-        int token[AP_ROWS], row[AP_ROWS];
-#pragma unroll
-        for (int n = 0; n < AP_ROWS; ++n) {
-            const int r = r0 + n * lanes;
-            row[n] = -1;
-            token[n] = 0;
-            if (r < total) {
-                token[n] = (int)__umulhi((unsigned)r, a.by_rows);
-                row[n] = r - token[n] * rows;
-                const long long t = first + token[n];
-                const bool is_v = row[n] >= q_heads + heads;
-                const T *from = row[n] < q_heads ? (const T *)a.q + t * a.q_tok + row[n] * a.q_head
-                                : is_v           ? (const T *)a.v + t * a.v_tok + (row[n] - q_heads - heads) * a.v_head
-                                                 : (const T *)a.k + t * a.k_tok + (row[n] - q_heads) * a.k_head;
-                kv_load_run<V>(x[n], from + (is_v ? v0 : b0), is_v ? vn0 : n0);
-                kv_load_run<V>(y[n], from + (is_v ? v0 + 8 : b1), is_v ? vn1 : n1);
-            }
-        }
-        if (r0 == mine) {            // the first time: weights that all heads share, angles and slots
-            for (int d = tid; d < 2 * dim; d += AP_THREADS) {
-                const int of_k = d >= dim, e = d - of_k * dim;
-                const void *w = of_k ? b.k_w : b.q_w;
-                if (w && (of_k ? b.k_w_head : b.q_w_head) == 0) weight[of_k][e] = b.w_float ? ((const float *)w)[e] : kv_float(((const T *)w)[e]);
-            }
-            for (int f = tid; f < tokens * half; f += AP_THREADS) {
-                const int k = f / half, q = f - k * half, lane = q >> 3, j = q & 7;
-                const double cycles = (double)a.positions[a.axis_of[q] * a.axis_stride + first + k] * (double)a.inv_freq[q] * 0.15915494309189533577;
-                const double turned_by = 2.0 * (cycles - rint(cycles));
-                float2 cs;
-                if constexpr (Q4) {
-                    double2 z;
-                    sincospi(turned_by, &z.y, &z.x);
-                    wide[(k * 8 + j) * turns + lane] = z;
-                    cs = make_float2((float)z.x, (float)z.y);
-                } else
-                    sincospif((float)turned_by, &cs.y, &cs.x);
-                ((float2 *)(turn + (k * 4 + (j >> 1)) * turns + lane))[j & 1] = cs;
-            }
-            for (int k = tid >> 5; k < tokens; k += AP_THREADS / 32) {
-                const long long t = first + k;
-                const int i = a.starts ? kv_seq_of(a.starts, a.num_seqs, t) : (int)t;
-                const long long left = a.starts ? a.starts[i + 1] - t : 1;       // this token and those behind it
-                const bool member = !a.starts || a.starts[i] <= t;               // not one in front of the first start
-                const int n = a.c.len(i);
-                const long long s = n - left;
-                const bool ok = member && left > 0 && s >= 0 && (!(a.weights || a.order) || s < a.num_slots);
-                if ((tid & 31) == 0) {
-                    if (!ok && n > 0) atomicOr(a.c.status, KV_OPS_BAD_LEN);
-                    kv_row[k] = ok ? a.c.slot(i, (int)s, a.layer * 2) : nullptr;
-                    meta[k] = i * a.m_seq + s;
-                    if (Q4) to_words[k] = ok ? a.c.to_words((int)s) : 0;
-                }
-            }
-            __syncthreads();
-        }
-#pragma unroll
-        for (int n = 0; n < AP_ROWS; ++n) {
-            if (row[n] < 0) continue;            // all lanes of the row
-            const bool is_q = row[n] < q_heads, is_v = row[n] >= q_heads + heads;
-            const int h = row[n] - (is_q ? 0 : is_v ? q_heads + heads : q_heads);
-            uint8_t *slot = kv_row[token[n]];
-            if (!is_q && !slot) continue;
-            const void *wp = is_q ? b.q_w : is_v ? nullptr : b.k_w;
-            const long long w_head = is_q ? b.q_w_head : b.k_w_head;
-            const float *ws = weight[is_q ? 0 : 1];
-            auto norm_weight = [&](int e) {
-                if (w_head == 0) return ws[e];
-                return b.w_float ? ((const float *)wp)[h * w_head + e] : kv_float(((const T *)wp)[h * w_head + e]);
-            };
-            if (Q4 && !is_q && !is_v) {          // a key in float64
-                double r = 1.0;
-                if (wp) {
-                    double sum = 0.0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 p = kv_unpair(x[n][j], T()), q = kv_unpair(y[n][j], T());
-                        sum = fma((double)p.x, (double)p.x, fma((double)p.y, (double)p.y, sum));
-                        sum = fma((double)q.x, (double)q.x, fma((double)q.y, (double)q.y, sum));
-                    }
-                    for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
-                    r = 1.0 / sqrt(sum / dim + (double)b.eps);
-                }
-                // elements p and q of the two runs, or neighbours p.x and p.y
-                auto normed = [&](float v, int e, bool on) { return wp && on ? (double)v * r * (double)norm_weight(e) : (double)v; };
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 p = kv_unpair(x[n][j], T()), q = kv_unpair(y[n][j], T());
-                    double p0 = normed(p.x, b0 + 2 * j, 2 * j < n0), p1 = normed(p.y, b0 + 2 * j + 1, 2 * j + 1 < n0);
-                    double q0 = normed(q.x, b1 + 2 * j, 2 * j < n1), q1 = normed(q.y, b1 + 2 * j + 1, 2 * j + 1 < n1);
-                    if (turned) {
-                        const double2 *cs = wide + token[n] * 8 * turns + u;
-                        auto rotate = [](double &f, double &g, double2 c) {
-                            const double t = f * c.x - g * c.y;
-                            g = f * c.y + g * c.x;
-                            f = t;
-                        };
-                        if (halves) {
-                            if (2 * j < n0) rotate(p0, q0, cs[2 * j * turns]);
-                            if (2 * j + 1 < n0) rotate(p1, q1, cs[(2 * j + 1) * turns]);
-                        } else {
-                            if (2 * j < n0) rotate(p0, p1, cs[j * turns]);
-                            if (2 * j < n1) rotate(q0, q1, cs[(4 + j) * turns]);
-                        }
-                    }
-                    x[n][j] = kv_pair((float)p0, (float)p1, T());
-                    y[n][j] = kv_pair((float)q0, (float)q1, T());
-                }
-            } else if (!is_v) {
-                float r = 1.f;
-                if (wp) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 p = kv_unpair(x[n][j], T()), q = kv_unpair(y[n][j], T());
-                        sum += p.x * p.x + p.y * p.y + (q.x * q.x + q.y * q.y);
-                    }
-                    for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
-                    r = 1.f / sqrtf(sum / dim + b.eps);
-                }
-                auto normed = [&](float v, int e, bool on) { return wp && on ? v * r * norm_weight(e) : v; };
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 p = kv_unpair(x[n][j], T()), q = kv_unpair(y[n][j], T());
-                    float p0 = normed(p.x, b0 + 2 * j, 2 * j < n0), p1 = normed(p.y, b0 + 2 * j + 1, 2 * j + 1 < n0);
-                    float q0 = normed(q.x, b1 + 2 * j, 2 * j < n1), q1 = normed(q.y, b1 + 2 * j + 1, 2 * j + 1 < n1);
-                    if (turned) {
-                        const float4 *cs = turn + token[n] * 4 * turns + u;
-                        auto rotate = [](float &f, float &g, float cosine, float sine) {
-                            const float t = f * cosine - g * sine;
-                            g = f * sine + g * cosine;
-                            f = t;
-                        };
-                        if (halves) {
-                            if (2 * j < n0) {
-                                const float4 c = cs[j * turns];
-                                rotate(p0, q0, c.x, c.y);
-                                if (2 * j + 1 < n0) rotate(p1, q1, c.z, c.w);
-                            }
-                        } else {
-                            if (2 * j < n0) {
-                                const float4 c = cs[(j >> 1) * turns];
-                                rotate(p0, p1, j & 1 ? c.z : c.x, j & 1 ? c.w : c.y);
-                            }
-                            if (2 * j < n1) {
-                                const float4 c = cs[(2 + (j >> 1)) * turns];
-                                rotate(q0, q1, j & 1 ? c.z : c.x, j & 1 ? c.w : c.y);
-                            }
-                        }
-                    }
-                    x[n][j] = kv_pair(p0, p1, T());
-                    y[n][j] = kv_pair(q0, q1, T());
-                }
-            }
-            if (is_q || !Q4) {
-                T *to = is_q ? (T *)a.q_out + (first + token[n]) * a.qo_tok + h * a.qo_head
-                             : (T *)(slot + (is_v ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride);
-                kv_store_run<V>(to + (is_v ? v0 : b0), x[n], is_v ? vn0 : n0);
-                kv_store_run<V>(to + (is_v ? v0 + 8 : b1), y[n], is_v ? vn1 : n1);
-                continue;
-            }
-            if constexpr (Q4) {
-                unsigned e[8], codes[2];
-                if (!is_v) {                     // from pairs to neighbours
-                    __syncwarp(mask);            // what an earlier key left is read
-                    kv_store_run<V>(cross + b0, x[n], n0);
-                    kv_store_run<V>(cross + b1, y[n], n1);
-                    __syncwarp(mask);
-                    if (vn0 > 0) kv_load_run<8>(x[n], cross + v0, 8);
-                    if (vn1 > 0) kv_load_run<8>(y[n], cross + v0 + 8, 8);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    e[j] = x[n][j];
-                    e[4 + j] = y[n][j];
-                }
-                const unsigned word = kv_quantise<T>(e, vn0 + vn1, mask, codes);
-                const int G = a.c.groups, g = u >> 1;
-                if (g >= G) continue;
-                uint8_t *at = slot + (is_v ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride;
-                if (is_v) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) ((unsigned short *)at)[((u & 1) * 4 + k) * G + g] = (unsigned short)(codes[k >> 1] >> (16 * (k & 1)));
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) ((unsigned *)at)[((u & 1) * 2 + k) * G + g] = codes[k];
-                }
-                if ((u & 1) == 0) ((unsigned *)(at + to_words[token[n]]))[g] = word;
-            }
+    unsigned x[4], y[4], x1[4], y1[4];                   // of the row at hand, and of the next one
+    int token1, row1;
+    auto fetch = [&](int r) {
+        row1 = -1;
+        if (r >= total) return;
+        token1 = b.splits > 1 ? 0 : (int)__umulhi((unsigned)r, a.by_rows);
+        row1 = row0 + r - token1 * rows;
+        const long long t = first + token1;
+        const bool is_v = row1 >= q_heads + heads;
+        const T *from = row1 < q_heads ? (const T *)a.q + t * a.q_tok + row1 * a.q_head
+                        : is_v         ? (const T *)a.v + t * a.v_tok + (row1 - q_heads - heads) * a.v_head
+                                       : (const T *)a.k + t * a.k_tok + (row1 - q_heads) * a.k_head;
+        kv_load_run<V>(x1, from + (is_v ? v0 : b0), is_v ? vn0 : n0);
+        kv_load_run<V>(y1, from + (is_v ? v0 + 8 : b1), is_v ? vn1 : n1);
+    };
+    fetch(mine);
+    // weights that all heads share, angles and slots, while that is on its way
+    const bool has_k = row0 + rows > q_heads && row0 < q_heads + heads;
+    for (int d = tid; d < 2 * dim; d += AP_THREADS) {
+        const int of_k = d >= dim, e = d - of_k * dim;
+        const void *w = of_k ? b.k_w : b.q_w;
+        if (w && (of_k ? b.k_w_head : b.q_w_head) == 0) {
+            const float v = b.w_float ? ((const float *)w)[e] : kv_float(((const T *)w)[e]);
+            if (Q4 && of_k) k_weight[e] = (double)v;
+            else weight[of_k][e] = v;
         }
     }
-    if (a.weights || a.order)
+    for (int f = tid; f < tokens * half; f += AP_THREADS) {
+        const int k = f / half, q = f - k * half, lane = q >> 3, j = q & 7;
+        const double cycles = (double)a.positions[a.axis_of[q] * a.axis_stride + first + k] * (double)a.inv_freq[q] * 0.15915494309189533577;
+        const double turned_by = 2.0 * (cycles - rint(cycles));
+        if (Q4 && has_k) {
+            double2 z;
+            sincospi(turned_by, &z.y, &z.x);
+            wide[(k * 8 + j) * turns + lane] = z;
+        }
+        float2 cs;
+        sincospif((float)turned_by, &cs.y, &cs.x);
+        ((float2 *)(turn + (k * 4 + (j >> 1)) * turns + lane))[j & 1] = cs;
+    }
+    for (int k = tid >> 5; k < tokens; k += AP_THREADS / 32) {
+        const long long t = first + k;
+        const int i = a.starts ? kv_seq_of(a.starts, a.num_seqs, t) : (int)t;
+        const long long left = a.starts ? a.starts[i + 1] - t : 1;       // this token and those behind it
+        const bool member = !a.starts || a.starts[i] <= t;               // not one in front of the first start
+        const int n = a.c.len(i);
+        const long long s = n - left;
+        const bool ok = member && left > 0 && s >= 0 && (!(a.weights || a.order) || s < a.num_slots);
+        if ((tid & 31) == 0) {
+            if (!ok && n > 0) atomicOr(a.c.status, KV_OPS_BAD_LEN);
+            kv_row[k] = ok ? a.c.slot(i, (int)s, a.layer * 2) : nullptr;
+            meta[k] = i * a.m_seq + s;
+            if (Q4) to_words[k] = ok ? a.c.to_words((int)s) : 0;
+        }
+    }
+    __syncthreads();
+    for (int r = mine; r < total; r += lanes) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = x1[j];
+            y[j] = y1[j];
+        }
+        const int token = token1, row = row1;
+        fetch(r + lanes);
+        const bool is_q = row < q_heads, is_v = row >= q_heads + heads;
+        const int h = row - (is_q ? 0 : is_v ? q_heads + heads : q_heads);
+        uint8_t *slot = kv_row[token];
+        if (!is_q && !slot) continue;            // all lanes of the row
+        if (Q4 && !is_q && !is_v) {              // a key in float64
+            double rn = 1.0;
+            if (b.k_w) {
+                double sum = 0.0, sum2 = 0.0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = kv_unpair(x[j], T()), g = kv_unpair(y[j], T());
+                    const double f0 = f.x, f1 = f.y, g0 = g.x, g1 = g.y;
+                    sum = fma(f0, f0, sum);
+                    sum2 = fma(f1, f1, sum2);
+                    sum = fma(g0, g0, sum);
+                    sum2 = fma(g1, g1, sum2);
+                }
+                sum += sum2;
+                for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
+                rn = 1.0 / sqrt(sum / dim + (double)b.eps);
+            }
+            const double2 *cs = wide + token * 8 * turns + u;
+            const bool own = b.k_w && b.k_w_head != 0;
+            auto weigh = [&](float v, int e) {   // elements of the last run that are none have any weight
+                if (!b.k_w) return (double)v;
+                const double w = !own ? k_weight[e] : e >= dim ? 0.0 : b.w_float ? (double)((const float *)b.k_w)[h * b.k_w_head + e] : (double)kv_float(((const T *)b.k_w)[h * b.k_w_head + e]);
+                return (double)v * rn * w;
+            };
+            auto rotate = [](double &f, double &g, double2 c) {
+                const double t = f * c.x - g * c.y;
+                g = f * c.y + g * c.x;
+                f = t;
+            };
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = kv_unpair(x[j], T()), g = kv_unpair(y[j], T());
+                double f0 = weigh(f.x, w0 + 2 * j), f1 = weigh(f.y, w0 + 2 * j + 1), g0 = weigh(g.x, w1 + 2 * j), g1 = weigh(g.y, w1 + 2 * j + 1);
+                if (turned) {
+                    if (halves) {
+                        rotate(f0, g0, cs[2 * j * turns]);
+                        rotate(f1, g1, cs[(2 * j + 1) * turns]);
+                    } else {
+                        rotate(f0, f1, cs[j * turns]);
+                        rotate(g0, g1, cs[(4 + j) * turns]);
+                    }
+                }
+                x[j] = kv_pair((float)f0, (float)f1, T());
+                y[j] = kv_pair((float)g0, (float)g1, T());
+            }
+        } else if (!is_v) {
+            float f[8], g[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 p = kv_unpair(x[j], T()), q = kv_unpair(y[j], T());
+                f[2 * j] = p.x, f[2 * j + 1] = p.y, g[2 * j] = q.x, g[2 * j + 1] = q.y;
+            }
+            const void *wp = is_q ? b.q_w : b.k_w;
+            if (wp) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = fmaf(f[j], f[j], fmaf(g[j], g[j], sum));
+                for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
+                const float rn = rsqrtf(sum / dim + b.eps);
+                const long long w_head = is_q ? b.q_w_head : b.k_w_head;
+                float w[8], z[8];
+                if (w_head == 0) {
+                    const float *ws = weight[is_q ? 0 : 1];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {        // runs of pairs begin anywhere
+                        w[j] = ws[w0 + j];
+                        z[j] = ws[w1 + j];
+                    }
+                } else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const long long e = h * w_head + b0 + j, e2 = h * w_head + b1 + j;
+                        w[j] = j >= n0 ? 0.f : b.w_float ? ((const float *)wp)[e] : kv_float(((const T *)wp)[e]);
+                        z[j] = j >= n1 ? 0.f : b.w_float ? ((const float *)wp)[e2] : kv_float(((const T *)wp)[e2]);
+                    }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    f[j] *= rn * w[j];
+                    g[j] *= rn * z[j];
+                }
+            }
+            if (turned) {
+                const float4 *cs = turn + token * 4 * turns + u;
+                auto rotate = [](float &p, float &q, float cosine, float sine) {
+                    const float t = p * cosine - q * sine;
+                    q = p * sine + q * cosine;
+                    p = t;
+                };
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {            // two frequencies
+                    const float4 c = cs[j * turns];
+                    if (halves) {
+                        rotate(f[2 * j], g[2 * j], c.x, c.y);
+                        rotate(f[2 * j + 1], g[2 * j + 1], c.z, c.w);
+                    } else if (j < 2) {
+                        rotate(f[4 * j], f[4 * j + 1], c.x, c.y);
+                        rotate(f[4 * j + 2], f[4 * j + 3], c.z, c.w);
+                    } else {
+                        rotate(g[4 * j - 8], g[4 * j - 7], c.x, c.y);
+                        rotate(g[4 * j - 6], g[4 * j - 5], c.z, c.w);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = kv_pair(f[2 * j], f[2 * j + 1], T());
+                y[j] = kv_pair(g[2 * j], g[2 * j + 1], T());
+            }
+        }
+        if (is_q || !Q4) {
+            T *to = is_q ? (T *)a.q_out + (first + token) * a.qo_tok + h * a.qo_head
+                         : (T *)(slot + (is_v ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride);
+            kv_store_run<V>(to + (is_v ? v0 : b0), x, is_v ? vn0 : n0);
+            kv_store_run<V>(to + (is_v ? v0 + 8 : b1), y, is_v ? vn1 : n1);
+            continue;
+        }
+        if constexpr (Q4) {
+            unsigned e[8], codes[2];
+            if (!is_v) {                         // from pairs to neighbours
+                __syncwarp(mask);                // what an earlier key left is read
+                kv_store_run<V>(cross + b0, x, n0);
+                kv_store_run<V>(cross + b1, y, n1);
+                __syncwarp(mask);
+                if (vn0 > 0) kv_load_run<8>(x, cross + v0, 8);
+                if (vn1 > 0) kv_load_run<8>(y, cross + v0 + 8, 8);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                e[j] = x[j];
+                e[4 + j] = y[j];
+            }
+            const unsigned word = kv_quantise<T>(e, vn0 + vn1, mask, codes);
+            const int G = a.c.groups, g = u >> 1;
+            if (g >= G) continue;
+            uint8_t *at = slot + (is_v ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride;
+            if (is_v) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) ((unsigned short *)at)[((u & 1) * 4 + k) * G + g] = (unsigned short)(codes[k >> 1] >> (16 * (k & 1)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) ((unsigned *)at)[((u & 1) * 2 + k) * G + g] = codes[k];
+            }
+            if ((u & 1) == 0) ((unsigned *)(at + to_words[token]))[g] = word;
+        }
+    }
+    if ((a.weights || a.order) && split == 0)
         for (int e = tid; e < tokens * heads; e += AP_THREADS) {
             const int k = e / heads, h = e - k * heads;
             if (!kv_row[k]) continue;

@@ -31,6 +31,12 @@ constexpr float KV_Q4_SLACK = 6.f, KV_Q4_LIFT = 8.f;
 constexpr int KV_Q4_LOWEST = -80;    // exponent of a step below which it counts as this: sums of 2^31 weights stay in range
 constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
 
+// Where sums and queries take more than 168 registers per thread, four warps come with the launch for the one that loads, and give
+// their registers to those that compute.  What they have together has to be there at the launch: kv_q4_fits
+__host__ __device__ constexpr bool kv_q4_wide(int groups, int tiles) { return groups * tiles > 4; }
+__host__ __device__ constexpr int kv_q4_loaders(int groups, int tiles) { return kv_q4_wide(groups, tiles) ? 4 : 1; }
+constexpr int KV_Q4_REGS = 224, KV_Q4_LOADER_REGS = 40;
+__host__ __device__ constexpr bool kv_q4_fits(int warps, int regs) { return warps * KV_Q4_REGS + 4 * KV_Q4_LOADER_REGS <= (warps + 4) * regs; }
 // tiles of 16 slots that a warp takes at once
 __host__ __device__ constexpr int kv_q4_sub(int groups, int tiles) { return groups * tiles <= 4 ? 2 : 1; }
 // bytes of a tile: K's and V's codes and words
@@ -42,6 +48,11 @@ __device__ __forceinline__ void kv_mma_f16(float (&c)[4], unsigned a0, unsigned 
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void kv_mma_f16_first(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a1, unsigned b0, unsigned b1, __half) { kv_mma_f16(c, a0, a1, a0, a1, b0, b1); }
 __device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a1, unsigned b0, unsigned b1, __nv_bfloat16)
@@ -95,14 +106,14 @@ __device__ __forceinline__ void kv_bulk(unsigned dst, const uint8_t *src, int by
 }
 
 template <typename T, int G, int NT>
-__global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) kv_attend_q4(const __grid_constant__ KvAttend a)
 {
     constexpr int PLANE = 320 * G, WORDS = 256 * G, HEADS = 8 * NT;     // bytes of a tile's plane, and of its codes
     constexpr int PARTS = G == 8 ? 2 : 1;        // matrix instructions for the sum over lo
     constexpr int SUB = kv_q4_sub(G, NT);
     constexpr bool EXACT = std::is_same<T, __half>::value;      // see R below
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int red[KV_Q4_WARPS + 1], s_at[2], gave_up;
+    __shared__ int red[KV_Q4_WARPS + 4], s_at[2], gave_up;
     __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
     __shared__ float s_lse[KV_ATTEND_WARPS][HEADS];
     __shared__ __align__(8) unsigned long long bars[2][KV_Q4_STAGES];    // filled, empty
@@ -151,11 +162,15 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
     __syncthreads();                 // the barriers are there
     const int k0 = pk;
 
-    if (warp == warps) {
+    if (warp >= (int)(blockDim.x >> 5) - kv_q4_loaders(G, NT)) {
+        if constexpr (kv_q4_wide(G, NT)) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(KV_Q4_LOADER_REGS));
+            if (warp & 3) return;
+        }
         // ---- the loading warp.  A stage is a step: [tile][K, V][KV head][codes, words].  The block ids of the next step are read while
-        // this one's copies are issued.  A lane looks after a tile, or, where blocks do not hold whole tiles, after four rows of
-        // one (blocks are multiples of four rows).
-        const int stage_bytes = a.tw * a.hc * 2 * PLANE, quads = a.whole_tiles ? 1 : 4, per = 16 / quads, roles = a.tw * quads;
+        // this one's copies are issued.  A lane looks after a tile, or, where blocks do not hold whole tiles, after the eight or four
+        // rows of one that always lie in one block (blocks are multiples of four rows).
+        const int stage_bytes = a.tw * a.hc * 2 * PLANE, runs = a.whole_tiles ? 1 : a.c.bs % 8 == 0 ? 2 : 4, per = 16 / runs, roles = a.tw * runs;
         const unsigned ring = (unsigned)__cvta_generic_to_shared(smem);
         const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
         KvSpan span(a, pi);
@@ -186,13 +201,13 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
             const bool load = mask != 0;
             const int r = row;
             const uint8_t *from = load ? kbase + id * a.c.blk_stride + (long long)(pch / a.group_chunks * a.hc) * a.c.head_stride : a.c.base;
-            if (quads == 4) {
-                mask <<= 4 * (lane & 3);
+            if (runs > 1) {
+                mask <<= per * (lane % runs);
                 mask |= __shfl_xor_sync(~0u, mask, 1);
-                mask |= __shfl_xor_sync(~0u, mask, 2);
+                if (runs == 4) mask |= __shfl_xor_sync(~0u, mask, 2);
             }
             const int bytes = __popc(__ballot_sync(~0u, load)) * per * 40 * G * a.hc;
-            const int4 what = make_int4((int)mask | flags, t0 + lane / quads * 16, pi, pch);
+            const int4 what = make_int4((int)mask | flags, t0 + lane / runs * 16, pi, pch);
             // the cursor moves, and the next step's ids are on their way while this one is issued
             if (++pk == psteps && n + 1 < todo) {
                 pk = 0;
@@ -205,7 +220,7 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
             }
             if (n + 1 < todo) peek();
             if (n >= a.stages) kv_mbar_wait(empty + 8 * put, (n / a.stages - 1) & 1, &gave_up, a.c.status);
-            if (lane < roles && lane % quads == 0) info[put][lane / quads] = what;
+            if (lane < roles && lane % runs == 0) info[put][lane / runs] = what;
             __syncwarp();
             const unsigned stage = ring + put * stage_bytes, bar = filled + 8 * put;
             if (lane == 0) kv_mbar_expect(bar, bytes);
@@ -220,7 +235,7 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
                     const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, role & 31);
                     const int on = __shfl_sync(~0u, (int)load, role & 31), in = __shfl_sync(~0u, r, role & 31);
                     if (role < roles && on)
-                        kv_bulk(stage + ((role / quads * 2 + plane) * a.hc + h) * PLANE + (words ? WORDS : 0) + role % quads * per * (words ? 4 : 16) * G,
+                        kv_bulk(stage + ((role / runs * 2 + plane) * a.hc + h) * PLANE + (words ? WORDS : 0) + role % runs * per * (words ? 4 : 16) * G,
                                 (const uint8_t *)p + (plane ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride + (words ? a.c.bs * 16 * G + in * 4 * G : in * 16 * G),
                                 per * (words ? 4 : 16) * G, bar);
                 }
@@ -230,6 +245,8 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
     }
 
     // ---- a computing warp
+    if constexpr (kv_q4_wide(G, NT)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(KV_Q4_REGS));
+    if (warp >= warps) return;
     const int hw = warp % a.hc, way = warp / a.hc, threads = warps * 32;
     auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); };
     const int rho = lane >> 2, j = lane & 3, slot = (rho >> 1) + 4 * (rho & 1);
@@ -245,7 +262,10 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
     int top_step = KV_Q4_LOWEST;
     int take = 0;
     unsigned parity = 0;
+    int h = 0, g0 = 0, heads = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
+    const int stage_bytes = a.tw * a.hc * 2 * PLANE, to_v = a.hc * PLANE, to_next = 2 * to_v;
+    const uint8_t *own = smem + (way * SUB * 2 * a.hc + hw) * PLANE;
     for (int n = 0; n < todo; ++n) {
         kv_mbar_wait(filled + 8 * take, parity, &gave_up, a.c.status);
         const int4 tile = info[take][way * SUB];
@@ -257,11 +277,11 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
             some |= mask[u];
             all &= mask[u];
         }
-        const uint8_t *kt = smem + ((take * a.tw + way * SUB) * 2 * a.hc + hw) * PLANE;
-        const int to_v = a.hc * PLANE, to_next = 2 * to_v;
-        const int h = tile.w / a.group_chunks * a.hc + hw, g0 = tile.w % a.group_chunks * HEADS;   // first query head in the group
-        const int heads = min(HEADS, a.group - g0);
+        const uint8_t *kt = own + take * stage_bytes;
         if (tile.x & 1 << 16) {
+            h = tile.w / a.group_chunks * a.hc + hw;
+            g0 = tile.w % a.group_chunks * HEADS;
+            heads = min(HEADS, a.group - g0);
             began = tile.x & 1 << 18;
             top_step = KV_Q4_LOWEST;
 #pragma unroll
@@ -320,12 +340,8 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
                 }
                 // columns of the instruction over lo: two groups, in a part per lane (or per register, of eight groups)
                 auto part = [](float x, int n) {
-                    float p = kv_float(kv_round<T>(x));
-                    for (int k = 0; k < n; ++k) {
-                        x -= p;
-                        p = kv_float(kv_round<T>(x));
-                    }
-                    return p;
+                    const float a0 = kv_float(kv_round<T>(x)), x1 = x - a0, a1 = kv_float(kv_round<T>(x1)), x2 = x1 - a1, a2 = kv_float(kv_round<T>(x2));
+                    return n & 2 ? n & 1 ? x2 - a2 : a2 : n & 1 ? a1 : a0;
                 };
                 if constexpr (G == 2) {
                     ql[nt][0][0] = kv_pair(part(sum[0], j), part(sum[1], j), T());
@@ -370,22 +386,16 @@ __global__ void __launch_bounds__(KV_Q4_WARPS * 32 + 32, 1) kv_attend_q4(const _
                 kv_lds(w0, at + word_at);
                 kv_lds(w1, at + word_at + 32 * G);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[u][nt][e] = 0.f;
-#pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const unsigned h0 = c0[g] >> 8, h1 = c1[g] >> 8;
                     const float s0 = __uint_as_float(w0[g] & 0xffff0000u), s1 = __uint_as_float(w1[g] & 0xffff0000u);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float x[4] = {0.f, 0.f, 0.f, 0.f};
-                        kv_mma_f16(x, c0[g] & 0x000f000fu, c1[g] & 0x000f000fu, c0[g] & 0x00f000f0u, c1[g] & 0x00f000f0u, qf[nt][g][0], qf[nt][g][1]);
+                        float x[4];
+                        kv_mma_f16_first(x, c0[g] & 0x000f000fu, c1[g] & 0x000f000fu, c0[g] & 0x00f000f0u, c1[g] & 0x00f000f0u, qf[nt][g][0], qf[nt][g][1]);
                         kv_mma_f16(x, h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u, qf[nt][g][2], qf[nt][g][3]);
-                        y[u][nt][0] = fmaf(s0, x[0], y[u][nt][0]);
-                        y[u][nt][1] = fmaf(s0, x[1], y[u][nt][1]);
-                        y[u][nt][2] = fmaf(s1, x[2], y[u][nt][2]);
-                        y[u][nt][3] = fmaf(s1, x[3], y[u][nt][3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[u][nt][e] = g == 0 ? (e < 2 ? s0 : s1) * x[e] : fmaf(e < 2 ? s0 : s1, x[e], y[u][nt][e]);
                     }
                 }
                 unsigned x0, x1, z0, z1;         // the two groups of this lane's columns

@@ -355,17 +355,24 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.part_ml = (float2 *)(o->ws + p.part_ml);
     k.part_o = (float *)(o->ws + p.part_o);
 
-    const bool bf16 = is_bf16(cache), q4 = k.c.groups != 0;
+    const bool bf16 = is_bf16(cache), q4 = k.c.groups != 0, wide = q4 && kv_q4_wide(k.c.groups, p.nt);
     const void *kernel = bf16 ? attend_kernel<__nv_bfloat16>(p.dp, p.nt, q4) : attend_kernel<__half>(p.dp, p.nt, q4);
     bool &ready = o->attend_ready[q4][bf16][p.dp / 128][p.nt - 1];
     if (!ready) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(227 * 1024 - 4096));
         if (e != cudaSuccess) return fail_cuda(o, e, "cudaFuncSetAttribute");
+        if (wide) {              // registers move between the warps: there must be enough of them at the launch
+            cudaFuncAttributes at;
+            const cudaError_t f = cudaFuncGetAttributes(&at, kernel);
+            if (f != cudaSuccess) return fail_cuda(o, f, "cudaFuncGetAttributes");
+            if (!kv_q4_fits(4, at.numRegs) || !kv_q4_fits(8, at.numRegs)) return fail(o, KV_ERR_UNSUPPORTED, "the kernel was built with too few registers");
+        }
         ready = true;
     }
+    const unsigned threads = 32 * (wide ? (p.warps + 3) / 4 * 4 + 4 : p.warps + (q4 ? 1 : 0));
     void *params[] = {&k};
     const unsigned rows = (unsigned)(k.seqs * k.head_chunks * k.group_chunks);
-    cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3((p.warps + (q4 ? 1 : 0)) * 32), params, p.smem, o->stream);
+    cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3(threads), params, p.smem, o->stream);
     if (e != cudaSuccess) return fail_cuda(o, e, "kv_attend");
     if (k.pieces) {
         // programmatic dependent launch: the join's CTAs come up while the last of the stream's finish
@@ -479,17 +486,24 @@ int32_t kv_append_normed(kv_ops_t *o, const kv_cache_t *cache, const kv_append_a
         const int lanes = std::max(r.turns + (int)ceil_div(cache->head_dim - a->rotary_dim, 16), 2 * k.c.groups);
         r.lanes_log2 = 0;
         while (1 << r.lanes_log2 < lanes) ++r.lanes_log2;
-        const int q4 = k.c.groups != 0, per_token = r.turns * (q4 ? 192 : 64);
-        if (per_token) k.per = std::min(k.per, 40 * 1024 / per_token);       // with the keys in passing 48 KB at most
+        const int q4 = k.c.groups != 0, per_token = r.turns * (q4 ? 192 : 64), at_once = AP_THREADS >> r.lanes_log2;
+        if (per_token) k.per = std::min(k.per, 32 * 1024 / per_token);       // with the keys in passing and the weights 46 KB at most
+        r.splits = 1;
+        r.per_split = (int)rows;
+        if (k.per == 1) {        // few tokens: their rows all at once, as far as there are SMs
+            r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, at_once), 4 * o->sms / a->num_tokens));
+            r.per_split = (int)ceil_div(rows, r.splits);
+            r.splits = (int)ceil_div(rows, r.per_split);
+        }
         r.p = k;
-        const size_t smem = (size_t)k.per * per_token + (q4 ? (size_t)(AP_THREADS >> r.lanes_log2) * k.c.groups * 64 : 0);
+        const size_t smem = (size_t)k.per * per_token + (q4 ? (size_t)at_once * k.c.groups * 64 : 0);
         const auto pick = [&](auto t) {
             using T = decltype(t);
             return q4 ? v == 8 ? kv_append_rows<T, 8, true> : v == 4 ? kv_append_rows<T, 4, true> : kv_append_rows<T, 1, true>
                       : v == 8 ? kv_append_rows<T, 8, false> : v == 4 ? kv_append_rows<T, 4, false> : kv_append_rows<T, 1, false>;
         };
         const auto kernel = bf16 ? pick(__nv_bfloat16()) : pick(__half());
-        kernel<<<(unsigned)ceil_div(a->num_tokens, k.per), AP_THREADS, smem, o->stream>>>(r);
+        kernel<<<(unsigned)(ceil_div(a->num_tokens, k.per) * r.splits), AP_THREADS, smem, o->stream>>>(r);
         return launched(o, "kv_append");
     }
     const unsigned grid = (unsigned)ceil_div(a->num_tokens, k.per);
