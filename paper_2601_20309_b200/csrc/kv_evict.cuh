@@ -123,14 +123,16 @@ struct KvWays {
 
 template <typename U, bool Q4> __device__ __forceinline__ void kv_evict_units(const KvEvict &a, int m, const KvWays &way)
 {
-    // units of K, then as many of V; in 4 bits a plane's are those of the codes, then of the words
+    // Units of K, then as many of V; in 4 bits a plane's are those of the codes, then of the words: 10 or 20 of a row, so ten per lane in
+    // flight are all of 32 rows
+    constexpr int FLIGHT = Q4 ? 10 : 8;
     const int lane = threadIdx.x & 31, codes = Q4 ? a.c.groups * 16 / (int)sizeof(U) : 0;
     const int half = Q4 ? a.c.groups * 20 / (int)sizeof(U) : a.c.dim / 8, units = 2 * half;
-    for (int e = lane; e < m * units; e += 32 * 8) {
-        U v[8];
-        uint8_t *to[8];
+    for (int e = lane; e < m * units; e += 32 * FLIGHT) {
+        U v[FLIGHT];
+        uint8_t *to[FLIGHT];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
+        for (int q = 0; q < FLIGHT; ++q) {
             const int f = e + q * 32, r = !Q4 && a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
             to[q] = nullptr;
             if (f < m * units) {
@@ -154,7 +156,7 @@ template <typename U, bool Q4> __device__ __forceinline__ void kv_evict_units(co
             }
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
+        for (int q = 0; q < FLIGHT; ++q)
             if (to[q]) *(U *)to[q] = v[q];
     }
 }

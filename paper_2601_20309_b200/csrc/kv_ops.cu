@@ -488,19 +488,35 @@ int32_t kv_append_normed(kv_ops_t *o, const kv_cache_t *cache, const kv_append_a
         while (1 << r.lanes_log2 < lanes) ++r.lanes_log2;
         const int q4 = k.c.groups != 0, per_token = r.turns * (q4 ? 192 : 64), at_once = AP_THREADS >> r.lanes_log2;
         if (per_token) k.per = std::min(k.per, 32 * 1024 / per_token);       // with the keys in passing and the weights 46 KB at most
+        const int abreast = 32 >> r.lanes_log2, warps = AP_THREADS / 32;
+        const int groups = (int)(ceil_div(a->q ? a->q_heads : 0, abreast) + 2 * ceil_div(cache->kv_heads, abreast));
         r.splits = 1;
-        r.per_split = (int)rows;
+        r.per_split = groups;
         if (k.per == 1) {        // few tokens: their rows all at once, as far as there are SMs
-            r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, at_once), 4 * o->sms / a->num_tokens));
-            r.per_split = (int)ceil_div(rows, r.splits);
-            r.splits = (int)ceil_div(rows, r.per_split);
+            r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(groups, warps), 4 * o->sms / a->num_tokens));
+            r.per_split = (int)ceil_div(groups, r.splits);
+            r.splits = (int)ceil_div(groups, r.per_split);
         }
+        // The number of runs a CTA's tokens are cut into: whichever gives the shortest way for the busiest warp, a task's beginning counted
+        // as a token's work
+        r.chunk = k.per;
+        for (int runs = 2; runs <= k.per; ++runs) {
+            const auto way = [&](int64_t chunk) { return ceil_div(groups * ceil_div(k.per, chunk), warps) * (chunk + 1); };
+            if (way(ceil_div(k.per, runs)) < way(r.chunk)) r.chunk = (int)ceil_div(k.per, runs);
+        }
+        r.by_groups = (unsigned)ceil_div(int64_t(1) << 32, groups);
+        r.by_dim = 1.f / cache->head_dim;
         r.p = k;
         const size_t smem = (size_t)k.per * per_token + (q4 ? (size_t)at_once * k.c.groups * 64 : 0);
+        // whole rows: heads of 64, 128 or 256, every lane's elements aligned and of one kind
+        const bool whole = v == 8 && lanes * 16 == cache->head_dim && lanes == 1 << r.lanes_log2 && lanes >= 4 && lanes <= 16;
         const auto pick = [&](auto t) {
             using T = decltype(t);
-            return q4 ? v == 8 ? kv_append_rows<T, 8, true> : v == 4 ? kv_append_rows<T, 4, true> : kv_append_rows<T, 1, true>
-                      : v == 8 ? kv_append_rows<T, 8, false> : v == 4 ? kv_append_rows<T, 4, false> : kv_append_rows<T, 1, false>;
+            using Kernel = void (*)(KvAppendRows);
+            const Kernel kernels[2][5] = {
+                {kv_append_rows<T, 1, false, 0>, kv_append_rows<T, 4, false, 0>, kv_append_rows<T, 8, false, 2>, kv_append_rows<T, 8, false, 3>, kv_append_rows<T, 8, false, 4>},
+                {kv_append_rows<T, 1, true, 0>, kv_append_rows<T, 4, true, 0>, kv_append_rows<T, 8, true, 2>, kv_append_rows<T, 8, true, 3>, kv_append_rows<T, 8, true, 4>}};
+            return kernels[q4][whole ? r.lanes_log2 : v >= 4 ? 1 : 0];
         };
         const auto kernel = bf16 ? pick(__nv_bfloat16()) : pick(__half());
         kernel<<<(unsigned)(ceil_div(a->num_tokens, k.per) * r.splits), AP_THREADS, smem, o->stream>>>(r);

@@ -64,11 +64,18 @@ __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant
             word[1] = ((const unsigned *)(row + to_words[token]))[g];
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
+                // a code in the lowest bits of a 16-bit word is code * 2^-24 in float16, four bits further code * 2^-20
                 const float lo = kv_unpair(word[p], T()).x, s = __uint_as_float(word[p] & 0xffff0000u);
+                const auto at = [&](float code, float unit) { return fmaf(s, code * unit, lo); };
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const unsigned c = codes[p][j >> 2] >> (8 * (j & 3));
-                    w[p][j] = kv_pair(fmaf(s, (float)(c & 15), lo), fmaf(s, (float)(c >> 4 & 15), lo), T());
+                for (int j = 0; j < 2; ++j) {
+                    const unsigned c = codes[p][j], d = c >> 8;
+                    const float2 x0 = kv_unpair(c & 0x000f000fu, __half()), x1 = kv_unpair(c & 0x00f000f0u, __half());     // elements 0 and 4, 1 and 5
+                    const float2 x2 = kv_unpair(d & 0x000f000fu, __half()), x3 = kv_unpair(d & 0x00f000f0u, __half());     // 2 and 6, 3 and 7
+                    w[p][4 * j] = kv_pair(at(x0.x, 0x1p24f), at(x1.x, 0x1p20f), T());
+                    w[p][4 * j + 1] = kv_pair(at(x2.x, 0x1p24f), at(x3.x, 0x1p20f), T());
+                    w[p][4 * j + 2] = kv_pair(at(x0.y, 0x1p24f), at(x1.y, 0x1p20f), T());
+                    w[p][4 * j + 3] = kv_pair(at(x2.y, 0x1p24f), at(x3.y, 0x1p20f), T());
                 }
             }
         } else {
