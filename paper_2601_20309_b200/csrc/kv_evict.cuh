@@ -121,48 +121,74 @@ struct KvWays {
     int2 words[32];          // in 4 bits: from there to the rows' words
 };
 
-template <typename U, bool Q4> __device__ __forceinline__ void kv_evict_units(const KvEvict &a, int m, const KvWays &way)
+__device__ __forceinline__ void kv_evict_units(const KvEvict &a, int m, const KvWays &way)
 {
-    // Units of K, then as many of V; in 4 bits a plane's are those of the codes, then of the words: 10 or 20 of a row, so ten per lane in
-    // flight are all of 32 rows
-    constexpr int FLIGHT = Q4 ? 10 : 8;
-    const int lane = threadIdx.x & 31, codes = Q4 ? a.c.groups * 16 / (int)sizeof(U) : 0;
-    const int half = Q4 ? a.c.groups * 20 / (int)sizeof(U) : a.c.dim / 8, units = 2 * half;
-    for (int e = lane; e < m * units; e += 32 * FLIGHT) {
-        U v[FLIGHT];
-        uint8_t *to[FLIGHT];
+    const int lane = threadIdx.x & 31, half = a.c.dim / 8, units = 2 * half;
+    for (int e = lane; e < m * units; e += 32 * 8) {
+        uint4 v[8];
+        uint8_t *to[8];
 #pragma unroll
-        for (int q = 0; q < FLIGHT; ++q) {
-            const int f = e + q * 32, r = !Q4 && a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
+        for (int q = 0; q < 8; ++q) {
+            const int f = e + q * 32, r = a.units_shift >= 0 ? f >> a.units_shift : f / units, u = f - r * units;
             to[q] = nullptr;
             if (f < m * units) {
                 const ulonglong2 w = way.row[r];
-                if constexpr (Q4) {
-                    const int in = u < half ? u : u - half;
-                    const int2 words = in < codes ? make_int2(in * (int)sizeof(U), in * (int)sizeof(U))
-                                                  : make_int2(way.words[r].x + (in - codes) * (int)sizeof(U), way.words[r].y + (in - codes) * (int)sizeof(U));
-                    const long long plane = u < half ? 0 : a.c.plane_stride;
-                    if (w.x) {
-                        v[q] = __ldcg((const U *)(w.x + plane + words.x));
-                        to[q] = (uint8_t *)(w.y + plane + words.y);
-                    }
-                } else {
-                    const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
-                    if (w.x) {
-                        v[q] = __ldcg((const U *)(w.x + off));
-                        to[q] = (uint8_t *)(w.y + off);
-                    }
+                const long long off = u < half ? u * 16 : a.c.plane_stride + (u - half) * 16;
+                if (w.x) {
+                    v[q] = __ldcg((const uint4 *)(w.x + off));
+                    to[q] = (uint8_t *)(w.y + off);
                 }
             }
         }
 #pragma unroll
-        for (int q = 0; q < FLIGHT; ++q)
-            if (to[q]) *(U *)to[q] = v[q];
+        for (int q = 0; q < 8; ++q)
+            if (to[q]) *(uint4 *)to[q] = v[q];
+    }
+}
+
+// The same in 4 bits.  K's and V's codes and words of a row are ten units of U (twenty of 16 bytes for eight groups); a lane has the same
+// unit of every third row (every row).  `box`: where the rows wait between reading and writing, so that all of them are on their way
+// at once and few registers are needed (in registers 107 us for 32 layers and 8 sequences in a steady state, so 93); without
+// one (few rows) three at a time
+constexpr int EV_BOX = 5120;
+template <typename U> __device__ __forceinline__ void kv_evict_units_q4(const KvEvict &a, int m, const KvWays &way, uint8_t *box)
+{
+    const int lane = threadIdx.x & 31, codes = a.c.groups * 16 / (int)sizeof(U), half = a.c.groups * 20 / (int)sizeof(U), units = 2 * half, abreast = 32 / units;
+    const int r0 = lane / units, u = lane - r0 * units, in = u < half ? u : u - half;
+    const long long plane = u < half ? 0 : a.c.plane_stride;
+    const bool word = in >= codes;
+    const int off = (word ? in - codes : in) * (int)sizeof(U);
+    if (box) {
+        const unsigned to = (unsigned)__cvta_generic_to_shared(box);
+        const int most = EV_BOX / (units * (int)sizeof(U));
+        for (int first = 0; first < m; first += most) {
+            const int end = min(m, first + most);
+            if (r0 < abreast)
+                for (int r = first + r0; r < end; r += abreast)
+                    if (way.row[r].x)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + ((r - first) * units + u) * (int)sizeof(U)),
+                                     "l"(way.row[r].x + plane + off + (word ? way.words[r].x : 0)), "n"((int)sizeof(U))
+                                     : "memory");
+            asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+            if (r0 < abreast)        // every lane writes what it read itself
+                for (int r = first + r0; r < end; r += abreast)
+                    if (way.row[r].x) *(U *)(way.row[r].y + plane + off + (word ? way.words[r].y : 0)) = *(const U *)(box + ((r - first) * units + u) * (int)sizeof(U));
+        }
+        return;
+    }
+    for (int r = r0; r < m; r += 3 * abreast) {
+        U v[3];
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            if (const int k = r + q * abreast; r0 < abreast && k < m && way.row[k].x) v[q] = __ldcg((const U *)(way.row[k].x + plane + off + (word ? way.words[k].x : 0)));
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            if (const int k = r + q * abreast; r0 < abreast && k < m && way.row[k].x) *(U *)(way.row[k].y + plane + off + (word ? way.words[k].y : 0)) = v[q];
     }
 }
 
 template <bool Q4>
-__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int m, int d, int s, KvWays &way)
+__device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem &p, int m, int d, int s, KvWays &way, uint8_t *box = nullptr)
 {
     const int lane = threadIdx.x & 31;
     if (lane < m) {
@@ -177,8 +203,9 @@ __device__ __forceinline__ void kv_evict_rows(const KvEvict &a, const KvProblem 
         }
     }
     __syncwarp();
-    if (Q4 && a.c.groups == 2) kv_evict_units<uint2, Q4>(a, m, way);     // words of two groups: 8 bytes
-    else kv_evict_units<uint4, Q4>(a, m, way);
+    if constexpr (!Q4) kv_evict_units(a, m, way);
+    else if (a.c.groups == 2) kv_evict_units_q4<uint2>(a, m, way, box);  // words of two groups: 8 bytes
+    else kv_evict_units_q4<uint4>(a, m, way, box);
     __syncwarp();
 }
 
@@ -722,12 +749,13 @@ template <bool Q4> __global__ void __launch_bounds__(EV_SMALL_THREADS) kv_evict_
 template <bool Q4> __global__ void __launch_bounds__(EV_MOVE_WARPS * 32) kv_evict_move(const __grid_constant__ KvEvict a)
 {
     __shared__ KvWays way[EV_MOVE_WARPS];
+    __shared__ __align__(16) uint8_t box[Q4 ? EV_MOVE_WARPS : 1][Q4 ? EV_BOX : 16];
     const int warp = threadIdx.x >> 5, j = blockIdx.x * 32, lane = threadIdx.x & 31;
     for (int y = blockIdx.y * EV_MOVE_WARPS + warp; y < a.problems; y += gridDim.y * EV_MOVE_WARPS) {
         const int n = a.count[y];
         if (j >= n) continue;
         const KvProblem p(a, y);
         const int at = min(j + lane, n - 1);
-        kv_evict_rows<Q4>(a, p, min(n - j, 32), a.holes[(long long)y * a.cap + at], a.srcs[(long long)y * a.cap + at], way[warp]);
+        kv_evict_rows<Q4>(a, p, min(n - j, 32), a.holes[(long long)y * a.cap + at], a.srcs[(long long)y * a.cap + at], way[warp], Q4 ? box[warp] : nullptr);
     }
 }
