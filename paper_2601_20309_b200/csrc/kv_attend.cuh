@@ -53,6 +53,7 @@ struct KvAttend {
     int pieces;          // CTAs the line of steps is cut for; 0: every row is one CTA's (no join)
     int min_steps;       // no piece is shorter
     int q_pairs;         // q may be read in pairs of elements
+    int block_tiles;     // of a 4-bit cache: tiles of a block where a step is made of whole blocks, else 0
     int q_vec, out_vec;  // of a 4-bit cache: q may be read in packs of 16 bytes, out written in packs of 8
     int whole_tiles;     // the block size is a multiple of 16: a tile lies in one block
     float *scores;       // [seq][kv_head][max_len][group], base 2; nullptr: no weights wanted

@@ -16,8 +16,8 @@
 //   scores: the running maximum plus the exponent of the largest step met so far, less 8.  Products below 2^-22 of the row's largest
 //   lose bits, below 2^-32 they vanish.  The reference moves only when a score passes it by 6 or a step is larger: a
 //   vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
-// Slots: row r of a matrix instruction is slot r/2 + 4 (r%2) of the tile for r < 8, and 8 more for the others, so that the lanes' reads
-// of V, two neighbouring rows of the contraction at once, fall into different banks.
+// Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
+// that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
 // Masked slots (beyond the length, before the window) are loaded with their tile where their block is known: codes are numbers
 // whatever they hold, scores are replaced by -inf and words by 0, so nothing of such a slot reaches a sum.
@@ -26,15 +26,14 @@
 
 #include "kv_attend.cuh"
 
-constexpr int KV_Q4_WARPS = 8, KV_Q4_STAGES = 6;     // warps that compute; one more loads
+constexpr int KV_Q4_WARPS = 8, KV_Q4_LOADERS = 4, KV_Q4_STAGES = 6;  // warps that compute, and that load
 constexpr float KV_Q4_SLACK = 6.f, KV_Q4_LIFT = 8.f;
 constexpr int KV_Q4_LOWEST = -80;    // exponent of a step below which it counts as this: sums of 2^31 weights stay in range
 constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
 
-// Where sums and queries take more than 168 registers per thread, four warps come with the launch for the one that loads, and give
-// their registers to those that compute.  What they have together has to be there at the launch: kv_q4_fits
+// Where sums and queries take more than 168 registers per thread, the warps that load give theirs to those that compute.  What all
+// have together has to be there at the launch: kv_q4_fits
 __host__ __device__ constexpr bool kv_q4_wide(int groups, int tiles) { return groups * tiles > 4; }
-__host__ __device__ constexpr int kv_q4_loaders(int groups, int tiles) { return kv_q4_wide(groups, tiles) ? 4 : 1; }
 constexpr int KV_Q4_REGS = 224, KV_Q4_LOADER_REGS = 40;
 __host__ __device__ constexpr bool kv_q4_fits(int warps, int regs) { return warps * KV_Q4_REGS + 4 * KV_Q4_LOADER_REGS <= (warps + 4) * regs; }
 // tiles of 16 slots that a warp takes at once
@@ -106,14 +105,14 @@ __device__ __forceinline__ void kv_bulk(unsigned dst, const uint8_t *src, int by
 }
 
 template <typename T, int G, int NT>
-__global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) kv_attend_q4(const __grid_constant__ KvAttend a)
+__global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_attend_q4(const __grid_constant__ KvAttend a)
 {
     constexpr int PLANE = 320 * G, WORDS = 256 * G, HEADS = 8 * NT;     // bytes of a tile's plane, and of its codes
     constexpr int PARTS = G == 8 ? 2 : 1;        // matrix instructions for the sum over lo
     constexpr int SUB = kv_q4_sub(G, NT);
     constexpr bool EXACT = std::is_same<T, __half>::value;      // see R below
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int red[KV_Q4_WARPS + 4], s_at[2], gave_up;
+    __shared__ int red[KV_Q4_WARPS + KV_Q4_LOADERS], s_at[2], gave_up;
     __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
     __shared__ float s_lse[KV_ATTEND_WARPS][HEADS];
     __shared__ __align__(8) unsigned long long bars[2][KV_Q4_STAGES];    // filled, empty
@@ -136,7 +135,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
     if (tid == 0) {
         gave_up = 0;
         for (int s = 0; s < a.stages; ++s) {
-            kv_mbar_init(filled + 8 * s, 1);
+            kv_mbar_init(filled + 8 * s, a.block_tiles ? 1 : 1 + 32 * KV_Q4_LOADERS);
             kv_mbar_init(empty + 8 * s, warps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -162,20 +161,24 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
     __syncthreads();                 // the barriers are there
     const int k0 = pk;
 
-    if (warp >= (int)(blockDim.x >> 5) - kv_q4_loaders(G, NT)) {
-        if constexpr (kv_q4_wide(G, NT)) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(KV_Q4_LOADER_REGS));
-            if (warp & 3) return;
-        }
-        // ---- the loading warp.  A stage is a step: [tile][K, V][KV head][codes, words].  The block ids of the next step are read while
-        // this one's copies are issued.  A lane looks after a tile, or, where blocks do not hold whole tiles, after the eight or four
-        // rows of one that always lie in one block (blocks are multiples of four rows).
+    const int loader = warp - ((int)(blockDim.x >> 5) - KV_Q4_LOADERS);
+    if (loader >= 0) {
+        if constexpr (kv_q4_wide(G, NT)) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(KV_Q4_LOADER_REGS));
+        // ---- loading.  A stage is a step.  The block ids of the next step are read while this one is on its way.  A lane looks after
+        // a tile, or, where blocks do not hold whole tiles, after the eight or four rows of one that always lie in one block (blocks
+        // are multiples of four rows).
+        //   Where a step is made of whole blocks, K and V of a block's heads are one bulk copy each, and the stage has what the blocks have:
+        // [block][K, V][KV head][codes of its tiles, words of its tiles].  One warp does that: a bulk copy takes the SM about 100 cycles,
+        // whatever its size, so 64 small ones for a step of 40 KB took 6600 cycles and four take what the memory takes.
+        //   Else four warps copy 16 bytes per lane: [tile][K, V][KV head][codes, words].
+        if (a.block_tiles && loader > 0) return;
         const int stage_bytes = a.tw * a.hc * 2 * PLANE, runs = a.whole_tiles ? 1 : a.c.bs % 8 == 0 ? 2 : 4, per = 16 / runs, roles = a.tw * runs;
         const unsigned ring = (unsigned)__cvta_generic_to_shared(smem);
         const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;
         KvSpan span(a, pi);
         int psteps = span.steps(a), id, row, put = 0;
         bool fresh = true;           // the next step begins this CTA's run in its row
+        constexpr int PIECES = (40 * G + 31) / 32;
         auto peek = [&]() {          // the lane's block id in the step the cursor is at
             const int t = span.base + pk * a.tw * 16 + lane * per;
             row = -1;                // no slot of the sequence
@@ -199,14 +202,14 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
                 mask = 0;
             }
             const bool load = mask != 0;
-            const int r = row;
+            const int r = row, tiles = a.block_tiles;
             const uint8_t *from = load ? kbase + id * a.c.blk_stride + (long long)(pch / a.group_chunks * a.hc) * a.c.head_stride : a.c.base;
             if (runs > 1) {
                 mask <<= per * (lane % runs);
                 mask |= __shfl_xor_sync(~0u, mask, 1);
                 if (runs == 4) mask |= __shfl_xor_sync(~0u, mask, 2);
             }
-            const int bytes = __popc(__ballot_sync(~0u, load)) * per * 40 * G * a.hc;
+            const int bytes = tiles ? __popc(__ballot_sync(~0u, load && lane % max(tiles, 1) == 0)) * tiles * 2 * a.hc * PLANE : 0;
             const int4 what = make_int4((int)mask | flags, t0 + lane / runs * 16, pi, pch);
             // the cursor moves, and the next step's ids are on their way while this one is issued
             if (++pk == psteps && n + 1 < todo) {
@@ -220,25 +223,35 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
             }
             if (n + 1 < todo) peek();
             if (n >= a.stages) kv_mbar_wait(empty + 8 * put, (n / a.stages - 1) & 1, &gave_up, a.c.status);
-            if (lane < roles && lane % runs == 0) info[put][lane / runs] = what;
+            if (loader == 0 && lane < roles && lane % runs == 0) info[put][lane / runs] = what;
             __syncwarp();
             const unsigned stage = ring + put * stage_bytes, bar = filled + 8 * put;
-            if (lane == 0) kv_mbar_expect(bar, bytes);
+            if (loader == 0 && lane == 0) kv_mbar_expect(bar, bytes);
             __syncwarp();
-            if (a.c.bs == 16) {      // a block's heads lie side by side: one copy per tile and plane
-                const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, lane >> 1);
-                const int on = __shfl_sync(~0u, (int)load, lane >> 1);
-                if (lane < 2 * a.tw && on) kv_bulk(stage + lane * a.hc * PLANE, (const uint8_t *)p + (lane & 1 ? a.c.plane_stride : 0), a.hc * PLANE, bar);
-            } else                   // (role, head, plane, codes or words)
-                for (int c0 = 0; c0 < roles * a.hc * 4; c0 += 32) {
-                    const int c = c0 + lane, words = c & 1, plane = c >> 1 & 1, rest = c >> 2, role = rest / a.hc, h = rest - role * a.hc;
-                    const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, role & 31);
-                    const int on = __shfl_sync(~0u, (int)load, role & 31), in = __shfl_sync(~0u, r, role & 31);
-                    if (role < roles && on)
-                        kv_bulk(stage + ((role / runs * 2 + plane) * a.hc + h) * PLANE + (words ? WORDS : 0) + role % runs * per * (words ? 4 : 16) * G,
-                                (const uint8_t *)p + (plane ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride + (words ? a.c.bs * 16 * G + in * 4 * G : in * 16 * G),
-                                per * (words ? 4 : 16) * G, bar);
+            if (tiles) {
+                const int block = lane >> 1, plane = lane & 1, blocks = a.tw / tiles;
+                const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, block * tiles);
+                const int on = __shfl_sync(~0u, (int)load, block * tiles);
+                if (block < blocks && on)
+                    kv_bulk(stage + lane * tiles * a.hc * PLANE, (const uint8_t *)p + (plane ? a.c.plane_stride : 0), tiles * a.hc * PLANE, bar);
+            } else {
+                for (int x = loader; x < a.tw * a.hc; x += KV_Q4_LOADERS) {
+                    const int tile = x / a.hc, h = x - tile * a.hc;
+                    const unsigned to = stage + (tile * 2 * a.hc + h) * PLANE;
+#pragma unroll
+                    for (int k = 0; k < PIECES; ++k) {
+                        const int c = min(lane + 32 * k, 40 * G - 1), v = c >= 20 * G, in = v ? c - 20 * G : c, w = in - 16 * G;
+                        // a piece of words may be of two rows: a run has four or more, so both lie in one
+                        const int of = w < 0 ? in / G : w * 4 / G, role = tile * runs + of / per, size = w < 0 ? 16 * G : 4 * G;
+                        const unsigned long long p = __shfl_sync(~0u, (unsigned long long)from, role);
+                        const int on = __shfl_sync(~0u, (int)load, role), first_row = __shfl_sync(~0u, r, role);
+                        const uint8_t *src = (const uint8_t *)p + (v ? a.c.plane_stride : 0) + (long long)h * a.c.head_stride + (w < 0 ? 0 : a.c.bs * 16 * G) +
+                                             (first_row + of % per) * size + (w < 0 ? in % G * 16 : G == 8 ? w % 2 * 16 : 0);
+                        if (on && lane + 32 * k < 40 * G) kv_cp16(to + (v ? a.hc * PLANE : 0) + in * 16, src, true);
+                    }
                 }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+            }
             put = put + 1 == a.stages ? 0 : put + 1;
         }
         return;                      // the computing warps wait for every copy before they leave
@@ -249,9 +262,9 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
     if (warp >= warps) return;
     const int hw = warp % a.hc, way = warp / a.hc, threads = warps * 32;
     auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); };
-    const int rho = lane >> 2, j = lane & 3, slot = (rho >> 1) + 4 * (rho & 1);
+    const int rho = lane >> 2, j = lane & 3, slot = rho ^ (rho >> 1 & 1);
     // where a lane reads in a plane of a tile
-    const int code_at = (slot * 4 + j) * 4 * G, word_at = WORDS + slot * 4 * G, v_at = j * 16 * G + rho * 2 * G;
+    const int code_at = (slot * 4 + j) * 4 * G, word_at = slot * 4 * G, v_at = (2 * j + (j & 1)) * 16 * G + rho * 2 * G, v_odd = (j & 1 ? -16 : 16) * G;
     unsigned qf[NT][G][4], ql[NT][PARTS][2];
     float fb[NT][2];
     float o[NT][G][2][4], lo[NT][G][2], m[NT][2], ref[NT][2], lim[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
@@ -264,8 +277,10 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
     unsigned parity = 0;
     int h = 0, g0 = 0, heads = 0;
     bool began = false;              // the run of tiles at hand begins where its row does
-    const int stage_bytes = a.tw * a.hc * 2 * PLANE, to_v = a.hc * PLANE, to_next = 2 * to_v;
-    const uint8_t *own = smem + (way * SUB * 2 * a.hc + hw) * PLANE;
+    // the warp's tiles in a stage: codes of the first, from tile to tile, from codes to words, from words to words, from K to V
+    const int block = max(a.block_tiles, 1), in_block = way * SUB % block, stage_bytes = a.tw * a.hc * 2 * PLANE, to_v = a.hc * block * PLANE;
+    const int to_next = block == 1 ? 2 * to_v : WORDS, to_words = block * WORDS - in_block * (WORDS - 64 * G), next_words = block == 1 ? to_next : 64 * G;
+    const uint8_t *own = smem + ((way * SUB / block * 2 * a.hc + hw) * block) * PLANE + in_block * WORDS;
     for (int n = 0; n < todo; ++n) {
         kv_mbar_wait(filled + 8 * take, parity, &gave_up, a.c.status);
         const int4 tile = info[take][way * SUB];
@@ -383,8 +398,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
                 unsigned c0[G], c1[G], w0[G], w1[G];
                 kv_lds(c0, at + code_at);
                 kv_lds(c1, at + code_at + 128 * G);
-                kv_lds(w0, at + word_at);
-                kv_lds(w1, at + word_at + 32 * G);
+                kv_lds(w0, kt + to_words + u * next_words + word_at);
+                kv_lds(w1, kt + to_words + u * next_words + word_at + 32 * G);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const unsigned h0 = c0[g] >> 8, h1 = c1[g] >> 8;
@@ -422,8 +437,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
             unsigned w0[SUB][G], w1[SUB][G];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                kv_lds(w0[u], kt + to_v + u * to_next + word_at);
-                kv_lds(w1[u], kt + to_v + u * to_next + word_at + 32 * G);
+                kv_lds(w0[u], kt + to_v + to_words + u * next_words + word_at);
+                kv_lds(w1[u], kt + to_v + to_words + u * next_words + word_at + 32 * G);
             }
             if (all != 0xffffu)
 #pragma unroll
@@ -534,7 +549,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + kv_q4_loaders(G, NT)) * 32, 1) 
             for (int u = 0; u < SUB; ++u) {
                 unsigned v[4][G / 2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + r * 64 * G);
+                for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);

@@ -206,6 +206,9 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
+    // whole blocks: of 2^n tiles, as many as a step has or fewer, and steps that begin where blocks do
+    const int tiles = c->block_size / 16;
+    k.block_tiles = G && k.whole_tiles && (tiles & (tiles - 1)) == 0 && k.tw % tiles == 0 && (tiles == 1 || a->window == 0) ? tiles : 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
     p.lse = align256(a->weights_out ? (int64_t)a->num_seqs * a->q_heads * a->max_len * 4 : 0);
     p.part_of = p.lse + align256(split ? (int64_t)a->num_seqs * a->q_heads * 4 : 0);
@@ -369,7 +372,7 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
         }
         ready = true;
     }
-    const unsigned threads = 32 * (wide ? (p.warps + 3) / 4 * 4 + 4 : p.warps + (q4 ? 1 : 0));
+    const unsigned threads = 32 * (q4 ? (p.warps + 3) / 4 * 4 + KV_Q4_LOADERS : p.warps);
     void *params[] = {&k};
     const unsigned rows = (unsigned)(k.seqs * k.head_chunks * k.group_chunks);
     cudaError_t e = cudaLaunchKernel(kernel, dim3(k.pieces ? k.pieces : rows), dim3(threads), params, p.smem, o->stream);

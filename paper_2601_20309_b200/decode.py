@@ -1,11 +1,12 @@
 """A decode loop on the pool, the block table and the operators on the device cache, as a serving engine would run it.
 
-    python -m paper_2601_20309_b200.decode [--layers L] [--requests R] [--prompt P] [--steps S] [--keep K] [--slack D]
+    python -m paper_2601_20309_b200.decode [--layers L] [--requests R] [--prompt P] [--steps S] [--keep K] [--slack D] [--norms]
         R requests with prompts of P tokens on the 8B shape's heads, S tokens each: per step and layer one kv_append and one
         kv_attend; whenever a request holds K + D tokens, kv_evict takes it back to K in all layers and the block table
         gets its blocks back; every 16 steps half of the requests are preempted to host memory and resumed.  Reports
-        the step's device time, the blocks held and the blocks a preemption moves, with and without eviction.  (Projections and
-        the rest of a model are left out: q, k and v are random.)
+        the step's device time, the blocks held, the blocks a preemption moves and their MB, with and without eviction, with the cache
+        in 16 bits and in 4.  --norms: queries and keys are normed per head.  (Projections and the rest of a model are left
+        out: q, k and v are random.)
 """
 from __future__ import annotations
 
@@ -18,22 +19,30 @@ from . import binding as B
 
 class Decoder:
     """Requests in `places` rows of a batch of fixed size, of up to max_tokens tokens each; a row without a request on the GPU is idle
-    (length 0).  Weights and ages of the slots are kept per layer and place; block tables and lengths go to the device once per call.
+    (length 0).  The cache is held in 16 or in 4 `bits`.  q_norm, k_norm: weights of norms per head in front of the rotation, [layers, head_dim] or
+    [layers, heads, head_dim] (``kv_append``), with norm_eps.  Weights and ages of the slots are kept per layer and place; block tables and lengths go to the device once per call.
     Kernels and copies run on the stream that is current when the decoder is made, in order with the stream a method is called under."""
 
     def __init__(self, num_layers, block_size, q_heads, kv_heads, head_dim, num_gpu_blocks, num_host_blocks, places, max_tokens, *, keep=0,
-                 slack=0, recent=0, sink=0, sections=None, theta=10000.0, device=0):
+                 slack=0, recent=0, sink=0, sections=None, theta=10000.0, device=0, bits=16, q_norm=None, k_norm=None, norm_eps=1e-6):
         import torch
+        if bits not in (16, 4):
+            raise ValueError("the cache is held in 16 or 4 bits")
         self.torch, self.device = torch, torch.device("cuda", device)
         self.layers, self.bs, self.q_heads, self.kv_heads, self.dim = num_layers, block_size, q_heads, kv_heads, head_dim
         self.keep, self.slack, self.recent, self.sink = keep, slack, recent, sink
-        self.store = torch.zeros(num_layers, 2, num_gpu_blocks, block_size, kv_heads, head_dim, dtype=torch.bfloat16, device=self.device)
-        self.pool = B.KVPool(num_layers, block_size, kv_heads, head_dim, num_gpu_blocks, num_host_blocks, self.store.data_ptr(), device_id=device)
+        self.q_norm, self.k_norm, self.norm_eps = q_norm, k_norm, norm_eps
+        dtype = "bf16" if bits == 16 else "bf16_q4"
+        units = B.kv_cache_row_units(dtype, head_dim)       # of a row: its elements, or its codes and words
+        if not units:
+            raise ValueError(f"no cache for heads of {head_dim}")
+        self.store = torch.zeros(num_layers, 2, num_gpu_blocks, block_size, kv_heads, units, dtype=torch.bfloat16, device=self.device)
+        self.pool = B.KVPool(num_layers, block_size, kv_heads, units, num_gpu_blocks, num_host_blocks, self.store.data_ptr(), device_id=device)
         self.table = B.KVTable(self.pool)
         self.own = torch.cuda.current_stream(self.device)
         self.stream = self.own.cuda_stream
         self.ops = B.KVOps(device, self.stream)
-        self.cache = self.pool.kv_pool_cache("bf16")
+        self.cache = self.pool.kv_pool_cache(dtype, head_dim)
         half = head_dim // 2
         self.inv_freq = (theta ** (-torch.arange(half, dtype=torch.float64) / half)).float().to(self.device)
         self.axis_of = [a for a, n in enumerate(sections) for _ in range(n)] if sections else [0] * half
@@ -46,6 +55,11 @@ class Decoder:
         self.running = [False] * places
         self.out = torch.zeros(num_layers, places, q_heads, head_dim, dtype=torch.bfloat16, device=self.device)
         self.turned = torch.zeros(places, q_heads, head_dim, dtype=torch.bfloat16, device=self.device)
+
+    def _norms(self, layer, q=True):
+        """What a layer's ``kv_append`` gets for its norms."""
+        return {"q_norm": self.q_norm[layer] if q and self.q_norm is not None else None,
+                "k_norm": self.k_norm[layer] if self.k_norm is not None else None, "norm_eps": self.norm_eps}
 
     def close(self):
         self.torch.cuda.synchronize(self.device)
@@ -112,7 +126,7 @@ class Decoder:
                     x = qkv[layer]
                     self.ops.kv_append(self.cache, layer, None, x[:, h:h + k], x[:, h + k:], tables[one], lens[one], positions=positions,
                                        inv_freq=self.inv_freq, axis_of=self.axis_of, seq_starts=starts, weights=self.weights[layer, one],
-                                       order=self.order[layer, one], token_order=numbers)
+                                       order=self.order[layer, one], token_order=numbers, **self._norms(layer, q=False))
         except BaseException:
             self.ops.kv_ops_sync(check=False)   # kernels of earlier layers may still write the blocks that go back
             self.table.kv_req_finish(req, check=False)
@@ -149,7 +163,7 @@ class Decoder:
                     x = qkv[layer]
                     self.ops.kv_append(self.cache, layer, x[:, :h], x[:, h:h + k], x[:, h + k:], tables, lens, positions=positions,
                                        inv_freq=self.inv_freq, axis_of=self.axis_of, q_out=self.turned, weights=self.weights[layer],
-                                       order=self.order[layer], token_order=numbers)
+                                       order=self.order[layer], token_order=numbers, **self._norms(layer))
                     self.ops.kv_attend(self.cache, layer, self.turned, tables, lens, longest, out=self.out[layer],
                                        weights_in=self.weights[layer], weights_out=self.weights[layer])
         except BaseException:               # no row keeps a token that was not written in every layer
@@ -188,14 +202,15 @@ class Decoder:
         self.pool.kv_stream_wait(self.stream)
 
 
-def run(layers, requests, prompt, steps, keep, slack, seed=1):
+def run(layers, requests, prompt, steps, keep, slack, seed=1, bits=16, norms=False):
     """The command's loop; a dict of what it measured."""
     import torch
+    weights = torch.ones(layers, 128, dtype=torch.bfloat16, device="cuda") if norms else None
     shape = dict(block_size=16, q_heads=32, kv_heads=8, head_dim=128)
     most = (max(prompt, keep) + slack + 1) if keep else prompt + steps
     blocks = requests * (-(-max(most, prompt) // 16) + 2)
     d = Decoder(layers, *shape.values(), blocks, 2 * blocks, requests, max(most, prompt + 1), keep=keep, slack=slack, recent=keep // 8,
-                sink=4, sections=(16, 24, 24))
+                sink=4, sections=(16, 24, 24), bits=bits, q_norm=weights, k_norm=weights)
     g = torch.Generator(device="cuda").manual_seed(seed)
     heads = shape["q_heads"] + 2 * shape["kv_heads"]
     for r in range(requests):
@@ -219,7 +234,9 @@ def run(layers, requests, prompt, steps, keep, slack, seed=1):
             d.rotate([], half)
     held = d.table.kv_table_get_stats()["free_gpu_blocks"]
     ms.sort()
-    res = {"step_ms_median": round(ms[len(ms) // 2], 3), "blocks_held": blocks - held, "blocks_moved_per_preemption": moved}
+    block_mb = 2 * layers * 16 * 8 * B.kv_cache_row_units("bf16" if bits == 16 else "bf16_q4", 128) * 2 / 1e6
+    res = {"step_ms_median": round(ms[len(ms) // 2], 3), "blocks_held": blocks - held, "blocks_moved_per_preemption": moved,
+           "mb_moved_per_preemption": [round(n * block_mb, 1) for n in moved]}
     d.close()
     return res
 
@@ -232,12 +249,14 @@ def main() -> None:
     ap.add_argument("--steps", type=int, default=64)
     ap.add_argument("--keep", type=int, default=1024)
     ap.add_argument("--slack", type=int, default=128)
+    ap.add_argument("--norms", action="store_true")
     a = ap.parse_args()
     import torch
     if not torch.cuda.is_available():
         sys.exit("decode needs a CUDA device")
-    print("whole cache  ", run(a.layers, a.requests, a.prompt, a.steps, 0, 0))
-    print("with eviction", run(a.layers, a.requests, a.prompt, a.steps, a.keep, a.slack))
+    for bits in (16, 4):
+        print(f"{bits:2} bits, whole cache  ", run(a.layers, a.requests, a.prompt, a.steps, 0, 0, bits=bits, norms=a.norms))
+        print(f"{bits:2} bits, with eviction", run(a.layers, a.requests, a.prompt, a.steps, a.keep, a.slack, bits=bits, norms=a.norms))
 
 
 if __name__ == "__main__":
