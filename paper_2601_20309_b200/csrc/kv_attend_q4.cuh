@@ -21,6 +21,18 @@
 //
 // Masked slots (beyond the length, before the window) are loaded with their tile where their block is known: codes are numbers
 // whatever they hold, scores are replaced by -inf and words by 0, so nothing of such a slot reaches a sum.
+//
+// Split.  Eight warps compute, a KV head each where there are eight, two tiles at once: what a step costs beside its tiles (waiting,
+// the vote, the compensated sum) then counts half (495 instructions per tile with one at once, 347 with two; 60 and 50 us for the 70B shape).
+// Other warps load, so that those that compute need no registers for addresses: with every warp filling its own ring by 16-byte
+// copies the same work took 67 us.  What was slower too: the scores of one step beside the sums of the one before it (60 us:
+// registers), twelve computing warps (69), rows joined by whichever CTA comes last (71 to 88: a row of 16384 slots has 23 parts, too
+// much for one SM).
+//
+// What bounds it.  70B shape, 133 MB: 49.3 us, of which 8.5 are the join, 5 the first chain of loads (lengths, block ids, first tile), 30 the line
+// of steps: 4.4 TB/s.  Without any arithmetic on the tiles the call takes 41 us, without the join 42.  No single part of the arithmetic
+// shows: without the masks (a fifth of the instructions) 51.2 us, without the transpositions 50.7, without the second product 49.4,
+// against 51.0 at the same time.
 #pragma once
 #include <type_traits>
 
@@ -132,6 +144,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
         }
 
     const unsigned filled = (unsigned)__cvta_generic_to_shared(bars[0]), empty = (unsigned)__cvta_generic_to_shared(bars[1]);
+    // what a computing warp finds in place of a step that it waited for in vain is a tile of the first sequence without slots
+    for (int e = tid; e < KV_Q4_STAGES * KV_Q4_WARPS * SUB; e += blockDim.x) (&info[0][0])[e] = make_int4(0, 0, 0, 0);
     if (tid == 0) {
         gave_up = 0;
         for (int s = 0; s < a.stages; ++s) {
@@ -171,7 +185,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
         // [block][K, V][KV head][codes of its tiles, words of its tiles].  One warp does that: a bulk copy takes the SM about 100 cycles,
         // whatever its size, so 64 small ones for a step of 40 KB took 6600 cycles and four take what the memory takes.
         //   Else four warps copy 16 bytes per lane: [tile][K, V][KV head][codes, words].
-        if (a.block_tiles && loader > 0) return;
+        if (a.block_tiles && loader > 0) return;         // (they came for their registers)
         const int stage_bytes = a.tw * a.hc * 2 * PLANE, runs = a.whole_tiles ? 1 : a.c.bs % 8 == 0 ? 2 : 4, per = 16 / runs, roles = a.tw * runs;
         const unsigned ring = (unsigned)__cvta_generic_to_shared(smem);
         const uint8_t *kbase = a.c.base + (long long)a.layer * 2 * a.c.plane_stride;

@@ -148,6 +148,9 @@ constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, les
 // with weights to add up): 4 sequences of 500 slots with weights 13.5 us whole, 17.6 split; 1 of 900 without 14.7 whole, 12.1 split.
 // Near the limit with weights few whole rows lose already: of 900 slots one takes 21.6 us whole and 16.7 split, 16 take 26.8 and 29.1
 constexpr int ATTEND_ALONE_STEPS = 4, ATTEND_ALONE_STEPS_WEIGHTS = 8;
+// In 4 bits a step is two tiles of each warp, and the limit the same with weights and without: one sequence of 1000 slots (4 steps) 13.7 us
+// whole and 14.3 split, with weights 18.7 and 19.4; of 2000 (8 steps) 22.3 and 14.5, 36.1 and 19.8; 64 of 100 (4 steps) 11.6 and 18.6
+constexpr int ATTEND_ALONE_STEPS_Q4 = 4;
 // No piece is shorter: with 1 step one sequence of 2000 slots takes 22.5 us, with 2 18.8, with 4 18.8; seven windows of 333 12.8, 14.9, 17.9
 constexpr int ATTEND_MIN_STEPS = 2;
 // CTAs of the join per piece that put rows together.  With weights there are KV_JOIN_SHARES others beside them: 64 sequences 90.6 us
@@ -193,7 +196,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     const bool one_head = (int64_t)a->num_seqs * c->kv_heads * k.group_chunks <= o->sms;
     int64_t longest = shape(one_head ? 1 : most);
     // query-head chunks of one KV head all add to the same weights: those go through the second kernel
-    const bool split = longest > (a->weights_out ? ATTEND_ALONE_STEPS_WEIGHTS : ATTEND_ALONE_STEPS) || (a->weights_out && k.group_chunks > 1);
+    const bool split = longest > (G ? ATTEND_ALONE_STEPS_Q4 : a->weights_out ? ATTEND_ALONE_STEPS_WEIGHTS : ATTEND_ALONE_STEPS) || (a->weights_out && k.group_chunks > 1);
     if (split && one_head) longest = shape(most);
     k.head_chunks = c->kv_heads / k.hc;
     const int64_t box = p.warps > k.hc ? (int64_t)p.warps / 2 * (G ? kv_q4_box(G, p.nt) : p.nt * (p.dp / 16 + 1) * 4) * 32 * 4 : 0;
@@ -206,7 +209,8 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
         return fail(o, KV_ERR_UNSUPPORTED, "num_seqs * max_len is too large for one call");
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
-    // whole blocks: of 2^n tiles, as many as a step has or fewer, and steps that begin where blocks do
+    // Whole blocks: of 2^n tiles, as many as a step has or fewer, and steps that begin where blocks do.  One sequence of 131072 slots in
+    // blocks of 64, 1 KV head: 20.4 us, and 26.4 with a bulk copy per tile, plane, codes and words
     const int tiles = c->block_size / 16;
     k.block_tiles = G && k.whole_tiles && (tiles & (tiles - 1)) == 0 && k.tw % tiles == 0 && (tiles == 1 || a->window == 0) ? tiles : 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
@@ -495,7 +499,8 @@ int32_t kv_append_normed(kv_ops_t *o, const kv_cache_t *cache, const kv_append_a
         const int groups = (int)(ceil_div(a->q ? a->q_heads : 0, abreast) + 2 * ceil_div(cache->kv_heads, abreast));
         r.splits = 1;
         r.per_split = groups;
-        if (k.per == 1) {        // few tokens: their rows all at once, as far as there are SMs
+        // Few tokens: their rows all at once, as far as there are SMs.  64 tokens of 64 + 8 + 8 heads with norms 5.1 us so, 7.0 with one CTA per token
+        if (k.per == 1) {
             r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(groups, warps), 4 * o->sms / a->num_tokens));
             r.per_split = (int)ceil_div(groups, r.splits);
             r.splits = (int)ceil_div(groups, r.per_split);
@@ -511,7 +516,8 @@ int32_t kv_append_normed(kv_ops_t *o, const kv_cache_t *cache, const kv_append_a
         r.by_dim = 1.f / cache->head_dim;
         r.p = k;
         const size_t smem = (size_t)k.per * per_token + (q4 ? (size_t)at_once * k.c.groups * 64 : 0);
-        // whole rows: heads of 64, 128 or 256, every lane's elements aligned and of one kind
+        // Whole rows: heads of 64, 128 or 256, every lane's elements aligned and of one kind.  14.3k prompt tokens with norms 74.6 us so and 91.1
+        // with guards and four elements at a time, into 4 bits and read back 133 and 163; one token 8.1 and 8.6
         const bool whole = v == 8 && lanes * 16 == cache->head_dim && lanes == 1 << r.lanes_log2 && lanes >= 4 && lanes <= 16;
         const auto pick = [&](auto t) {
             using T = decltype(t);
@@ -561,7 +567,7 @@ int32_t kv_read(kv_ops_t *o, const kv_cache_t *cache, const kv_read_args_t *a)
     k.v_tok = a->v_token_stride;
     k.v_head = a->v_head_stride;
     k.starts = a->seq_starts;
-    k.units = (int)ceil_div(cache->head_dim, 16);
+    k.units = k.c.groups ? 4 : (int)ceil_div(cache->head_dim, 16);
     const int per_token = k.units * cache->kv_heads;
     k.by_units = (unsigned)ceil_div(int64_t(1) << 32, per_token);
     k.per = (int)std::min<int64_t>(RD_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
@@ -569,7 +575,10 @@ int32_t kv_read(kv_ops_t *o, const kv_cache_t *cache, const kv_read_args_t *a)
     const bool vec = (!a->k || fits(a->k, a->k_token_stride, a->k_head_stride)) && (!a->v || fits(a->v, a->v_token_stride, a->v_head_stride));
     const auto pick = [&](auto t) {
         using T = decltype(t);
-        return k.c.groups ? vec ? kv_read_rows<T, true, true> : kv_read_rows<T, false, true> : vec ? kv_read_rows<T, true, false> : kv_read_rows<T, false, false>;
+        using Kernel = void (*)(KvRead);
+        const Kernel kernels[2][4] = {{kv_read_rows<T, false, 0>, kv_read_rows<T, false, 2>, kv_read_rows<T, false, 4>, kv_read_rows<T, false, 8>},
+                                      {kv_read_rows<T, true, 0>, kv_read_rows<T, true, 2>, kv_read_rows<T, true, 4>, kv_read_rows<T, true, 8>}};
+        return kernels[vec][k.c.groups == 8 ? 3 : k.c.groups / 2];
     };
     const auto kernel = is_bf16(cache) ? pick(__nv_bfloat16()) : pick(__half());
     kernel<<<(unsigned)ceil_div(a->num_tokens, k.per), AP_THREADS, 0, o->stream>>>(k);

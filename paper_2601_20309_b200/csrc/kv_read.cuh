@@ -2,7 +2,8 @@
 // (the attention of a prompt that arrives in pieces, an export).  element = lo + s * code, one fused operation, one rounding.
 //
 // What bounds it: the bytes written, 3.2 times those read from a cache in 4 bits.  A thread writes 16 neighbouring elements of one
-// head of K and of V; the tokens' slots (a search, a length, a block id) are found once per CTA.
+// head of K and of V, or, in 4 bits, eight of every group, which is what G neighbouring words of codes hold; the tokens' slots (a search, a length, a block id) are found once per CTA.  14.3k tokens of 8 heads of 128, 77 MB:
+// 23 us, 3.3 TB/s; loads of 2 and 4 bytes wait for one another there (a fifth of the issue slots is lost to them).
 #pragma once
 #include "kv_append.cuh"
 
@@ -14,13 +15,28 @@ struct KvRead {
     long long k_tok, k_head, v_tok, v_head;
     const int *starts;
     int per;                     // tokens per CTA
-    int units;                   // runs of 16 elements of a head
+    int units;                   // threads of a row and head
     unsigned by_units;           // 2^32 / (units * heads), rounded up
 };
 
 constexpr int RD_TOKENS = 32;
 
-template <typename T, bool VEC, bool Q4>
+// neighbouring words
+template <int N> __device__ __forceinline__ void kv_words(unsigned (&r)[N], const uint8_t *at)
+{
+    if constexpr (N == 2) {
+        const uint2 v = *(const uint2 *)at;
+        r[0] = v.x, r[1] = v.y;
+    } else
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const uint4 v = *(const uint4 *)(at + k * 4);
+            r[k] = v.x, r[k + 1] = v.y, r[k + 2] = v.z, r[k + 3] = v.w;
+        }
+}
+
+// G: groups of a cache in 4 bits, 0: 16 bits
+template <typename T, bool VEC, int G>
 __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant__ KvRead a)
 {
     __shared__ const uint8_t *kv_row[RD_TOKENS];
@@ -39,7 +55,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant
         if ((tid & 31) == 0) {
             if (!ok && n > 0) atomicOr(a.c.status, KV_OPS_BAD_LEN);
             kv_row[k] = ok ? a.c.slot(i, (int)s, a.layer * 2) : nullptr;
-            if (Q4) to_words[k] = ok ? a.c.to_words((int)s) : 0;
+            if (G) to_words[k] = ok ? a.c.to_words((int)s) : 0;
         }
     }
     __syncthreads();
@@ -48,58 +64,46 @@ __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant
         const uint8_t *row = kv_row[token];
         if (!row) continue;
         row += (long long)h * a.c.head_stride;
-        const int runs = min(2, (dim - 16 * u) >> 3);    // of eight elements
-        unsigned w[2][8];
-        if constexpr (Q4) {
-            const int G = a.c.groups, g = u >> 1;
-            unsigned codes[2][2], word[2];
+        T *k_to = a.k ? (T *)a.k + (first + token) * a.k_tok + h * a.k_head : nullptr, *v_to = a.v ? (T *)a.v + (first + token) * a.v_tok + h * a.v_head : nullptr;
+        auto put = [](T *to, const uint4 &v) {           // eight elements
+            if (VEC) *(uint4 *)to = v;
+            else {
+                const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) codes[0][j] = ((const unsigned *)row)[((u & 1) * 2 + j) * G + g];
-            word[0] = ((const unsigned *)(row + to_words[token]))[g];
-            row += a.c.plane_stride;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                codes[1][j] = ((const unsigned short *)row)[((u & 1) * 4 + 2 * j) * G + g] |
-                              (unsigned)((const unsigned short *)row)[((u & 1) * 4 + 2 * j + 1) * G + g] << 16;
-            word[1] = ((const unsigned *)(row + to_words[token]))[g];
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                // a code in the lowest bits of a 16-bit word is code * 2^-24 in float16, four bits further code * 2^-20
-                const float lo = kv_unpair(word[p], T()).x, s = __uint_as_float(word[p] & 0xffff0000u);
-                const auto at = [&](float code, float unit) { return fmaf(s, code * unit, lo); };
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const unsigned c = codes[p][j], d = c >> 8;
-                    const float2 x0 = kv_unpair(c & 0x000f000fu, __half()), x1 = kv_unpair(c & 0x00f000f0u, __half());     // elements 0 and 4, 1 and 5
-                    const float2 x2 = kv_unpair(d & 0x000f000fu, __half()), x3 = kv_unpair(d & 0x00f000f0u, __half());     // 2 and 6, 3 and 7
-                    w[p][4 * j] = kv_pair(at(x0.x, 0x1p24f), at(x1.x, 0x1p20f), T());
-                    w[p][4 * j + 1] = kv_pair(at(x2.x, 0x1p24f), at(x3.x, 0x1p20f), T());
-                    w[p][4 * j + 2] = kv_pair(at(x0.y, 0x1p24f), at(x1.y, 0x1p20f), T());
-                    w[p][4 * j + 3] = kv_pair(at(x2.y, 0x1p24f), at(x3.y, 0x1p20f), T());
-                }
+                for (int e = 0; e < 8; ++e) ((unsigned short *)to)[e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
             }
-        } else {
-#pragma unroll
-            for (int p = 0; p < 2; ++p, row += a.c.plane_stride)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (j < runs) {
-                        const uint4 v = ((const uint4 *)row)[2 * u + j];
-                        w[p][4 * j] = v.x, w[p][4 * j + 1] = v.y, w[p][4 * j + 2] = v.z, w[p][4 * j + 3] = v.w;
-                    }
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            void *base = p ? a.v : a.k;
-            if (!base) continue;
-            T *to = (T *)base + (first + token) * (p ? a.v_tok : a.k_tok) + h * (p ? a.v_head : a.k_head) + 16 * u;
+        };
+        if constexpr (G == 0) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                if (j >= runs) continue;
-                if (VEC) ((uint4 *)to)[j] = make_uint4(w[p][4 * j], w[p][4 * j + 1], w[p][4 * j + 2], w[p][4 * j + 3]);
-                else
+                const int d = 16 * u + 8 * j;
+                if (d >= dim) continue;
+                if (k_to) put(k_to + d, *(const uint4 *)(row + 2 * d));
+                if (v_to) put(v_to + d, *(const uint4 *)(row + a.c.plane_stride + 2 * d));
+            }
+        } else {
+            // elements 32 g + 8 u .. + 7 of every group g: G words of K's codes side by side, as many half words twice of V's
+            unsigned codes[2][G], words[2][G];
+            kv_words(codes[0], row + 4 * G * u);
+            kv_words(codes[1], row + a.c.plane_stride + 4 * G * u);
+            kv_words(words[0], row + to_words[token]);
+            kv_words(words[1], row + a.c.plane_stride + to_words[token]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ((unsigned short *)to)[8 * j + e] = (unsigned short)(w[p][4 * j + (e >> 1)] >> (16 * (e & 1)));
+            for (int p = 0; p < 2; ++p) {
+                T *to = p ? v_to : k_to;
+                if (!to) continue;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    if (32 * g + 8 * u >= dim) continue;
+                    const unsigned c = p ? __byte_perm(codes[1][g >> 1], codes[1][G / 2 + (g >> 1)], g & 1 ? 0x7632 : 0x5410) : codes[0][g], d = c >> 8;
+                    // a code in the lowest bits of a 16-bit word is code * 2^-24 in float16, four bits further code * 2^-20
+                    const float lo = kv_unpair(words[p][g], T()).x, s = __uint_as_float(words[p][g] & 0xffff0000u);
+                    const auto at = [&](float code, float unit) { return fmaf(s, code * unit, lo); };
+                    const float2 x0 = kv_unpair(c & 0x000f000fu, __half()), x1 = kv_unpair(c & 0x00f000f0u, __half());     // elements 0 and 4, 1 and 5
+                    const float2 x2 = kv_unpair(d & 0x000f000fu, __half()), x3 = kv_unpair(d & 0x00f000f0u, __half());     // 2 and 6, 3 and 7
+                    put(to + 32 * g + 8 * u, make_uint4(kv_pair(at(x0.x, 0x1p24f), at(x1.x, 0x1p20f), T()), kv_pair(at(x2.x, 0x1p24f), at(x3.x, 0x1p20f), T()),
+                                                        kv_pair(at(x0.y, 0x1p24f), at(x1.y, 0x1p20f), T()), kv_pair(at(x2.y, 0x1p24f), at(x3.y, 0x1p20f), T())));
+                }
             }
         }
     }
