@@ -403,7 +403,13 @@ __global__ void __launch_bounds__(AP_THREADS, Q4 ? 3 : 4) kv_append_rows(const _
                         const float2 f = kv_unpair(x[j], T()), g = kv_unpair(y[j], T());
                         double f0 = f.x, f1 = f.y, g0 = g.x, g1 = g.y;
                         if (b.k_w) {             // elements of the last run that are none have any weight
-                            if (b.k_w_head == 0) {
+                            if (WHOLE && b.k_w_head == 0) {
+                                const double2 p = *(const double2 *)(k_weight + w0 + 2 * j), q = *(const double2 *)(k_weight + w1 + 2 * j);
+                                f0 *= rn * p.x;
+                                f1 *= rn * p.y;
+                                g0 *= rn * q.x;
+                                g1 *= rn * q.y;
+                            } else if (b.k_w_head == 0) {
                                 f0 *= rn * k_weight[w0 + 2 * j];
                                 f1 *= rn * k_weight[w0 + 2 * j + 1];
                                 g0 *= rn * k_weight[w1 + 2 * j];

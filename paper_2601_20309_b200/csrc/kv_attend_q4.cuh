@@ -72,6 +72,11 @@ __device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ unsigned kv_add2(unsigned x, unsigned y)
+{
+    const __half2 v = __hadd2(*(const __half2 *)&x, *(const __half2 *)&y);
+    return *(const unsigned *)&v;
+}
 __device__ __forceinline__ unsigned kv_transpose(unsigned x)
 {
     unsigned y;
@@ -122,7 +127,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     constexpr int PLANE = 320 * G, WORDS = 256 * G, HEADS = 8 * NT;     // bytes of a tile's plane, and of its codes
     constexpr int PARTS = G == 8 ? 2 : 1;        // matrix instructions for the sum over lo
     constexpr int SUB = kv_q4_sub(G, NT);
-    constexpr bool EXACT = std::is_same<T, __half>::value;      // see R below
+    constexpr bool EXACT = std::is_same<T, __half>::value;      // see the sums over V
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int red[KV_Q4_WARPS + KV_Q4_LOADERS], s_at[2], gave_up;
     __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
@@ -282,10 +287,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     unsigned qf[NT][G][4], ql[NT][PARTS][2];
     float fb[NT][2];
     float o[NT][G][2][4], lo[NT][G][2], m[NT][2], ref[NT][2], lim[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
-    // The rounding of p s is multiplied by a code, 0 to 15, where the element itself may lie near 0.  For f16 outputs, fine enough to
-    // show it, R = the sum of the rounded p s over the slots (row g of the fragment: group g) moves the codes to -8 to 7:
-    // sum (p s) code + sum p lo = sum (p s)' (code - 8) + sum p (lo + 8 s), with ' the rounded ones
-    float R[NT][EXACT ? 4 : 1];
     int top_step = KV_Q4_LOWEST;
     int take = 0;
     unsigned parity = 0;
@@ -401,7 +402,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     for (int e = 0; e < 8; ++e) o[nt][b][e >> 2][e & 3] = 0.f;
                     lo[nt][b][0] = lo[nt][b][1] = 0.f;
                 }
-                if constexpr (EXACT) R[nt][0] = R[nt][1] = R[nt][2] = R[nt][3] = 0.f;
             }
         }
         if (some) {
@@ -530,7 +530,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                         lim[nt][e] = (x + KV_Q4_SLACK) / fb[nt][e];
                         l[nt][e] *= alpha;
                         rest[nt][e] *= alpha;
-                        if constexpr (EXACT) R[nt][e] *= alpha;
 #pragma unroll
                         for (int g = 0; g < G; ++g) {
                             lo[nt][g][e] *= alpha;
@@ -561,6 +560,10 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
+                // The rounding of p s is multiplied by a code, 0 to 15, where the element itself may lie near 0, and the sum over lo takes away
+                // most of what the codes add up to.  For f16 outputs, fine enough to show both, codes are -8 to 7 and lo is lo + 8 s
+                const auto even = [](unsigned x) { return EXACT ? kv_add2(x & 0x000f000fu, 0x80088008u) : x & 0x000f000fu; };
+                const auto odd = [](unsigned x) { return EXACT ? kv_add2(x & 0x00f000f0u, 0x80808080u) : x & 0x00f000f0u; };
                 unsigned v[4][G / 2];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
@@ -578,12 +581,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     for (int nt = 0; nt < NT; ++nt) {
                         const float(&p)[4] = y[u][nt];
                         const unsigned p0 = kv_transpose(kv_pair(p[0] * s0, p[1] * s0, __half())), p1 = kv_transpose(kv_pair(p[2] * s1, p[3] * s1, __half()));
-                        kv_mma_f16(o[nt][g][0], r0 & 0x000f000fu, r0 & 0x00f000f0u, r1 & 0x000f000fu, r1 & 0x00f000f0u, p0, p1);
-                        kv_mma_f16(o[nt][g][1], h0 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x000f000fu, h1 & 0x00f000f0u, p0, p1);
-                        if constexpr (EXACT) {
-                            const unsigned one = rho == g ? 0x3c003c00u : 0u;
-                            kv_mma_f16(R[nt], one, 0u, one, 0u, p0, p1);
-                        }
+                        kv_mma_f16(o[nt][g][0], even(r0), odd(r0), even(r1), odd(r1), p0, p1);
+                        kv_mma_f16(o[nt][g][1], even(h0), odd(h0), even(h1), odd(h1), p0, p1);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(p[e], z0, fmaf(p[e + 2], z1, lo[nt][g][e]));
                     }
@@ -615,7 +614,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     for (int g = 0; g < G; ++g) {
 #pragma unroll
                         for (int x = 4; x <= 16; x <<= 1) lo[nt][g][e] += __shfl_xor_sync(~0u, lo[nt][g][e], x);
-                        if constexpr (EXACT) lo[nt][g][e] -= 8.f * __shfl_sync(~0u, R[nt][e], 4 * g + j);
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll

@@ -85,6 +85,14 @@ ATTEND = [
     ([130, 260], 6, 3, 40, 28, "f16", 0, 1),
     ([3] * 300, 4, 2, 64, 16, "bf16", 0, 0),
     ([(i * 37) % 200 for i in range(150)], 8, 4, 128, 16, "f16", 0, 0),
+    # steps of whole blocks of several tiles, and blocks that steps do not hold: with a window, of three tiles, longer than a step
+    ([1500, 90, 4], 4, 1, 64, 32, "bf16", 1, 0),
+    ([900, 333], 8, 2, 128, 64, "f16", 0, 0),
+    ([900, 333], 8, 2, 128, 64, "bf16", 0, 300),
+    ([500, 90], 8, 8, 128, 48, "f16", 1, 0),
+    ([2100, 5], 16, 1, 256, 128, "bf16", 0, 0),
+    ([1100], 9, 1, 128, 512, "bf16", 0, 0),
+    ([600, 70], 10, 5, 128, 32, "bf16", 0, 0),
 ]
 
 
@@ -171,6 +179,16 @@ def test_attend_not_finite(ops):
     q[1, 2, 5] = math.inf
     out, _, _, _ = run_attend(ops, c, q, weights=False)
     assert torch.isnan(out[1, 2]).all() and not torch.isnan(out[1, [0, 1, 3]]).any()
+
+
+def test_attend_f16_is_as_fine_as_its_type(ops):
+    """Over many slots the roundings of the products are as small as the output's: each has 2^-11 / sqrt(3) of the value at the lower end of a
+    power of two, less elsewhere, and together stay below 2^-11 in the mean."""
+    c = Q.Cache([20000], 1, 128, 64, "f16", seed=20, layers=1)
+    q = randn(c.g, 1, 8, 128, dtype="f16")
+    out, _, _, _ = run_attend(ops, c, q, weights=False, layer=0)
+    want = torch.stack([row[0] for row in Q.attend(c, 0, q)[0]])
+    assert float((out[0] - want).norm() / want.norm()) <= 2.0 ** -11
 
 
 def test_attend_long_row(ops):
