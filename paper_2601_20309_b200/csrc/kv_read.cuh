@@ -3,7 +3,7 @@
 //
 // What bounds it: the bytes written, 3.2 times those read from a cache in 4 bits.  A thread writes 16 neighbouring elements of one
 // head of K and of V, or, in 4 bits, eight of every group, which is what G neighbouring words of codes hold; the tokens' slots (a search, a length, a block id) are found once per CTA.  14.3k tokens of 8 heads of 128, 77 MB:
-// 23 us, 3.3 TB/s; loads of 2 and 4 bytes wait for one another there (a fifth of the issue slots is lost to them).
+// 17 us, 4.5 TB/s (23 us with 16 neighbouring elements per thread here too: loads of 2 and 4 bytes).
 #pragma once
 #include "kv_append.cuh"
 
