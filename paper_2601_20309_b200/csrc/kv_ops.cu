@@ -569,7 +569,7 @@ int32_t kv_read(kv_ops_t *o, const kv_cache_t *cache, const kv_read_args_t *a)
     k.starts = a->seq_starts;
     k.units = k.c.groups ? 4 : (int)ceil_div(cache->head_dim, 16);
     const int per_token = k.units * cache->kv_heads;
-    k.by_units = (unsigned)ceil_div(int64_t(1) << 32, per_token);
+    k.by_units = per_token == 1 ? 0 : (unsigned)ceil_div(int64_t(1) << 32, per_token);     // 2^32 has no place in 32 bits
     k.per = (int)std::min<int64_t>(RD_TOKENS, ceil_div(a->num_tokens, 8 * o->sms));
     const auto fits = [](const void *p, int64_t x, int64_t y) { return (uintptr_t)p % 16 == 0 && x % 8 == 0 && y % 8 == 0; };
     const bool vec = (!a->k || fits(a->k, a->k_token_stride, a->k_head_stride)) && (!a->v || fits(a->v, a->v_token_stride, a->v_head_stride));

@@ -2,8 +2,9 @@
 // (the attention of a prompt that arrives in pieces, an export).  element = lo + s * code, one fused operation, one rounding.
 //
 // What bounds it: the bytes written, 3.2 times those read from a cache in 4 bits.  A thread writes 16 neighbouring elements of one
-// head of K and of V, or, in 4 bits, eight of every group, which is what G neighbouring words of codes hold; the tokens' slots (a search, a length, a block id) are found once per CTA.  14.3k tokens of 8 heads of 128, 77 MB:
-// 17 us, 4.5 TB/s (23 us with 16 neighbouring elements per thread here too: loads of 2 and 4 bytes).
+// head of K and of V, or, in 4 bits, eight of every group, which is what G neighbouring words of codes hold; the tokens' slots (a
+// search, a length, a block id) are found once per CTA.  14.3k tokens of 8 heads of 128, 77 MB: 17 us, 4.5 TB/s (23 us with 16
+// neighbouring elements per thread here too: loads of 2 and 4 bytes).
 #pragma once
 #include "kv_append.cuh"
 
@@ -16,7 +17,7 @@ struct KvRead {
     const int *starts;
     int per;                     // tokens per CTA
     int units;                   // threads of a row and head
-    unsigned by_units;           // 2^32 / (units * heads), rounded up
+    unsigned by_units;           // 2^32 / (units * heads), rounded up; 0: units * heads is 1
 };
 
 constexpr int RD_TOKENS = 32;
@@ -60,7 +61,7 @@ __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant
     }
     __syncthreads();
     for (int f = tid; f < total; f += AP_THREADS) {
-        const int token = (int)__umulhi((unsigned)f, a.by_units), rest = f - token * per_token, h = rest / a.units, u = rest - h * a.units;
+        const int token = a.by_units ? (int)__umulhi((unsigned)f, a.by_units) : f, rest = f - token * per_token, h = rest / a.units, u = rest - h * a.units;
         const uint8_t *row = kv_row[token];
         if (!row) continue;
         row += (long long)h * a.c.head_stride;

@@ -393,6 +393,26 @@ def test_read(ops, dim, bs, dtype, layout, q4):
     assert (last[2] == 7).all() and torch.equal(last[3], v[75, 2:5, room - dim:]) and torch.equal(last[0], v[71, 2:5, room - dim:])
 
 
+@pytest.mark.parametrize("dim,heads,q4", [(8, 1, False), (16, 1, False), (24, 1, False), (8, 2, False), (8, 1, True), (16, 1, True)])
+def test_read_of_the_smallest_rows(ops, dim, heads, q4):
+    """One thread may have a token's whole row."""
+    lens = [70, 300]
+    c = (Q if q4 else R).Cache(lens, heads, dim, 16, seed=dim + heads)
+    k, v = (torch.full((sum(lens) + 1, heads, dim), 7.0, dtype=c.tdtype, device="cuda") for _ in range(2))
+    starts = torch.tensor([0, 70, 370], dtype=torch.int32, device="cuda")
+    ops.kv_read(c.handle(B), 1, c.tables, c.lens, k_out=k[:-1], v_out=v[:-1], seq_starts=starts)
+    ops.kv_ops_sync()
+    for plane, have in enumerate((k, v)):
+        assert (have[-1] == 7).all()
+        for i, n in enumerate(lens):
+            if q4:
+                lo, step, code = c.held(i, 1, plane)
+                want = (lo + step * code).float().to(c.tdtype)
+            else:
+                want = c.read(i, 1, plane).cpu()
+            assert torch.equal(have[70 * i:70 * i + n].cpu(), want), (plane, i)
+
+
 # ---- evict ----------------------------------------------------------------------------------------------------------
 
 
