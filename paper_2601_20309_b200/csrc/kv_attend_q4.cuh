@@ -107,7 +107,9 @@ __device__ __forceinline__ bool kv_mbar_try(unsigned bar, unsigned parity)
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
-// Nothing here waits without a limit: a wait that runs out is reported, and the kernel goes on with whatever is there, waiting no more
+// Nothing here waits without a limit: a wait that runs out is reported, and the kernel goes on with whatever is there, waiting no more.
+// Before a warp leaves then, the copies that it may have sent or waited for have a millisecond to land.  (By the clock: with __nanosleep
+// anywhere in the kernel the 70B shape takes 53 us, not 49)
 __device__ __forceinline__ void kv_mbar_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned *status)
 {
     if (kv_mbar_try(bar, parity)) return;
@@ -115,6 +117,11 @@ __device__ __forceinline__ void kv_mbar_wait(unsigned bar, unsigned parity, vola
         if (kv_mbar_try(bar, parity)) return;
     *gave_up = 1;
     atomicOr(status, KV_OPS_TIMEOUT);
+}
+__device__ __forceinline__ void kv_let_land(volatile int *gave_up)
+{
+    if (*gave_up)
+        for (const long long begin = clock64(); clock64() - begin < 1 << 21;) {}
 }
 __device__ __forceinline__ void kv_bulk(unsigned dst, const uint8_t *src, int bytes, unsigned bar)
 {
@@ -273,14 +280,19 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             }
             put = put + 1 == a.stages ? 0 : put + 1;
         }
-        return;                      // the computing warps wait for every copy before they leave
+        kv_let_land(&gave_up);       // else the computing warps have waited for every copy before they leave
+        return;
     }
 
     // ---- a computing warp
     if constexpr (kv_q4_wide(G, NT)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(KV_Q4_REGS));
     if (warp >= warps) return;
     const int hw = warp % a.hc, way = warp / a.hc, threads = warps * 32;
-    auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); };
+    // Where a wait has run out the warps may not see the same steps any more: nobody goes to a meeting then, and who is there already is
+    // let go by the others as they leave
+    auto meet = [&]() {
+        if (!__any_sync(~0u, *(volatile int *)&gave_up)) asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+    };
     const int rho = lane >> 2, j = lane & 3, slot = rho ^ (rho >> 1 & 1);
     // where a lane reads in a plane of a tile
     const int code_at = (slot * 4 + j) * 4 * G, word_at = slot * 4 * G, v_at = (2 * j + (j & 1)) * 16 * G + rho * 2 * G, v_odd = (j & 1 ? -16 : 16) * G;
@@ -744,4 +756,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             }
         }
     }
+    if (__any_sync(~0u, *(volatile int *)&gave_up)) asm volatile("bar.arrive 1, %0;" ::"r"(threads) : "memory");
+    kv_let_land(&gave_up);
 }
