@@ -12,10 +12,11 @@
 //   which makes it float16 without loss down to 2^-26 of that.  The sum over lo is one more instruction in the cache's type, with Q_g
 //   split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
 //   O^T[dim, 8 heads] = V^T (P s)^T, again by groups; p s is rounded to float16, the only rounding besides the output's (p itself, for
-//   the sum over lo and the row's sum, stays in float32).  What keeps p s in float16's range is the reference that is subtracted from the
-//   scores: the running maximum plus the exponent of the largest step met so far, less 8.  Products below 2^-22 of the row's largest
-//   lose bits, below 2^-32 they vanish.  The reference moves only when a score passes it by 6 or a step is larger: a
-//   vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
+//   the sum over lo and the row's sum, stays in float32).  The maximum that is subtracted from the scores is taken anew only when a step's
+//   weights add up to more than 64 in a lane: a vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
+//   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest step met so far; the row's
+//   maximum and sum, and with them lse and weights, know nothing of V.  Products below 2^-22 of the largest weight times the largest
+//   step lose bits, below 2^-32 they vanish.
 // Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
 // that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
@@ -34,13 +35,16 @@
 // shows: without the masks (a fifth of the instructions) 51.2 us, without the transpositions 50.7, without the second product 49.4,
 // against 51.0 at the same time.
 #pragma once
+#include <cfloat>
 #include <type_traits>
 
 #include "kv_attend.cuh"
 
 constexpr int KV_Q4_WARPS = 8, KV_Q4_LOADERS = 4, KV_Q4_STAGES = 6;  // warps that compute, and that load
-constexpr float KV_Q4_SLACK = 6.f, KV_Q4_LIFT = 8.f;
-constexpr int KV_Q4_LOWEST = -80;    // exponent of a step below which it counts as this: sums of 2^31 weights stay in range
+constexpr float KV_Q4_SUM = 64.f;    // what the weights of a step may add up to in a lane before the maximum is taken anew
+constexpr float KV_Q4_STEP = 0x1p9f; // what a step of V may be in the sums' unit; a new unit makes the largest 2^8 or more
+constexpr int KV_Q4_LIFT = 8;
+constexpr int KV_Q4_LOWEST = -110;   // exponent of the smallest unit: weights up to 2^8 stay in range in it
 constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
 
 // Where sums and queries take more than 168 registers per thread, the warps that load give theirs to those that compute.  What all
@@ -298,8 +302,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     const int code_at = (slot * 4 + j) * 4 * G, word_at = slot * 4 * G, v_at = (2 * j + (j & 1)) * 16 * G + rho * 2 * G, v_odd = (j & 1 ? -16 : 16) * G;
     unsigned qf[NT][G][4], ql[NT][PARTS][2];
     float fb[NT][2];
-    float o[NT][G][2][4], lo[NT][G][2], m[NT][2], ref[NT][2], lim[NT][2], l[NT][2], rest[NT][2];     // rest: what l is too coarse for
-    int top_step = KV_Q4_LOWEST;
+    float o[NT][G][2][4], lo[NT][G][2], m[NT][2], per[NT][2], l[NT][2], rest[NT][2];     // per: one over the unit of o; rest: what l is too coarse for
     int take = 0;
     unsigned parity = 0;
     int h = 0, g0 = 0, heads = 0;
@@ -325,7 +328,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             g0 = tile.w % a.group_chunks * HEADS;
             heads = min(HEADS, a.group - g0);
             began = tile.x & 1 << 18;
-            top_step = KV_Q4_LOWEST;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int g = nt * 8 + rho;
@@ -403,9 +405,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     fb[nt][e] = __shfl_sync(~0u, scale, (2 * j + e) * 4);
-                    m[nt][e] = -INFINITY;
-                    lim[nt][e] = -INFINITY;
-                    ref[nt][e] = (float)KV_Q4_LOWEST - KV_Q4_LIFT;
+                    m[nt][e] = -FLT_MAX;             // any score moves it, -inf does not
+                    per[nt][e] = __uint_as_float((127 - KV_Q4_LOWEST) << 23);
                     l[nt][e] = rest[nt][e] = 0.f;
                 }
 #pragma unroll
@@ -480,6 +481,13 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                         w1[u][g] = on1 ? w1[u][g] : 0u;
                     }
                 }
+            // the scores are rounded here, so that the largest less the maximum is 0 whatever its size
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][nt][e] *= fb[nt][e & 1];
             if (a.scores)
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
@@ -490,56 +498,62 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                         for (int b = 0; b < 2; ++b, to += 8 * a.group) {
                             if (t + b * 8 >= a.c.max_len) continue;
-                            const float2 score = make_float2(y[u][nt][2 * b] * fb[nt][0], y[u][nt][2 * b + 1] * fb[nt][1]);
-                            if ((a.group & 1) == 0 && g < heads) *(float2 *)to = score;
+                            if ((a.group & 1) == 0 && g < heads) *(float2 *)to = make_float2(y[u][nt][2 * b], y[u][nt][2 * b + 1]);
                             else {
-                                if (g < heads) to[0] = score.x;
-                                if (g + 1 < heads) to[1] = score.y;
+                                if (g < heads) to[0] = y[u][nt][2 * b];
+                                if (g + 1 < heads) to[1] = y[u][nt][2 * b + 1];
                             }
                         }
                     }
-            // the largest step of the tiles: words are in the order of their steps; those of a group that is not finite do not count
-            unsigned most = 0;
+            // the lane's largest step (as its word, 2^-7 above it at most); groups that are not finite do not count
+            float most = 0.f;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int g = 0; g < G; ++g) most = max(most, max(w0[u][g], w1[u][g]));
-            most = __reduce_max_sync(~0u, most);
-            if (most >= 0x7f800000u) {
-                most = 0;
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int g = 0; g < G; ++g) most = max(most, max(w0[u][g] < 0x7f800000u ? w0[u][g] : 0u, w1[u][g] < 0x7f800000u ? w1[u][g] : 0u));
-                most = __reduce_max_sync(~0u, most);
-            }
-            const int step = (int)(most >> 23) - 127;
-            float top[NT][2];
-            bool moves = step > top_step;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    top[nt][e] = fmaxf(y[0][nt][e], y[0][nt][e + 2]);
-#pragma unroll
-                    for (int u = 1; u < SUB; ++u) top[nt][e] = fmaxf(top[nt][e], fmaxf(y[u][nt][e], y[u][nt][e + 2]));
-                    moves |= top[nt][e] > lim[nt][e];
-                }
-            if (__any_sync(~0u, moves)) {
-                top_step = max(top_step, step);
+                for (int g = 0; g < G; ++g) most = fmaxf(most, fmaxf(__uint_as_float(w0[u][g]), __uint_as_float(w1[u][g])));
+            float p[SUB][NT][4], sum[NT][2];
+            const auto add = [&]() {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float x = top[nt][e];
-                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
-                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                        x = fmaxf(x * fb[nt][e], m[nt][e]);
-                        const float now = kv_ref(x) + ((float)top_step - KV_Q4_LIFT), alpha = m[nt][e] == -INFINITY ? 0.f : kv_exp2(ref[nt][e] - now);
-                        m[nt][e] = x;
-                        ref[nt][e] = now;
-                        lim[nt][e] = (x + KV_Q4_SLACK) / fb[nt][e];
+                        sum[nt][e] = p[0][nt][e] + p[0][nt][e + 2];
+#pragma unroll
+                        for (int u = 1; u < SUB; ++u) sum[nt][e] += p[u][nt][e] + p[u][nt][e + 2];
+                    }
+            };
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[u][nt][e] = kv_exp2(y[u][nt][e] - m[nt][e & 1]);
+            add();
+            bool moves = most * per[0][0] > KV_Q4_STEP;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) moves |= sum[nt][e] > KV_Q4_SUM;
+            if (__any_sync(~0u, moves)) {
+                const int unit = 127 - (int)(__float_as_uint(per[0][0]) >> 23),
+                          now = max(unit, (int)(__reduce_max_sync(~0u, __float_as_uint(most)) >> 23) - 127 - KV_Q4_LIFT);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = m[nt][e];
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u) top = fmaxf(top, fmaxf(y[u][nt][e], y[u][nt][e + 2]));
+#pragma unroll
+                        for (int x = 4; x <= 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+                        top = ceilf(top);            // factors between maxima and between units are powers of two: nothing is rounded
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) p[u][nt][2 * b + e] = kv_exp2(y[u][nt][2 * b + e] - top);
+                        const float rise = top - m[nt][e], alpha = kv_exp2(-rise), beta = kv_exp2((float)(unit - now) - rise);
+                        m[nt][e] = top;
+                        per[nt][e] = __uint_as_float((127 - now) << 23);
                         l[nt][e] *= alpha;
                         rest[nt][e] *= alpha;
 #pragma unroll
@@ -547,29 +561,21 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                             lo[nt][g][e] *= alpha;
 #pragma unroll
                             for (int t = 0; t < 2; ++t) {
-                                o[nt][g][t][e] *= alpha;
-                                o[nt][g][t][e + 2] *= alpha;
+                                o[nt][g][t][e] *= beta;
+                                o[nt][g][t][e + 2] *= beta;
                             }
                         }
                     }
+                add();
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[u][nt][e] = kv_exp2(fmaf(y[u][nt][e], fb[nt][e & 1], -ref[nt][e & 1]));
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {            // compensated: weights of 2^-25 of the largest would vanish one by one
-                    float x = y[0][nt][e] + y[0][nt][e + 2];
-#pragma unroll
-                    for (int u = 1; u < SUB; ++u) x += y[u][nt][e] + y[u][nt][e + 2];
-                    x += rest[nt][e];
-                    const float sum = l[nt][e] + x;
-                    rest[nt][e] = x - (sum - l[nt][e]);
-                    l[nt][e] = sum;
+                    const float x = sum[nt][e] + rest[nt][e], total = l[nt][e] + x;
+                    rest[nt][e] = x - (total - l[nt][e]);
+                    l[nt][e] = total;
                 }
-            }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
                 // The rounding of p s is multiplied by a code, 0 to 15, where the element itself may lie near 0, and the sum over lo takes away
@@ -591,12 +597,13 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        const float(&p)[4] = y[u][nt];
-                        const unsigned p0 = kv_transpose(kv_pair(p[0] * s0, p[1] * s0, __half())), p1 = kv_transpose(kv_pair(p[2] * s1, p[3] * s1, __half()));
+                        const float(&q)[4] = p[u][nt];
+                        const unsigned p0 = kv_transpose(kv_pair(q[0] * per[nt][0] * s0, q[1] * per[nt][1] * s0, __half())),
+                                       p1 = kv_transpose(kv_pair(q[2] * per[nt][0] * s1, q[3] * per[nt][1] * s1, __half()));
                         kv_mma_f16(o[nt][g][0], even(r0), odd(r0), even(r1), odd(r1), p0, p1);
                         kv_mma_f16(o[nt][g][1], even(h0), odd(h0), even(h1), odd(h1), p0, p1);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(p[e], z0, fmaf(p[e + 2], z1, lo[nt][g][e]));
+                        for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(q[e], z0, fmaf(q[e + 2], z1, lo[nt][g][e]));
                     }
                 }
             }
@@ -621,7 +628,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     l[nt][e] += rest[nt][e];
 #pragma unroll
                     for (int x = 4; x <= 16; x <<= 1) l[nt][e] += __shfl_xor_sync(~0u, l[nt][e], x);
-                    m[nt][e] = l[nt][e] == 0.f ? -INFINITY : ref[nt][e];
+                    if (l[nt][e] == 0.f) m[nt][e] = -INFINITY;
+                    const float unit = __uint_as_float((254u << 23) - __float_as_uint(per[nt][e]));
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
 #pragma unroll
@@ -629,7 +637,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) o[nt][g][t][2 * b + e] = fmaf(o[nt][g][t][2 * b + e], b ? 0x1p20f : 0x1p24f, lo[nt][g][e]);
+                            for (int b = 0; b < 2; ++b) o[nt][g][t][2 * b + e] = fmaf(o[nt][g][t][2 * b + e] * (b ? 0x1p20f : 0x1p24f), unit, lo[nt][g][e]);
                     }
                 }
             const bool whole = began && (tile.x & 1 << 19);

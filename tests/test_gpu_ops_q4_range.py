@@ -1,0 +1,102 @@
+"""Attention over a cache in 4 bits at the ends of its number range: scores of any size, V of very different sizes, and what is left of the
+weights' bits.  Keys here are of one value per group, so that scores are known exactly and bounds need no term for them."""
+import math
+
+import pytest
+import torch
+
+import ops_reference as R
+import ops_reference_q4 as Q
+from paper_2601_20309_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    with B.KVOps(0) as o:
+        yield o
+
+
+def cache(scores, v, dtype="bf16", heads=1, bs=16, dim=128):
+    """One sequence per row of `scores`, a list of lists: K's first group holds a slot's score in every element, the others 0; V as given,
+    [slots, heads, dim] per sequence."""
+    c = Q.Cache([len(s) for s in scores], heads, dim, bs, dtype, layers=1, seed=1)
+    for i, s in enumerate(scores):
+        k = torch.zeros(len(s), heads, dim)
+        k[:, :, :32] = torch.tensor(s)[:, None, None]
+        assert torch.equal(k, k.to(c.tdtype).float())
+        c.write(i, 0, 0, k.to(c.tdtype))
+        c.write(i, 0, 1, v[i].to(c.tdtype))
+    return c
+
+
+def run(ops, c, factors, weights=False):
+    """Query head g's scores are factors[g] times the slots'.  (out, lse, weights out)"""
+    q = torch.zeros(len(c.lens_list), len(factors), c.dim, dtype=c.tdtype, device="cuda")
+    q[:, :, 0] = torch.tensor(factors)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device="cuda")
+    w = torch.zeros(len(c.lens_list), c.heads, c.longest, device="cuda") if weights else None
+    ops.kv_attend(c.handle(B), 0, q, c.tables, c.lens, c.longest, out=out, lse=lse, scale=1.0, weights_out=w)
+    ops.kv_ops_sync()
+    return out.double().cpu(), lse.double().cpu(), w.double().cpu() if weights else None
+
+
+def expected(c, scores, factor, i, h):
+    """(out, lse, p, p * step per slot and element, the same times what a code counts in a product: 0 to 15, or -8 to 7; size of the terms) in float64."""
+    s = torch.tensor(scores[i], dtype=torch.float64) * factor
+    top = s.max()
+    e = (s - top).exp()
+    p = e / e.sum()
+    lo, step, code = (x[:, h] for x in c.held(i, 0, 1))
+    count = torch.maximum(code, (code - 8).abs())
+    return (p @ (lo + step * code), float(top + e.sum().log()), p, p[:, None] * step, p[:, None] * step * count, p @ (lo.abs() + 8 * step + step * count))
+
+
+def check(c, scores, factors, got, left):
+    """`left`: what a weight times a step may be off by, of itself (2^-11: a rounding to float16).  Besides, and per slot, 2^-25 of a unit in which
+    the row's largest product is 2^8 or more, times a code of up to 15; exponentials, sums and the scores' one rounding 2^-18 (the largest weight's
+    score is off by 2^-23 of itself, and that of weights that count by no more than 2^-23 * (its size)); the output's rounding."""
+    out, lse, w = got
+    group = len(factors) // c.heads
+    for i in range(len(scores)):
+        total = torch.zeros(c.heads, len(scores[i]), dtype=torch.float64)
+        for g, f in enumerate(factors):
+            o, z, p, ps, terms, size = expected(c, scores, f, i, g // group)
+            near = 2.0 ** -18 + 2.0 ** -22 * max(abs(f * s) for s in scores[i])
+            bound = R.UNIT[c.dtype] * o.abs() + left * terms.sum(0) + near * size + len(scores[i]) * 15 * 2.0 ** -33 * ps.max() + (2.0 ** -25 if c.dtype == "f16" else 0)
+            bad = (out[i, g] - o).abs() - bound
+            assert (bad <= 0).all(), (i, g, float(bad.max()), float(bound.max()), out[i, g], o)
+            assert abs(lse[i, g] - z) <= 2.0 ** -20 * (1 + abs(z)), (i, g, float(lse[i, g]), z)
+            total[g // group] += p
+        if w is not None:
+            assert ((w[i, :, :len(scores[i])] - total).abs() <= 2.0 ** -17 * total + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("key,factor,size", [(32768.0, 50.0 * 128, 0.008), (32768.0, 33.0 * 128, 0.008 / 128), (61440.0, 60000.0, 1.0), (61440.0, 60000.0, 1e-4)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scores_of_any_size(ops, dtype, key, factor, size):
+    """Scores of 2e8 to 4e9: all the same, and one of them the largest."""
+    if dtype == "bf16":
+        key, factor = (float(torch.tensor(x).to(torch.bfloat16)) for x in (key, factor))
+    n = 100
+    scores = [[key] * n, [key / 2] * 37 + [key] + [key / 2] * (n - 38)]
+    g = torch.Generator().manual_seed(2)
+    v = [torch.randn(n, 1, 128, generator=g) * size for _ in scores]
+    c = cache(scores, v, dtype)
+    check(c, scores, [factor, -factor], run(ops, c, [factor, -factor]), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("power", [47, 60, 95, -60, -95])
+@pytest.mark.parametrize("n", [40, 300, 3000])
+def test_sums_and_weights_know_nothing_of_v(ops, power, n):
+    """V is 0 in the first slots and large or small behind them, in one CTA and in parts that meet: the slots in front keep their weight."""
+    g = torch.Generator().manual_seed(3)
+    scores = [(torch.randint(-32, 32, (n,), generator=g) / 16).tolist(), (torch.arange(n) // 64 / 4).tolist(), [1.0] * n]
+    scores[0][n - 1] = 6.0
+    v = [torch.randn(n, 2, 128, generator=g) * 2.0 ** power for _ in scores]
+    for i, first in enumerate((n // 2, n - 3, 5)):
+        v[i][:first] = 0.0
+    c = cache(scores, v, heads=2)
+    factors = [1.0, 0.25, -1.0, 0.0]
+    check(c, scores, factors, run(ops, c, factors, weights=True), 2.0 ** -11)
