@@ -14,9 +14,9 @@
 //   O^T[dim, 8 heads] = V^T (P s)^T, again by groups; p s is rounded to float16, the only rounding besides the output's (p itself, for
 //   the sum over lo and the row's sum, stays in float32).  The maximum that is subtracted from the scores is taken anew only when a step's
 //   weights add up to more than 64 in a lane: a vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
-//   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest step met so far; the row's
-//   maximum and sum, and with them lse and weights, know nothing of V.  Products below 2^-22 of the largest weight times the largest
-//   step lose bits, below 2^-32 they vanish.
+//   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest p s met so far, up where
+//   a larger one comes and down as the maximum rises; the row's maximum and sum, and with them lse and weights, know nothing of V, and
+//   a slot without weight sets no unit.  Products below 2^-22 of the row's largest lose bits, below 2^-33 they vanish.
 // Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
 // that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
@@ -42,7 +42,7 @@
 
 constexpr int KV_Q4_WARPS = 8, KV_Q4_LOADERS = 4, KV_Q4_STAGES = 6;  // warps that compute, and that load
 constexpr float KV_Q4_SUM = 64.f;    // what the weights of a step may add up to in a lane before the maximum is taken anew
-constexpr float KV_Q4_STEP = 0x1p9f; // what a step of V may be in the sums' unit; a new unit makes the largest 2^8 or more
+constexpr float KV_Q4_TOP = 0x1p15f; // what a product may be in the sums' unit; a new unit makes the step's largest 2^8 or more
 constexpr int KV_Q4_LIFT = 8;
 constexpr int KV_Q4_LOWEST = -110;   // exponent of the smallest unit: weights up to 2^8 stay in range in it
 constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
@@ -505,43 +505,45 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                             }
                         }
                     }
-            // the lane's largest step (as its word, 2^-7 above it at most); groups that are not finite do not count
-            float most = 0.f;
+            // the largest step of each of the lane's slots (as its word, 2^-7 above it at most); groups that are not finite do not count
+            float big[SUB][2], most = 0.f;
 #pragma unroll
-            for (int u = 0; u < SUB; ++u)
+            for (int u = 0; u < SUB; ++u) {
+                big[u][0] = big[u][1] = 0.f;
 #pragma unroll
-                for (int g = 0; g < G; ++g) most = fmaxf(most, fmaxf(__uint_as_float(w0[u][g]), __uint_as_float(w1[u][g])));
+                for (int g = 0; g < G; ++g) {
+                    big[u][0] = fmaxf(big[u][0], __uint_as_float(w0[u][g]));
+                    big[u][1] = fmaxf(big[u][1], __uint_as_float(w1[u][g]));
+                }
+                most = fmaxf(most, fmaxf(big[u][0], big[u][1]));
+            }
             float p[SUB][NT][4], sum[NT][2];
-            const auto add = [&]() {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        sum[nt][e] = p[0][nt][e] + p[0][nt][e + 2];
-#pragma unroll
-                        for (int u = 1; u < SUB; ++u) sum[nt][e] += p[u][nt][e] + p[u][nt][e + 2];
-                    }
-            };
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) p[u][nt][e] = kv_exp2(y[u][nt][e] - m[nt][e & 1]);
-            add();
-            bool moves = most * per[0][0] > KV_Q4_STEP;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) moves |= sum[nt][e] > KV_Q4_SUM;
-            if (__any_sync(~0u, moves)) {
-                const int unit = 127 - (int)(__float_as_uint(per[0][0]) >> 23),
-                          now = max(unit, (int)(__reduce_max_sync(~0u, __float_as_uint(most)) >> 23) - 127 - KV_Q4_LIFT);
+                for (int e = 0; e < 2; ++e) {
+                    sum[nt][e] = p[0][nt][e] + p[0][nt][e + 2];
+#pragma unroll
+                    for (int u = 1; u < SUB; ++u) sum[nt][e] += p[u][nt][e] + p[u][nt][e + 2];
+                }
+            // no product is above the lane's sum times its largest step (each of them looked at takes the 70B shape 0.3 us more)
+            bool moves = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) moves |= sum[nt][e] > KV_Q4_SUM || sum[nt][e] * per[nt][e] * most > KV_Q4_TOP;
+            if (__any_sync(~0u, moves))
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = m[nt][e];
+                        float top = m[nt][e], part = 0.f;
 #pragma unroll
                         for (int u = 0; u < SUB; ++u) top = fmaxf(top, fmaxf(y[u][nt][e], y[u][nt][e + 2]));
 #pragma unroll
@@ -550,8 +552,19 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) p[u][nt][2 * b + e] = kv_exp2(y[u][nt][2 * b + e] - top);
-                        const float rise = top - m[nt][e], alpha = kv_exp2(-rise), beta = kv_exp2((float)(unit - now) - rise);
+                            for (int b = 0; b < 2; ++b) {
+                                p[u][nt][2 * b + e] = kv_exp2(y[u][nt][2 * b + e] - top);
+                                part = fmaxf(part, p[u][nt][2 * b + e] * big[u][b]);
+                            }
+                        sum[nt][e] = p[0][nt][e] + p[0][nt][e + 2];
+#pragma unroll
+                        for (int u = 1; u < SUB; ++u) sum[nt][e] += p[u][nt][e] + p[u][nt][e + 2];
+#pragma unroll
+                        for (int x = 4; x <= 16; x <<= 1) part = fmaxf(part, __shfl_xor_sync(~0u, part, x));
+                        const float rise = top - m[nt][e];
+                        const int unit = 127 - (int)(__float_as_uint(per[nt][e]) >> 23),
+                                  now = max(max(unit - (int)fminf(rise, 1000.f), KV_Q4_LOWEST), (int)(__float_as_uint(part) >> 23) - 127 - KV_Q4_LIFT);
+                        const float alpha = kv_exp2(-rise), beta = kv_exp2((float)(unit - now) - rise);
                         m[nt][e] = top;
                         per[nt][e] = __uint_as_float((127 - now) << 23);
                         l[nt][e] *= alpha;
@@ -566,8 +579,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                             }
                         }
                     }
-                add();
-            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

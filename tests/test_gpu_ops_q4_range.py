@@ -100,3 +100,32 @@ def test_sums_and_weights_know_nothing_of_v(ops, power, n):
     c = cache(scores, v, heads=2)
     factors = [1.0, 0.25, -1.0, 0.0]
     check(c, scores, factors, run(ops, c, factors, weights=True), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("power", [10, 26, 36, 80])
+@pytest.mark.parametrize("n,where", [(64, 0), (64, 40), (700, 0), (700, 333), (700, 699), (6000, 5000)])
+def test_a_slot_without_weight_takes_nothing_from_the_others(ops, power, n, where):
+    """One slot scores far below all others and its V is 2^power times theirs; and one that was the largest until the others came."""
+    g = torch.Generator().manual_seed(4)
+    low = (torch.randint(-16, 16, (n,), generator=g) / 8).tolist()
+    low[where] = -300.0
+    late = [300.0] * n
+    late[0] = 0.0
+    v = [torch.randn(n, 1, 128, generator=g) for _ in range(2)]
+    v[0][where] *= 2.0 ** power
+    v[1][0] *= 2.0 ** power
+    c = cache([low, late], v)
+    check(c, [low, late], [1.0, 0.5, 2.0], run(ops, c, [1.0, 0.5, 2.0], weights=True), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("power", [20, 60])
+def test_a_small_weight_of_a_large_value_counts(ops, power):
+    """Products of the same size from weights and steps of very different sizes, in either order; the maximum rises in every step."""
+    n = 500
+    for turn in (1, -1):
+        scores = [torch.linspace(-power, 0, n).mul(16).round().div(16).tolist()[::turn]]
+        g = torch.Generator().manual_seed(5)
+        v = [torch.randn(n, 1, 128, generator=g) * torch.exp(-torch.tensor(scores[0]))[:, None, None]]
+        scores = [torch.tensor(scores[0]).to(torch.bfloat16).float().tolist()]
+        c = cache(scores, v)
+        check(c, scores, [1.0, 0.5], run(ops, c, [1.0, 0.5], weights=True), 2.0 ** -11)
