@@ -11,8 +11,10 @@
 //   S^T[16 slots, 8 heads] = K Q^T, one group at a time.  q is scaled by a power of two so that its largest element lies in [2^8, 2^9),
 //   which makes it float16 without loss down to 2^-26 of that.  The sum over lo is one more instruction in the cache's type, with Q_g
 //   split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
-//   O^T[dim, 8 heads] = V^T (P s)^T, again by groups; p s is rounded to float16, the only rounding besides the output's (p itself, for
-//   the sum over lo and the row's sum, stays in float32).  The maximum that is subtracted from the scores is taken anew only when a step's
+//   O^T[dim, 8 heads] = V^T (P s)^T, again by groups, on codes less 8, so that they and lo + 8 s add up to little each.  p s is rounded to
+//   float16.  f16 outputs are fine enough to show that (over 131072 slots they were off by 2.8e-4, and with float32 weights are by 2.1e-4), so there
+//   what the rounding leaves goes through the same product: 20.7 to 21.7 us.  bf16 outputs are not (0.00173 and 0.00171), and the 70B shape would
+//   take 57.3 instead of 52.0 us.  (p itself, for the sum over lo and the row's sum, stays in float32.)  The maximum that is subtracted from the scores is taken anew only when a step's
 //   weights add up to more than 64 in a lane: a vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
 //   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest p s met so far, up where
 //   a larger one comes and down as the maximum rises; the row's maximum and sum, and with them lse and weights, know nothing of V, and
@@ -81,6 +83,13 @@ __device__ __forceinline__ unsigned kv_add2(unsigned x, unsigned y)
     const __half2 v = __hadd2(*(const __half2 *)&x, *(const __half2 *)&y);
     return *(const unsigned *)&v;
 }
+// what two numbers have beyond their roundings to float16, as float16
+__device__ __forceinline__ unsigned kv_left(unsigned rounded, float x, float y)
+{
+    float a, b;
+    asm("{ .reg .b16 l, h, m; mov.b32 {l, h}, %2; mov.b16 m, 0xbc00; fma.rn.f32.f16 %0, l, m, %3; fma.rn.f32.f16 %1, h, m, %4; }" : "=f"(a), "=f"(b) : "r"(rounded), "f"(x), "f"(y));
+    return kv_pair(a, b, __half());
+}
 __device__ __forceinline__ unsigned kv_transpose(unsigned x)
 {
     unsigned y;
@@ -138,7 +147,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     constexpr int PLANE = 320 * G, WORDS = 256 * G, HEADS = 8 * NT;     // bytes of a tile's plane, and of its codes
     constexpr int PARTS = G == 8 ? 2 : 1;        // matrix instructions for the sum over lo
     constexpr int SUB = kv_q4_sub(G, NT);
-    constexpr bool EXACT = std::is_same<T, __half>::value;      // see the sums over V
+    constexpr bool EXACT = std::is_same<T, __half>::value;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int red[KV_Q4_WARPS + KV_Q4_LOADERS], s_at[2], gave_up;
     __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
@@ -589,10 +598,10 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                 }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                // The rounding of p s is multiplied by a code, 0 to 15, where the element itself may lie near 0, and the sum over lo takes away
-                // most of what the codes add up to.  For f16 outputs, fine enough to show both, codes are -8 to 7 and lo is lo + 8 s
-                const auto even = [](unsigned x) { return EXACT ? kv_add2(x & 0x000f000fu, 0x80088008u) : x & 0x000f000fu; };
-                const auto odd = [](unsigned x) { return EXACT ? kv_add2(x & 0x00f000f0u, 0x80808080u) : x & 0x00f000f0u; };
+                // The sum over lo would take away most of what codes from 0 to 15 add up to, but not what was rounded: they are -8 to 7
+                // and lo is lo + 8 s
+                const auto even = [](unsigned x) { return kv_add2(x & 0x000f000fu, 0x80088008u); };
+                const auto odd = [](unsigned x) { return kv_add2(x & 0x00f000f0u, 0x80808080u); };
                 unsigned v[4][G / 2];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
@@ -601,18 +610,22 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);
                     const unsigned h0 = r0 >> 8, h1 = r1 >> 8;
                     const float s0 = __uint_as_float(w0[u][g] & 0xffff0000u), s1 = __uint_as_float(w1[u][g] & 0xffff0000u);
-                    float z0 = kv_unpair(w0[u][g], T()).x, z1 = kv_unpair(w1[u][g], T()).x;
-                    if constexpr (EXACT) {
-                        z0 = fmaf(8.f, s0, z0);
-                        z1 = fmaf(8.f, s1, z1);
-                    }
+                    const float z0 = fmaf(8.f, s0, kv_unpair(w0[u][g], T()).x), z1 = fmaf(8.f, s1, kv_unpair(w1[u][g], T()).x);
+                    const unsigned a0 = even(r0), a1 = odd(r0), a2 = even(r1), a3 = odd(r1), b0 = even(h0), b1 = odd(h0), b2 = even(h1), b3 = odd(h1);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         const float(&q)[4] = p[u][nt];
-                        const unsigned p0 = kv_transpose(kv_pair(q[0] * per[nt][0] * s0, q[1] * per[nt][1] * s0, __half())),
-                                       p1 = kv_transpose(kv_pair(q[2] * per[nt][0] * s1, q[3] * per[nt][1] * s1, __half()));
-                        kv_mma_f16(o[nt][g][0], even(r0), odd(r0), even(r1), odd(r1), p0, p1);
-                        kv_mma_f16(o[nt][g][1], even(h0), odd(h0), even(h1), odd(h1), p0, p1);
+                        const float x0 = q[0] * per[nt][0] * s0, x1 = q[1] * per[nt][1] * s0, x2 = q[2] * per[nt][0] * s1, x3 = q[3] * per[nt][1] * s1;
+                        const unsigned lower = kv_pair(x0, x1, __half()), upper = kv_pair(x2, x3, __half());
+                        unsigned p0 = kv_transpose(lower), p1 = kv_transpose(upper);
+                        kv_mma_f16(o[nt][g][0], a0, a1, a2, a3, p0, p1);
+                        kv_mma_f16(o[nt][g][1], b0, b1, b2, b3, p0, p1);
+                        if constexpr (EXACT) {
+                            p0 = kv_transpose(kv_left(lower, x0, x1));
+                            p1 = kv_transpose(kv_left(upper, x2, x3));
+                            kv_mma_f16(o[nt][g][0], a0, a1, a2, a3, p0, p1);
+                            kv_mma_f16(o[nt][g][1], b0, b1, b2, b3, p0, p1);
+                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) lo[nt][g][e] = fmaf(q[e], z0, fmaf(q[e + 2], z1, lo[nt][g][e]));
                     }

@@ -53,10 +53,11 @@ def expected(c, scores, factor, i, h):
     return (p @ (lo + step * code), float(top + e.sum().log()), p, p[:, None] * step, p[:, None] * step * count, p @ (lo.abs() + 8 * step + step * count))
 
 
-def check(c, scores, factors, got, left):
+def check(c, scores, factors, got, left, centred=False):
     """`left`: what a weight times a step may be off by, of itself (2^-11: a rounding to float16).  Besides, and per slot, 2^-25 of a unit in which
     the row's largest product is 2^8 or more, times a code of up to 15; exponentials, sums and the scores' one rounding 2^-18 (the largest weight's
-    score is off by 2^-23 of itself, and that of weights that count by no more than 2^-23 * (its size)); the output's rounding."""
+    score is off by 2^-23 of itself, and that of weights that count by no more than 2^-23 * (its size)); the output's rounding.  `centred`: codes count from -8
+    to 7."""
     out, lse, w = got
     group = len(factors) // c.heads
     for i in range(len(scores)):
@@ -64,6 +65,9 @@ def check(c, scores, factors, got, left):
         for g, f in enumerate(factors):
             o, z, p, ps, terms, size = expected(c, scores, f, i, g // group)
             near = 2.0 ** -18 + 2.0 ** -22 * max(abs(f * s) for s in scores[i])
+            if centred:
+                lo, step, code = (x[:, g // group] for x in c.held(i, 0, 1))
+                terms = ps * (code - 8).abs()
             bound = R.UNIT[c.dtype] * o.abs() + left * terms.sum(0) + near * size + len(scores[i]) * 15 * 2.0 ** -33 * ps.max() + (2.0 ** -25 if c.dtype == "f16" else 0)
             bad = (out[i, g] - o).abs() - bound
             assert (bad <= 0).all(), (i, g, float(bad.max()), float(bound.max()), out[i, g], o)
@@ -129,3 +133,31 @@ def test_a_small_weight_of_a_large_value_counts(ops, power):
         scores = [torch.tensor(scores[0]).to(torch.bfloat16).float().tolist()]
         c = cache(scores, v)
         check(c, scores, [1.0, 0.5], run(ops, c, [1.0, 0.5], weights=True), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("n", [5, 40, 333, 5000])
+def test_f16_outputs_have_the_weights_in_float32(ops, n):
+    """What the rounding of a weight times a step to float16 leaves is there too: 2^-22 of it is lost at most."""
+    g = torch.Generator().manual_seed(6)
+    scores = [(torch.randint(-64, 64, (n,), generator=g) / 32).tolist() for _ in range(2)]
+    c = cache(scores, [torch.randn(n, 2, 128, generator=g) for _ in range(2)], "f16", heads=2)
+    check(c, scores, [1.0, 0.5, 1.5, -1.0], run(ops, c, [1.0, 0.5, 1.5, -1.0]), 2.0 ** -22, centred=True)
+
+
+def test_one_rounding_of_all_weights(ops):
+    """Every sixteenth slot has a larger score and V of zeros, the others one score and one step (V is -1 or 1), so that their weights are rounded alike,
+    by up to 2^-11.  That is 2^-11 of the sum of what they are multiplied with, not of the sum of its sizes: V adds up to little."""
+    n = 4000
+    g = torch.Generator().manual_seed(7)
+    scores = [[4.25 if t % 16 == 0 else 0.25 for t in range(n)]]
+    v = [torch.randint(0, 2, (n, 1, 128), generator=g).float() * 2 - 1]
+    v[0][::16] = 0.0
+    c = cache(scores, v)
+    factors = torch.tensor([0.1 + 0.05 * k for k in range(16)]).to(torch.bfloat16).float().tolist()
+    out, _, _ = run(ops, c, factors)
+    lo, step, code = (x[:, 0] for x in c.held(0, 0, 1))
+    for k, f in enumerate(factors):
+        o, _, p, ps, _, _ = expected(c, scores, f, 0, 0)
+        # exponentials: 2^-18 of the output (all alike); float32 sums: 2^-20 of the terms' sizes
+        bound = (2.0 ** -8 + 2.0 ** -18) * o.abs() + 2.0 ** -11 * (ps * (code - 8)).sum(0).abs() + 2.0 ** -20 * (p[:, None] * (lo.abs() + 8 * step)).sum(0) + n * 15 * 2.0 ** -33 * ps.max()
+        assert ((out[0, k] - o).abs() <= bound).all(), (k, float(((out[0, k] - o).abs() - bound).max()), float(bound.max()))
