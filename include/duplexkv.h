@@ -573,6 +573,11 @@ int32_t kv_ops_destroy(kv_ops_t *ops);
 /* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA of earlier calls, or KV_ERR_TIMEOUT where a bounded
  * wait inside a kernel ran out (its results are not to be used). */
 int32_t kv_ops_sync(kv_ops_t *ops);
+/* Limit of the waits inside the kernels (attention over a cache in 4 bits has some, for copies that it sent itself): `polls` looks, then more
+ * for `ns` nanoseconds (default 64 and 2 s; ns <= 60 s).  A wait that runs out ends its kernel, which waits for the copies it has in flight,
+ * with the default limit; its results are not to be used and kv_ops_sync returns KV_ERR_TIMEOUT from then on.  0 and 0: every such wait
+ * gives up without looking, which is how that path is exercised on a healthy GPU.  Applies to calls issued (and graphs captured) afterwards. */
+int32_t kv_ops_set_wait_limit(kv_ops_t *ops, uint32_t polls, uint64_t ns);
 /* Makes the workspace at least `bytes` large.  A call that needs more than there is does this itself, with a
  * cudaMalloc (not possible during stream capture: KV_ERR_NOMEM).  Outgrown workspaces stay allocated until
  * kv_ops_destroy, so graphs captured with them keep working. */

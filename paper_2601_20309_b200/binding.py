@@ -160,7 +160,7 @@ EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_set_path", "kv_swap_out
            "kv_req_info", "kv_req_blocks", "kv_table_get_stats", "kv_table_fail_pool_call",
            "kv_pool_set_wait_limit", "kv_pool_set_call_timing", "kv_completion_event", "kv_pool_set_ctas",
            "kv_debug_pair_in_bounds", "kv_rotate_req", "kv_debug_ring_shape",
-           "kv_ops_create", "kv_ops_destroy", "kv_ops_sync", "kv_ops_reserve", "kv_ops_last_error", "kv_pool_cache",
+           "kv_ops_create", "kv_ops_destroy", "kv_ops_sync", "kv_ops_reserve", "kv_ops_set_wait_limit", "kv_ops_last_error", "kv_pool_cache",
            "kv_attend", "kv_attend_workspace", "kv_append", "kv_append_normed", "kv_read", "kv_evict", "kv_evict_workspace",
            "kv_cache_row_units", "kv_req_shrink"]
 
@@ -268,6 +268,8 @@ def lib() -> C.CDLL:
         getattr(L, name).argtypes = [vp]
     L.kv_ops_reserve.restype = C.c_int32
     L.kv_ops_reserve.argtypes = [vp, i64]
+    L.kv_ops_set_wait_limit.restype = C.c_int32
+    L.kv_ops_set_wait_limit.argtypes = [vp, C.c_uint32, C.c_uint64]
     L.kv_ops_last_error.restype = C.c_char_p
     L.kv_ops_last_error.argtypes = [vp]
     L.kv_pool_cache.restype = C.c_int32
@@ -712,6 +714,10 @@ class KVOps:
 
     def kv_ops_reserve(self, nbytes: int, check: bool = True) -> int:
         return self._ret(lib().kv_ops_reserve(self._h, nbytes), check)
+
+    def kv_ops_set_wait_limit(self, polls: int, ns: int, check: bool = True) -> int:
+        """Limit of the waits inside kernels, for calls issued afterwards; 0 and 0: they give up without looking."""
+        return self._ret(lib().kv_ops_set_wait_limit(self._h, polls, ns), check)
 
     def kv_attend(self, cache: KVCache, layer: int, q, block_tables, lens, max_len: int, *, out, lse=None, window: int = 0,
                   scale: float = 0.0, weights_in=None, weights_out=None, check: bool = True) -> int:

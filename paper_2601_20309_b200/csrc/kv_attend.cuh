@@ -55,6 +55,8 @@ struct KvAttend {
     int q_pairs;         // q may be read in pairs of elements
     int block_tiles;     // of a 4-bit cache: tiles of a block where a step is made of whole blocks, else 0
     int q_vec, out_vec;  // of a 4-bit cache: q may be read in packs of 16 bytes, out written in packs of 8
+    unsigned wait_polls; // of a 4-bit cache: limit of a wait inside the kernel, looks and nanoseconds
+    unsigned long long wait_ns;
     int whole_tiles;     // the block size is a multiple of 16: a tile lies in one block
     float *scores;       // [seq][kv_head][max_len][group], base 2; nullptr: no weights wanted
     float2 *part_ml;     // [piece][2][hc][8*NT]: maximum and sum

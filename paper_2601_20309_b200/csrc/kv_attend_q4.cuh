@@ -47,7 +47,6 @@ constexpr float KV_Q4_SUM = 64.f;    // what the weights of a step may add up to
 constexpr float KV_Q4_TOP = 0x1p15f; // what a product may be in the sums' unit; a new unit makes the step's largest 2^8 or more
 constexpr int KV_Q4_LIFT = 8;
 constexpr int KV_Q4_LOWEST = -110;   // exponent of the smallest unit: weights up to 2^8 stay in range in it
-constexpr int KV_Q4_POLLS = 1 << 20; // a wait gives up after so many
 
 // Where sums and queries take more than 168 registers per thread, the warps that load give theirs to those that compute.  What all
 // have together has to be there at the launch: kv_q4_fits
@@ -120,21 +119,30 @@ __device__ __forceinline__ bool kv_mbar_try(unsigned bar, unsigned parity)
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
-// Nothing here waits without a limit: a wait that runs out is reported, and the kernel goes on with whatever is there, waiting no more.
-// Before a warp leaves then, the copies that it may have sent or waited for have a millisecond to land.  (By the clock: with __nanosleep
-// anywhere in the kernel the 70B shape takes 53 us, not 49)
-__device__ __forceinline__ void kv_mbar_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned *status)
+__device__ __forceinline__ unsigned long long kv_now()
 {
-    if (kv_mbar_try(bar, parity)) return;
-    for (int polls = 0; polls < KV_Q4_POLLS && !*gave_up; ++polls)
-        if (kv_mbar_try(bar, parity)) return;
-    *gave_up = 1;
-    atomicOr(status, KV_OPS_TIMEOUT);
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
 }
-__device__ __forceinline__ void kv_let_land(volatile int *gave_up)
+// Nothing here waits without a limit: `polls` looks, then looks for another `ns` (0 and 0: not one).  By a whole warp, and the same for all its
+// lanes: true when the phase is over, false when the limit is reached or another warp has given up before.
+__device__ __forceinline__ bool kv_mbar_wait(unsigned bar, unsigned parity, unsigned polls, unsigned long long ns, const volatile int *gave_up)
 {
-    if (*gave_up)
-        for (const long long begin = clock64(); clock64() - begin < 1 << 21;) {}
+    bool there = polls && kv_mbar_try(bar, parity);
+    if (__all_sync(~0u, there)) return true;
+    unsigned long long begin = 0;
+    for (unsigned n = 1;; ++n) {
+        bool out = gave_up && *gave_up;
+        if (n >= polls) {
+            const unsigned long long now = kv_now();
+            if (!begin) begin = now;
+            out |= now - begin >= ns;
+        }
+        if (__any_sync(~0u, out)) return false;
+        there = there || kv_mbar_try(bar, parity);
+        if (__all_sync(~0u, there)) return true;
+    }
 }
 __device__ __forceinline__ void kv_bulk(unsigned dst, const uint8_t *src, int bytes, unsigned bar)
 {
@@ -169,8 +177,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
         }
 
     const unsigned filled = (unsigned)__cvta_generic_to_shared(bars[0]), empty = (unsigned)__cvta_generic_to_shared(bars[1]);
-    // what a computing warp finds in place of a step that it waited for in vain is a tile of the first sequence without slots
-    for (int e = tid; e < KV_Q4_STAGES * KV_Q4_WARPS * SUB; e += blockDim.x) (&info[0][0])[e] = make_int4(0, 0, 0, 0);
     if (tid == 0) {
         gave_up = 0;
         for (int s = 0; s < a.stages; ++s) {
@@ -199,6 +205,16 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     if (todo <= 0) return;
     __syncthreads();                 // the barriers are there
     const int k0 = pk;
+    // A wait that has run out is reported, and ends the step loops of all warps: as each of them next waits, if not before.  A stage is
+    // written only after all who read it have said so, so that until then every warp finds in it what it expects.
+    const auto in_time = [&](unsigned bar, unsigned parity) {
+        if (kv_mbar_wait(bar, parity, a.wait_polls, a.wait_ns, &gave_up)) return true;
+        if (lane == 0) {
+            *(volatile int *)&gave_up = 1;
+            atomicOr(a.c.status, KV_OPS_TIMEOUT);
+        }
+        return false;
+    };
 
     const int loader = warp - ((int)(blockDim.x >> 5) - KV_Q4_LOADERS);
     if (loader >= 0) {
@@ -229,7 +245,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             }
         };
         peek();
-        for (int n = 0; n < todo; ++n) {
+        int n = 0;
+        for (; n < todo; ++n) {
             const int t0 = span.base + pk * a.tw * 16, t = t0 + lane * per, lo = max(span.first - t, 0), hi = min(span.n - t, per);
             const bool ends = pk == psteps - 1;
             const int flags = (fresh ? 1 << 16 : 0) | (ends || n == todo - 1 ? 1 << 17 : 0) | (pk == 0 ? 1 << 18 : 0) | (ends ? 1 << 19 : 0);
@@ -261,7 +278,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                 }
             }
             if (n + 1 < todo) peek();
-            if (n >= a.stages) kv_mbar_wait(empty + 8 * put, (n / a.stages - 1) & 1, &gave_up, a.c.status);
+            if (n >= a.stages && !in_time(empty + 8 * put, (n / a.stages - 1) & 1)) break;
             if (loader == 0 && lane < roles && lane % runs == 0) info[put][lane / runs] = what;
             __syncwarp();
             const unsigned stage = ring + put * stage_bytes, bar = filled + 8 * put;
@@ -293,7 +310,11 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             }
             put = put + 1 == a.stages ? 0 : put + 1;
         }
-        kv_let_land(&gave_up);       // else the computing warps have waited for every copy before they leave
+        // the CTA does not end before its copies: whether or not anybody still waits for them, this warp does
+        if (!a.block_tiles) asm volatile("cp.async.wait_all;" ::: "memory");
+        else
+            for (int k = max(n - a.stages, 0); k < n; ++k)
+                if (!kv_mbar_wait(filled + 8 * (k % a.stages), (k / a.stages) & 1, KV_OPS_WAIT_POLLS, KV_OPS_WAIT_NS, nullptr) && lane == 0) atomicOr(a.c.status, KV_OPS_TIMEOUT);
         return;
     }
 
@@ -301,8 +322,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     if constexpr (kv_q4_wide(G, NT)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(KV_Q4_REGS));
     if (warp >= warps) return;
     const int hw = warp % a.hc, way = warp / a.hc, threads = warps * 32;
-    // Where a wait has run out the warps may not see the same steps any more: nobody goes to a meeting then, and who is there already is
-    // let go by the others as they leave
+    // Where a wait has run out not every warp comes to a meeting any more: nobody goes to one then, and who is there already is let go by the
+    // others as they leave
     auto meet = [&]() {
         if (!__any_sync(~0u, *(volatile int *)&gave_up)) asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
     };
@@ -321,7 +342,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     const int to_next = block == 1 ? 2 * to_v : WORDS, to_words = block * WORDS - in_block * (WORDS - 64 * G), next_words = block == 1 ? to_next : 64 * G;
     const uint8_t *own = smem + ((way * SUB / block * 2 * a.hc + hw) * block) * PLANE + in_block * WORDS;
     for (int n = 0; n < todo; ++n) {
-        kv_mbar_wait(filled + 8 * take, parity, &gave_up, a.c.status);
+        if (!in_time(filled + 8 * take, parity)) break;
         const int4 tile = info[take][way * SUB];
         unsigned mask[SUB], some = tile.x & 0xffff, all = some;
         mask[0] = some;
@@ -789,5 +810,4 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
         }
     }
     if (__any_sync(~0u, *(volatile int *)&gave_up)) asm volatile("bar.arrive 1, %0;" ::"r"(threads) : "memory");
-    kv_let_land(&gave_up);
 }

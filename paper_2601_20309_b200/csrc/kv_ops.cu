@@ -22,6 +22,8 @@ struct kv_ops {
     std::vector<void *> outgrown;    // earlier workspaces: captured graphs may hold them
     unsigned *status_host = nullptr, *status_dev = nullptr;
     int32_t sticky = KV_OK;
+    unsigned wait_polls = KV_OPS_WAIT_POLLS;      // kv_ops_set_wait_limit
+    unsigned long long wait_ns = KV_OPS_WAIT_NS;
     bool attend_ready[2][2][3][2] = {};   // [4 bits][bf16][head dimension][query tiles]: shared-memory limit raised
     char err[256];
 };
@@ -297,6 +299,15 @@ int32_t kv_ops_reserve(kv_ops_t *o, int64_t bytes)
     return grow_workspace(o, bytes);
 }
 
+int32_t kv_ops_set_wait_limit(kv_ops_t *o, uint32_t polls, uint64_t ns)
+{
+    if (!o) return KV_ERR_INVALID_ARG;
+    if (ns > 60000000000ull) return fail(o, KV_ERR_INVALID_ARG, "a wait of more than 60 s");
+    o->wait_polls = polls;
+    o->wait_ns = ns;
+    return KV_OK;
+}
+
 int32_t kv_ops_sync(kv_ops_t *o)
 {
     if (!o) return KV_ERR_INVALID_ARG;
@@ -361,6 +372,8 @@ int32_t kv_attend(kv_ops_t *o, const kv_cache_t *cache, const kv_attend_args_t *
     k.part_of = (int4 *)(o->ws + p.part_of);
     k.part_ml = (float2 *)(o->ws + p.part_ml);
     k.part_o = (float *)(o->ws + p.part_o);
+    k.wait_polls = o->wait_polls;
+    k.wait_ns = o->wait_ns;
 
     const bool bf16 = is_bf16(cache), q4 = k.c.groups != 0, wide = q4 && kv_q4_wide(k.c.groups, p.nt);
     const void *kernel = bf16 ? attend_kernel<__nv_bfloat16>(p.dp, p.nt, q4) : attend_kernel<__half>(p.dp, p.nt, q4);

@@ -18,6 +18,10 @@
 #define KV_OPS_TIMEOUT   4u   // a wait inside a kernel ran out: its results are not to be used
 #define KV_OPS_BAD_LEN   2u   // a length outside [0, max_len]: the sequence was taken as empty
 
+// limit of a wait inside a kernel, where the context has no other: so many looks (each may take the hardware some microseconds), then two seconds
+constexpr unsigned KV_OPS_WAIT_POLLS = 64;
+constexpr unsigned long long KV_OPS_WAIT_NS = 2000000000ull;
+
 struct KvView {
     uint8_t *base;
     long long blk_stride, plane_stride;   // bytes
