@@ -571,7 +571,7 @@ int32_t kv_ops_create(int32_t device_id, void *stream, kv_ops_t **out);
 /* Waits for the stream, then frees the context and its workspace. */
 int32_t kv_ops_destroy(kv_ops_t *ops);
 /* Waits for the stream.  KV_OK, or the sticky KV_ERR_RANGE / KV_ERR_CUDA of earlier calls, or KV_ERR_TIMEOUT where a bounded
- * wait inside a kernel ran out (its results are not to be used). */
+ * wait inside a kernel ran out (its results are not to be used; takes the place of a KV_ERR_RANGE). */
 int32_t kv_ops_sync(kv_ops_t *ops);
 /* Limit of the waits inside the kernels (attention over a cache in 4 bits has some, for copies that it sent itself): `polls` looks, then more
  * for `ns` nanoseconds (default 64 and 2 s; ns <= 60 s).  A wait that runs out ends its kernel, which waits for the copies it has in flight,

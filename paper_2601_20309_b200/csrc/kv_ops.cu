@@ -315,12 +315,14 @@ int32_t kv_ops_sync(kv_ops_t *o)
     const cudaError_t e = cudaStreamSynchronize(o->stream);
     if (e != cudaSuccess) return fail_cuda(o, e, "cudaStreamSynchronize");
     const unsigned st = *(volatile unsigned *)o->status_host;
-    if (st && o->sticky == KV_OK) {
-        o->sticky = st & KV_OPS_TIMEOUT ? KV_ERR_TIMEOUT : KV_ERR_RANGE;
-        if (st & KV_OPS_TIMEOUT) snprintf(o->err, 256, "a wait inside a kernel ran out (status 0x%x)", st);
-        else
-            snprintf(o->err, 256, "a kernel met %s and skipped it (status 0x%x)",
-                     st & KV_OPS_BAD_BLOCK ? "a block id outside the cache" : "a length outside its bounds", st);
+    // results that are not to be used outrank slots that were skipped
+    if (st & KV_OPS_TIMEOUT && (o->sticky == KV_OK || o->sticky == KV_ERR_RANGE)) {
+        o->sticky = KV_ERR_TIMEOUT;
+        snprintf(o->err, 256, "a wait inside a kernel ran out (status 0x%x)", st);
+    } else if (st && o->sticky == KV_OK) {
+        o->sticky = KV_ERR_RANGE;
+        snprintf(o->err, 256, "a kernel met %s and skipped it (status 0x%x)",
+                 st & KV_OPS_BAD_BLOCK ? "a block id outside the cache" : "a length outside its bounds", st);
     }
     return o->sticky;
 }

@@ -73,3 +73,28 @@ def test_wait_limit_arguments():
         q = torch.randn(1, 8, 128, generator=c.g).to(c.tdtype).cuda()
         call(ops, c, q, 0, True)
         ops.kv_ops_sync()
+
+
+def test_a_timeout_outranks_a_bad_length():
+    """A context that has skipped a sequence before says so, and says that results are not to be used once a wait has run out."""
+    c = Q.Cache([300, 20], 2, 128, 16, seed=3, layers=1)
+    q = torch.randn(2, 8, 128, generator=c.g).to(c.tdtype).cuda()
+    with B.KVOps(0) as ops:
+        lens, right = torch.tensor([300, 500], dtype=torch.int32, device="cuda"), c.lens
+        c.lens = lens
+        call(ops, c, q, 0, False)
+        assert ops.kv_ops_sync(check=False) == B.KV_ERR_RANGE
+        c.lens = right
+        call(ops, c, q, 0, False)
+        assert ops.kv_ops_sync(check=False) == B.KV_ERR_RANGE
+        ops.kv_ops_set_wait_limit(0, 0)
+        call(ops, c, q, 0, False)
+        with pytest.raises(B.KVError, match="ran out") as e:
+            ops.kv_ops_sync()
+        assert e.value.code == B.KV_ERR_TIMEOUT
+        # and a bad length afterwards does not hide it
+        ops.kv_ops_set_wait_limit(64, 2 * 10 ** 9)
+        c.lens = lens
+        call(ops, c, q, 0, False)
+        assert ops.kv_ops_sync(check=False) == B.KV_ERR_TIMEOUT
+        c.lens = right
