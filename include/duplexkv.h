@@ -665,7 +665,7 @@ int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t
  * kv_append with norms of q and k over the elements of each head, in front of the rotation and in the same pass:
  *     x_d -> x_d / sqrt(sum_d x_d^2 / head_dim + eps) * weight_d
  * in float32 (keys of a 4-bit cache in float64, so that their codes are those of the formula), rounded once, after the rotation.  In
- * float32 the squares have to stay in range: elements between 2^-60 and 2^60 or 0.  norms NULL, or both weights NULL: kv_append.
+ * float32 the squares of a row and their sum have to stay in range: elements between 2^-60 and 2^59 or 0.  norms NULL, or both weights NULL: kv_append.
  */
 typedef struct {
     const void *q_weight, *k_weight;        /* [heads][head_dim]; NULL: q (k) is not normed                  */
