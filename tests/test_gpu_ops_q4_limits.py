@@ -1,4 +1,4 @@
-"""Norms of rows at the limits the header names, keys included."""
+"""Norms of rows at the limits the header names, keys included; tokens of no sequence are reported by kv_read."""
 import math
 
 import pytest
@@ -55,3 +55,15 @@ def test_norms_at_their_limits(ops, dim, q4):
             assert torch.equal(k.cpu(), (lo + step * code).float().to(torch.bfloat16))
         else:
             assert ((k.double().cpu() - want).abs() <= near).all()
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_read_reports_tokens_of_no_sequence(q4):
+    c = (Q if q4 else R).Cache([20, 9], 2, 64, 16, seed=3)
+    for starts, status in (([0, 20, 29], B.KV_OK), ([1, 20, 29], B.KV_ERR_RANGE), ([0, 20, 28], B.KV_ERR_RANGE), ([0, 21, 29], B.KV_ERR_RANGE)):
+        k = torch.full((29, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        with B.KVOps(0) as ops:
+            ops.kv_read(c.handle(B), 0, c.tables, c.lens, k_out=k, seq_starts=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+            assert ops.kv_ops_sync(check=False) == status, starts
+        nobody = [t for t in range(29) if t < starts[0] or t >= starts[2] or (starts[1] == 21 and t == 0)]
+        assert (k[nobody] == 7).all() and not (k[[t for t in range(29) if t not in nobody]] == 7).all(-1).any()
