@@ -659,6 +659,7 @@ typedef struct {
     const int32_t *token_order;     /* [num_tokens]: what goes into order; NULL = positions of axis 0   */
     uint8_t axis_of[128];           /* HOST, by value: axis of each frequency                           */
 } kv_append_args_t;
+/* q's, k's and v's heads are 4096 at most, together. */
 int32_t kv_append(kv_ops_t *ops, const kv_cache_t *cache, const kv_append_args_t *args);
 
 /*
@@ -678,7 +679,7 @@ int32_t kv_append_normed(kv_ops_t *ops, const kv_cache_t *cache, const kv_append
 /*
  * Rows of the cache, side by side and in 16 bits (of a 4-bit cache the values its codes stand for, rounded once).  The tokens are
  * those of a kv_append with the same seq_starts and lens: token j of sequence i's n_i comes from slot lens[i] - n_i + j.  A token
- * of no sequence, of an idle one, of a bad length or block is left as it was in k and v (and reported as there).
+ * of no sequence, of an idle one, of a bad length or block is left as it was in k and v (and reported as there).  At most 512 KV heads.
  */
 typedef struct {
     int32_t layer, num_seqs;

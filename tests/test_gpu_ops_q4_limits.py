@@ -1,4 +1,4 @@
-"""Norms of rows at the limits the header names, keys included; tokens of no sequence are reported by kv_read."""
+"""Norms of rows at the limits the header names, keys included; tokens of no sequence are reported by kv_read; the numbers of heads the calls take."""
 import math
 
 import pytest
@@ -67,3 +67,34 @@ def test_read_reports_tokens_of_no_sequence(q4):
             assert ops.kv_ops_sync(check=False) == status, starts
         nobody = [t for t in range(29) if t < starts[0] or t >= starts[2] or (starts[1] == 21 and t == 0)]
         assert (k[nobody] == 7).all() and not (k[[t for t in range(29) if t not in nobody]] == 7).all(-1).any()
+
+
+def test_numbers_of_heads(ops):
+    """kv_read takes up to 512 KV heads, kv_append up to 4096 rows per token, q's, k's and v's together; both refuse more."""
+    lens = torch.ones(1, dtype=torch.int32, device="cuda")
+    tables = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    store = torch.zeros(2 * 4 * 2048 * 20, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+
+    def rows(heads):
+        return torch.randn(1, heads, 8, device="cuda").to(torch.bfloat16)
+
+    def append(heads, q_heads):
+        cache = B.KVCache(store.data_ptr(), 1, 4, heads, 8, 1, dtype="bf16_q4")
+        q = rows(q_heads) if q_heads else None
+        ops.kv_append(cache, 0, q, rows(heads), rows(heads), tables, lens, positions=torch.zeros(1, 1, dtype=torch.int32, device="cuda"), inv_freq=angles(8), q_out=q)
+
+    cache = B.KVCache(store.data_ptr(), 1, 4, 512, 8, 1, dtype="bf16_q4")
+    k, out = rows(512), rows(512)
+    ops.kv_append(cache, 0, None, k, k, tables, lens, positions=torch.zeros(1, 1, dtype=torch.int32, device="cuda"), inv_freq=angles(8))
+    ops.kv_read(cache, 0, tables, lens, k_out=out)
+    ops.kv_ops_sync()
+    lo, step, code = Q.quantise(k.cpu())
+    assert torch.equal(out.cpu(), (lo + step * code).float().to(torch.bfloat16))
+    append(2048, 0)
+    append(1000, 2096)
+    ops.kv_ops_sync()
+    with pytest.raises(B.KVError, match="too many heads"):
+        append(2048, 1)
+    with pytest.raises(B.KVError, match="too many heads"):
+        ops.kv_read(B.KVCache(store.data_ptr(), 1, 4, 513, 8, 1, dtype="bf16_q4"), 0, tables, lens, k_out=rows(513))
