@@ -491,6 +491,14 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                         for (int p = 0; p < PARTS; ++p) kv_mma_lo(y[u][nt], p0, p1, ql[nt][p][0], ql[nt][p][1], T());
                 }
             }
+            // the scores are rounded here, so that the largest less the maximum is 0 whatever its size.  (Masked
+            // slots become -inf after that: a factor may be 0)
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][nt][e] *= fb[nt][e & 1];
             unsigned w0[SUB][G], w1[SUB][G];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
@@ -511,13 +519,6 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                         w1[u][g] = on1 ? w1[u][g] : 0u;
                     }
                 }
-            // the scores are rounded here, so that the largest less the maximum is 0 whatever its size
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[u][nt][e] *= fb[nt][e & 1];
             if (a.scores)
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)

@@ -161,3 +161,18 @@ def test_one_rounding_of_all_weights(ops):
         # exponentials: 2^-18 of the output (all alike); float32 sums: 2^-20 of the terms' sizes
         bound = (2.0 ** -8 + 2.0 ** -18) * o.abs() + 2.0 ** -11 * (ps * (code - 8)).sum(0).abs() + 2.0 ** -20 * (p[:, None] * (lo.abs() + 8 * step)).sum(0) + n * 15 * 2.0 ** -33 * ps.max()
         assert ((out[0, k] - o).abs() <= bound).all(), (k, float(((out[0, k] - o).abs() - bound).max()), float(bound.max()))
+
+
+@pytest.mark.parametrize("dtype,tiny", [("bf16", 2.0 ** -100), ("f16", 2.0 ** -24)])
+@pytest.mark.parametrize("n", [5, 45])
+def test_scores_too_small_for_float32_are_alike(ops, dtype, tiny, n):
+    """A factor that is 0 in float32 makes nothing of the slots that are masked."""
+    g = torch.Generator().manual_seed(8)
+    c = cache([[1.0] * n], [torch.randn(n, 1, 128, generator=g)], dtype)
+    q = torch.full((1, 2, 128), tiny, dtype=c.tdtype, device="cuda")
+    out, lse = torch.full_like(q, math.nan), torch.full((1, 2), math.nan, device="cuda")
+    ops.kv_attend(c.handle(B), 0, q, c.tables, c.lens, n, out=out, lse=lse, scale=2.0 ** -140)
+    ops.kv_ops_sync()
+    o, z, _, _, terms, size = expected(c, [[0.0] * n], 1.0, 0, 0)
+    assert ((out[0].double().cpu() - o).abs() <= R.UNIT[dtype] * o.abs() + 2.0 ** -11 * terms.sum(0) + 2.0 ** -18 * size).all()
+    assert ((lse.double().cpu() - z).abs() <= 2.0 ** -20 * (1 + z)).all()
