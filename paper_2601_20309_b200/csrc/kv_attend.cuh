@@ -66,6 +66,7 @@ struct KvAttend {
 };
 
 constexpr int KV_ATTEND_WARPS = 8, KV_ATTEND_STAGES = 6;
+static_assert(KV_ATTEND_STAGES <= 6, "the kernel knows how to wait for so many");
 constexpr float KV_LN2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float kv_exp2(float x)

@@ -43,6 +43,7 @@
 #include "kv_attend.cuh"
 
 constexpr int KV_Q4_WARPS = 8, KV_Q4_LOADERS = 4, KV_Q4_STAGES = 6;  // warps that compute, and that load
+static_assert(2 * KV_Q4_WARPS <= 16, "a lane looks after each plane of a block, two tiles per warp, and four lanes after a tile of one per warp");
 constexpr float KV_Q4_SUM = 64.f;    // what the weights of a step may add up to in a lane before the maximum is taken anew
 constexpr float KV_Q4_TOP = 0x1p15f; // what a product may be in the sums' unit; a new unit makes the step's largest 2^8 or more
 constexpr int KV_Q4_LIFT = 8;
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int red[KV_Q4_WARPS + KV_Q4_LOADERS], s_at[2], gave_up;
     __shared__ int4 info[KV_Q4_STAGES][KV_Q4_WARPS * SUB];
-    __shared__ float s_lse[KV_ATTEND_WARPS][HEADS];
+    __shared__ float s_lse[KV_Q4_WARPS][HEADS];
     __shared__ __align__(8) unsigned long long bars[2][KV_Q4_STAGES];    // filled, empty
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ways = a.tw / SUB, warps = a.hc * ways;
     const int rows_of_seq = a.head_chunks * a.group_chunks;

@@ -186,7 +186,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     // where one step is all there is, 6.9 (7.2) against 6.7 (6.8).
     auto shape = [&](int heads_wanted) {
         k.hc = 1;
-        for (int d = 2; d <= std::min(heads_wanted, KV_ATTEND_WARPS); ++d)
+        for (int d = 2; d <= std::min(heads_wanted, G ? KV_Q4_WARPS : KV_ATTEND_WARPS); ++d)
             if (c->kv_heads % d == 0) k.hc = d;
         k.tw = 1;
         while (k.hc * k.tw * 2 <= most && !(G && !k.whole_tiles && k.tw * 2 * kv_q4_sub(G, p.nt) > 8)) k.tw *= 2;   // rows are looked up by a warp: 8 tiles by fours
@@ -203,7 +203,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     k.head_chunks = c->kv_heads / k.hc;
     const int64_t box = p.warps > k.hc ? (int64_t)p.warps / 2 * (G ? kv_q4_box(G, p.nt) : p.nt * (p.dp / 16 + 1) * 4) * 32 * 4 : 0;
     const int64_t stage = G ? (int64_t)k.tw * k.hc * kv_q4_tile(G) : (int64_t)p.warps * 64 * p.dp;
-    k.stages = (int)std::min<int64_t>(KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);
+    k.stages = (int)std::min<int64_t>(G ? KV_Q4_STAGES : KV_ATTEND_STAGES, (ATTEND_SMEM - box) / stage);     // the kernels' tables have so many
     if (!split) k.stages = (int)std::max<int64_t>(1, std::min<int64_t>(k.stages, longest));
     p.smem = (size_t)(k.stages * stage + box);
     // the kernels round the number of steps up to their numbers of CTAs in 32 bits
