@@ -8,8 +8,8 @@
 // becomes a float16 number by a mask alone: four bits in the lowest places of a 16-bit word are code * 2^-24, in the next four places
 // code * 2^-20, both subnormal numbers that m16n8k16 multiplies exactly.  Eight codes cost four masks and a shift.  (The powers
 // of two are taken back in q, in the scale, and in the outputs.)
-//   S^T[16 slots, 8 heads] = K Q^T, one group at a time.  q is scaled by a power of two so that its largest element lies in [2^8, 2^9),
-//   which makes it float16 without loss down to 2^-26 of that.  The sum over lo is one more instruction in the cache's type, with Q_g
+//   S^T[16 slots, 8 heads] = K Q^T, one group at a time.  q is scaled by a power of two so that its largest element lies in [2^8, 2^9), and
+//   becomes float16: elements are off by 2^-33 of the largest at most, odd ones, which are taken times 2^-4 on top, by 2^-29.  The sum over lo is one more instruction in the cache's type, with Q_g
 //   split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
 //   O^T[dim, 8 heads] = V^T (P s)^T, again by groups, on codes less 8, so that they and lo + 8 s add up to little each.  p s is rounded to
 //   float16.  f16 outputs are fine enough to show that (over 131072 slots they were off by 2.8e-4, and with float32 weights are by 2.1e-4), so there
@@ -61,6 +61,7 @@ __host__ __device__ constexpr int kv_q4_tile(int groups) { return 640 * groups; 
 // floats of a lane that one way hands to another
 __host__ __device__ constexpr int kv_q4_box(int groups, int tiles) { return tiles * (8 * groups + 4); }
 
+// (these and kv_transpose may change places with what stands beside them, unlike those of the other kernel)
 __device__ __forceinline__ void kv_mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -95,20 +96,6 @@ __device__ __forceinline__ unsigned kv_transpose(unsigned x)
     unsigned y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
-}
-
-template <int N> __device__ __forceinline__ void kv_lds(unsigned (&r)[N], const uint8_t *at)
-{
-    if constexpr (N == 1) r[0] = *(const unsigned *)at;
-    else if constexpr (N == 2) {
-        const uint2 v = *(const uint2 *)at;
-        r[0] = v.x, r[1] = v.y;
-    } else
-#pragma unroll
-        for (int k = 0; k < N; k += 4) {
-            const uint4 v = *(const uint4 *)(at + k * 4);
-            r[k] = v.x, r[k + 1] = v.y, r[k + 2] = v.z, r[k + 3] = v.w;
-        }
 }
 
 __device__ __forceinline__ void kv_mbar_init(unsigned bar, int count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -454,10 +441,10 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             for (int u = 0; u < SUB; ++u) {
                 const uint8_t *at = kt + u * to_next;
                 unsigned c0[G], c1[G], w0[G], w1[G];
-                kv_lds(c0, at + code_at);
-                kv_lds(c1, at + code_at + 128 * G);
-                kv_lds(w0, kt + to_words + u * next_words + word_at);
-                kv_lds(w1, kt + to_words + u * next_words + word_at + 32 * G);
+                kv_words(c0, at + code_at);
+                kv_words(c1, at + code_at + 128 * G);
+                kv_words(w0, kt + to_words + u * next_words + word_at);
+                kv_words(w1, kt + to_words + u * next_words + word_at + 32 * G);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const unsigned h0 = c0[g] >> 8, h1 = c1[g] >> 8;
@@ -503,8 +490,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             unsigned w0[SUB][G], w1[SUB][G];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                kv_lds(w0[u], kt + to_v + to_words + u * next_words + word_at);
-                kv_lds(w1[u], kt + to_v + to_words + u * next_words + word_at + 32 * G);
+                kv_words(w0[u], kt + to_v + to_words + u * next_words + word_at);
+                kv_words(w1[u], kt + to_v + to_words + u * next_words + word_at + 32 * G);
             }
             if (all != 0xffffu)
 #pragma unroll
@@ -627,7 +614,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                 const auto odd = [](unsigned x) { return kv_add2(x & 0x00f000f0u, 0x80808080u); };
                 unsigned v[4][G / 2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) kv_lds(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
+                for (int r = 0; r < 4; ++r) kv_words(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);

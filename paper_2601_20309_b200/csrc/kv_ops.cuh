@@ -78,6 +78,21 @@ __device__ __forceinline__ unsigned kv_pair(float lo, float hi, __half)
     return *(const unsigned *)&v;
 }
 
+// neighbouring words, aligned to all of them or to 16 bytes
+template <int N> __device__ __forceinline__ void kv_words(unsigned (&r)[N], const uint8_t *at)
+{
+    if constexpr (N == 1) r[0] = *(const unsigned *)at;
+    else if constexpr (N == 2) {
+        const uint2 v = *(const uint2 *)at;
+        r[0] = v.x, r[1] = v.y;
+    } else
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const uint4 v = *(const uint4 *)(at + k * 4);
+            r[k] = v.x, r[k + 1] = v.y, r[k + 2] = v.z, r[k + 3] = v.w;
+        }
+}
+
 // the sequence that token t belongs to: the last one that starts at or before it.  A warp looks at 32 places at once
 __device__ __forceinline__ int kv_seq_of(const int *starts, int num_seqs, long long t)
 {

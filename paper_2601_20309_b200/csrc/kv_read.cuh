@@ -22,20 +22,6 @@ struct KvRead {
 
 constexpr int RD_TOKENS = 32;
 
-// neighbouring words
-template <int N> __device__ __forceinline__ void kv_words(unsigned (&r)[N], const uint8_t *at)
-{
-    if constexpr (N == 2) {
-        const uint2 v = *(const uint2 *)at;
-        r[0] = v.x, r[1] = v.y;
-    } else
-#pragma unroll
-        for (int k = 0; k < N; k += 4) {
-            const uint4 v = *(const uint4 *)(at + k * 4);
-            r[k] = v.x, r[k + 1] = v.y, r[k + 2] = v.z, r[k + 3] = v.w;
-        }
-}
-
 // G: groups of a cache in 4 bits, 0: 16 bits
 template <typename T, bool VEC, int G>
 __global__ void __launch_bounds__(AP_THREADS) kv_read_rows(const __grid_constant__ KvRead a)
