@@ -599,7 +599,8 @@ int32_t kv_pool_cache(kv_pool_t *pool, int32_t dtype, kv_cache_t *out);
  * A sequence without slots, or whose s are all -inf, has out 0, lse -inf and adds nothing, whatever V holds.  Else every
  * slot counts, one of weight 0 too: an infinite or NaN element of its V makes that element of out infinite or NaN.  (Of a cache in
  * 4 bits a query head with an element that is not finite gives NaN; |q|, |K| and |V| have to stay below 2^100, scores within float32.
- * Weights times steps are rounded to float16 there, 2^-11 of them, where the output is bf16; products below 2^-22 of the row's largest lose more.)
+ * Weights times steps are rounded to float16 there, 2^-11 of them, where the output is bf16; products below 2^-22 of the row's largest lose
+ * more, and so does V below 2^-108.)
  */
 typedef struct {
     int32_t layer, num_seqs, q_heads, window;

@@ -47,7 +47,7 @@ static_assert(2 * KV_Q4_WARPS <= 16, "a lane looks after each plane of a block, 
 constexpr float KV_Q4_SUM = 64.f;    // what the weights of a step may add up to in a lane before the maximum is taken anew
 constexpr float KV_Q4_TOP = 0x1p15f; // what a product may be in the sums' unit; a new unit makes the step's largest 2^8 or more
 constexpr int KV_Q4_LIFT = 8;
-constexpr int KV_Q4_LOWEST = -110;   // exponent of the smallest unit: weights up to 2^8 stay in range in it
+constexpr int KV_Q4_LOWEST = -120;   // exponent of the smallest unit: in it weights up to 2^6 stay in range
 
 // Where sums and queries take more than 168 registers per thread, the warps that load give theirs to those that compute.  What all
 // have together has to be there at the launch: kv_q4_fits

@@ -176,3 +176,13 @@ def test_scores_too_small_for_float32_are_alike(ops, dtype, tiny, n):
     o, z, _, _, terms, size = expected(c, [[0.0] * n], 1.0, 0, 0)
     assert ((out[0].double().cpu() - o).abs() <= R.UNIT[dtype] * o.abs() + 2.0 ** -11 * terms.sum(0) + 2.0 ** -18 * size).all()
     assert ((lse.double().cpu() - z).abs() <= 2.0 ** -20 * (1 + z)).all()
+
+
+@pytest.mark.parametrize("n", [40, 300, 3000])
+def test_v_at_the_lower_limit(ops, n):
+    """Elements around 2^-108, steps of 2^-112 and more: products keep their bits."""
+    g = torch.Generator().manual_seed(9)
+    scores = [(torch.randint(-32, 32, (n,), generator=g) / 8).tolist()]
+    c = cache(scores, [torch.randn(n, 1, 128, generator=g) * 2.0 ** -108])
+    assert float(c.held(0, 0, 1)[1].min()) >= 2.0 ** -112
+    check(c, scores, [1.0, 0.5, -1.0], run(ops, c, [1.0, 0.5, -1.0], weights=True), 2.0 ** -11)
