@@ -6,19 +6,23 @@
 //     out_d    = sum_t (p_t s_tg) code_td              + sum_t p_t lo_tg
 // so codes go into the matrix instructions as they are and the steps are applied to 16 x 8 results, not to elements.  A code
 // becomes a float16 number by a mask alone: four bits in the lowest places of a 16-bit word are code * 2^-24, in the next four places
-// code * 2^-20, both subnormal numbers that m16n8k16 multiplies exactly.  Eight codes cost four masks and a shift.  (The powers
-// of two are taken back in q, in the scale, and in the outputs.)
+// code * 2^-20, both subnormal.  Eight codes cost four masks and a shift.  (The powers of two are taken back in q, in the scale, and in
+// the outputs.)
 //   S^T[16 slots, 8 heads] = K Q^T, one group at a time.  q is scaled by a power of two so that its largest element lies in [2^8, 2^9), and
-//   becomes float16: elements are off by 2^-33 of the largest at most, odd ones, which are taken times 2^-4 on top, by 2^-29.  The sum over lo is one more instruction in the cache's type, with Q_g
-//   split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
+//   becomes float16: elements are off by 2^-33 of the largest at most, odd ones, which are taken times 2^-4 on top, by 2^-29.  The sum over
+//   lo is one more instruction in the cache's type, with Q_g split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
 //   O^T[dim, 8 heads] = V^T (P s)^T, again by groups, on codes less 8, so that they and lo + 8 s add up to little each.  p s is rounded to
-//   float16.  f16 outputs are fine enough to show that (over 131072 slots they were off by 2.8e-4, and with float32 weights are by 2.1e-4), so there
-//   what the rounding leaves goes through the same product: 20.7 to 21.7 us.  bf16 outputs are not (0.00173 and 0.00171), and the 70B shape would
-//   take 57.3 instead of 52.0 us.  (p itself, for the sum over lo and the row's sum, stays in float32.)  The maximum that is subtracted from the scores is taken anew only when a step's
-//   weights add up to more than 64 in a lane: a vote instead of a maximum over the lanes, the sums stay what they are in exact arithmetic.
+//   float16 (p itself, for the sum over lo and the row's sum, stays in float32).
+//   The maximum that is subtracted from the scores is taken anew only when a step's weights add up to more than 64 in a lane: a vote instead
+//   of a maximum over the lanes, the sums stay what they are in exact arithmetic.
 //   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest p s met so far, up where
 //   a larger one comes and down as the maximum rises; the row's maximum and sum, and with them lse and weights, know nothing of V, and
 //   a slot without weight sets no unit.  Products below 2^-22 of the row's largest lose bits, below 2^-33 they vanish.
+// f16 outputs are fine enough to show two things more, and where the type is f16 both are done: what the rounding of p s leaves goes through
+// the same product, and codes become normal numbers by an addition (products of subnormal ones lose bits at their lower end: they seem to be
+// placed by their exponents, which say 7 to 10 bits more than there is).  Over 131072 slots the output is 2.06e-4 off, as with float32 weights,
+// with the first alone 2.12e-4, with neither 2.8e-4; lse of one slot 2e-7 and, with subnormal codes, 1.2e-6; 22.1, 21.3 and 20.6 us.  In bf16 the
+// output is 0.00173 off, and 0.00171 with float32 weights; the first would take the 70B shape from 52.3 to 57.3 us, the second to 57.
 // Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
 // that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
@@ -84,6 +88,8 @@ __device__ __forceinline__ unsigned kv_add2(unsigned x, unsigned y)
     const __half2 v = __hadd2(*(const __half2 *)&x, *(const __half2 *)&y);
     return *(const unsigned *)&v;
 }
+// Codes, or codes * 16, as float16 numbers of their own size: 1024 + c has c in its lowest bits, and `less`, -1024 or below, takes that away
+__device__ __forceinline__ unsigned kv_codes(unsigned masked, unsigned less) { return kv_add2(masked | 0x64006400u, less); }
 // what two numbers have beyond their roundings to float16, as float16
 __device__ __forceinline__ unsigned kv_left(unsigned rounded, float x, float y)
 {
@@ -440,6 +446,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
                 const uint8_t *at = kt + u * to_next;
+                const auto even = [](unsigned x) { return EXACT ? kv_codes(x & 0x000f000fu, 0xe400e400u) : x & 0x000f000fu; };
+                const auto odd = [](unsigned x) { return EXACT ? kv_codes(x & 0x00f000f0u, 0xe400e400u) : x & 0x00f000f0u; };
                 unsigned c0[G], c1[G], w0[G], w1[G];
                 kv_words(c0, at + code_at);
                 kv_words(c1, at + code_at + 128 * G);
@@ -452,8 +460,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float x[4];
-                        kv_mma_f16_first(x, c0[g] & 0x000f000fu, c1[g] & 0x000f000fu, c0[g] & 0x00f000f0u, c1[g] & 0x00f000f0u, qf[nt][g][0], qf[nt][g][1]);
-                        kv_mma_f16(x, h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u, qf[nt][g][2], qf[nt][g][3]);
+                        kv_mma_f16_first(x, even(c0[g]), even(c1[g]), odd(c0[g]), odd(c1[g]), qf[nt][g][0], qf[nt][g][1]);
+                        kv_mma_f16(x, even(h0), even(h1), odd(h0), odd(h1), qf[nt][g][2], qf[nt][g][3]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[u][nt][e] = g == 0 ? (e < 2 ? s0 : s1) * x[e] : fmaf(e < 2 ? s0 : s1, x[e], y[u][nt][e]);
                     }
@@ -468,15 +476,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                 const unsigned p0 = __byte_perm(x0, z0, 0x5410), p1 = __byte_perm(x1, z1, 0x5410);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    if constexpr (EXACT) {
-                        float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int p = 0; p < PARTS; ++p) kv_mma_lo(x, p0, p1, ql[nt][p][0], ql[nt][p][1], T());
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[u][nt][e] = fmaf(y[u][nt][e], 0x1p24f, x[e]);
-                    } else
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) kv_mma_lo(y[u][nt], p0, p1, ql[nt][p][0], ql[nt][p][1], T());
+                    for (int p = 0; p < PARTS; ++p) kv_mma_lo(y[u][nt], p0, p1, ql[nt][p][0], ql[nt][p][1], T());
                 }
             }
             // the scores are rounded here, so that the largest less the maximum is 0 whatever its size.  (Masked
@@ -610,8 +611,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
             for (int u = 0; u < SUB; ++u) {
                 // The sum over lo would take away most of what codes from 0 to 15 add up to, but not what was rounded: they are -8 to 7
                 // and lo is lo + 8 s
-                const auto even = [](unsigned x) { return kv_add2(x & 0x000f000fu, 0x80088008u); };
-                const auto odd = [](unsigned x) { return kv_add2(x & 0x00f000f0u, 0x80808080u); };
+                const auto even = [](unsigned x) { return EXACT ? kv_codes(x & 0x000f000fu, 0xe408e408u) : kv_add2(x & 0x000f000fu, 0x80088008u); };  // -1032, -8 * 2^-24
+                const auto odd = [](unsigned x) { return EXACT ? kv_codes(x & 0x00f000f0u, 0xe480e480u) : kv_add2(x & 0x00f000f0u, 0x80808080u); };   // -1152, -8 * 2^-20
                 unsigned v[4][G / 2];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) kv_words(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
@@ -671,7 +672,7 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) o[nt][g][t][2 * b + e] = fmaf(o[nt][g][t][2 * b + e] * (b ? 0x1p20f : 0x1p24f), unit, lo[nt][g][e]);
+                            for (int b = 0; b < 2; ++b) o[nt][g][t][2 * b + e] = fmaf(o[nt][g][t][2 * b + e] * (EXACT ? b ? 0x1p-4f : 1.f : b ? 0x1p20f : 0x1p24f), unit, lo[nt][g][e]);
                     }
                 }
             const bool whole = began && (tile.x & 1 << 19);

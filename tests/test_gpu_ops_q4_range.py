@@ -186,3 +186,24 @@ def test_v_at_the_lower_limit(ops, n):
     c = cache(scores, [torch.randn(n, 1, 128, generator=g) * 2.0 ** -108])
     assert float(c.held(0, 0, 1)[1].min()) >= 2.0 ** -112
     check(c, scores, [1.0, 0.5, -1.0], run(ops, c, [1.0, 0.5, -1.0], weights=True), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_f16_scores_have_float32s_bits(ops, dim):
+    """lse of one slot is its score, the sum of 2 G float32 sums, s * sum of q * code and lo * sum of q.  Each comes from two instructions that add 16
+    products, and is added to the others: a dozen truncations at its own size at most, by 2^-23 of it, whose mean square is 2^-46 / 3 each if their
+    errors are as good as independent: 16 * 2^-48 of the sizes' squares in all, over 2048 scores."""
+    n = 64
+    c = Q.Cache([1] * n, 2, dim, 16, "f16", seed=10, layers=1)
+    q = torch.randn(n, 32, dim, generator=c.g).to(torch.float16).cuda()
+    out, lse = torch.zeros_like(q), torch.zeros(n, 32, device="cuda")
+    ops.kv_attend(c.handle(B), 0, q, c.tables, c.lens, 1, out=out, lse=lse)
+    ops.kv_ops_sync()
+    far, sizes = 0.0, 0.0
+    for i in range(n):
+        lo, step, code = (x[0].repeat_interleave(16, 0) for x in c.held(i, 0, 0))
+        x = q[i].double().cpu()
+        far += float(((lse[i].double().cpu() - ((lo + step * code) * x).sum(-1) / dim ** 0.5) ** 2).sum())
+        groups = ((y * x).unflatten(-1, (-1, 32)).sum(-1) for y in (step * code, lo))
+        sizes += float(sum((y ** 2).sum() for y in groups)) / dim
+    assert far <= 16 * 2.0 ** -48 * sizes, ((far / n / 32) ** 0.5, (sizes / n / 32) ** 0.5)
