@@ -22,7 +22,8 @@
 // the same product, and codes become normal numbers by an addition (products of subnormal ones lose bits at their lower end: they seem to be
 // placed by their exponents, which say 7 to 10 bits more than there is).  Over 131072 slots the output is 2.06e-4 off, as with float32 weights,
 // with the first alone 2.12e-4, with neither 2.8e-4; lse of one slot 2e-7 and, with subnormal codes, 1.2e-6; 22.1, 21.3 and 20.6 us.  In bf16 the
-// output is 0.00173 off, and 0.00171 with float32 weights; the first would take the 70B shape from 52.3 to 57.3 us, the second to 57.
+// output is 0.00173 off, and 0.00171 with float32 weights; the first would take the 70B shape from 52.3 to 57.3 us, the
+// second, in either of the two products, to 55.
 // Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
 // that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
@@ -30,16 +31,14 @@
 // whatever they hold, scores are replaced by -inf and words by 0, so nothing of such a slot reaches a sum.
 //
 // Split.  Eight warps compute, a KV head each where there are eight, two tiles at once: what a step costs beside its tiles (waiting,
-// the vote, the compensated sum) then counts half (495 instructions per tile with one at once, 347 with two; 60 and 50 us for the 70B shape).
-// Other warps load, so that those that compute need no registers for addresses: with every warp filling its own ring by 16-byte
-// copies the same work took 67 us.  What was slower too: the scores of one step beside the sums of the one before it (60 us:
-// registers), twelve computing warps (69), rows joined by whichever CTA comes last (71 to 88: a row of 16384 slots has 23 parts, too
-// much for one SM).
+// the vote, the compensated sum) then counts half.  Other warps load, so that those that compute need no registers for addresses.  When
+// these were compared the 70B shape took 50 us so; with one tile at once 60 (495 instead of 347 instructions per tile; now 400), with every
+// warp filling its own ring by 16-byte copies 67, with the scores of one step beside the sums of the one before it 60 (registers), with
+// twelve computing warps 69, with rows joined by whichever CTA comes last 71 to 88 (a row of 16384 slots has 23 parts, too much for one SM).
 //
-// What bounds it.  70B shape, 133 MB: 49.3 us, of which 8.5 are the join, 5 the first chain of loads (lengths, block ids, first tile), 30 the line
-// of steps: 4.4 TB/s.  Without any arithmetic on the tiles the call takes 41 us, without the join 42.  No single part of the arithmetic
-// shows: without the masks (a fifth of the instructions) 51.2 us, without the transpositions 50.7, without the second product 49.4,
-// against 51.0 at the same time.
+// What bounds it.  70B shape, 133 MB: 52.4 us, of which 8.5 are the join, 5 the first chain of loads (lengths, block ids, first tile), 33 the line
+// of steps: 4.0 TB/s.  Without any arithmetic on the tiles the call takes 41 us.  No single part of the arithmetic shows: at 51.0 us, without
+// the masks (a fifth of the instructions) 51.2, without the transpositions 50.7, without the second product 49.4.
 #pragma once
 #include <cfloat>
 #include <type_traits>

@@ -150,8 +150,8 @@ constexpr int64_t ATTEND_SMEM = 227 * 1024 - 4096;   // what a CTA may have, les
 // with weights to add up): 4 sequences of 500 slots with weights 13.5 us whole, 17.6 split; 1 of 900 without 14.7 whole, 12.1 split.
 // Near the limit with weights few whole rows lose already: of 900 slots one takes 21.6 us whole and 16.7 split, 16 take 26.8 and 29.1
 constexpr int ATTEND_ALONE_STEPS = 4, ATTEND_ALONE_STEPS_WEIGHTS = 8;
-// In 4 bits a step is two tiles of each warp, and the limit the same with weights and without: one sequence of 1000 slots (4 steps) 13.7 us
-// whole and 14.3 split, with weights 18.7 and 19.4; of 2000 (8 steps) 22.3 and 14.5, 36.1 and 19.8; 64 of 100 (4 steps) 11.6 and 18.6
+// In 4 bits a step is two tiles of each warp, and the limit the same with weights and without: one sequence of 1000 slots (4 steps) 14.5 us
+// whole and 14.7 split, with weights 17.6 and 19.7; of 2000 (8 steps) 23.9 and 15.0, 33.4 and 20.1; 64 of 100 (4 steps) 12.3 and 15.7
 constexpr int ATTEND_ALONE_STEPS_Q4 = 4;
 // No piece is shorter: with 1 step one sequence of 2000 slots takes 22.5 us, with 2 18.8, with 4 18.8; seven windows of 333 12.8, 14.9, 17.9
 constexpr int ATTEND_MIN_STEPS = 2;
@@ -212,7 +212,7 @@ int32_t plan_attend(kv_ops *o, const kv_cache_t *c, const kv_attend_args_t *a, K
     k.pieces = split ? o->sms : 0;
     k.min_steps = ATTEND_MIN_STEPS;
     // Whole blocks: of 2^n tiles, as many as a step has or fewer, and steps that begin where blocks do.  One sequence of 131072 slots in
-    // blocks of 64, 1 KV head: 20.4 us, and 26.4 with a bulk copy per tile, plane, codes and words
+    // blocks of 64, 1 KV head: 20.4 us when that was compared, and 26.4 with a bulk copy per tile, plane, codes and words
     const int tiles = c->block_size / 16;
     k.block_tiles = G && k.whole_tiles && (tiles & (tiles - 1)) == 0 && k.tw % tiles == 0 && (tiles == 1 || a->window == 0) ? tiles : 0;
     const int64_t parts = (int64_t)k.pieces * 2 * k.hc * 8 * p.nt;
