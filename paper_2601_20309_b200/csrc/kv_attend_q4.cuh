@@ -11,19 +11,21 @@
 //   S^T[16 slots, 8 heads] = K Q^T, one group at a time.  q is scaled by a power of two so that its largest element lies in [2^8, 2^9), and
 //   becomes float16: elements are off by 2^-33 of the largest at most, odd ones, which are taken times 2^-4 on top, by 2^-29.  The sum over
 //   lo is one more instruction in the cache's type, with Q_g split into up to four parts of that type (32 bits of a bf16, 22 of an f16 Q_g).
-//   O^T[dim, 8 heads] = V^T (P s)^T, again by groups, on codes less 8, so that they and lo + 8 s add up to little each.  p s is rounded to
-//   float16 (p itself, for the sum over lo and the row's sum, stays in float32).
+//   O^T[dim, 8 heads] = V^T (P s)^T, again by groups; p s is rounded to float16 (p itself, for the sum over lo and the row's sum, stays in
+//   float32).
 //   The maximum that is subtracted from the scores is taken anew only when a step's weights add up to more than 64 in a lane: a vote instead
 //   of a maximum over the lanes, the sums stay what they are in exact arithmetic.
 //   What keeps p s in float16's range is a unit of the sums over codes, a power of two that follows the largest p s met so far, up where
 //   a larger one comes and down as the maximum rises; the row's maximum and sum, and with them lse and weights, know nothing of V, and
 //   a slot without weight sets no unit.  Products below 2^-22 of the row's largest lose bits, below 2^-33 they vanish.
-// f16 outputs are fine enough to show two things more, and where the type is f16 both are done: what the rounding of p s leaves goes through
-// the same product, and codes become normal numbers by an addition (products of subnormal ones lose bits at their lower end: they seem to be
-// placed by their exponents, which say 7 to 10 bits more than there is).  Over 131072 slots the output is 2.06e-4 off, as with float32 weights,
-// with the first alone 2.12e-4, with neither 2.8e-4; lse of one slot 2e-7 and, with subnormal codes, 1.2e-6; 22.1, 21.3 and 20.6 us.  In bf16 the
-// output is 0.00173 off, and 0.00171 with float32 weights; the first would take the 70B shape from 52.3 to 57.3 us, the
-// second, in either of the two products, to 55.
+// f16 outputs are fine enough to show three things more, and where the type is f16 they are taken care of.  What the rounding of p s leaves goes
+// through the same product.  Codes of V are -8 to 7, and lo is lo + 8 s: the two sums would take most of each other away, but not what was
+// rounded.  And codes become normal numbers by the addition that this takes anyway: products of subnormal ones lose bits at their lower end
+// (they seem to be placed by their exponents, which say 7 to 10 bits more than there is).  Over 131072 slots the output is 2.06e-4 off, as with
+// float32 weights, without the third 2.12e-4, without the first and the third 2.8e-4; lse of one slot 2e-7 and, with subnormal codes, 1.2e-6; 22.1,
+// 21.3 and 20.6 us.  In bf16 the output is 0.00178 off and 0.00171 with float32 weights, over 2000 slots 0.00171 and 0.00165: next to the output's own
+// rounding that is little for 54.5 us of the 70B shape instead of 50.7 (the first alone) or 57.3 (the first and second).  The second alone (52.3)
+// would give noise of 2^-13 of a group's range to outputs that are 0.
 // Slots: rows 2, 3, 6 and 7 of a matrix instruction are slots 3, 2, 7 and 6 of the tile, the others their own, 8 more for the second half, so
 // that the lanes' reads of K do not collide and those of V, every other row of the contraction at once, by twos only.
 //
@@ -32,12 +34,12 @@
 //
 // Split.  Eight warps compute, a KV head each where there are eight, two tiles at once: what a step costs beside its tiles (waiting,
 // the vote, the compensated sum) then counts half.  Other warps load, so that those that compute need no registers for addresses.  When
-// these were compared the 70B shape took 50 us so; with one tile at once 60 (495 instead of 347 instructions per tile; now 400), with every
+// these were compared the 70B shape took 50 us so; with one tile at once 60 (495 instead of 347 instructions per tile; now 362), with every
 // warp filling its own ring by 16-byte copies 67, with the scores of one step beside the sums of the one before it 60 (registers), with
 // twelve computing warps 69, with rows joined by whichever CTA comes last 71 to 88 (a row of 16384 slots has 23 parts, too much for one SM).
 //
-// What bounds it.  70B shape, 133 MB: 52.4 us, of which 8.5 are the join, 5 the first chain of loads (lengths, block ids, first tile), 33 the line
-// of steps: 4.0 TB/s.  Without any arithmetic on the tiles the call takes 41 us.  No single part of the arithmetic shows: at 51.0 us, without
+// What bounds it.  70B shape, 133 MB: 51.2 us, of which 8.5 are the join, 5 the first chain of loads (lengths, block ids, first tile), 32 the line
+// of steps: 4.2 TB/s.  Without any arithmetic on the tiles the call takes 41 us.  No single part of the arithmetic shows: at 51.0 us, without
 // the masks (a fifth of the instructions) 51.2, without the transpositions 50.7, without the second product 49.4.
 #pragma once
 #include <cfloat>
@@ -82,13 +84,13 @@ __device__ __forceinline__ void kv_mma_lo(float (&c)[4], unsigned a0, unsigned a
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ unsigned kv_add2(unsigned x, unsigned y)
+// Codes, or codes * 16, as float16 numbers of their own size: 1024 + c has c in its lowest bits, and `less`, -1024 or below, takes that away
+__device__ __forceinline__ unsigned kv_codes(unsigned masked, unsigned less)
 {
-    const __half2 v = __hadd2(*(const __half2 *)&x, *(const __half2 *)&y);
+    const unsigned x = masked | 0x64006400u;
+    const __half2 v = __hadd2(*(const __half2 *)&x, *(const __half2 *)&less);
     return *(const unsigned *)&v;
 }
-// Codes, or codes * 16, as float16 numbers of their own size: 1024 + c has c in its lowest bits, and `less`, -1024 or below, takes that away
-__device__ __forceinline__ unsigned kv_codes(unsigned masked, unsigned less) { return kv_add2(masked | 0x64006400u, less); }
 // what two numbers have beyond their roundings to float16, as float16
 __device__ __forceinline__ unsigned kv_left(unsigned rounded, float x, float y)
 {
@@ -608,10 +610,8 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                 }
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                // The sum over lo would take away most of what codes from 0 to 15 add up to, but not what was rounded: they are -8 to 7
-                // and lo is lo + 8 s
-                const auto even = [](unsigned x) { return EXACT ? kv_codes(x & 0x000f000fu, 0xe408e408u) : kv_add2(x & 0x000f000fu, 0x80088008u); };  // -1032, -8 * 2^-24
-                const auto odd = [](unsigned x) { return EXACT ? kv_codes(x & 0x00f000f0u, 0xe480e480u) : kv_add2(x & 0x00f000f0u, 0x80808080u); };   // -1152, -8 * 2^-20
+                const auto even = [](unsigned x) { return EXACT ? kv_codes(x & 0x000f000fu, 0xe408e408u) : x & 0x000f000fu; };     // -1032
+                const auto odd = [](unsigned x) { return EXACT ? kv_codes(x & 0x00f000f0u, 0xe480e480u) : x & 0x00f000f0u; };      // -1152
                 unsigned v[4][G / 2];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) kv_words(v[r], kt + to_v + u * to_next + v_at + (r & 1 ? v_odd : 0) + r / 2 * 128 * G);
@@ -620,7 +620,11 @@ __global__ void __launch_bounds__((KV_Q4_WARPS + KV_Q4_LOADERS) * 32, 1) kv_atte
                     const unsigned r0 = __byte_perm(v[0][g >> 1], v[1][g >> 1], g & 1 ? 0x7632 : 0x5410), r1 = __byte_perm(v[2][g >> 1], v[3][g >> 1], g & 1 ? 0x7632 : 0x5410);
                     const unsigned h0 = r0 >> 8, h1 = r1 >> 8;
                     const float s0 = __uint_as_float(w0[u][g] & 0xffff0000u), s1 = __uint_as_float(w1[u][g] & 0xffff0000u);
-                    const float z0 = fmaf(8.f, s0, kv_unpair(w0[u][g], T()).x), z1 = fmaf(8.f, s1, kv_unpair(w1[u][g], T()).x);
+                    float z0 = kv_unpair(w0[u][g], T()).x, z1 = kv_unpair(w1[u][g], T()).x;
+                    if constexpr (EXACT) {
+                        z0 = fmaf(8.f, s0, z0);
+                        z1 = fmaf(8.f, s1, z1);
+                    }
                     const unsigned a0 = even(r0), a1 = odd(r0), a2 = even(r1), a3 = odd(r1), b0 = even(h0), b1 = odd(h0), b2 = even(h1), b3 = odd(h1);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {

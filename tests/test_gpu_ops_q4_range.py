@@ -146,20 +146,21 @@ def test_f16_outputs_have_the_weights_in_float32(ops, n):
 
 def test_one_rounding_of_all_weights(ops):
     """Every sixteenth slot has a larger score and V of zeros, the others one score and one step (V is -1 or 1), so that their weights are rounded alike,
-    by up to 2^-11.  That is 2^-11 of the sum of what they are multiplied with, not of the sum of its sizes: V adds up to little."""
+    by up to 2^-11.  In f16 that is 2^-11 of the sum of what they are multiplied with at most, not of the sum of its sizes: V adds up to little.  (In
+    bf16 it is 2^-11 of the sizes, as for weights that are rounded each in its own way.)"""
     n = 4000
     g = torch.Generator().manual_seed(7)
     scores = [[4.25 if t % 16 == 0 else 0.25 for t in range(n)]]
     v = [torch.randint(0, 2, (n, 1, 128), generator=g).float() * 2 - 1]
     v[0][::16] = 0.0
-    c = cache(scores, v)
-    factors = torch.tensor([0.1 + 0.05 * k for k in range(16)]).to(torch.bfloat16).float().tolist()
+    c = cache(scores, v, "f16")
+    factors = torch.tensor([0.1 + 0.05 * k for k in range(16)]).to(torch.float16).float().tolist()
     out, _, _ = run(ops, c, factors)
     lo, step, code = (x[:, 0] for x in c.held(0, 0, 1))
     for k, f in enumerate(factors):
         o, _, p, ps, _, _ = expected(c, scores, f, 0, 0)
         # exponentials: 2^-18 of the output (all alike); float32 sums: 2^-20 of the terms' sizes
-        bound = (2.0 ** -8 + 2.0 ** -18) * o.abs() + 2.0 ** -11 * (ps * (code - 8)).sum(0).abs() + 2.0 ** -20 * (p[:, None] * (lo.abs() + 8 * step)).sum(0) + n * 15 * 2.0 ** -33 * ps.max()
+        bound = (2.0 ** -11 + 2.0 ** -18) * o.abs() + 2.0 ** -25 + 2.0 ** -11 * (ps * (code - 8)).sum(0).abs() + 2.0 ** -20 * (p[:, None] * (lo.abs() + 8 * step)).sum(0) + n * 15 * 2.0 ** -33 * ps.max()
         assert ((out[0, k] - o).abs() <= bound).all(), (k, float(((out[0, k] - o).abs() - bound).max()), float(bound.max()))
 
 
@@ -207,3 +208,22 @@ def test_f16_scores_have_float32s_bits(ops, dim):
         groups = ((y * x).unflatten(-1, (-1, 32)).sum(-1) for y in (step * code, lo))
         sizes += float(sum((y ** 2).sum() for y in groups)) / dim
     assert far <= 16 * 2.0 ** -48 * sizes, ((far / n / 32) ** 0.5, (sizes / n / 32) ** 0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [1, 50, 3000])
+def test_zeros_that_are_the_lowest_of_their_group(ops, dtype, n):
+    """V is 0 in every other element and not negative elsewhere: the outputs of those elements are 0 in bf16, where code and lowest value are, and no more
+    than what is lost of 2^-22 of eight steps, and of float32 sums of them, in f16."""
+    g = torch.Generator().manual_seed(11)
+    scores = [(torch.randint(-64, 64, (n,), generator=g) / 32).tolist()]
+    v = torch.randn(n, 1, 128, generator=g).abs()
+    v[..., ::2] = 0.0
+    c = cache(scores, [v], dtype)
+    factors = [1.0, 0.3125, -1.0, 1.5]
+    out, lse, _ = got = run(ops, c, factors)
+    check(c, scores, factors, got, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
+    for k, f in enumerate(factors):
+        _, _, _, ps, _, _ = expected(c, scores, f, 0, 0)
+        most = 0.0 if dtype == "bf16" else (2.0 ** -22 + 2.0 ** -20) * 8 * ps.sum(0)[::2] + n * 15 * 2.0 ** -33 * ps.max() + 2.0 ** -25
+        assert (out[0, k, ::2].abs() <= most).all()
